@@ -59,7 +59,8 @@ typedef enum {
     HCCS_ERR_NOT_UPLOADED   = 3,  /* hccs_forward before hccs_params_upload                      */
     HCCS_ERR_UNSUPPORTED    = 4,  /* shape the kernels cannot take (documented per call)         */
     HCCS_ERR_CUDA           = 5,  /* a CUDA runtime call failed; see hccs_last_cuda_error        */
-    HCCS_ERR_DEVICE_TIMEOUT = 6   /* a bounded device-side wait gave up (hccs_device_status)     */
+    HCCS_ERR_DEVICE_TIMEOUT = 6,  /* a bounded device-side wait gave up (hccs_device_status)     */
+    HCCS_ERR_DEVICE_INDEX   = 7   /* a page, slot or length in device memory was out of range (hccs_device_status) */
 } hccs_status_t;
 
 /* flags of hccs_forward / hccs_attention_fused (bitwise OR) */
@@ -70,6 +71,17 @@ enum {
     HCCS_RECIP_CLB = 2,   /* leading-bit reciprocal (Eq. 9); uint8 results saturate at 255      */
     HCCS_CAUSAL    = 4    /* key j of query i takes part iff j <= i + (Lk - Lq); others give 0  */
 };
+
+/* a further reciprocal, of hccs_attention_cached only: the scores are divided by their sum as real numbers */
+enum { HCCS_RECIP_REAL = 8 };
+
+/* element types of the cache entry points */
+typedef enum {
+    HCCS_I32  = 0,
+    HCCS_F32  = 1,
+    HCCS_BF16 = 2,
+    HCCS_F16  = 3
+} hccs_type_t;
 
 /* Creates a context on CUDA device `device` (allocates a small parameter table lazily and a
  * 4-byte device status word).  *out receives the context.  Synchronous. */
@@ -236,9 +248,145 @@ hccs_status_t hccs_calibrate(const int8_t *logits, int32_t B, int32_t H, int32_t
                              double alpha, const hccs_calib_grid_t *grid, hccs_head_params_t *best,
                              double *best_kl, void *cuda_stream);
 
-/* Reads (and clears) the device status word: 0 = no kernel gave up a bounded wait.  Synchronises
- * `cuda_stream`.  Returns HCCS_ERR_DEVICE_TIMEOUT when the word was non-zero; *word (may be NULL)
- * receives it. */
+/*
+ * ---- Generation over an int8 key/value cache (not in the paper: its models are encoders) ----
+ *
+ * The cache is two pools of pages, int8 [num_pages, Hkv, page_size, d] each, one for keys and one for
+ * values; page_size is a power of two from 16 to 65536, d is 64 or 128.  A sequence is a row of a page
+ * table: its token j lives in page table[j / page_size], at place j % page_size.  A slot is
+ * page * page_size + place.  Codes stand for code * step with one step per head.  The pools, tables and
+ * every workspace belong to the caller; nothing here allocates, copies from pageable memory or
+ * synchronises, so all of it can be captured into a CUDA graph (host arrays are taken by value).
+ * At most HCCS_MAX_CACHE_HEADS query heads and HCCS_MAX_CACHE_KEYS keys per sequence.
+ */
+#define HCCS_MAX_CACHE_HEADS 256
+#define HCCS_MAX_CACHE_KEYS 131072
+#define HCCS_MAX_ROT_DIM 128
+
+/* Rotary positions: the pair i of a head, (a, b) = dims (i, i + rot_dim/2), or (2i, 2i+1) where
+ * interleaved, becomes (a*c - b*s, b*c + a*s) with c = scale*cos(t), s = scale*sin(t) and
+ * t = position * freq[i], one rounding to fp64.  Dims from rot_dim on are left as they are. */
+typedef struct {
+    int32_t rot_dim;                          /* even, 0..d */
+    int32_t interleaved;                      /* 0: halves, 1: neighbours */
+    double  scale;                            /* finite */
+    double  freq[HCCS_MAX_ROT_DIM / 2];       /* radians per position, finite */
+} hccs_rope_t;
+
+/* How frequencies f_i = base^(-2i/rot_dim) are changed for contexts longer than a model was trained on.
+ *   NONE        as they are
+ *   LINEAR      f / factor
+ *   BASE        base * factor^(rot_dim / (rot_dim - 2)) in the place of base (rot_dim > 2)
+ *   WAVELENGTH  with n = original_len * f / (2 pi), the turns over the original length:
+ *               keep = clamp((n - low) / (high - low), 0, 1), f*keep + (f/factor)*(1 - keep)
+ *   DIMENSION   the same mixture, keep falling linearly over the pair index from the pair that makes
+ *               `high` turns (rounded down) to the one that makes `low` (rounded up), both kept within
+ *               0 .. rot_dim - 1; scale = 0.1 ln(factor) + 1 (the other kinds: scale = 1)
+ */
+enum { HCCS_ROPE_NONE = 0, HCCS_ROPE_LINEAR = 1, HCCS_ROPE_BASE = 2, HCCS_ROPE_WAVELENGTH = 3, HCCS_ROPE_DIMENSION = 4 };
+typedef struct {
+    int32_t kind;
+    double factor;                            /* >= 1 */
+    double low, high;                         /* WAVELENGTH, DIMENSION: 0 < low < high */
+    double original_len;                      /* WAVELENGTH, DIMENSION: > 0 */
+} hccs_rope_scaling_t;
+
+/* Fills *rope (host only, no CUDA call).  `scaling` may be NULL (NONE).  HCCS_ERR_INVALID_ARG for a NULL
+ * rope, an odd rot_dim or one outside 2..HCCS_MAX_ROT_DIM, base <= 1, or a scaling outside its ranges. */
+hccs_status_t hccs_rope_frequencies(hccs_rope_t *rope, int32_t rot_dim, int32_t interleaved, double base,
+                                    const hccs_rope_scaling_t *scaling);
+
+/*
+ * Rotates and quantises new tokens: queries to q8, keys and values into the cache.
+ *   q, k, v      device [T, Hq | Hkv, d] of `type` (HCCS_F32, HCCS_BF16 or HCCS_F16); head and dim are
+ *                contiguous, tokens are q_stride, k_stride, v_stride ELEMENTS apart (views of one fused
+ *                projection, for instance); 16-byte aligned, and so are the strides
+ *                (HCCS_ERR_UNSUPPORTED otherwise).  q may be NULL (Hq is then ignored), or both k and v
+ *   positions    device int32 [T], any values; may be NULL without rope
+ *   slots        device int64 [T]: where the token's key and value go; a negative slot skips them (padding
+ *                tokens); the others of one call must differ.  A slot at or beyond num_pages * page_size is
+ *                skipped as well and reported (hccs_device_status).  May be NULL where k and v are
+ *   rope         HOST, or NULL for none; applied to q and k
+ *   *_step       HOST float [Hq], [Hkv], [Hkv], finite and > 0: the value of one code
+ *   q8           device int8 [T, Hq, d];  k_pages, v_pages  the pools; 16-byte aligned
+ * A code is clamp(round(y / step), -128, 127), the exact quotient rounded to nearest, ties to even: the
+ * kernel works in fp32 and repeats in fp64 what lies next to a border, so the codes are those of a
+ * computation in fp64.  NaN gives 0.  Nothing else in the pools is touched.
+ */
+hccs_status_t hccs_cache_write(hccs_ctx_t *ctx, const void *q, const void *k, const void *v, hccs_type_t type,
+                               int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                               const int32_t *positions, const int64_t *slots, const hccs_rope_t *rope,
+                               const float *q_step, const float *k_step, const float *v_step,
+                               int8_t *q8, int8_t *k_pages, int8_t *v_pages,
+                               int32_t T, int32_t Hq, int32_t Hkv, int32_t d,
+                               int32_t num_pages, int32_t page_size, void *cuda_stream);
+
+/*
+ * Reads sequences back: token j of sequence b goes to row out_start[b] + j of the outputs.
+ *   page_table   device int32 [B, max_pages]
+ *   out_start    device int32 [B+1], not falling; sequence b has out_start[b+1] - out_start[b] tokens, at
+ *                most max_len (host) and max_pages * page_size of which are read; more is reported, and so
+ *                is a page outside 0..num_pages-1, whose rows become zeros
+ *   k_out, v_out device [rows, Hkv, d] of `type`; rows (host) is the size of the outputs: sequences that
+ *                reach beyond it are cut there and reported.  Rows no sequence has are left as they are.
+ *                16-byte aligned.  Either may be NULL
+ * Values are code * step in fp32, rounded to `type`.
+ */
+hccs_status_t hccs_cache_read(hccs_ctx_t *ctx, const int8_t *k_pages, const int8_t *v_pages,
+                              const int32_t *page_table, const int32_t *out_start,
+                              const float *k_step, const float *v_step, void *k_out, void *v_out, hccs_type_t type,
+                              int32_t B, int32_t max_pages, int32_t max_len, int32_t rows, int32_t Hkv, int32_t d,
+                              int32_t num_pages, int32_t page_size, void *cuda_stream);
+
+/*
+ * hccs_params_upload for caches longer than the paper's int16 row sums allow (n*B <= 32767 leaves a table
+ * of constants at 16384 keys): Dmax in 1..127, S in 0..127, 1 <= B <= 32767, B - S*Dmax >= 0, n_design in
+ * 1..HCCS_MAX_CACHE_KEYS.  Such a table serves hccs_attention_cached with HCCS_RECIP_REAL alone; the other
+ * calls return HCCS_ERR_CONSTRAINT until hccs_params_upload puts an ordinary table in its place.
+ */
+hccs_status_t hccs_params_upload_wide(hccs_ctx_t *ctx, const hccs_head_params_t *params, int32_t num_heads,
+                                      int32_t n_design, int32_t *bad_head, void *cuda_stream);
+
+/*
+ * HCCS attention of new tokens over the cache, which already holds their keys and values.  Sequence b has
+ * nq = q_start[b+1] - q_start[b] queries, the last nq of its kv_len[b] keys being their own.  For query i of
+ * head h and the keys j it sees, kv head h / (Hq/Hkv):
+ *   acc = sum_c Q[i,c] K[j,c];  x = clamp((acc*M_h + 2^(shift-1)) >> shift, -128, 127)
+ *   s_j = B_h - S_h * min(max x - x_j, Dmax_h);  Z = sum s_j                               (Eq. 1 to 5)
+ *   HCCS_RECIP_DIV, HCCS_RECIP_CLB   O = rho * sum s_j V[j,:], rho of the int16 path       (Eq. 6, 7, 9)
+ *   HCCS_RECIP_REAL                  O = (sum s_j V[j,:] / Z) * out_scale[h]
+ * The sums are exact integers whatever the split over the GPU, so results do not depend on it.
+ * Which keys: all before the new ones; of the new ones those at or before the query itself, or, with
+ * tree_mask, those whose bit is set: bit j % 32 of word j / 32 of row i for the j-th new key of the
+ * sequence (a tree of drafted tokens: itself and its ancestors).  A query that sees no key gives zeros.
+ *   Q            device int8 [T, Hq, d], 16-byte aligned
+ *   page_table   device int32 [B, max_pages];  q_start  device int32 [B+1], not falling;  kv_len  device int32 [B]
+ *   tree_mask    device int32 [T, tree_words], or NULL
+ *   requant_mult HOST int32 [Hq], each in [0, 2^13) and below 2^(shift-1) (HCCS_ERR_UNSUPPORTED beyond);
+ *                requant_shift in 1..24
+ *   out_scale    HOST float [Hq]; NULL for HCCS_I32 output, whose O is the exact integer
+ *   O            device [T, Hq, d] of out_type; float types hold the fp32 product with out_scale[h], rounded
+ *                once more to the type; HCCS_I32 goes with DIV and CLB only.  16-byte aligned
+ *   max_q, max_kv (host)  bounds of the lengths of this call, which choose kernel and grid: queries beyond
+ *                max_q are not computed and keys beyond max_kv are not seen, both reported.  max_kv beyond
+ *                n_design is HCCS_ERR_CONSTRAINT, beyond HCCS_MAX_CACHE_KEYS HCCS_ERR_UNSUPPORTED
+ *   flags        one HCCS_RECIP_*; nothing else
+ * kv_len outside 0 .. max_pages * page_size is cut and reported; a page outside 0..num_pages-1 is reported
+ * and its keys are not seen; q_start is cut to 0..T.  Rows behind the last sequence are left as they are.
+ */
+hccs_status_t hccs_attention_cached(hccs_ctx_t *ctx, const int8_t *Q, const int8_t *k_pages, const int8_t *v_pages,
+                                    const int32_t *page_table, const int32_t *q_start, const int32_t *kv_len,
+                                    const int32_t *tree_mask, int32_t tree_words,
+                                    const int32_t *requant_mult, int32_t requant_shift, const float *out_scale,
+                                    void *O, hccs_type_t out_type,
+                                    int32_t T, int32_t B, int32_t Hq, int32_t Hkv, int32_t d, int32_t max_pages,
+                                    int32_t num_pages, int32_t page_size, int32_t max_q, int32_t max_kv,
+                                    uint32_t flags, void *cuda_stream);
+
+/* Reads (and clears) the device status word: 0 = no kernel gave up a bounded wait or met an index out of
+ * range.  Synchronises `cuda_stream`.  Returns HCCS_ERR_DEVICE_TIMEOUT when a wait was given up (bits 0
+ * and 1), else HCCS_ERR_DEVICE_INDEX when the word was non-zero (bit 2: slot, bit 3: page, bit 4: length);
+ * *word (may be NULL) receives it. */
 hccs_status_t hccs_device_status(hccs_ctx_t *ctx, uint32_t *word, void *cuda_stream);
 
 /*

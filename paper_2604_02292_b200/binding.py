@@ -28,17 +28,26 @@ HCCS_ERR_NOT_UPLOADED = 3
 HCCS_ERR_UNSUPPORTED = 4
 HCCS_ERR_CUDA = 5
 HCCS_ERR_DEVICE_TIMEOUT = 6
+HCCS_ERR_DEVICE_INDEX = 7
 
 HCCS_OUT_U8 = 0
 HCCS_OUT_U16 = 1
 HCCS_RECIP_DIV = 0
 HCCS_RECIP_CLB = 2
 HCCS_CAUSAL = 4
+HCCS_RECIP_REAL = 8
+
+HCCS_I32, HCCS_F32, HCCS_BF16, HCCS_F16 = 0, 1, 2, 3
+HCCS_ROPE_NONE, HCCS_ROPE_LINEAR, HCCS_ROPE_BASE, HCCS_ROPE_WAVELENGTH, HCCS_ROPE_DIMENSION = 0, 1, 2, 3, 4
+HCCS_MAX_CACHE_HEADS = 256
+HCCS_MAX_CACHE_KEYS = 131072
+HCCS_MAX_ROT_DIM = 128
 
 EXPORTS = ("hccs_create", "hccs_destroy", "hccs_params_check", "hccs_params_upload", "hccs_forward",
            "hccs_forward_keylen", "hccs_forward_host",
            "hccs_attention_fused", "hccs_attention_fused_keylen", "hccs_attention_fused_f32", "hccs_attention_fused_i8", "hccs_device_status", "hccs_last_cuda_error", "hccs_status_string",
-           "hccs_launch_count", "hccs_forward_static_scratch", "hccs_calibrate", "hccs_debug_wait_timeout")
+           "hccs_launch_count", "hccs_forward_static_scratch", "hccs_calibrate", "hccs_debug_wait_timeout",
+           "hccs_rope_frequencies", "hccs_cache_write", "hccs_cache_read", "hccs_params_upload_wide", "hccs_attention_cached")
 
 _vp, _i32, _u32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint32
 
@@ -83,6 +92,52 @@ _lib.hccs_debug_wait_timeout.restype = ctypes.c_int
 _lib.hccs_forward_static_scratch.argtypes = [_vp, _i32, _i32, _i32, _vp, _vp, _i32, _i32, _i32, _i32, _u32,
                                              ctypes.POINTER(_u32), _vp]
 _lib.hccs_forward_static_scratch.restype = ctypes.c_int
+
+
+class Rope(ctypes.Structure):
+    """``hccs_rope_t``: rotary frequencies in radians per position, one per pair of rotated dims."""
+    _fields_ = [("rot_dim", _i32), ("interleaved", _i32), ("scale", ctypes.c_double),
+                ("freq", ctypes.c_double * (HCCS_MAX_ROT_DIM // 2))]
+
+    def __init__(self, freq=(), interleaved: bool = False, scale: float = 1.0):
+        freq = [float(f) for f in freq]
+        if len(freq) > HCCS_MAX_ROT_DIM // 2:
+            raise ValueError(f"at most {HCCS_MAX_ROT_DIM // 2} frequencies, got {len(freq)}")
+        super().__init__(2 * len(freq), int(bool(interleaved)), float(scale))
+        for i, f in enumerate(freq):
+            self.freq[i] = f
+
+
+class _RopeScaling(ctypes.Structure):
+    _fields_ = [("kind", _i32), ("factor", ctypes.c_double), ("low", ctypes.c_double), ("high", ctypes.c_double),
+                ("original_len", ctypes.c_double)]
+
+
+_i64 = ctypes.c_int64
+_lib.hccs_rope_frequencies.argtypes = [ctypes.POINTER(Rope), _i32, _i32, ctypes.c_double, ctypes.POINTER(_RopeScaling)]
+_lib.hccs_rope_frequencies.restype = ctypes.c_int
+_lib.hccs_cache_write.argtypes = [_vp, _vp, _vp, _vp, ctypes.c_int, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
+                                  _i32, _i32, _i32, _i32, _i32, _i32, _vp]
+_lib.hccs_cache_write.restype = ctypes.c_int
+_lib.hccs_cache_read.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, ctypes.c_int, _i32, _i32, _i32, _i32, _i32, _i32,
+                                 _i32, _i32, _vp]
+_lib.hccs_cache_read.restype = ctypes.c_int
+_lib.hccs_params_upload_wide.argtypes = [_vp, _vp, _i32, _i32, ctypes.POINTER(_i32), _vp]
+_lib.hccs_params_upload_wide.restype = ctypes.c_int
+_lib.hccs_attention_cached.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _vp, _i32, _vp, _vp, ctypes.c_int,
+                                       _i32, _i32, _i32, _i32, _i32, _i32, _i32, _i32, _i32, _i32, _u32, _vp]
+_lib.hccs_attention_cached.restype = ctypes.c_int
+
+
+def hccs_rope_frequencies(rot_dim: int, base: float = 10000.0, interleaved: bool = False, kind: int = HCCS_ROPE_NONE,
+                          factor: float = 1.0, low: float = 1.0, high: float = 4.0, original_len: float = 8192.0) -> Rope:
+    """A :class:`Rope` with the frequencies base^(-2i/rot_dim), changed for longer contexts as ``kind`` says."""
+    rope = Rope()
+    sc = _RopeScaling(int(kind), float(factor), float(low), float(high), float(original_len))
+    st = _lib.hccs_rope_frequencies(ctypes.byref(rope), int(rot_dim), int(bool(interleaved)), float(base), ctypes.byref(sc))
+    if st != HCCS_OK:
+        raise HccsError(st, "hccs_rope_frequencies")
+    return rope
 
 
 class _CalibGrid(ctypes.Structure):
@@ -272,11 +327,140 @@ class Context:
         if st != HCCS_OK:
             raise HccsError(st, "hccs_attention_fused_i8")
 
+    # -- hccs_params_upload_wide
+    def hccs_params_upload_wide(self, params, n_design: int, stream=None) -> None:
+        arr = np.ascontiguousarray(params, dtype=np.int32).reshape(-1, 3)
+        bad = _i32(-1)
+        st = _lib.hccs_params_upload_wide(self._h, arr.ctypes.data_as(_vp), arr.shape[0], int(n_design),
+                                          ctypes.byref(bad), self._stream(stream))
+        if st != HCCS_OK:
+            raise HccsError(st, "hccs_params_upload_wide", f"(head {bad.value})" if bad.value >= 0 else "")
+
+    # -- hccs_cache_write
+    def hccs_cache_write(self, q, k, v, q8, k_pages, v_pages, positions, slots, q_step, k_step, v_step,
+                         rope: Rope | None = None, stream=None) -> None:
+        """Rotates and quantises tokens: q [T,Hq,d] to q8, k and v [T,Hkv,d] into the pools at ``slots``.  q (with q8 and
+        q_step) may be None, or k and v (with the pools, the slots and their steps).  q, k and v may be views whose tokens
+        are any multiple of 16 bytes apart."""
+        some = q if q is not None else k
+        if some is None:
+            raise ValueError("q or k and v must be given")
+        T, _, d = some.shape
+        Hq = Hkv = pages = size = 0
+        strides = [0, 0, 0]
+        for n, (name, t) in enumerate((("q", q), ("k", k), ("v", v))):
+            if t is None:
+                continue
+            self._on_device(t, name)
+            if t.dtype != some.dtype or t.dim() != 3 or t.shape[0] != T or t.shape[2] != d:
+                raise ValueError(f"{name} must be [{T}, heads, {d}] of {some.dtype}, got {tuple(t.shape)} of {t.dtype}")
+            if t.numel() and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != d)):
+                raise ValueError(f"{name} must be contiguous inside a token")
+            strides[n] = t.stride(0)
+        if q is not None:
+            Hq = q.shape[1]
+            self._check(q8, "q8", 1, (T, Hq, d))
+            q_step = _floats(q_step, "q_step", Hq)
+        if (k is None) != (v is None):
+            raise ValueError("k and v go together")
+        if k is not None:
+            Hkv = k.shape[1]
+            pages, _, size, _ = k_pages.shape
+            if v.shape != k.shape:
+                raise ValueError("k and v must have one shape")
+            self._check(k_pages, "k_pages", 1, (pages, Hkv, size, d))
+            self._check(v_pages, "v_pages", 1, (pages, Hkv, size, d))
+            self._check(slots, "slots", 8, (T,))
+            k_step, v_step = _floats(k_step, "k_step", Hkv), _floats(v_step, "v_step", Hkv)
+        if positions is not None:
+            self._check(positions, "positions", 4, (T,))
+        st = _lib.hccs_cache_write(
+            self._h, _ptr(q), _ptr(k), _ptr(v), _type_of(some), strides[0], strides[1], strides[2], _ptr(positions),
+            _ptr(slots) if k is not None else None, ctypes.byref(rope) if rope is not None else None,
+            _host(q_step) if q is not None else None, _host(k_step) if k is not None else None,
+            _host(v_step) if k is not None else None, _ptr(q8) if q is not None else None,
+            _ptr(k_pages) if k is not None else None, _ptr(v_pages) if k is not None else None,
+            T, Hq, Hkv, d, pages, size, self._stream(stream))
+        if st != HCCS_OK:
+            raise HccsError(st, "hccs_cache_write")
+
+    # -- hccs_cache_read
+    def hccs_cache_read(self, k_pages, v_pages, page_table, out_start, k_out, v_out, k_step, v_step, max_len: int,
+                        stream=None) -> None:
+        """Values of the sequences of ``page_table`` [B,max_pages]: token j of sequence b to row out_start[b] + j of k_out and
+        v_out [rows,Hkv,d] (either may be None)."""
+        pages, Hkv, size, d = k_pages.shape
+        B, max_pages = page_table.shape
+        some = k_out if k_out is not None else v_out
+        if some is None:
+            raise ValueError("k_out or v_out must be given")
+        rows = some.shape[0]
+        self._check(k_pages, "k_pages", 1)
+        self._check(v_pages, "v_pages", 1, k_pages.shape)
+        self._check(page_table, "page_table", 4)
+        self._check(out_start, "out_start", 4, (B + 1,))
+        for name, t in (("k_out", k_out), ("v_out", v_out)):
+            if t is not None:
+                self._check(t, name, some.element_size(), (rows, Hkv, d))
+                if t.dtype != some.dtype:
+                    raise ValueError("k_out and v_out must have one type")
+        st = _lib.hccs_cache_read(self._h, _ptr(k_pages), _ptr(v_pages), _ptr(page_table), _ptr(out_start),
+                                  _host(_floats(k_step, "k_step", Hkv)), _host(_floats(v_step, "v_step", Hkv)),
+                                  _ptr(k_out), _ptr(v_out), _type_of(some), B, max_pages, int(max_len), rows, Hkv, d, pages,
+                                  size, self._stream(stream))
+        if st != HCCS_OK:
+            raise HccsError(st, "hccs_cache_read")
+
+    # -- hccs_attention_cached
+    def hccs_attention_cached(self, Q, k_pages, v_pages, page_table, q_start, kv_len, O, requant_mult, requant_shift: int,
+                              max_q: int, max_kv: int, tree_mask=None, out_scale=None, flags: int = 0, stream=None) -> None:
+        """HCCS attention of the new tokens Q [T,Hq,d] over the cache.  O [T,Hq,d] is int32 (no out_scale), or float32,
+        bfloat16 or float16."""
+        T, Hq, d = Q.shape
+        pages, Hkv, size, dk = k_pages.shape
+        B, max_pages = page_table.shape
+        if dk != d:
+            raise ValueError(f"the cache holds heads of {dk}, Q of {d}")
+        self._check(Q, "Q", 1)
+        self._check(k_pages, "k_pages", 1)
+        self._check(v_pages, "v_pages", 1, k_pages.shape)
+        self._check(page_table, "page_table", 4)
+        self._check(q_start, "q_start", 4, (B + 1,))
+        self._check(kv_len, "kv_len", 4, (B,))
+        self._check(O, "O", O.element_size(), Q.shape)
+        words = 0
+        if tree_mask is not None:
+            words = tree_mask.shape[-1]
+            self._check(tree_mask, "tree_mask", 4, (T, words))
+        mult = _ints(requant_mult, "requant_mult", Hq)
+        scale = _floats(out_scale, "out_scale", Hq) if out_scale is not None else None
+        st = _lib.hccs_attention_cached(self._h, _ptr(Q), _ptr(k_pages), _ptr(v_pages), _ptr(page_table), _ptr(q_start),
+                                        _ptr(kv_len), _ptr(tree_mask), words, _host(mult), int(requant_shift),
+                                        _host(scale) if scale is not None else None, _ptr(O), _type_of(O), T, B, Hq, Hkv, d,
+                                        max_pages, pages, size, int(max_q), int(max_kv), int(flags), self._stream(stream))
+        if st != HCCS_OK:
+            raise HccsError(st, "hccs_attention_cached")
+
+    # The cache calls run on the context's device: its current stream, and tensors that live there.
+    def _stream(self, stream):
+        if stream is None:
+            import torch
+            return _vp(torch.cuda.current_stream(self.device).cuda_stream)
+        return _stream_ptr(stream)
+
+    def _on_device(self, t, name):
+        if t.device.type != "cuda" or t.device.index != self.device:
+            raise ValueError(f"{name} must live on cuda:{self.device}, not {t.device}")
+
+    def _check(self, t, name, itemsize, shape=None):
+        self._on_device(t, name)
+        _check_tensor(t, name, itemsize, shape)
+
     # -- hccs_device_status / hccs_last_cuda_error / hccs_launch_count
     def hccs_device_status(self, stream=None) -> int:
         w = _u32(0)
         st = _lib.hccs_device_status(self._h, ctypes.byref(w), _stream_ptr(stream))
-        if st not in (HCCS_OK, HCCS_ERR_DEVICE_TIMEOUT):
+        if st not in (HCCS_OK, HCCS_ERR_DEVICE_TIMEOUT, HCCS_ERR_DEVICE_INDEX):
             raise HccsError(st, "hccs_device_status")
         return int(w.value)
 
@@ -310,6 +494,33 @@ def hccs_forward_static_scratch(params, n_design: int, logits, probs, flags: int
     if st != HCCS_OK:
         raise HccsError(st, "hccs_forward_static_scratch")
     return int(word.value)
+
+
+def _type_of(t) -> int:
+    import torch
+    kinds = {torch.int32: HCCS_I32, torch.float32: HCCS_F32, torch.bfloat16: HCCS_BF16, torch.float16: HCCS_F16}
+    if t.dtype not in kinds:
+        raise ValueError(f"int32, float32, bfloat16 or float16 is wanted, got {t.dtype}")
+    return kinds[t.dtype]
+
+
+def _array(v, name, n, dtype):
+    arr = np.ascontiguousarray(v, dtype=dtype).reshape(-1)
+    if arr.size != n:
+        raise ValueError(f"{name} must have {n} entries, got {arr.size}")
+    return arr
+
+
+def _floats(v, name, n):
+    return _array(v, name, n, np.float32)
+
+
+def _ints(v, name, n):
+    return _array(v, name, n, np.int32)
+
+
+def _host(arr):
+    return arr.__array_interface__["data"][0]
 
 
 def _check_tensor(t, name, itemsize, shape=None, device="cuda"):

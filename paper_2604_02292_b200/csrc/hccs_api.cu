@@ -1,5 +1,6 @@
 // C ABI of libhccs: context, parameter-table validation and upload, argument checks, dispatch.
 #include <cuda_runtime.h>
+#include <math.h>
 #include <stdint.h>
 #include <string.h>
 
@@ -20,6 +21,7 @@ struct hccs_ctx {
     int32_t num_heads = 0;                  // 0 = nothing uploaded
     int32_t n_design = 0;
     int32_t out_shift = 0;
+    bool wide = false;                      // the table came from hccs_params_upload_wide
     uint32_t *d_status = nullptr;           // device status word (bounded waits report here)
     uint32_t *h_status = nullptr;           // pinned landing place for it
     cudaEvent_t table_copied = nullptr;     // the staging buffers may be rewritten after this
@@ -120,7 +122,7 @@ hccs_status_t check_forward_args(hccs_ctx *ctx, const void *in, const void *out,
     if (flags & ~7u) return HCCS_ERR_INVALID_ARG;
     if (ctx->num_heads == 0) return HCCS_ERR_NOT_UPLOADED;
     if (H != ctx->num_heads) return HCCS_ERR_INVALID_ARG;
-    if (Lk > ctx->n_design) return HCCS_ERR_CONSTRAINT;
+    if (ctx->wide || Lk > ctx->n_design) return HCCS_ERR_CONSTRAINT;
     const int64_t rows = (int64_t)B * H * Lq;
     if (rows >= (1ll << 31)) return HCCS_ERR_UNSUPPORTED;
     if (rows * Lk != 0 && (!in || !out)) return HCCS_ERR_INVALID_ARG;
@@ -217,14 +219,9 @@ hccs_status_t hccs_params_check(const hccs_head_params_t *params, int32_t num_he
     return HCCS_OK;
 }
 
-hccs_status_t hccs_params_upload(hccs_ctx_t *ctx, const hccs_head_params_t *params,
-                                 int32_t num_heads, int32_t n_design, int32_t out_shift,
-                                 int32_t *bad_head, void *cuda_stream) {
-    if (bad_head) *bad_head = -1;
-    if (!ctx) return HCCS_ERR_INVALID_ARG;
-    if (out_shift < 0 || out_shift > 8) return HCCS_ERR_INVALID_ARG;
-    hccs_status_t chk = hccs_params_check(params, num_heads, n_design, bad_head);
-    if (chk != HCCS_OK) return chk;
+// The checked table goes up on `stream`, and the context takes it.
+static hccs_status_t upload_table(hccs_ctx_t *ctx, const hccs_head_params_t *params, int32_t num_heads,
+                                  int32_t n_design, int32_t out_shift, bool wide, void *cuda_stream) {
     DeviceGuard g(ctx->device);
     if (!g.ok) return cuda_fail(ctx, cudaErrorInvalidDevice);
     hccs_status_t st = ensure_capacity(ctx, num_heads);
@@ -246,7 +243,34 @@ hccs_status_t hccs_params_upload(hccs_ctx_t *ctx, const hccs_head_params_t *para
     ctx->num_heads = num_heads;
     ctx->n_design = n_design;
     ctx->out_shift = out_shift;
+    ctx->wide = wide;
     return HCCS_OK;
+}
+
+hccs_status_t hccs_params_upload(hccs_ctx_t *ctx, const hccs_head_params_t *params,
+                                 int32_t num_heads, int32_t n_design, int32_t out_shift,
+                                 int32_t *bad_head, void *cuda_stream) {
+    if (bad_head) *bad_head = -1;
+    if (!ctx) return HCCS_ERR_INVALID_ARG;
+    if (out_shift < 0 || out_shift > 8) return HCCS_ERR_INVALID_ARG;
+    hccs_status_t chk = hccs_params_check(params, num_heads, n_design, bad_head);
+    if (chk != HCCS_OK) return chk;
+    return upload_table(ctx, params, num_heads, n_design, out_shift, false, cuda_stream);
+}
+
+hccs_status_t hccs_params_upload_wide(hccs_ctx_t *ctx, const hccs_head_params_t *params, int32_t num_heads,
+                                      int32_t n_design, int32_t *bad_head, void *cuda_stream) {
+    if (bad_head) *bad_head = -1;
+    if (!ctx || !params || num_heads < 1 || num_heads > HCCS_MAX_CACHE_HEADS) return HCCS_ERR_INVALID_ARG;
+    if (n_design < 1 || n_design > HCCS_MAX_CACHE_KEYS) return HCCS_ERR_INVALID_ARG;
+    for (int32_t h = 0; h < num_heads; ++h) {
+        const int64_t B = params[h].B, S = params[h].S, D = params[h].Dmax;
+        if (D < 1 || D > 127 || S < 0 || S > 127 || B < 1 || B > 32767 || B - S * D < 0) {
+            if (bad_head) *bad_head = h;
+            return HCCS_ERR_CONSTRAINT;
+        }
+    }
+    return upload_table(ctx, params, num_heads, n_design, 0, true, cuda_stream);
 }
 
 hccs_status_t hccs_forward(hccs_ctx_t *ctx, const int8_t *logits, void *probs,
@@ -348,7 +372,7 @@ static hccs_status_t fused_common(hccs_ctx_t *ctx, const int8_t *Q, const int8_t
     // the kernel requantises with the multiplier pre-shifted by 32 - requant_shift bits
     for (int32_t h = 0; h < H; ++h)
         if ((int64_t)requant_mult[h] << (32 - requant_shift) >= (1ll << 31)) return HCCS_ERR_UNSUPPORTED;
-    if (L > ctx->n_design) return HCCS_ERR_CONSTRAINT;
+    if (ctx->wide || L > ctx->n_design) return HCCS_ERR_CONSTRAINT;
     if ((int64_t)B * H * L * d == 0) return HCCS_OK;
     if (!Q || !K || !V || !O) return HCCS_ERR_INVALID_ARG;
     if (!hccs::fused_shape_supported(L, d)) return HCCS_ERR_UNSUPPORTED;
@@ -477,7 +501,211 @@ hccs_status_t hccs_device_status(hccs_ctx_t *ctx, uint32_t *word, void *cuda_str
     HCCS_CUDA(ctx, cudaStreamSynchronize(stream));
     const uint32_t w = *ctx->h_status;
     if (word) *word = w;
-    return w ? HCCS_ERR_DEVICE_TIMEOUT : HCCS_OK;
+    if (w & (hccs::STATUS_ROW_TMA_TIMEOUT | hccs::STATUS_FUSED_TIMEOUT)) return HCCS_ERR_DEVICE_TIMEOUT;
+    return w ? HCCS_ERR_DEVICE_INDEX : HCCS_OK;
+}
+
+// ---- generation over an int8 cache
+
+static bool cache_shape(int32_t Hkv, int32_t d, int32_t num_pages, int32_t page_size, int32_t *page_shift) {
+    if (Hkv < 1 || Hkv > HCCS_MAX_CACHE_HEADS || num_pages < 1 || page_size < 16 || page_size > 65536) return false;
+    if ((page_size & (page_size - 1)) != 0) return false;
+    *page_shift = 0;
+    while ((1 << *page_shift) < page_size) ++*page_shift;
+    return d == 64 || d == 128;
+}
+
+static bool steps_ok(const float *s, int32_t n) {
+    if (!s) return false;
+    for (int32_t i = 0; i < n; ++i)
+        if (!(s[i] > 0.0f) || !isfinite(s[i])) return false;
+    return true;
+}
+
+static bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
+
+hccs_status_t hccs_rope_frequencies(hccs_rope_t *rope, int32_t rot_dim, int32_t interleaved, double base,
+                                    const hccs_rope_scaling_t *scaling) {
+    if (!rope || rot_dim < 2 || rot_dim > HCCS_MAX_ROT_DIM || (rot_dim & 1)) return HCCS_ERR_INVALID_ARG;
+    if (!(base > 1.0) || !isfinite(base)) return HCCS_ERR_INVALID_ARG;
+    const int32_t kind = scaling ? scaling->kind : HCCS_ROPE_NONE;
+    const double factor = kind == HCCS_ROPE_NONE ? 1.0 : scaling->factor;
+    if (kind < HCCS_ROPE_NONE || kind > HCCS_ROPE_DIMENSION || !(factor >= 1.0) || !isfinite(factor)) return HCCS_ERR_INVALID_ARG;
+    if (kind == HCCS_ROPE_BASE && rot_dim <= 2) return HCCS_ERR_INVALID_ARG;
+    const bool mixed = kind == HCCS_ROPE_WAVELENGTH || kind == HCCS_ROPE_DIMENSION;
+    if (mixed && (!(scaling->low > 0.0) || !(scaling->high > scaling->low) || !isfinite(scaling->high) ||
+                  !(scaling->original_len > 0.0) || !isfinite(scaling->original_len)))
+        return HCCS_ERR_INVALID_ARG;
+    const double two_pi = 6.283185307179586476925;
+    if (kind == HCCS_ROPE_BASE) base *= pow(factor, (double)rot_dim / (rot_dim - 2));
+    double first = 0.0, last = 0.0;                  // DIMENSION: the pairs between which the mixture changes
+    if (kind == HCCS_ROPE_DIMENSION) {
+        first = floor(rot_dim * log(scaling->original_len / (scaling->high * two_pi)) / (2.0 * log(base)));
+        last = ceil(rot_dim * log(scaling->original_len / (scaling->low * two_pi)) / (2.0 * log(base)));
+        first = fmax(first, 0.0);
+        last = fmin(last, (double)(rot_dim - 1));
+        if (last <= first) last = first + 0.001;
+    }
+    rope->rot_dim = rot_dim;
+    rope->interleaved = interleaved ? 1 : 0;
+    rope->scale = kind == HCCS_ROPE_DIMENSION ? 0.1 * log(factor) + 1.0 : 1.0;
+    for (int32_t i = 0; i < HCCS_MAX_ROT_DIM / 2; ++i) {
+        if (i >= rot_dim / 2) { rope->freq[i] = 0.0; continue; }
+        double f = pow(base, -2.0 * i / rot_dim);
+        if (kind == HCCS_ROPE_LINEAR) f /= factor;
+        if (mixed) {
+            double keep;
+            if (kind == HCCS_ROPE_WAVELENGTH)
+                keep = (scaling->original_len * f / two_pi - scaling->low) / (scaling->high - scaling->low);
+            else
+                keep = 1.0 - (i - first) / (last - first);
+            keep = fmin(fmax(keep, 0.0), 1.0);
+            f = f * keep + f / factor * (1.0 - keep);
+        }
+        rope->freq[i] = f;
+    }
+    return HCCS_OK;
+}
+
+hccs_status_t hccs_cache_write(hccs_ctx_t *ctx, const void *q, const void *k, const void *v, hccs_type_t type,
+                               int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                               const int32_t *positions, const int64_t *slots, const hccs_rope_t *rope,
+                               const float *q_step, const float *k_step, const float *v_step,
+                               int8_t *q8, int8_t *k_pages, int8_t *v_pages,
+                               int32_t T, int32_t Hq, int32_t Hkv, int32_t d,
+                               int32_t num_pages, int32_t page_size, void *cuda_stream) {
+    if (T < 0) return HCCS_ERR_INVALID_ARG;
+    if (type != HCCS_F32 && type != HCCS_BF16 && type != HCCS_F16) return HCCS_ERR_INVALID_ARG;
+    const bool with_q = q != nullptr, with_kv = k != nullptr;
+    if ((k == nullptr) != (v == nullptr)) return HCCS_ERR_INVALID_ARG;
+    int32_t page_shift = 0;
+    if (d != 64 && d != 128) return HCCS_ERR_UNSUPPORTED;
+    if (with_kv && !cache_shape(Hkv, d, num_pages, page_size, &page_shift)) return HCCS_ERR_INVALID_ARG;
+    if (with_q && (Hq < 1 || Hq > HCCS_MAX_CACHE_HEADS)) return HCCS_ERR_INVALID_ARG;
+    if (with_q && !steps_ok(q_step, Hq)) return HCCS_ERR_INVALID_ARG;
+    if (with_kv && (!steps_ok(k_step, Hkv) || !steps_ok(v_step, Hkv))) return HCCS_ERR_INVALID_ARG;
+    if (rope) {
+        if (rope->rot_dim < 0 || rope->rot_dim > d || (rope->rot_dim & 1) || !isfinite(rope->scale)) return HCCS_ERR_INVALID_ARG;
+        for (int32_t i = 0; i < rope->rot_dim / 2; ++i)
+            if (!isfinite(rope->freq[i])) return HCCS_ERR_INVALID_ARG;
+    }
+    const bool turns = rope && rope->rot_dim > 0;
+    if (T == 0 || (!with_q && !with_kv)) return ctx ? HCCS_OK : HCCS_ERR_INVALID_ARG;
+    if ((turns && !positions) || (with_q && !q8) || (with_kv && (!slots || !k_pages || !v_pages))) return HCCS_ERR_INVALID_ARG;
+    const int64_t esz = type == HCCS_F32 ? 4 : 2;
+    if (with_q && (!aligned16(q) || !aligned16(q8) || (q_stride * esz) % 16 != 0)) return HCCS_ERR_UNSUPPORTED;
+    if (with_kv && (!aligned16(k) || !aligned16(v) || !aligned16(k_pages) || !aligned16(v_pages) ||
+                    (k_stride * esz) % 16 != 0 || (v_stride * esz) % 16 != 0))
+        return HCCS_ERR_UNSUPPORTED;
+    if (!ctx) return HCCS_ERR_INVALID_ARG;
+    DeviceGuard g(ctx->device);
+    if (!g.ok) return cuda_fail(ctx, cudaErrorInvalidDevice);
+    hccs::CacheWriteArgs a;
+    memset(&a, 0, sizeof(a));
+    a.q = q; a.k = k; a.v = v;
+    a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride;
+    a.positions = positions; a.slots = slots;
+    a.q8 = q8; a.k_pages = k_pages; a.v_pages = v_pages;
+    a.status = ctx->d_status;
+    a.num_slots = with_kv ? (int64_t)num_pages * page_size : 0;
+    a.T = T; a.Hq = with_q ? Hq : 0; a.Hkv = with_kv ? Hkv : 0; a.d = d; a.page_shift = page_shift;
+    if (turns) a.rope = *rope;
+    if (with_q) memcpy(a.step, q_step, sizeof(float) * Hq);
+    if (with_kv) {
+        memcpy(a.step + HCCS_MAX_CACHE_HEADS, k_step, sizeof(float) * Hkv);
+        memcpy(a.step + 2 * HCCS_MAX_CACHE_HEADS, v_step, sizeof(float) * Hkv);
+    }
+    HCCS_CUDA(ctx, hccs::launch_cache_write(a, type, (cudaStream_t)cuda_stream, &ctx->launches));
+    return HCCS_OK;
+}
+
+hccs_status_t hccs_cache_read(hccs_ctx_t *ctx, const int8_t *k_pages, const int8_t *v_pages,
+                              const int32_t *page_table, const int32_t *out_start,
+                              const float *k_step, const float *v_step, void *k_out, void *v_out, hccs_type_t type,
+                              int32_t B, int32_t max_pages, int32_t max_len, int32_t rows, int32_t Hkv, int32_t d,
+                              int32_t num_pages, int32_t page_size, void *cuda_stream) {
+    if (B < 0 || max_pages < 0 || max_len < 0 || rows < 0) return HCCS_ERR_INVALID_ARG;
+    if (type != HCCS_F32 && type != HCCS_BF16 && type != HCCS_F16) return HCCS_ERR_INVALID_ARG;
+    if (d != 64 && d != 128) return HCCS_ERR_UNSUPPORTED;
+    int32_t page_shift = 0;
+    if (!cache_shape(Hkv, d, num_pages, page_size, &page_shift)) return HCCS_ERR_INVALID_ARG;
+    if ((k_out && (!k_pages || !steps_ok(k_step, Hkv))) || (v_out && (!v_pages || !steps_ok(v_step, Hkv)))) return HCCS_ERR_INVALID_ARG;
+    if (B > 65535) return HCCS_ERR_UNSUPPORTED;
+    if (B == 0 || max_len == 0 || rows == 0 || (!k_out && !v_out)) return ctx ? HCCS_OK : HCCS_ERR_INVALID_ARG;
+    if (!page_table || !out_start) return HCCS_ERR_INVALID_ARG;
+    if (!aligned16(k_pages) || !aligned16(v_pages) || !aligned16(k_out) || !aligned16(v_out)) return HCCS_ERR_UNSUPPORTED;
+    if (!ctx) return HCCS_ERR_INVALID_ARG;
+    DeviceGuard g(ctx->device);
+    if (!g.ok) return cuda_fail(ctx, cudaErrorInvalidDevice);
+    hccs::CacheReadArgs a;
+    memset(&a, 0, sizeof(a));
+    a.k_pages = k_pages; a.v_pages = v_pages;
+    a.page_table = page_table; a.out_start = out_start;
+    a.k_out = k_out; a.v_out = v_out;
+    a.status = ctx->d_status;
+    a.B = B; a.max_pages = max_pages; a.max_len = max_len; a.rows = rows;
+    a.Hkv = Hkv; a.d = d; a.num_pages = num_pages; a.page_shift = page_shift;
+    if (k_out) memcpy(a.step, k_step, sizeof(float) * Hkv);
+    if (v_out) memcpy(a.step + HCCS_MAX_CACHE_HEADS, v_step, sizeof(float) * Hkv);
+    HCCS_CUDA(ctx, hccs::launch_cache_read(a, type, (cudaStream_t)cuda_stream, &ctx->launches));
+    return HCCS_OK;
+}
+
+hccs_status_t hccs_attention_cached(hccs_ctx_t *ctx, const int8_t *Q, const int8_t *k_pages, const int8_t *v_pages,
+                                    const int32_t *page_table, const int32_t *q_start, const int32_t *kv_len,
+                                    const int32_t *tree_mask, int32_t tree_words,
+                                    const int32_t *requant_mult, int32_t requant_shift, const float *out_scale,
+                                    void *O, hccs_type_t out_type,
+                                    int32_t T, int32_t B, int32_t Hq, int32_t Hkv, int32_t d, int32_t max_pages,
+                                    int32_t num_pages, int32_t page_size, int32_t max_q, int32_t max_kv,
+                                    uint32_t flags, void *cuda_stream) {
+    // what needs no context first
+    if (T < 0 || B < 0 || max_pages < 0 || max_q < 0 || max_kv < 0) return HCCS_ERR_INVALID_ARG;
+    if (flags != HCCS_RECIP_DIV && flags != HCCS_RECIP_CLB && flags != HCCS_RECIP_REAL) return HCCS_ERR_INVALID_ARG;
+    if (out_type != HCCS_I32 && out_type != HCCS_F32 && out_type != HCCS_BF16 && out_type != HCCS_F16) return HCCS_ERR_INVALID_ARG;
+    if (out_type == HCCS_I32 ? (flags == HCCS_RECIP_REAL || out_scale) : !out_scale) return HCCS_ERR_INVALID_ARG;
+    if (d != 64 && d != 128) return HCCS_ERR_UNSUPPORTED;
+    int32_t page_shift = 0;
+    if (!requant_mult || Hq < 1 || !cache_shape(Hkv, d, num_pages, page_size, &page_shift) || Hq % Hkv != 0) return HCCS_ERR_INVALID_ARG;
+    if (Hq > HCCS_MAX_CACHE_HEADS || B > 65535 || max_kv > HCCS_MAX_CACHE_KEYS) return HCCS_ERR_UNSUPPORTED;
+    if ((int64_t)max_q * (Hq / Hkv) > (1ll << 30)) return HCCS_ERR_UNSUPPORTED;
+    if (requant_shift < 1 || requant_shift > 24) return HCCS_ERR_INVALID_ARG;
+    for (int32_t h = 0; h < Hq; ++h)
+        if (requant_mult[h] < 0 || requant_mult[h] >= (1 << 13)) return HCCS_ERR_INVALID_ARG;
+    for (int32_t h = 0; h < Hq; ++h)      // the steps of the requantisation stay below one
+        if ((int64_t)requant_mult[h] >= (1ll << (requant_shift - 1))) return HCCS_ERR_UNSUPPORTED;
+    if (out_scale)
+        for (int32_t h = 0; h < Hq; ++h)
+            if (!isfinite(out_scale[h])) return HCCS_ERR_INVALID_ARG;
+    if (tree_mask && (tree_words < 1 || (int64_t)tree_words * 32 < max_q)) return HCCS_ERR_INVALID_ARG;
+    const bool empty = T == 0 || B == 0 || max_q == 0;
+    if (!empty && (!Q || !k_pages || !v_pages || !page_table || !q_start || !kv_len || !O)) return HCCS_ERR_INVALID_ARG;
+    if (!aligned16(Q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(O)) return HCCS_ERR_UNSUPPORTED;
+    if (!ctx) return HCCS_ERR_INVALID_ARG;
+    if (ctx->num_heads == 0) return HCCS_ERR_NOT_UPLOADED;
+    if (Hq != ctx->num_heads) return HCCS_ERR_INVALID_ARG;
+    if ((ctx->wide && flags != HCCS_RECIP_REAL) || max_kv > ctx->n_design) return HCCS_ERR_CONSTRAINT;
+    if (empty) return HCCS_OK;
+    DeviceGuard g(ctx->device);
+    if (!g.ok) return cuda_fail(ctx, cudaErrorInvalidDevice);
+    hccs::CachedAttnArgs a;
+    memset(&a, 0, sizeof(a));
+    a.Q = Q; a.k_pages = k_pages; a.v_pages = v_pages;
+    a.page_table = page_table; a.q_start = q_start; a.kv_len = kv_len; a.tree_mask = tree_mask;
+    a.O = O;
+    a.table = ctx->d_table;
+    a.status = ctx->d_status;
+    a.wait_cycles = hccs::kDefaultWaitCycles;
+    a.tree_words = tree_words; a.out_type = out_type; a.recip = (int32_t)flags;
+    a.T = T; a.B = B; a.Hq = Hq; a.Hkv = Hkv; a.group = Hq / Hkv; a.d = d;
+    a.max_pages = max_pages; a.num_pages = num_pages; a.page_shift = page_shift;
+    a.max_q = max_q; a.max_kv = max_kv; a.requant_shift = requant_shift;
+    for (int32_t h = 0; h < Hq; ++h) {
+        a.mult[h] = (uint16_t)requant_mult[h];
+        a.scale[h] = out_scale ? out_scale[h] : 1.0f;
+    }
+    HCCS_CUDA(ctx, hccs::launch_cached_attention(a, (cudaStream_t)cuda_stream, &ctx->launches));
+    return HCCS_OK;
 }
 
 hccs_status_t hccs_debug_wait_timeout(hccs_ctx_t *ctx, int32_t mode, int64_t limit_cycles, void *cuda_stream) {
@@ -503,6 +731,7 @@ const char *hccs_status_string(hccs_status_t status) {
         case HCCS_ERR_UNSUPPORTED: return "HCCS_ERR_UNSUPPORTED";
         case HCCS_ERR_CUDA: return "HCCS_ERR_CUDA";
         case HCCS_ERR_DEVICE_TIMEOUT: return "HCCS_ERR_DEVICE_TIMEOUT";
+        case HCCS_ERR_DEVICE_INDEX: return "HCCS_ERR_DEVICE_INDEX";
     }
     return "HCCS_<unknown status>";
 }

@@ -42,6 +42,9 @@ struct RowArgs {
 enum : uint32_t {
     STATUS_ROW_TMA_TIMEOUT = 1u,     // CTA-per-row kernel: a bulk copy never completed
     STATUS_FUSED_TIMEOUT = 2u,       // fused kernel: an mbarrier wait gave up
+    STATUS_BAD_SLOT = 4u,            // cache write: a slot beyond the pools
+    STATUS_BAD_PAGE = 8u,            // cache read and cached attention: a page outside the pools
+    STATUS_BAD_LENGTH = 16u,         // cache read and cached attention: a length beyond its bound
 };
 
 struct FusedArgs {
@@ -59,6 +62,47 @@ struct FusedArgs {
     int32_t out_shift;
     uint32_t flags;
 };
+
+// ---- generation over an int8 cache (hccs_cache.cu, hccs_cached_*.cu).  What a call takes from host arrays
+// travels by value in the kernel's arguments, so that a captured graph holds it.
+struct CacheWriteArgs {
+    const void *q, *k, *v;
+    int64_t q_stride, k_stride, v_stride;       // elements between tokens
+    const int32_t *positions;
+    const int64_t *slots;
+    int8_t *q8, *k_pages, *v_pages;
+    uint32_t *status;
+    int64_t num_slots;                          // num_pages * page_size
+    int32_t T, Hq, Hkv, d, page_shift;
+    hccs_rope_t rope;                           // rot_dim 0: none
+    float step[3 * HCCS_MAX_CACHE_HEADS];       // q, k and v, HCCS_MAX_CACHE_HEADS apart
+};
+
+struct CacheReadArgs {
+    const int8_t *k_pages, *v_pages;
+    const int32_t *page_table, *out_start;
+    void *k_out, *v_out;
+    uint32_t *status;
+    int32_t B, max_pages, max_len, rows, Hkv, d, num_pages, page_shift;
+    float step[2 * HCCS_MAX_CACHE_HEADS];       // k and v
+};
+
+struct CachedAttnArgs {
+    const int8_t *Q, *k_pages, *v_pages;
+    const int32_t *page_table, *q_start, *kv_len, *tree_mask;
+    void *O;
+    const HeadEntry *table;
+    uint32_t *status;
+    long long wait_cycles;
+    int32_t tree_words, out_type, recip;        // recip: HCCS_RECIP_*
+    int32_t T, B, Hq, Hkv, group, d, max_pages, num_pages, page_shift, max_q, max_kv, requant_shift;
+    uint16_t mult[HCCS_MAX_CACHE_HEADS];
+    float scale[HCCS_MAX_CACHE_HEADS];
+};
+
+cudaError_t launch_cache_write(const CacheWriteArgs &a, int type, cudaStream_t stream, uint64_t *launches);
+cudaError_t launch_cache_read(const CacheReadArgs &a, int type, cudaStream_t stream, uint64_t *launches);
+cudaError_t launch_cached_attention(const CachedAttnArgs &a, cudaStream_t stream, uint64_t *launches);
 
 // Launchers.  Each returns the CUDA error of the launch and adds to *launches.
 cudaError_t launch_rows(const int8_t *logits, void *probs, const RowArgs &a, uint32_t flags,
