@@ -368,7 +368,7 @@ hccs_status_t hccs_params_upload_wide(hccs_ctx_t *ctx, const hccs_head_params_t 
  *   O            device [T, Hq, d] of out_type; float types hold the fp32 product with out_scale[h], rounded
  *                once more to the type; HCCS_I32 goes with DIV and CLB only.  16-byte aligned
  *   max_q, max_kv (host)  bounds of the lengths of this call, which choose kernel and grid: queries beyond
- *                max_q are not computed and keys beyond max_kv are not seen, both reported.  max_kv beyond
+ *                max_q are not computed (nor are their keys seen by a tree), and keys beyond max_kv are not seen, both reported.  max_kv beyond
  *                n_design is HCCS_ERR_CONSTRAINT, beyond HCCS_MAX_CACHE_KEYS HCCS_ERR_UNSUPPORTED
  *   flags        one HCCS_RECIP_*; nothing else
  * kv_len outside 0 .. max_pages * page_size is cut and reported; a page outside 0..num_pages-1 is reported

@@ -1,0 +1,120 @@
+// What the kernels of HCCS attention over the int8 cache share.
+//
+// With r_j = max(x_j + D - m, 0) in 0..127 a score is s_j = F + S*r_j, F = B - S*D >= 0, so that
+//     Z = F*count + S*sum r,   sum s V = F*sum V + S*sum r V
+// hold exactly in integers: sum r V is an int8 x int8 contraction that never leaves int32
+// (127 * 128 * 131072 < 2^31), whatever the table, and sums of parts join without rounding.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "hccs_device.cuh"
+#include "hccs_internal.h"
+
+namespace hccs {
+
+// Where the new tokens and the keys of a sequence are.
+struct SequenceAt {
+    int s0, nq;        // first token, number of queries (those beyond max_q are not computed)
+    int n;             // keys that may be seen
+    int prefix;        // keys before the new ones (negative where there are fewer keys than queries)
+    bool cut;          // a length was beyond its bound
+};
+__device__ __forceinline__ SequenceAt sequence_at(const CachedAttnArgs &a, int b) {
+    SequenceAt q;
+    const int s0 = min(max(a.q_start[b], 0), a.T), s1 = min(max(a.q_start[b + 1], s0), a.T);
+    const int kv = a.kv_len[b];
+    const int pos = (int)max(min((int64_t)kv, (int64_t)a.max_pages << a.page_shift), (int64_t)0);
+    q.s0 = s0;
+    q.nq = s1 - s0;
+    q.n = min(pos, a.max_kv);
+    q.prefix = pos - q.nq;
+    q.cut = q.n != kv || q.nq > a.max_q;
+    return q;
+}
+
+// Requantisation of one head, x = clamp((acc*M + R) >> sh, -128, 127) with R = 2^(sh-1), as one clamp and one
+// multiply-add: with lo and hi the accumulators between which x moves from -128 to 127 (steps below one, so
+// both ends are reached) and k = 24 - sh, clamp(acc - lo, 0, hi - lo) * (M << k) + ((lo*M + R) << k) has x as
+// its (signed) top byte; every value fits 32 bits.  M = 0 gives x = 0.
+struct Requant {
+    uint32_t mk, ck;
+    int neg_lo, span;
+};
+constexpr int kAccLimit = 1 << 21;         // |acc| <= 128 * 128 * 128
+__device__ __forceinline__ Requant make_requant(int M, int sh) {
+    Requant q;
+    const int64_t R = 1ll << (sh - 1);
+    int lo = -kAccLimit, hi = kAccLimit;
+    if (M > 0) {
+        // floors of quotients below 2^32 by divisors below 2^13: exact through one fp64 division, whose
+        // error (2^-21) is below the distance of a fraction from the next integer (2^-13)
+        const double m = (double)M;
+        const double a = floor((double)((128ll << sh) + R) / m), b = floor((double)((128ll << sh) - 1 - R) / m);
+        if (a < (double)kAccLimit) lo = -(int)a;
+        if (b < (double)kAccLimit) hi = (int)b;
+    }
+    q.mk = (uint32_t)M << (24 - sh);
+    q.ck = (uint32_t)(uint64_t)(((int64_t)lo * M + R) << (24 - sh));
+    q.neg_lo = -lo;
+    q.span = hi - lo;
+    return q;
+}
+__device__ __forceinline__ uint32_t requant_top(const Requant &q, int acc) {
+    return (uint32_t)__viaddmin_s32_relu(acc, q.neg_lo, q.span) * q.mk + q.ck;
+}
+
+// One output value from num = sum s V and the row's Z (0: the row sees nothing): the integer of the int16
+// path, or its product with the scale, or num * (scale / Z); each step rounded once to fp32.
+struct RowFactor {
+    float scale;       // real: scale / Z; integer modes: the scale
+    int rho;           // integer modes
+};
+__device__ __forceinline__ RowFactor row_factor(const CachedAttnArgs &a, int64_t Z, float scale) {
+    RowFactor f;
+    f.rho = 0;
+    f.scale = 0.0f;
+    if (Z > 0) {
+        if (a.recip == HCCS_RECIP_REAL) {
+            f.scale = scale / (float)Z;
+        } else {
+            f.rho = (int)(a.recip == HCCS_RECIP_CLB ? reciprocal<true, true>((uint32_t)Z) : reciprocal<true, false>((uint32_t)Z));
+            f.scale = scale;
+        }
+    }
+    return f;
+}
+// Four neighbouring values; `at` is the index of the first.
+__device__ __forceinline__ void store_output4(const CachedAttnArgs &a, int64_t at, const int64_t (&num)[4], const RowFactor &f) {
+    int o[4];
+    float y[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if (a.recip == HCCS_RECIP_REAL) {
+            o[e] = 0;
+            y[e] = (float)num[e] * f.scale;
+        } else {
+            o[e] = (int)num[e] * f.rho;
+            y[e] = (float)o[e] * f.scale;
+        }
+    }
+    if (a.out_type == HCCS_I32) {
+        *reinterpret_cast<int4 *>(static_cast<int32_t *>(a.O) + at) = make_int4(o[0], o[1], o[2], o[3]);
+    } else if (a.out_type == HCCS_F32) {
+        *reinterpret_cast<float4 *>(static_cast<float *>(a.O) + at) = make_float4(y[0], y[1], y[2], y[3]);
+    } else {
+        uint2 w;
+        if (a.out_type == HCCS_BF16) {
+            __nv_bfloat162 lo = __floats2bfloat162_rn(y[0], y[1]), hi = __floats2bfloat162_rn(y[2], y[3]);
+            w = make_uint2(*reinterpret_cast<uint32_t *>(&lo), *reinterpret_cast<uint32_t *>(&hi));
+        } else {
+            __half2 lo = __floats2half2_rn(y[0], y[1]), hi = __floats2half2_rn(y[2], y[3]);
+            w = make_uint2(*reinterpret_cast<uint32_t *>(&lo), *reinterpret_cast<uint32_t *>(&hi));
+        }
+        *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.O) + at) = w;
+    }
+}
+
+}  // namespace hccs

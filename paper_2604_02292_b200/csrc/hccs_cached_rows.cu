@@ -52,7 +52,7 @@ __global__ void __launch_bounds__(kThreads) cached_rows_kernel(const __grid_cons
         bool seen = true;
         if (j >= prefix) {
             const int jj = j - prefix;
-            seen = a.tree_mask ? (jj < nq && jj < 32 * a.tree_words && ((a.tree_mask[(int64_t)t * a.tree_words + (jj >> 5)] >> (jj & 31)) & 1))
+            seen = a.tree_mask ? (jj < nq && jj < a.max_q && jj < 32 * a.tree_words && ((a.tree_mask[(int64_t)t * a.tree_words + (jj >> 5)] >> (jj & 31)) & 1))
                                : jj <= i;
         }
         const int page = table[j >> a.page_shift];
@@ -128,6 +128,11 @@ __global__ void __launch_bounds__(kThreads) cached_rows_kernel(const __grid_cons
 }  // namespace
 
 cudaError_t launch_cached_attention(const CachedAttnArgs &a, cudaStream_t stream, uint64_t *launches) {
+    if (a.max_q == 1) {
+        const cudaError_t e = launch_cached_decode(a, stream);
+        if (e == cudaSuccess && launches) ++*launches;
+        return e;
+    }
     const size_t smem = (size_t)a.max_kv + 16 + a.max_kv / 8 + 4;
     if (smem > 200 * 1024) return cudaErrorInvalidValue;
     cudaError_t e = cudaFuncSetAttribute(cached_rows_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);

@@ -102,6 +102,7 @@ struct CachedAttnArgs {
 
 cudaError_t launch_cache_write(const CacheWriteArgs &a, int type, cudaStream_t stream, uint64_t *launches);
 cudaError_t launch_cache_read(const CacheReadArgs &a, int type, cudaStream_t stream, uint64_t *launches);
+cudaError_t launch_cached_decode(const CachedAttnArgs &a, cudaStream_t stream);      // max_q == 1
 cudaError_t launch_cached_attention(const CachedAttnArgs &a, cudaStream_t stream, uint64_t *launches);
 
 // Launchers.  Each returns the CUDA error of the launch and adds to *launches.
