@@ -1,0 +1,534 @@
+// HCCS attention over the int8 cache for several new tokens per sequence: trees of drafted tokens, chunks of a
+// prompt.  A CTA owns 128 rows (query, head of the group) of one kv head and walks over blocks of 128 keys.
+//
+// The two contractions run on the tensor cores (tcgen05.mma kind::i8, accumulators in tensor memory), as in the
+// fused attention kernel.  There is no probability pass: r = max(x + D - m, 0) fits seven bits, so
+//     sum s V = F*sum V + S*sum r V
+// needs only r, which leaves the accumulators by one clamp, one multiply-add and a byte pick per logit; F and S
+// join at the end, where the sums are complete.  The clamp needs the row maximum first, so Q.K^T is computed
+// twice: once for the maximum of the raw accumulators (the requantisation is monotone), once for r.  sum V over
+// the keys a row sees is a contraction of its own, with the 0/1 bytes of the mask in the place of r.
+//
+// Roles: sixteen row warps (four threads per row, 32 keys of every block each; TMEM lane = row), two warps that copy
+// (cp.async, 16 bytes each: any page size, swizzled by hand into the layouts the tensor core wants), one thread
+// that issues Q.K^T and one that issues the two products with V.  K blocks of the first pass, then K and V blocks
+// in turn, stream through one ring; load number x uses slot x % kSlots.
+//
+// Few rows and many keys: the key blocks of a row tile are split over the CTAs of a cluster, which exchange row
+// maxima between the passes and sums at the end through distributed shared memory (exact integers: the split
+// changes no bit).  Row warps whose 32 rows lie behind the tile's last row do nothing.
+#include <cooperative_groups.h>
+
+#include "hccs_cached.cuh"
+#include "hccs_tcgen05.cuh"
+
+namespace hccs {
+
+namespace {
+
+namespace cg = cooperative_groups;
+
+constexpr int kRowThreads = 512, kCopyThreads = 64;
+constexpr int kCopyWarp = 16, kQkWarp = 18, kPvWarp = 19;
+constexpr int kThreads = 640;
+constexpr int kTile = 128;
+constexpr int kHalfBytes = kTile * 64;           // 128 rows x 64 bytes, 64-byte swizzle
+constexpr int kPanelBytes = kTile * 128;         // 128 rows x 128 keys, 128-byte swizzle
+constexpr int kSlots = 6;
+constexpr int kAhead = 3;                        // copies in flight
+constexpr uint32_t kTmemCols = 512;
+constexpr uint32_t kIdescQK = instr_desc(1, 1, 0, 128, 128);
+constexpr uint32_t kIdescPV = instr_desc(0, 1, 1, 128, 64);
+constexpr int kNone = -(1 << 30);                // below every accumulator
+
+struct TileBarriers {
+    uint64_t q_full, o_full;
+    uint64_t full[kSlots], free[kSlots];
+    uint64_t s_full[3], s_free[3];
+    uint64_t r_ready[2], r_free[2];
+};
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, bool real) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+__device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; }
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, int split) {
+    constexpr int kHalves = D / 64;
+    constexpr int kTileBytes = kTile * D;
+    constexpr int kSBufs = D == 128 ? 2 : 3;
+    constexpr uint32_t kTmemO = kSBufs * 128, kTmemW = kTmemO + D;
+    constexpr int kCols = D / 4;                 // columns of O and W per row thread
+    constexpr int kDump = D + 4;                 // row pitch of the joined sums, in words
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) TileBarriers bars;
+    __shared__ uint32_t tmem_slot;
+    __shared__ int abort_flag, any_bad;
+    __shared__ int part_max[4][kTile], cta_max[kTile];
+    __shared__ int part_sum[4][kTile], part_cnt[4][kTile];
+    __shared__ int cta_sum[kTile], cta_cnt[kTile];
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int b = blockIdx.z, kvh = blockIdx.y;
+    const int rank = (int)blockIdx.x % split;
+    const int rt = (int)(gridDim.x / split - 1 - blockIdx.x / split);      // the tiles with the most keys first
+    const SequenceAt seq = sequence_at(a, b);
+    if (seq.cut && tid == 0 && blockIdx.x + blockIdx.y == 0) atomicOr(a.status, STATUS_BAD_LENGTH);
+    const int queries = min(seq.nq, a.max_q);
+    const int row0 = rt * kTile;
+    const int vrows = min(kTile, queries * a.group - row0);
+    if (vrows <= 0) return;                                                // the whole cluster
+    const int quarters = (vrows + 31) >> 5;                                // TMEM lane quarters with rows
+    const int row_threads = quarters * 128;
+    // key blocks of the tile (of its last query, where the rows are causal), and this CTA's share of them
+    const int last_query = (row0 + vrows - 1) / a.group;
+    const int n_tile = a.tree_mask ? seq.n : min(max(seq.prefix + last_query + 1, 0), seq.n);
+    const int blocks = (n_tile + kTile - 1) / kTile;
+    const int per = (blocks + split - 1) / split;
+    const int kb0 = min(rank * per, blocks), nb = min(kb0 + per, blocks) - kb0;
+    const int32_t *table = a.page_table + (int64_t)b * a.max_pages;
+    volatile int *abortp = &abort_flag;
+
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t *gen = smem_raw + (base - smem_u32(smem_raw));
+    const uint32_t s_q = base, s_ring = s_q + kTileBytes, s_r = s_ring + kSlots * kTileBytes, s_w = s_r + 2 * kPanelBytes;
+    uint8_t *g_r = gen + (s_r - base), *g_w = gen + (s_w - base);
+
+    if (tid == 0) {
+        abort_flag = 0;
+        any_bad = 0;
+        mbar_init(smem_u32(&bars.q_full), kCopyThreads);
+        mbar_init(smem_u32(&bars.o_full), 1);
+        for (int i = 0; i < kSlots; ++i) { mbar_init(smem_u32(&bars.full[i]), kCopyThreads); mbar_init(smem_u32(&bars.free[i]), 1); }
+        for (int i = 0; i < 3; ++i) { mbar_init(smem_u32(&bars.s_full[i]), 1); mbar_init(smem_u32(&bars.s_free[i]), row_threads); }
+        for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&bars.r_ready[i]), row_threads); mbar_init(smem_u32(&bars.r_free[i]), 1); }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == kPvWarp) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(kTmemCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tcgen05_fence_before();
+    __syncthreads();
+    // pages outside the pools: a look at this CTA's part of the table tells whether the masks have to care
+    {
+        const int key_end = min((kb0 + nb) * kTile, seq.n);
+        for (int p = (kb0 * kTile >> a.page_shift) + tid; (int64_t)p << a.page_shift < key_end; p += kThreads)
+            if ((uint32_t)table[p] >= (uint32_t)a.num_pages) any_bad = 1;
+    }
+    __syncthreads();
+    tcgen05_fence_after();
+    const uint32_t tmem = tmem_slot;
+    const bool bad = any_bad != 0;
+    if (bad && tid == 0) atomicOr(a.status, STATUS_BAD_PAGE);
+    auto wait = [&](uint64_t *bar, uint32_t parity) { return mbar_wait(smem_u32(bar), parity, abortp, a.status, a.wait_cycles); };
+
+    if (warp == kCopyWarp || warp == kCopyWarp + 1) {
+        // ===================================================== copies
+        if (split > 1) cluster_arrive();
+        constexpr int kChunks = D / 16, kRowsPass = kCopyThreads / kChunks, kPasses = kTile / kRowsPass;
+        const int pt = tid - kCopyWarp * 32, chunk = pt % kChunks, r0 = pt / kChunks;
+        // 16-byte chunk `chunk` of row r of a tile of two 64-byte halves
+        auto at = [&](int r) -> uint32_t {
+            return (uint32_t)((chunk >> 2) * kHalfBytes + r * 64 + (((chunk & 3) ^ ((r >> 1) & 3)) << 4));
+        };
+        for (int p = 0; p < kPasses; ++p) {
+            const int r = p * kRowsPass + r0;
+            const bool real = r < vrows;
+            const int row = row0 + (real ? r : 0), q = row / a.group;
+            cp_async16(s_q + at(r), a.Q + (((int64_t)seq.s0 + q) * a.Hq + kvh * a.group + (row - q * a.group)) * D + chunk * 16, real);
+        }
+        cp_commit();
+        // lane l (of 8) looks up the page of 16-key group l of a block; -1: no such key, or no such page
+        auto page_of = [&](int kb) -> int {
+            const int key = (kb0 + kb) * kTile + 16 * (lane & 7);
+            int page = -1;
+            if (key < seq.n) {
+                page = __ldg(table + (key >> a.page_shift));
+                if ((uint32_t)page >= (uint32_t)a.num_pages) page = -1;
+            }
+            return page;
+        };
+        const int loads = 3 * nb;
+        bool ok = true;
+        auto landed = [&](int g) {               // group g: 0 is Q, g + 1 load number g
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            mbar_arrive(g == 0 ? smem_u32(&bars.q_full) : smem_u32(&bars.full[(g - 1) % kSlots]));
+        };
+        int page = nb > 0 ? page_of(0) : -1;
+        for (int x = 0; ok && x < loads; ++x) {
+            const int kb = x < nb ? x : (x - nb) >> 1;
+            const bool values = x >= nb && ((x - nb) & 1);
+            const int nx = x + 1, nkb = nx < nb ? nx : (nx - nb) >> 1;
+            const int next_page = nx < loads && nkb != kb ? page_of(nkb) : page;
+            if (x >= kSlots) ok = __all_sync(~0u, wait(&bars.free[x % kSlots], (x / kSlots - 1) & 1));
+            if (!ok) break;
+            const uint32_t dst = s_ring + (x % kSlots) * kTileBytes;
+            const int8_t *pool = values ? a.v_pages : a.k_pages;
+#pragma unroll
+            for (int p = 0; p < kPasses; ++p) {
+                const int r = p * kRowsPass + r0;
+                const int pg = __shfl_sync(~0u, page, (p * kRowsPass) >> 4);
+                const int place = ((kb0 + kb) * kTile + r) & ((1 << a.page_shift) - 1);
+                const int8_t *src = pool + ((((int64_t)max(pg, 0) * a.Hkv + kvh) << a.page_shift) + place) * D + chunk * 16;
+                cp_async16(dst + at(r), src, pg >= 0);
+            }
+            cp_commit();
+            cp_wait<kAhead>();
+            if (x + 1 - kAhead >= 0) landed(x + 1 - kAhead);
+            page = next_page;
+        }
+        cp_wait<0>();
+        if (ok)
+            for (int g = max(0, loads + 1 - kAhead); g <= loads; ++g) landed(g);
+    } else if (warp == kQkWarp) {
+        // ===================================================== S = Q.K^T, twice
+        if (split > 1) cluster_arrive();
+        if (lane == 0 && nb > 0) {
+            bool ok = wait(&bars.q_full, 0);
+            const uint64_t dq = smem_desc(s_q, 16, 512, kSwizzle64), dk = smem_desc(s_ring, 16, 512, kSwizzle64);
+            const uint32_t dq_lo = (uint32_t)dq, dq_hi = (uint32_t)(dq >> 32), dk_lo = (uint32_t)dk, dk_hi = (uint32_t)(dk >> 32);
+            uint32_t sb = 0, cyc = 0;
+            for (int g = 0; ok && g < 2 * nb; ++g) {
+                const int x = g < nb ? g : nb + 2 * (g - nb);
+                const int slot = x % kSlots;
+                if (cyc > 0) ok = wait(&bars.s_free[sb], (cyc - 1) & 1);
+                if (ok) ok = wait(&bars.full[slot], (x / kSlots) & 1);
+                if (!ok) break;
+                tcgen05_fence_after();
+                const uint32_t koff = (uint32_t)(slot * kTileBytes) >> 4;
+#pragma unroll
+                for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+                    for (int ks = 0; ks < 2; ++ks) {
+                        const uint32_t off = (uint32_t)(h * kHalfBytes + ks * 32) >> 4;
+                        tcgen05_mma_i8(tmem + sb * 128, make_u64(dq_lo + off, dq_hi), make_u64(dk_lo + koff + off, dk_hi), kIdescQK, (h | ks) != 0);
+                    }
+                tcgen05_commit(smem_u32(&bars.s_full[sb]));
+                tcgen05_commit(smem_u32(&bars.free[slot]));
+                if (++sb == kSBufs) { sb = 0; ++cyc; }
+            }
+        }
+        __syncwarp();
+    } else if (warp == kPvWarp) {
+        // ===================================================== O += r.V, W += mask.V
+        if (split > 1) cluster_arrive();
+        if (lane == 0 && nb > 0) {
+            bool ok = true;
+            const uint64_t dr = smem_desc(s_r, 16, 1024, kSwizzle128), dv = smem_desc(s_ring, 512, 512, kSwizzle64);
+            const uint32_t dr_lo = (uint32_t)dr, dr_hi = (uint32_t)(dr >> 32), dv_lo = (uint32_t)dv, dv_hi = (uint32_t)(dv >> 32);
+            for (int kb = 0; ok && kb < nb; ++kb) {
+                const int x = nb + 2 * kb + 1, slot = x % kSlots, buf = kb & 1;
+                ok = wait(&bars.full[slot], (x / kSlots) & 1);
+                if (ok) ok = wait(&bars.r_ready[buf], (kb >> 1) & 1);
+                if (!ok) break;
+                tcgen05_fence_after();
+#pragma unroll
+                for (int w = 0; w < 2; ++w)
+#pragma unroll
+                    for (int ks = 0; ks < 4; ++ks) {
+                        const uint32_t roff = (uint32_t)((2 * w + buf) * kPanelBytes + ks * 32) >> 4;
+#pragma unroll
+                        for (int h = 0; h < kHalves; ++h) {
+                            const uint32_t voff = (uint32_t)(slot * kTileBytes + h * kHalfBytes + ks * 32 * 64) >> 4;
+                            tcgen05_mma_i8(tmem + (w ? kTmemW : kTmemO) + h * 64, make_u64(dr_lo + roff, dr_hi), make_u64(dv_lo + voff, dv_hi), kIdescPV,
+                                           (kb | ks) != 0);
+                        }
+                    }
+                tcgen05_commit(smem_u32(&bars.free[slot]));
+                tcgen05_commit(smem_u32(&bars.r_free[buf]));
+            }
+            if (ok) tcgen05_commit(smem_u32(&bars.o_full));
+        }
+        __syncwarp();
+    } else {
+        // ===================================================== row warps: threads t, t+128, t+256, t+384 own row t
+        const int t = tid & (kTile - 1), grp = tid >> 7;
+        const bool active = (warp & 3) < quarters;
+        cg::cluster_group cluster = cg::this_cluster();
+        auto row_barrier = [&]() { asm volatile("bar.sync 1, %0;" ::"r"(row_threads) : "memory"); };
+        const bool real = t < vrows;
+        const int row = row0 + (real ? t : 0), qi = row / a.group, h = kvh * a.group + (row - qi * a.group);
+        const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
+        bool ok = true;
+        HeadEntry th;
+        Requant rq;
+        int M = 0;
+        int rsum = 0, count = 0;
+        int xmax = 0;
+        uint32_t s_buf = 0, s_cyc = 0;
+        // which of the thread's 32 keys of block kb its row sees
+        const int seen_all = !real ? 0 : min(a.tree_mask ? seq.prefix : seq.prefix + qi + 1, seq.n);
+        const uint32_t *tree = a.tree_mask ? reinterpret_cast<const uint32_t *>(a.tree_mask) + ((int64_t)seq.s0 + qi) * a.tree_words : nullptr;
+        auto mask_of = [&](int kb) -> uint32_t {
+            const int c0 = (kb0 + kb) * kTile + grp * 32;
+            uint32_t m = low_bits(seen_all - c0);
+            if (tree && real && m != 0xffffffffu) {
+                // new key number j0 + k sits at bit k; words beyond max_q's last are never read
+                const int j0 = c0 - seq.prefix;
+                uint32_t bits = 0;
+                if (j0 > -32) {
+                    const int w = j0 >> 5, s = j0 & 31;                     // (floor: w = -1 for negative j0)
+                    const uint32_t lo = w >= 0 && w * 32 < a.max_q ? tree[w] & low_bits(a.max_q - w * 32) : 0u;
+                    const uint32_t hi = (w + 1) * 32 < a.max_q ? tree[w + 1] & low_bits(a.max_q - (w + 1) * 32) : 0u;
+                    bits = __funnelshift_r(lo, hi, s);
+                }
+                m |= bits & low_bits(seq.n - c0);
+            }
+            if (bad) {
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                    const int key = c0 + 16 * g;
+                    if (key >= seq.n || (uint32_t)table[key >> a.page_shift] >= (uint32_t)a.num_pages) m &= ~(0xffffu << (16 * g));
+                }
+            }
+            return m;
+        };
+        if (active) {
+            const int4 e = *reinterpret_cast<const int4 *>(a.table + h);
+            th.B = e.x; th.S = e.y; th.D = e.z;
+            M = a.mult[h];
+            rq = make_requant(M, a.requant_shift);
+            // ---- first pass: the largest accumulator
+            int amax = kNone;
+            for (int kb = 0; ok && kb < nb; ++kb) {
+                const uint32_t mask = mask_of(kb);
+                ok = __all_sync(~0u, wait(&bars.s_full[s_buf], s_cyc & 1));
+                if (!ok) break;
+                tcgen05_fence_after();
+                uint32_t acc[32];
+                tmem_ld32(tmem + lane_addr + s_buf * 128 + grp * 32, acc);
+                tcgen05_fence_before();
+                mbar_arrive(smem_u32(&bars.s_free[s_buf]));
+                if (++s_buf == kSBufs) { s_buf = 0; ++s_cyc; }
+                if (mask != 0xffffffffu) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        if (!((mask >> i) & 1)) acc[i] = (uint32_t)kNone;
+                }
+#pragma unroll
+                for (int i = 0; i < 32; i += 2) amax = __vimax3_s32(amax, (int)acc[i], (int)acc[i + 1]);
+            }
+            part_max[grp][t] = amax;
+            row_barrier();
+            xmax = max(max(part_max[0][t], part_max[1][t]), max(part_max[2][t], part_max[3][t]));
+        }
+        if (split > 1) {
+            if (active && grp == 0) cta_max[t] = xmax;
+            cluster_arrive();
+            cluster_wait();
+            if (active)
+                for (int r = 0; r < split; ++r) xmax = max(xmax, cluster.map_shared_rank(cta_max, r)[t]);
+        }
+        if (active) {
+            xmax = (int)requant_top(rq, xmax) >> 24;
+            // ---- second pass: with u = m - D, accumulators are clamped to [lo_u, hi], lo_u the smallest whose
+            // logit reaches max(u, -128); then clamp(acc - lo_u, 0, hi - lo_u)*(M << k) + (((lo_u*M + R) << k) - (u << 24))
+            // lies in [0, 2^31) and has r as its top byte
+            const int u = xmax - th.D, sh = a.requant_shift, k = 24 - sh;
+            const int lo = -rq.neg_lo, hi = lo + rq.span;
+            const int64_t R = 1ll << (sh - 1);
+            int lo_u = lo;
+            if (M > 0) {      // ceil of a quotient below 2^33 by M < 2^13: exact through one fp64 division
+                const double q = ceil((double)((int64_t)u * (1ll << sh) - R) / (double)M);
+                lo_u = (int)fmin(fmax(q, (double)lo), (double)hi);
+            }
+            const int neg_lo = -lo_u, span = hi - lo_u;
+            const uint32_t mk = rq.mk, ck = ((uint32_t)((int64_t)lo_u * M + R) << k) - ((uint32_t)u << 24);
+            const int swz = t & 7;
+            const uint32_t row_off = (uint32_t)((t >> 3) * 1024 + (t & 7) * 128);
+            uint32_t held[2] = {0xdeadbeefu, 0xdeadbeefu};       // the masks whose bytes the two buffers hold, see below
+            bool fresh[2] = {true, true};
+            for (int kb = 0; ok && kb < nb; ++kb) {
+                const uint32_t mask = mask_of(kb);
+                ok = __all_sync(~0u, wait(&bars.s_full[s_buf], s_cyc & 1));
+                if (!ok) break;
+                tcgen05_fence_after();
+                uint32_t acc[32];
+                tmem_ld32(tmem + lane_addr + s_buf * 128 + grp * 32, acc);
+                tcgen05_fence_before();
+                mbar_arrive(smem_u32(&bars.s_free[s_buf]));
+                if (++s_buf == kSBufs) { s_buf = 0; ++s_cyc; }
+#pragma unroll
+                for (int i = 0; i < 32; ++i) acc[i] = (uint32_t)__viaddmin_s32_relu((int)acc[i], neg_lo, span) * mk + ck;
+                if (mask != 0xffffffffu) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        if (!((mask >> i) & 1)) acc[i] = 0u;
+                }
+                uint32_t w[8];
+#pragma unroll
+                for (int g = 0; g < 8; ++g) {
+                    w[g] = __byte_perm(__byte_perm(acc[4 * g], acc[4 * g + 1], 0x0073), __byte_perm(acc[4 * g + 2], acc[4 * g + 3], 0x0073), 0x5410);
+                    rsum = (int)__dp4a(w[g], 0x01010101u, (uint32_t)rsum);
+                }
+                count += __popc(mask);
+                const int buf = kb & 1;
+                if (kb >= 2) ok = __all_sync(~0u, wait(&bars.r_free[buf], ((kb >> 1) - 1) & 1));
+                if (!ok) break;
+                uint8_t *p = g_r + buf * kPanelBytes + row_off;
+                *reinterpret_cast<uint4 *>(p + (((2 * grp) ^ swz) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+                *reinterpret_cast<uint4 *>(p + (((2 * grp + 1) ^ swz) << 4)) = make_uint4(w[4], w[5], w[6], w[7]);
+                // the mask's bytes are written only where they differ from what the buffer holds: full blocks, the
+                // common case, write them once
+                if (buf == 0 ? (fresh[0] || held[0] != mask) : (fresh[1] || held[1] != mask)) {
+#pragma unroll
+                    for (int g = 0; g < 8; ++g) w[g] = (((mask >> (4 * g)) & 15u) * 0x00204081u) & 0x01010101u;
+                    uint8_t *pw = g_w + buf * kPanelBytes + row_off;
+                    *reinterpret_cast<uint4 *>(pw + (((2 * grp) ^ swz) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+                    *reinterpret_cast<uint4 *>(pw + (((2 * grp + 1) ^ swz) << 4)) = make_uint4(w[4], w[5], w[6], w[7]);
+                    if (buf == 0) { held[0] = mask; fresh[0] = false; } else { held[1] = mask; fresh[1] = false; }
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                mbar_arrive(smem_u32(&bars.r_ready[buf]));
+            }
+            part_sum[grp][t] = rsum;
+            part_cnt[grp][t] = count;
+            row_barrier();
+            rsum = part_sum[0][t] + part_sum[1][t] + part_sum[2][t] + part_sum[3][t];
+            count = part_cnt[0][t] + part_cnt[1][t] + part_cnt[2][t] + part_cnt[3][t];
+            if (ok && nb > 0) ok = __all_sync(~0u, wait(&bars.o_full, 0));
+            tcgen05_fence_after();
+        }
+        // ---- join
+        const int64_t at0 = ((int64_t)seq.s0 * a.Hq + (int64_t)kvh * a.group) * D;
+        if (split == 1) {
+            if (active && ok) {
+                const int64_t F = th.B - th.S * th.D;
+                const RowFactor f = row_factor(a, F * count + (int64_t)th.S * rsum, a.scale[h]);
+                const int64_t at = at0 + ((int64_t)qi * a.Hq + (row - qi * a.group)) * D + grp * kCols;
+#pragma unroll
+                for (int part = 0; part < kCols / 16; ++part) {
+                    uint32_t o[16], w[16];
+                    if (nb > 0) {
+                        tmem_ld16(tmem + lane_addr + kTmemO + grp * kCols + 16 * part, o);
+                        tmem_ld16(tmem + lane_addr + kTmemW + grp * kCols + 16 * part, w);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) o[i] = w[i] = 0u;
+                    }
+                    if (real) {
+#pragma unroll
+                        for (int g = 0; g < 4; ++g) {
+                            int64_t num[4];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) num[i] = F * (int)w[4 * g + i] + (int64_t)th.S * (int)o[4 * g + i];
+                            store_output4(a, at + 16 * part + 4 * g, num, f);
+                        }
+                    }
+                }
+            }
+        } else {
+            // the CTA's sums go to shared memory (the operands' place: every product is complete)
+            int *dump_o = reinterpret_cast<int *>(gen), *dump_w = dump_o + kTile * kDump;
+            if (active) {
+#pragma unroll
+                for (int part = 0; part < kCols / 8; ++part) {      // 16 columns of O, then of W
+                    const bool which = part >= kCols / 16;
+                    const int col = grp * kCols + 16 * (part % (kCols / 16));
+                    uint32_t v[16];
+                    if (nb > 0 && ok) {
+                        tmem_ld16(tmem + lane_addr + (which ? kTmemW : kTmemO) + col, v);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) v[i] = 0u;
+                    }
+                    int *d = (which ? dump_w : dump_o) + t * kDump + col;
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) *reinterpret_cast<uint4 *>(d + 4 * g) = make_uint4(v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]);
+                }
+                if (grp == 0) { cta_sum[t] = rsum; cta_cnt[t] = count; }
+            }
+            cluster_arrive();
+            cluster_wait();
+            // rows shared out over the cluster, four dims per thread and step
+            for (int i = rank * kRowThreads + tid; i < vrows * (D / 4); i += split * kRowThreads) {
+                const int r = i / (D / 4), dim = (i % (D / 4)) * 4;
+                int o[4] = {0, 0, 0, 0}, w[4] = {0, 0, 0, 0}, rs = 0, cn = 0;
+                for (int c = 0; c < split; ++c) {
+                    const int4 ov = *reinterpret_cast<const int4 *>(cluster.map_shared_rank(dump_o, c) + r * kDump + dim);
+                    const int4 wv = *reinterpret_cast<const int4 *>(cluster.map_shared_rank(dump_w, c) + r * kDump + dim);
+                    o[0] += ov.x; o[1] += ov.y; o[2] += ov.z; o[3] += ov.w;
+                    w[0] += wv.x; w[1] += wv.y; w[2] += wv.z; w[3] += wv.w;
+                    rs += cluster.map_shared_rank(cta_sum, c)[r];
+                    cn += cluster.map_shared_rank(cta_cnt, c)[r];
+                }
+                const int rr = row0 + r, q = rr / a.group, hh = rr - q * a.group;
+                const HeadEntry e = a.table[kvh * a.group + hh];
+                const int64_t F = e.B - e.S * e.D;
+                int64_t num[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) num[j] = F * w[j] + (int64_t)e.S * o[j];
+                store_output4(a, at0 + ((int64_t)q * a.Hq + hh) * D + dim, num, row_factor(a, F * cn + (int64_t)e.S * rs, a.scale[kvh * a.group + hh]));
+            }
+            cluster_arrive();
+            cluster_wait();
+        }
+    }
+    if (split > 1 && warp >= kCopyWarp) {        // the other warps' part of the three cluster barriers
+        cluster_wait();
+        cluster_arrive();
+        cluster_wait();
+        cluster_arrive();
+        cluster_wait();
+    }
+    tcgen05_fence_before();
+    __syncthreads();
+    if (warp == kPvWarp) {
+        tcgen05_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+    }
+}
+
+template <int D>
+cudaError_t launch_typed(const CachedAttnArgs &a, cudaStream_t stream) {
+    const int64_t rows = (int64_t)a.max_q * a.group;
+    const int row_tiles = (int)((rows + kTile - 1) / kTile);
+    const int blocks = (a.max_kv + kTile - 1) / kTile;
+    const int64_t ctas = (int64_t)row_tiles * a.Hkv * a.B;
+    // Cluster size: waves of 148 CTAs times the blocks each walks over, plus about six blocks' time of set-up and join
+    int split = 1;
+    int64_t best = -1;
+    for (int s = 1; s <= 16 && (s == 1 || blocks >= 2 * s); s *= 2) {
+        const int64_t cost = ((ctas * s + 147) / 148) * ((blocks + s - 1) / s + 6 + (s > 1 ? 4 : 0));
+        if (best < 0 || cost < best) { best = cost; split = s; }
+    }
+    if ((int64_t)row_tiles * split > 0x7fffffff) return cudaErrorInvalidValue;
+    constexpr size_t smem = 1024 + (size_t)(1 + kSlots) * kTile * D + 4 * kPanelBytes;
+    static_assert(smem - 1024 >= 2 * sizeof(int) * kTile * (D + 4), "the joined sums fit the operands' place");
+    auto kernel = cached_tile_kernel<D>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(row_tiles * split), (unsigned)a.Hkv, (unsigned)a.B);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)split;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, a, split);
+}
+
+}  // namespace
+
+cudaError_t launch_cached_attention(const CachedAttnArgs &a, cudaStream_t stream, uint64_t *launches) {
+    const cudaError_t e = a.max_q == 1 ? launch_cached_decode(a, stream)
+                          : a.d == 128 ? launch_typed<128>(a, stream) : launch_typed<64>(a, stream);
+    if (e == cudaSuccess && launches) ++*launches;
+    return e;
+}
+
+}  // namespace hccs
