@@ -9,10 +9,10 @@
 // twice: once for the maximum of the raw accumulators (the requantisation is monotone), once for r.  sum V over
 // the keys a row sees is a contraction of its own, with the 0/1 bytes of the mask in the place of r.
 //
-// Roles: sixteen row warps (four threads per row, 32 keys of every block each; TMEM lane = row), two warps that copy
-// (cp.async, 16 bytes each: any page size, swizzled by hand into the layouts the tensor core wants), one thread
-// that issues Q.K^T and one that issues the two products with V.  K blocks of the first pass, then K and V blocks
-// in turn, stream through one ring; load number x uses slot x % kSlots.
+// Roles: sixteen row warps (four threads per row, 32 keys of every block each; TMEM lane = row), three warps that
+// issue the TMA loads of every third block (a box per page, or per 128 keys of a larger one, a lane each), one
+// thread that issues Q.K^T and one that issues the two products with V.  K blocks of the first pass, then K and V
+// blocks in turn, stream through one ring; load number x uses slot x % kSlots.
 //
 // Few rows and many keys: the key blocks of a row tile are split over the CTAs of a cluster, which exchange row
 // maxima between the passes and sums at the end through distributed shared memory (exact integers: the split
@@ -28,40 +28,40 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kRowThreads = 512, kCopyThreads = 64;
-constexpr int kCopyWarp = 16, kQkWarp = 18, kPvWarp = 19;
-constexpr int kThreads = 640;
+constexpr int kRowThreads = 512;
+constexpr int kCopyWarp = 16, kCopyWarps = 3, kQkWarp = 19, kPvWarp = 20;
+constexpr int kThreads = 672;
 constexpr int kTile = 128;
-constexpr int kHalfBytes = kTile * 64;           // 128 rows x 64 bytes, 64-byte swizzle
 constexpr int kPanelBytes = kTile * 128;         // 128 rows x 128 keys, 128-byte swizzle
-constexpr int kSlots = 6;
-constexpr int kAhead = 3;                        // copies in flight
+constexpr int kMaxSlots = 12;
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kIdescQK = instr_desc(1, 1, 0, 128, 128);
-constexpr uint32_t kIdescPV = instr_desc(0, 1, 1, 128, 64);
 constexpr int kNone = -(1 << 30);                // below every accumulator
 
 struct TileBarriers {
-    uint64_t q_full, o_full;
-    uint64_t full[kSlots], free[kSlots];
+    uint64_t o_full;
+    uint64_t full[kMaxSlots], free[kMaxSlots];
     uint64_t s_full[3], s_free[3];
     uint64_t r_ready[2], r_free[2];
 };
 
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, bool real) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 __device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; }
 
+template <int D> constexpr int kSlotsOf = D == 128 ? 8 : kMaxSlots;
+template <int D> constexpr uint32_t kIdescPVOf = instr_desc(0, 1, 1, 128, D);   // r.V and mask.V: uint8 x int8, V MN-major
+
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
-cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, int split) {
-    constexpr int kHalves = D / 64;
+cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_constant__ CUtensorMap map_k,
+                   const __grid_constant__ CUtensorMap map_v, int split) {
+    // Q, K and V tiles are 128 rows of D bytes, swizzled over the whole row: K-major operands for Q and K, the
+    // MN-major one for V as it is stored
     constexpr int kTileBytes = kTile * D;
+    constexpr uint64_t kSwizzle = D == 128 ? kSwizzle128 : kSwizzle64;
+    constexpr uint32_t kIdescPV = kIdescPVOf<D>;
+    constexpr int kSlots = kSlotsOf<D>;
     constexpr int kSBufs = D == 128 ? 2 : 3;
     constexpr uint32_t kTmemO = kSBufs * 128, kTmemW = kTmemO + D;
     constexpr int kCols = D / 4;                 // columns of O and W per row thread
@@ -103,9 +103,8 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, int split) {
     if (tid == 0) {
         abort_flag = 0;
         any_bad = 0;
-        mbar_init(smem_u32(&bars.q_full), kCopyThreads);
         mbar_init(smem_u32(&bars.o_full), 1);
-        for (int i = 0; i < kSlots; ++i) { mbar_init(smem_u32(&bars.full[i]), kCopyThreads); mbar_init(smem_u32(&bars.free[i]), 1); }
+        for (int i = 0; i < kSlots; ++i) { mbar_init(smem_u32(&bars.full[i]), 1); mbar_init(smem_u32(&bars.free[i]), 1); }
         for (int i = 0; i < 3; ++i) { mbar_init(smem_u32(&bars.s_full[i]), 1); mbar_init(smem_u32(&bars.s_free[i]), row_threads); }
         for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&bars.r_ready[i]), row_threads); mbar_init(smem_u32(&bars.r_free[i]), 1); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -123,6 +122,18 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, int split) {
         for (int p = (kb0 * kTile >> a.page_shift) + tid; (int64_t)p << a.page_shift < key_end; p += kThreads)
             if ((uint32_t)table[p] >= (uint32_t)a.num_pages) any_bad = 1;
     }
+    // Q, swizzled by hand: the rows of a tile are (query, head) pairs, not a box of the tensor
+    constexpr int kChunks = D / 16;
+    for (int i = tid; i < kTile * kChunks; i += kThreads) {
+        const int r = i / kChunks, chunk = i % kChunks;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (r < vrows) {
+            const int row = row0 + r, q = row / a.group;
+            v = *reinterpret_cast<const uint4 *>(a.Q + (((int64_t)seq.s0 + q) * a.Hq + kvh * a.group + (row - q * a.group)) * D + chunk * 16);
+        }
+        *reinterpret_cast<uint4 *>(gen + r * D + ((chunk ^ (D == 128 ? r & 7 : (r >> 1) & 3)) << 4)) = v;
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncthreads();
     tcgen05_fence_after();
     const uint32_t tmem = tmem_slot;
@@ -130,70 +141,40 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, int split) {
     if (bad && tid == 0) atomicOr(a.status, STATUS_BAD_PAGE);
     auto wait = [&](uint64_t *bar, uint32_t parity) { return mbar_wait(smem_u32(bar), parity, abortp, a.status, a.wait_cycles); };
 
-    if (warp == kCopyWarp || warp == kCopyWarp + 1) {
-        // ===================================================== copies
+    if (warp >= kCopyWarp && warp < kCopyWarp + kCopyWarps) {
+        // ===================================================== copies: load number x by warp x % kCopyWarps (a thread
+        // gets through one TMA copy per several hundred cycles, the copies of different warps and lanes overlap)
         if (split > 1) cluster_arrive();
-        constexpr int kChunks = D / 16, kRowsPass = kCopyThreads / kChunks, kPasses = kTile / kRowsPass;
-        const int pt = tid - kCopyWarp * 32, chunk = pt % kChunks, r0 = pt / kChunks;
-        // 16-byte chunk `chunk` of row r of a tile of two 64-byte halves
-        auto at = [&](int r) -> uint32_t {
-            return (uint32_t)((chunk >> 2) * kHalfBytes + r * 64 + (((chunk & 3) ^ ((r >> 1) & 3)) << 4));
-        };
-        for (int p = 0; p < kPasses; ++p) {
-            const int r = p * kRowsPass + r0;
-            const bool real = r < vrows;
-            const int row = row0 + (real ? r : 0), q = row / a.group;
-            cp_async16(s_q + at(r), a.Q + (((int64_t)seq.s0 + q) * a.Hq + kvh * a.group + (row - q * a.group)) * D + chunk * 16, real);
-        }
-        cp_commit();
-        // lane l (of 8) looks up the page of 16-key group l of a block; -1: no such key, or no such page
-        auto page_of = [&](int kb) -> int {
-            const int key = (kb0 + kb) * kTile + 16 * (lane & 7);
+        const int box = min(1 << a.page_shift, kTile), boxes = kTile / box;
+        const int loads = 3 * nb;
+        bool ok = true;
+        for (int x = warp - kCopyWarp; ok && x < loads; x += kCopyWarps) {
+            const int kb = x < nb ? x : (x - nb) >> 1;
+            const bool values = x >= nb && ((x - nb) & 1);
+            // lane l of `boxes` copies keys l * box ... of the block; keys that are not there, or whose page is not,
+            // are left out (their masks are clear and what the slot held is finite)
+            const int key = (kb0 + kb) * kTile + lane * box;
             int page = -1;
-            if (key < seq.n) {
+            if (lane < boxes && key < seq.n) {
                 page = __ldg(table + (key >> a.page_shift));
                 if ((uint32_t)page >= (uint32_t)a.num_pages) page = -1;
             }
-            return page;
-        };
-        const int loads = 3 * nb;
-        bool ok = true;
-        auto landed = [&](int g) {               // group g: 0 is Q, g + 1 load number g
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            mbar_arrive(g == 0 ? smem_u32(&bars.q_full) : smem_u32(&bars.full[(g - 1) % kSlots]));
-        };
-        int page = nb > 0 ? page_of(0) : -1;
-        for (int x = 0; ok && x < loads; ++x) {
-            const int kb = x < nb ? x : (x - nb) >> 1;
-            const bool values = x >= nb && ((x - nb) & 1);
-            const int nx = x + 1, nkb = nx < nb ? nx : (nx - nb) >> 1;
-            const int next_page = nx < loads && nkb != kb ? page_of(nkb) : page;
+            const int count = __popc(__ballot_sync(~0u, page >= 0));
             if (x >= kSlots) ok = __all_sync(~0u, wait(&bars.free[x % kSlots], (x / kSlots - 1) & 1));
             if (!ok) break;
-            const uint32_t dst = s_ring + (x % kSlots) * kTileBytes;
-            const int8_t *pool = values ? a.v_pages : a.k_pages;
-#pragma unroll
-            for (int p = 0; p < kPasses; ++p) {
-                const int r = p * kRowsPass + r0;
-                const int pg = __shfl_sync(~0u, page, (p * kRowsPass) >> 4);
-                const int place = ((kb0 + kb) * kTile + r) & ((1 << a.page_shift) - 1);
-                const int8_t *src = pool + ((((int64_t)max(pg, 0) * a.Hkv + kvh) << a.page_shift) + place) * D + chunk * 16;
-                cp_async16(dst + at(r), src, pg >= 0);
-            }
-            cp_commit();
-            cp_wait<kAhead>();
-            if (x + 1 - kAhead >= 0) landed(x + 1 - kAhead);
-            page = next_page;
+            const uint32_t bar = smem_u32(&bars.full[x % kSlots]);
+            if (lane == 0) mbar_expect_tx(bar, (uint32_t)(count * box * D));
+            __syncwarp();
+            if (page >= 0)
+                tma_load_3d(s_ring + (x % kSlots) * kTileBytes + lane * box * D, values ? &map_v : &map_k, 0,
+                            key & ((1 << a.page_shift) - 1), page * a.Hkv + kvh, bar);
         }
-        cp_wait<0>();
-        if (ok)
-            for (int g = max(0, loads + 1 - kAhead); g <= loads; ++g) landed(g);
     } else if (warp == kQkWarp) {
         // ===================================================== S = Q.K^T, twice
         if (split > 1) cluster_arrive();
         if (lane == 0 && nb > 0) {
-            bool ok = wait(&bars.q_full, 0);
-            const uint64_t dq = smem_desc(s_q, 16, 512, kSwizzle64), dk = smem_desc(s_ring, 16, 512, kSwizzle64);
+            bool ok = true;
+            const uint64_t dq = smem_desc(s_q, 16, 8 * D, kSwizzle), dk = smem_desc(s_ring, 16, 8 * D, kSwizzle);
             const uint32_t dq_lo = (uint32_t)dq, dq_hi = (uint32_t)(dq >> 32), dk_lo = (uint32_t)dk, dk_hi = (uint32_t)(dk >> 32);
             uint32_t sb = 0, cyc = 0;
             for (int g = 0; ok && g < 2 * nb; ++g) {
@@ -205,12 +186,10 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, int split) {
                 tcgen05_fence_after();
                 const uint32_t koff = (uint32_t)(slot * kTileBytes) >> 4;
 #pragma unroll
-                for (int h = 0; h < kHalves; ++h)
-#pragma unroll
-                    for (int ks = 0; ks < 2; ++ks) {
-                        const uint32_t off = (uint32_t)(h * kHalfBytes + ks * 32) >> 4;
-                        tcgen05_mma_i8(tmem + sb * 128, make_u64(dq_lo + off, dq_hi), make_u64(dk_lo + koff + off, dk_hi), kIdescQK, (h | ks) != 0);
-                    }
+                for (int ks = 0; ks < D / 32; ++ks) {
+                    const uint32_t off = (uint32_t)(ks * 32) >> 4;
+                    tcgen05_mma_i8(tmem + sb * 128, make_u64(dq_lo + off, dq_hi), make_u64(dk_lo + koff + off, dk_hi), kIdescQK, ks != 0);
+                }
                 tcgen05_commit(smem_u32(&bars.s_full[sb]));
                 tcgen05_commit(smem_u32(&bars.free[slot]));
                 if (++sb == kSBufs) { sb = 0; ++cyc; }
@@ -222,7 +201,7 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, int split) {
         if (split > 1) cluster_arrive();
         if (lane == 0 && nb > 0) {
             bool ok = true;
-            const uint64_t dr = smem_desc(s_r, 16, 1024, kSwizzle128), dv = smem_desc(s_ring, 512, 512, kSwizzle64);
+            const uint64_t dr = smem_desc(s_r, 16, 1024, kSwizzle128), dv = smem_desc(s_ring, 8 * D, 8 * D, kSwizzle);
             const uint32_t dr_lo = (uint32_t)dr, dr_hi = (uint32_t)(dr >> 32), dv_lo = (uint32_t)dv, dv_hi = (uint32_t)(dv >> 32);
             for (int kb = 0; ok && kb < nb; ++kb) {
                 const int x = nb + 2 * kb + 1, slot = x % kSlots, buf = kb & 1;
@@ -235,12 +214,8 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, int split) {
 #pragma unroll
                     for (int ks = 0; ks < 4; ++ks) {
                         const uint32_t roff = (uint32_t)((2 * w + buf) * kPanelBytes + ks * 32) >> 4;
-#pragma unroll
-                        for (int h = 0; h < kHalves; ++h) {
-                            const uint32_t voff = (uint32_t)(slot * kTileBytes + h * kHalfBytes + ks * 32 * 64) >> 4;
-                            tcgen05_mma_i8(tmem + (w ? kTmemW : kTmemO) + h * 64, make_u64(dr_lo + roff, dr_hi), make_u64(dv_lo + voff, dv_hi), kIdescPV,
-                                           (kb | ks) != 0);
-                        }
+                        const uint32_t voff = (uint32_t)(slot * kTileBytes + ks * 32 * D) >> 4;
+                        tcgen05_mma_i8(tmem + (w ? kTmemW : kTmemO), make_u64(dr_lo + roff, dr_hi), make_u64(dv_lo + voff, dv_hi), kIdescPV, (kb | ks) != 0);
                     }
                 tcgen05_commit(smem_u32(&bars.free[slot]));
                 tcgen05_commit(smem_u32(&bars.r_free[buf]));
@@ -487,6 +462,20 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, int split) {
     }
 }
 
+// A pool as [num_pages * Hkv][page_size][D] bytes, boxes of a page's rows (128 at most), swizzled over the whole row.
+bool make_page_map(CUtensorMap *map, const void *pool, const CachedAttnArgs &a, int d) {
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    const cuuint64_t page = (cuuint64_t)1 << a.page_shift;
+    const cuuint64_t dims[3] = {(cuuint64_t)d, page, (cuuint64_t)a.num_pages * a.Hkv};
+    const cuuint64_t strides[2] = {(cuuint64_t)d, page * d};
+    const cuuint32_t box[3] = {(cuuint32_t)d, page < kTile ? (cuuint32_t)page : (cuuint32_t)kTile, 1};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void *>(pool), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              d == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int D>
 cudaError_t launch_typed(const CachedAttnArgs &a, cudaStream_t stream) {
     const int64_t rows = (int64_t)a.max_q * a.group;
@@ -501,8 +490,10 @@ cudaError_t launch_typed(const CachedAttnArgs &a, cudaStream_t stream) {
         if (best < 0 || cost < best) { best = cost; split = s; }
     }
     if ((int64_t)row_tiles * split > 0x7fffffff) return cudaErrorInvalidValue;
-    constexpr size_t smem = 1024 + (size_t)(1 + kSlots) * kTile * D + 4 * kPanelBytes;
+    constexpr size_t smem = 1024 + (size_t)(1 + kSlotsOf<D>) * kTile * D + 4 * kPanelBytes;
     static_assert(smem - 1024 >= 2 * sizeof(int) * kTile * (D + 4), "the joined sums fit the operands' place");
+    CUtensorMap mk, mv;
+    if (!make_page_map(&mk, a.k_pages, a, D) || !make_page_map(&mv, a.v_pages, a, D)) return cudaErrorInvalidValue;
     auto kernel = cached_tile_kernel<D>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
@@ -519,7 +510,7 @@ cudaError_t launch_typed(const CachedAttnArgs &a, cudaStream_t stream) {
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, a, split);
+    return cudaLaunchKernelEx(&cfg, kernel, a, mk, mv, split);
 }
 
 }  // namespace

@@ -40,6 +40,22 @@
 
 namespace hccs {
 
+static EncodeTiledFn lookup_encode_tiled() {
+    void *p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess ||
+        q != cudaDriverEntryPointSuccess) {
+        (void)cudaGetLastError();
+        return nullptr;
+    }
+    return reinterpret_cast<EncodeTiledFn>(p);
+}
+
+EncodeTiledFn encode_tiled_fn() {
+    static const EncodeTiledFn fn = lookup_encode_tiled();   // initialised once, thread-safe
+    return fn;
+}
+
 namespace {
 
 constexpr int kRowThreads = 512;           // four per query row
@@ -726,26 +742,6 @@ fused_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
 }
 
 // ---------------------------------------------------------------- host side
-typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
-                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn lookup_encode_tiled() {
-    void *p = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess ||
-        q != cudaDriverEntryPointSuccess) {
-        (void)cudaGetLastError();
-        return nullptr;
-    }
-    return reinterpret_cast<EncodeTiledFn>(p);
-}
-
-EncodeTiledFn encode_tiled_fn() {
-    static const EncodeTiledFn fn = lookup_encode_tiled();   // initialised once, thread-safe
-    return fn;
-}
-
 // [rows, d] uint8 tensor, boxes of 128 rows x 64 bytes (one column half of a tile), 64-byte swizzle.
 bool make_tile_map(CUtensorMap *map, const void *ptr, uint64_t rows, uint32_t d) {
     EncodeTiledFn fn = encode_tiled_fn();
