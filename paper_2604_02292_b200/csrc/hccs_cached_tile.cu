@@ -9,10 +9,11 @@
 // twice: once for the maximum of the raw accumulators (the requantisation is monotone), once for r.  sum V over
 // the keys a row sees is a contraction of its own, with the 0/1 bytes of the mask in the place of r.
 //
-// Roles: sixteen row warps (four threads per row, 32 keys of every block each; TMEM lane = row), three warps that
-// issue the TMA loads of every third block (a box per page, or per 128 keys of a larger one, a lane each), one
-// thread that issues Q.K^T and one that issues the two products with V.  K blocks of the first pass, then K and V
-// blocks in turn, stream through one ring; load number x uses slot x % kSlots.
+// Roles: sixteen row warps in two groups that take alternate blocks (two threads per row and group, 64 keys of a
+// block each; TMEM lane = row), two warps that issue the TMA loads of alternate tiles (a box per page, or per 128
+// keys of a larger one, a lane each), one thread that issues Q.K^T and one that issues the two products with V (and
+// in the first pass, where there are none, every second Q.K^T).  K blocks of the first pass, then K and V blocks
+// in turn, stream through one ring; load number x uses slot x % kSlots.
 //
 // Few rows and many keys: the key blocks of a row tile are split over the CTAs of a cluster, which exchange row
 // maxima between the passes and sums at the end through distributed shared memory (exact integers: the split
@@ -29,8 +30,8 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr int kRowThreads = 512;
-constexpr int kCopyWarp = 16, kCopyWarps = 3, kQkWarp = 19, kPvWarp = 20;
-constexpr int kThreads = 672;
+constexpr int kCopyWarp = 16, kCopyWarps = 2, kQkWarp = 18, kPvWarp = 19;
+constexpr int kThreads = 640;                    // 20 warps: 96 registers a thread
 constexpr int kTile = 128;
 constexpr int kPanelBytes = kTile * 128;         // 128 rows x 128 keys, 128-byte swizzle
 constexpr int kMaxSlots = 12;
@@ -41,8 +42,9 @@ constexpr int kNone = -(1 << 30);                // below every accumulator
 struct TileBarriers {
     uint64_t o_full;
     uint64_t full[kMaxSlots], free[kMaxSlots];
-    uint64_t s_full[3], s_free[3];
-    uint64_t r_ready[2], r_free[2];
+    uint64_t m_full[4], m_free[4];      // S blocks of the first pass (all of tensor memory holds four)
+    uint64_t s_full[2], s_free[2];      // S blocks of the second: block kb in buffer kb & 1, group kb & 1
+    uint64_t r_ready[2], r_free[2];     // r and mask panels of block kb in buffer kb & 1
 };
 
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
@@ -62,8 +64,7 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
     constexpr uint64_t kSwizzle = D == 128 ? kSwizzle128 : kSwizzle64;
     constexpr uint32_t kIdescPV = kIdescPVOf<D>;
     constexpr int kSlots = kSlotsOf<D>;
-    constexpr int kSBufs = D == 128 ? 2 : 3;
-    constexpr uint32_t kTmemO = kSBufs * 128, kTmemW = kTmemO + D;
+    constexpr uint32_t kTmemO = 256, kTmemW = kTmemO + D;      // S in columns 0..255 (0..511 in the first pass)
     constexpr int kCols = D / 4;                 // columns of O and W per row thread
     constexpr int kDump = D + 4;                 // row pitch of the joined sums, in words
     extern __shared__ uint8_t smem_raw[];
@@ -105,8 +106,13 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
         any_bad = 0;
         mbar_init(smem_u32(&bars.o_full), 1);
         for (int i = 0; i < kSlots; ++i) { mbar_init(smem_u32(&bars.full[i]), 1); mbar_init(smem_u32(&bars.free[i]), 1); }
-        for (int i = 0; i < 3; ++i) { mbar_init(smem_u32(&bars.s_full[i]), 1); mbar_init(smem_u32(&bars.s_free[i]), row_threads); }
-        for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&bars.r_ready[i]), row_threads); mbar_init(smem_u32(&bars.r_free[i]), 1); }
+        for (int i = 0; i < 4; ++i) { mbar_init(smem_u32(&bars.m_full[i]), 1); mbar_init(smem_u32(&bars.m_free[i]), row_threads / 2); }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_u32(&bars.s_full[i]), 1);
+            mbar_init(smem_u32(&bars.s_free[i]), row_threads / 2);
+            mbar_init(smem_u32(&bars.r_ready[i]), row_threads / 2);
+            mbar_init(smem_u32(&bars.r_free[i]), 1);
+        }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -148,84 +154,97 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
         const int box = min(1 << a.page_shift, kTile), boxes = kTile / box;
         const int loads = 3 * nb;
         bool ok = true;
-        for (int x = warp - kCopyWarp; ok && x < loads; x += kCopyWarps) {
-            const int kb = x < nb ? x : (x - nb) >> 1;
-            const bool values = x >= nb && ((x - nb) & 1);
-            // lane l of `boxes` copies keys l * box ... of the block; keys that are not there, or whose page is not,
-            // are left out (their masks are clear and what the slot held is finite)
-            const int key = (kb0 + kb) * kTile + lane * box;
+        // lane l of `boxes` copies keys l * box ... of the block; keys that are not there, or whose page is not, are left
+        // out (their masks are clear and what the slot held is finite).  The page of the next load is looked up early.
+        auto block_of = [&](int x) { return x < nb ? x : (x - nb) >> 1; };
+        auto page_of = [&](int x) -> int {
+            const int key = (kb0 + block_of(x)) * kTile + lane * box;
             int page = -1;
-            if (lane < boxes && key < seq.n) {
-                page = __ldg(table + (key >> a.page_shift));
-                if ((uint32_t)page >= (uint32_t)a.num_pages) page = -1;
-            }
-            const int count = __popc(__ballot_sync(~0u, page >= 0));
+            if (lane < boxes && key < seq.n) page = __ldg(table + (key >> a.page_shift));
+            return page;
+        };
+        const int x0 = warp - kCopyWarp;
+        int page = x0 < loads ? page_of(x0) : -1;
+        for (int x = x0; ok && x < loads; x += kCopyWarps) {
+            const bool values = x >= nb && ((x - nb) & 1);
+            const bool there = (uint32_t)page < (uint32_t)a.num_pages;
+            const int count = __popc(__ballot_sync(~0u, there));
+            const int next = x + kCopyWarps < loads ? page_of(x + kCopyWarps) : -1;
             if (x >= kSlots) ok = __all_sync(~0u, wait(&bars.free[x % kSlots], (x / kSlots - 1) & 1));
             if (!ok) break;
             const uint32_t bar = smem_u32(&bars.full[x % kSlots]);
             if (lane == 0) mbar_expect_tx(bar, (uint32_t)(count * box * D));
             __syncwarp();
-            if (page >= 0)
+            if (there)
                 tma_load_3d(s_ring + (x % kSlots) * kTileBytes + lane * box * D, values ? &map_v : &map_k, 0,
-                            key & ((1 << a.page_shift) - 1), page * a.Hkv + kvh, bar);
+                            (block_of(x) * kTile + kb0 * kTile + lane * box) & ((1 << a.page_shift) - 1), page * a.Hkv + kvh, bar);
+            page = next;
         }
-    } else if (warp == kQkWarp) {
-        // ===================================================== S = Q.K^T, twice
+    } else if (warp == kQkWarp || warp == kPvWarp) {
+        // ===================================================== the products, issued by one thread of each warp
         if (split > 1) cluster_arrive();
         if (lane == 0 && nb > 0) {
+            const int me = warp == kQkWarp ? 0 : 1;
             bool ok = true;
             const uint64_t dq = smem_desc(s_q, 16, 8 * D, kSwizzle), dk = smem_desc(s_ring, 16, 8 * D, kSwizzle);
             const uint32_t dq_lo = (uint32_t)dq, dq_hi = (uint32_t)(dq >> 32), dk_lo = (uint32_t)dk, dk_hi = (uint32_t)(dk >> 32);
-            uint32_t sb = 0, cyc = 0;
-            for (int g = 0; ok && g < 2 * nb; ++g) {
-                const int x = g < nb ? g : nb + 2 * (g - nb);
-                const int slot = x % kSlots;
-                if (cyc > 0) ok = wait(&bars.s_free[sb], (cyc - 1) & 1);
-                if (ok) ok = wait(&bars.full[slot], (x / kSlots) & 1);
-                if (!ok) break;
+            auto qk = [&](int slot, uint32_t column, uint64_t *full) {
                 tcgen05_fence_after();
-                const uint32_t koff = (uint32_t)(slot * kTileBytes) >> 4;
+                const uint32_t k_lo = dk_lo + ((uint32_t)(slot * kTileBytes) >> 4);
 #pragma unroll
-                for (int ks = 0; ks < D / 32; ++ks) {
-                    const uint32_t off = (uint32_t)(ks * 32) >> 4;
-                    tcgen05_mma_i8(tmem + sb * 128, make_u64(dq_lo + off, dq_hi), make_u64(dk_lo + koff + off, dk_hi), kIdescQK, ks != 0);
-                }
-                tcgen05_commit(smem_u32(&bars.s_full[sb]));
+                for (int ks = 0; ks < D / 32; ++ks)
+                    tcgen05_mma_i8(tmem + column, make_u64(dq_lo + 2 * ks, dq_hi), make_u64(k_lo + 2 * ks, dk_hi), kIdescQK, ks != 0);
+                tcgen05_commit(smem_u32(full));
                 tcgen05_commit(smem_u32(&bars.free[slot]));
-                if (++sb == kSBufs) { sb = 0; ++cyc; }
+            };
+            // first pass: S = Q.K^T, the blocks in turn between the two threads
+            for (int g = me; ok && g < nb; g += 2) {
+                const int slot = g % kSlots, sb = g & 3;
+                if (g >= 4) ok = wait(&bars.m_free[sb], ((g >> 2) - 1) & 1);
+                if (ok) ok = wait(&bars.full[slot], (g / kSlots) & 1);
+                if (ok) qk(slot, sb * 128, &bars.m_full[sb]);
             }
-        }
-        __syncwarp();
-    } else if (warp == kPvWarp) {
-        // ===================================================== O += r.V, W += mask.V
-        if (split > 1) cluster_arrive();
-        if (lane == 0 && nb > 0) {
-            bool ok = true;
-            const uint64_t dr = smem_desc(s_r, 16, 1024, kSwizzle128), dv = smem_desc(s_ring, 8 * D, 8 * D, kSwizzle);
-            const uint32_t dr_lo = (uint32_t)dr, dr_hi = (uint32_t)(dr >> 32), dv_lo = (uint32_t)dv, dv_hi = (uint32_t)(dv >> 32);
-            for (int kb = 0; ok && kb < nb; ++kb) {
-                const int x = nb + 2 * kb + 1, slot = x % kSlots, buf = kb & 1;
-                ok = wait(&bars.full[slot], (x / kSlots) & 1);
-                if (ok) ok = wait(&bars.r_ready[buf], (kb >> 1) & 1);
-                if (!ok) break;
-                tcgen05_fence_after();
-#pragma unroll
-                for (int w = 0; w < 2; ++w)
-#pragma unroll
-                    for (int ks = 0; ks < 4; ++ks) {
-                        const uint32_t roff = (uint32_t)((2 * w + buf) * kPanelBytes + ks * 32) >> 4;
-                        const uint32_t voff = (uint32_t)(slot * kTileBytes + ks * 32 * D) >> 4;
-                        tcgen05_mma_i8(tmem + (w ? kTmemW : kTmemO), make_u64(dr_lo + roff, dr_hi), make_u64(dv_lo + voff, dv_hi), kIdescPV, (kb | ks) != 0);
+            if (me == 0) {
+                // second pass: S again
+                for (int kb = 0; ok && kb < nb; ++kb) {
+                    const int x = nb + 2 * kb, slot = x % kSlots, sb = kb & 1;
+                    if (kb >= 2) {
+                        ok = wait(&bars.s_free[sb], ((kb >> 1) - 1) & 1);
+                    } else {      // the buffer's last block of the first pass has been read
+                        const int uses = (nb - kb + 3) >> 2;
+                        if (uses > 0) ok = wait(&bars.m_free[kb], (uses - 1) & 1);
                     }
-                tcgen05_commit(smem_u32(&bars.free[slot]));
-                tcgen05_commit(smem_u32(&bars.r_free[buf]));
+                    if (ok) ok = wait(&bars.full[slot], (x / kSlots) & 1);
+                    if (ok) qk(slot, sb * 128, &bars.s_full[sb]);
+                }
+            } else {
+                // O += r.V, W += mask.V
+                const uint64_t dr = smem_desc(s_r, 16, 1024, kSwizzle128), dv = smem_desc(s_ring, 8 * D, 8 * D, kSwizzle);
+                const uint32_t dr_lo = (uint32_t)dr, dr_hi = (uint32_t)(dr >> 32), dv_lo = (uint32_t)dv, dv_hi = (uint32_t)(dv >> 32);
+                for (int kb = 0; ok && kb < nb; ++kb) {
+                    const int x = nb + 2 * kb + 1, slot = x % kSlots, buf = kb & 1;
+                    ok = wait(&bars.full[slot], (x / kSlots) & 1);
+                    if (ok) ok = wait(&bars.r_ready[buf], (kb >> 1) & 1);
+                    if (!ok) break;
+                    tcgen05_fence_after();
+                    const uint32_t v_lo = dv_lo + ((uint32_t)(slot * kTileBytes) >> 4), r_lo = dr_lo + (uint32_t)(buf * kPanelBytes >> 4);
+#pragma unroll
+                    for (int w = 0; w < 2; ++w)
+#pragma unroll
+                        for (int ks = 0; ks < 4; ++ks)
+                            tcgen05_mma_i8(tmem + (w ? kTmemW : kTmemO), make_u64(r_lo + (2 * w * kPanelBytes >> 4) + 2 * ks, dr_hi),
+                                           make_u64(v_lo + (ks * 32 * D >> 4), dv_hi), kIdescPV, (kb | ks) != 0);
+                    tcgen05_commit(smem_u32(&bars.free[slot]));
+                    tcgen05_commit(smem_u32(&bars.r_free[buf]));
+                }
+                if (ok) tcgen05_commit(smem_u32(&bars.o_full));
             }
-            if (ok) tcgen05_commit(smem_u32(&bars.o_full));
         }
         __syncwarp();
     } else {
-        // ===================================================== row warps: threads t, t+128, t+256, t+384 own row t
-        const int t = tid & (kTile - 1), grp = tid >> 7;
+        // ===================================================== row warps: threads t, t+128, t+256, t+384 own row t, the
+        // first two the halves of the even blocks, the others those of the odd ones
+        const int t = tid & (kTile - 1), grp = tid >> 7, group = grp >> 1, half = grp & 1;
         const bool active = (warp & 3) < quarters;
         cg::cluster_group cluster = cg::this_cluster();
         auto row_barrier = [&]() { asm volatile("bar.sync 1, %0;" ::"r"(row_threads) : "memory"); };
@@ -238,12 +257,11 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
         int M = 0;
         int rsum = 0, count = 0;
         int xmax = 0;
-        uint32_t s_buf = 0, s_cyc = 0;
-        // which of the thread's 32 keys of block kb its row sees
+        // which of keys 64 * half + 32 * part ... of block kb the thread's row sees
         const int seen_all = !real ? 0 : min(a.tree_mask ? seq.prefix : seq.prefix + qi + 1, seq.n);
         const uint32_t *tree = a.tree_mask ? reinterpret_cast<const uint32_t *>(a.tree_mask) + ((int64_t)seq.s0 + qi) * a.tree_words : nullptr;
-        auto mask_of = [&](int kb) -> uint32_t {
-            const int c0 = (kb0 + kb) * kTile + grp * 32;
+        auto mask_of = [&](int kb, int part) -> uint32_t {
+            const int c0 = (kb0 + kb) * kTile + half * 64 + part * 32;
             uint32_t m = low_bits(seen_all - c0);
             if (tree && real && m != 0xffffffffu) {
                 // new key number j0 + k sits at bit k; words beyond max_q's last are never read
@@ -273,23 +291,28 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
             rq = make_requant(M, a.requant_shift);
             // ---- first pass: the largest accumulator
             int amax = kNone;
-            for (int kb = 0; ok && kb < nb; ++kb) {
-                const uint32_t mask = mask_of(kb);
-                ok = __all_sync(~0u, wait(&bars.s_full[s_buf], s_cyc & 1));
+            for (int kb = group; ok && kb < nb; kb += 2) {
+                const int sb = kb & 3;
+                ok = __all_sync(~0u, wait(&bars.m_full[sb], (kb >> 2) & 1));
                 if (!ok) break;
                 tcgen05_fence_after();
-                uint32_t acc[32];
-                tmem_ld32(tmem + lane_addr + s_buf * 128 + grp * 32, acc);
-                tcgen05_fence_before();
-                mbar_arrive(smem_u32(&bars.s_free[s_buf]));
-                if (++s_buf == kSBufs) { s_buf = 0; ++s_cyc; }
-                if (mask != 0xffffffffu) {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (!((mask >> i) & 1)) acc[i] = (uint32_t)kNone;
+                for (int part = 0; part < 2; ++part) {
+                    uint32_t acc[32];
+                    tmem_ld32(tmem + lane_addr + sb * 128 + half * 64 + part * 32, acc);
+                    if (part == 1) {
+                        tcgen05_fence_before();
+                        mbar_arrive(smem_u32(&bars.m_free[sb]));
+                    }
+                    const uint32_t mask = mask_of(kb, part);
+                    if (mask != 0xffffffffu) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (!((mask >> i) & 1)) acc[i] = (uint32_t)kNone;
+                    }
+#pragma unroll
+                    for (int i = 0; i < 32; i += 2) amax = __vimax3_s32(amax, (int)acc[i], (int)acc[i + 1]);
                 }
-#pragma unroll
-                for (int i = 0; i < 32; i += 2) amax = __vimax3_s32(amax, (int)acc[i], (int)acc[i + 1]);
             }
             part_max[grp][t] = amax;
             row_barrier();
@@ -319,50 +342,56 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
             const uint32_t mk = rq.mk, ck = ((uint32_t)((int64_t)lo_u * M + R) << k) - ((uint32_t)u << 24);
             const int swz = t & 7;
             const uint32_t row_off = (uint32_t)((t >> 3) * 1024 + (t & 7) * 128);
-            uint32_t held[2] = {0xdeadbeefu, 0xdeadbeefu};       // the masks whose bytes the two buffers hold, see below
-            bool fresh[2] = {true, true};
-            for (int kb = 0; ok && kb < nb; ++kb) {
-                const uint32_t mask = mask_of(kb);
-                ok = __all_sync(~0u, wait(&bars.s_full[s_buf], s_cyc & 1));
+            // r and mask panels of this group's blocks: buffer `group` of each
+            uint8_t *pr = g_r + group * kPanelBytes + row_off, *pw = g_w + group * kPanelBytes + row_off;
+            uint32_t held[2];                        // the masks whose bytes the mask panel holds, once `fresh` is false
+            bool fresh = true;
+            for (int kb = group; ok && kb < nb; kb += 2) {
+                ok = __all_sync(~0u, wait(&bars.s_full[group], (kb >> 1) & 1));
                 if (!ok) break;
                 tcgen05_fence_after();
-                uint32_t acc[32];
-                tmem_ld32(tmem + lane_addr + s_buf * 128 + grp * 32, acc);
-                tcgen05_fence_before();
-                mbar_arrive(smem_u32(&bars.s_free[s_buf]));
-                if (++s_buf == kSBufs) { s_buf = 0; ++s_cyc; }
 #pragma unroll
-                for (int i = 0; i < 32; ++i) acc[i] = (uint32_t)__viaddmin_s32_relu((int)acc[i], neg_lo, span) * mk + ck;
-                if (mask != 0xffffffffu) {
+                for (int part = 0; part < 2; ++part) {
+                    uint32_t acc[32];
+                    tmem_ld32(tmem + lane_addr + group * 128 + half * 64 + part * 32, acc);
+                    if (part == 1) {
+                        tcgen05_fence_before();
+                        mbar_arrive(smem_u32(&bars.s_free[group]));
+                    }
+                    const uint32_t mask = mask_of(kb, part);
 #pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (!((mask >> i) & 1)) acc[i] = 0u;
+                    for (int i = 0; i < 32; ++i) acc[i] = (uint32_t)__viaddmin_s32_relu((int)acc[i], neg_lo, span) * mk + ck;
+                    if (mask != 0xffffffffu) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (!((mask >> i) & 1)) acc[i] = 0u;
+                    }
+                    uint32_t w[8];
+#pragma unroll
+                    for (int g = 0; g < 8; ++g) {
+                        w[g] = __byte_perm(__byte_perm(acc[4 * g], acc[4 * g + 1], 0x0073), __byte_perm(acc[4 * g + 2], acc[4 * g + 3], 0x0073), 0x5410);
+                        rsum = (int)__dp4a(w[g], 0x01010101u, (uint32_t)rsum);
+                    }
+                    count += __popc(mask);
+                    // the products of the buffer's previous block have read it
+                    if (part == 0 && kb >= 2) ok = __all_sync(~0u, wait(&bars.r_free[group], ((kb >> 1) - 1) & 1));
+                    const int c16 = 4 * half + 2 * part;
+                    *reinterpret_cast<uint4 *>(pr + ((c16 ^ swz) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+                    *reinterpret_cast<uint4 *>(pr + (((c16 + 1) ^ swz) << 4)) = make_uint4(w[4], w[5], w[6], w[7]);
+                    // the mask's bytes are written only where they differ from what the panel holds: full blocks,
+                    // the common case, write them once
+                    if (fresh || held[part] != mask) {
+#pragma unroll
+                        for (int g = 0; g < 8; ++g) w[g] = (((mask >> (4 * g)) & 15u) * 0x00204081u) & 0x01010101u;
+                        *reinterpret_cast<uint4 *>(pw + ((c16 ^ swz) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+                        *reinterpret_cast<uint4 *>(pw + (((c16 + 1) ^ swz) << 4)) = make_uint4(w[4], w[5], w[6], w[7]);
+                        held[part] = mask;
+                    }
                 }
-                uint32_t w[8];
-#pragma unroll
-                for (int g = 0; g < 8; ++g) {
-                    w[g] = __byte_perm(__byte_perm(acc[4 * g], acc[4 * g + 1], 0x0073), __byte_perm(acc[4 * g + 2], acc[4 * g + 3], 0x0073), 0x5410);
-                    rsum = (int)__dp4a(w[g], 0x01010101u, (uint32_t)rsum);
-                }
-                count += __popc(mask);
-                const int buf = kb & 1;
-                if (kb >= 2) ok = __all_sync(~0u, wait(&bars.r_free[buf], ((kb >> 1) - 1) & 1));
                 if (!ok) break;
-                uint8_t *p = g_r + buf * kPanelBytes + row_off;
-                *reinterpret_cast<uint4 *>(p + (((2 * grp) ^ swz) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
-                *reinterpret_cast<uint4 *>(p + (((2 * grp + 1) ^ swz) << 4)) = make_uint4(w[4], w[5], w[6], w[7]);
-                // the mask's bytes are written only where they differ from what the buffer holds: full blocks, the
-                // common case, write them once
-                if (buf == 0 ? (fresh[0] || held[0] != mask) : (fresh[1] || held[1] != mask)) {
-#pragma unroll
-                    for (int g = 0; g < 8; ++g) w[g] = (((mask >> (4 * g)) & 15u) * 0x00204081u) & 0x01010101u;
-                    uint8_t *pw = g_w + buf * kPanelBytes + row_off;
-                    *reinterpret_cast<uint4 *>(pw + (((2 * grp) ^ swz) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
-                    *reinterpret_cast<uint4 *>(pw + (((2 * grp + 1) ^ swz) << 4)) = make_uint4(w[4], w[5], w[6], w[7]);
-                    if (buf == 0) { held[0] = mask; fresh[0] = false; } else { held[1] = mask; fresh[1] = false; }
-                }
+                fresh = false;
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                mbar_arrive(smem_u32(&bars.r_ready[buf]));
+                mbar_arrive(smem_u32(&bars.r_ready[group]));
             }
             part_sum[grp][t] = rsum;
             part_cnt[grp][t] = count;
