@@ -41,6 +41,7 @@ constexpr int kNone = -(1 << 30);                // below every accumulator
 
 struct TileBarriers {
     uint64_t o_full;
+    uint64_t m_done;                    // every row thread has read its last S block of the first pass
     uint64_t full[kMaxSlots], free[kMaxSlots];
     uint64_t m_full[4], m_free[4];      // S blocks of the first pass (all of tensor memory holds four)
     uint64_t s_full[2], s_free[2];      // S blocks of the second: block kb in buffer kb & 1, group kb & 1
@@ -64,6 +65,7 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
     constexpr uint64_t kSwizzle = D == 128 ? kSwizzle128 : kSwizzle64;
     constexpr uint32_t kIdescPV = kIdescPVOf<D>;
     constexpr int kSlots = kSlotsOf<D>;
+    static_assert(kSlots % 2 == 0 && kCopyWarps == 2, "a slot belongs to one copy warp, and in each pass to one issuer");
     constexpr uint32_t kTmemO = 256, kTmemW = kTmemO + D;      // S in columns 0..255 (0..511 in the first pass)
     constexpr int kCols = D / 4;                 // columns of O and W per row thread
     constexpr int kDump = D + 4;                 // row pitch of the joined sums, in words
@@ -75,7 +77,8 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
     __shared__ int part_sum[4][kTile], part_cnt[4][kTile];
     __shared__ int cta_sum[kTile], cta_cnt[kTile];
 
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, lane = tid & 31;
+    const int warp = __shfl_sync(~0u, tid >> 5, 0);                        // (uniform in the compiler's eyes too)
     const int b = blockIdx.z, kvh = blockIdx.y;
     const int rank = (int)blockIdx.x % split;
     const int rt = (int)(gridDim.x / split - 1 - blockIdx.x / split);      // the tiles with the most keys first
@@ -105,6 +108,7 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
         abort_flag = 0;
         any_bad = 0;
         mbar_init(smem_u32(&bars.o_full), 1);
+        mbar_init(smem_u32(&bars.m_done), row_threads);
         for (int i = 0; i < kSlots; ++i) { mbar_init(smem_u32(&bars.full[i]), 1); mbar_init(smem_u32(&bars.free[i]), 1); }
         for (int i = 0; i < 4; ++i) { mbar_init(smem_u32(&bars.m_full[i]), 1); mbar_init(smem_u32(&bars.m_free[i]), row_threads / 2); }
         for (int i = 0; i < 2; ++i) {
@@ -181,21 +185,29 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
             page = next;
         }
     } else if (warp == kQkWarp || warp == kPvWarp) {
-        // ===================================================== the products, issued by one thread of each warp
+        // ===================================================== the products, issued by one thread of each warp.  The whole
+        // warp walks through the loops and only the instructions themselves are the elected thread's: in a branch of one
+        // lane the operands, which have to be uniform, cost about 100 cycles per product
         if (split > 1) cluster_arrive();
-        if (lane == 0 && nb > 0) {
+        if (nb > 0) {
             const int me = warp == kQkWarp ? 0 : 1;
             bool ok = true;
+            auto wait = [&](uint64_t *bar, uint32_t parity) -> bool {
+                return __all_sync(~0u, mbar_wait(smem_u32(bar), parity, abortp, a.status, a.wait_cycles));
+            };
             const uint64_t dq = smem_desc(s_q, 16, 8 * D, kSwizzle), dk = smem_desc(s_ring, 16, 8 * D, kSwizzle);
             const uint32_t dq_lo = (uint32_t)dq, dq_hi = (uint32_t)(dq >> 32), dk_lo = (uint32_t)dk, dk_hi = (uint32_t)(dk >> 32);
             auto qk = [&](int slot, uint32_t column, uint64_t *full) {
                 tcgen05_fence_after();
                 const uint32_t k_lo = dk_lo + ((uint32_t)(slot * kTileBytes) >> 4);
+                if (elect_one()) {
 #pragma unroll
-                for (int ks = 0; ks < D / 32; ++ks)
-                    tcgen05_mma_i8(tmem + column, make_u64(dq_lo + 2 * ks, dq_hi), make_u64(k_lo + 2 * ks, dk_hi), kIdescQK, ks != 0);
-                tcgen05_commit(smem_u32(full));
-                tcgen05_commit(smem_u32(&bars.free[slot]));
+                    for (int ks = 0; ks < D / 32; ++ks)
+                        tcgen05_mma_i8(tmem + column, make_u64(dq_lo + 2 * ks, dq_hi), make_u64(k_lo + 2 * ks, dk_hi), kIdescQK, ks != 0);
+                    tcgen05_commit(smem_u32(full));
+                    tcgen05_commit(smem_u32(&bars.free[slot]));
+                }
+                __syncwarp();
             };
             // first pass: S = Q.K^T, the blocks in turn between the two threads
             for (int g = me; ok && g < nb; g += 2) {
@@ -204,16 +216,15 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
                 if (ok) ok = wait(&bars.full[slot], (g / kSlots) & 1);
                 if (ok) qk(slot, sb * 128, &bars.m_full[sb]);
             }
+            // Between the passes buffers and slots change hands: tensor memory from S to O and W, a ring slot from one of
+            // these threads to the other where nb is odd.  A wait by parity must not be two phases behind its barrier, so
+            // both threads see the first pass finished (all its loads landed, all its products read) before they go on.
+            if (ok) ok = wait(&bars.m_done, 0);
             if (me == 0) {
                 // second pass: S again
                 for (int kb = 0; ok && kb < nb; ++kb) {
                     const int x = nb + 2 * kb, slot = x % kSlots, sb = kb & 1;
-                    if (kb >= 2) {
-                        ok = wait(&bars.s_free[sb], ((kb >> 1) - 1) & 1);
-                    } else {      // the buffer's last block of the first pass has been read
-                        const int uses = (nb - kb + 3) >> 2;
-                        if (uses > 0) ok = wait(&bars.m_free[kb], (uses - 1) & 1);
-                    }
+                    if (kb >= 2) ok = wait(&bars.s_free[sb], ((kb >> 1) - 1) & 1);
                     if (ok) ok = wait(&bars.full[slot], (x / kSlots) & 1);
                     if (ok) qk(slot, sb * 128, &bars.s_full[sb]);
                 }
@@ -228,16 +239,19 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
                     if (!ok) break;
                     tcgen05_fence_after();
                     const uint32_t v_lo = dv_lo + ((uint32_t)(slot * kTileBytes) >> 4), r_lo = dr_lo + (uint32_t)(buf * kPanelBytes >> 4);
+                    if (elect_one()) {
 #pragma unroll
-                    for (int w = 0; w < 2; ++w)
+                        for (int w = 0; w < 2; ++w)
 #pragma unroll
-                        for (int ks = 0; ks < 4; ++ks)
-                            tcgen05_mma_i8(tmem + (w ? kTmemW : kTmemO), make_u64(r_lo + (2 * w * kPanelBytes >> 4) + 2 * ks, dr_hi),
-                                           make_u64(v_lo + (ks * 32 * D >> 4), dv_hi), kIdescPV, (kb | ks) != 0);
-                    tcgen05_commit(smem_u32(&bars.free[slot]));
-                    tcgen05_commit(smem_u32(&bars.r_free[buf]));
+                            for (int ks = 0; ks < 4; ++ks)
+                                tcgen05_mma_i8(tmem + (w ? kTmemW : kTmemO), make_u64(r_lo + (2 * w * kPanelBytes >> 4) + 2 * ks, dr_hi),
+                                               make_u64(v_lo + (ks * 32 * D >> 4), dv_hi), kIdescPV, (kb | ks) != 0);
+                        tcgen05_commit(smem_u32(&bars.free[slot]));
+                        tcgen05_commit(smem_u32(&bars.r_free[buf]));
+                        if (kb == nb - 1) tcgen05_commit(smem_u32(&bars.o_full));
+                    }
+                    __syncwarp();
                 }
-                if (ok) tcgen05_commit(smem_u32(&bars.o_full));
             }
         }
         __syncwarp();
@@ -314,6 +328,7 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
                     for (int i = 0; i < 32; i += 2) amax = __vimax3_s32(amax, (int)acc[i], (int)acc[i + 1]);
                 }
             }
+            mbar_arrive(smem_u32(&bars.m_done));
             part_max[grp][t] = amax;
             row_barrier();
             xmax = max(max(part_max[0][t], part_max[1][t]), max(part_max[2][t], part_max[3][t]));

@@ -471,6 +471,38 @@ def test_trees(hccs, q_lens, kv_lens, hq, hkv, d, page, norm, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("B,q_len,kv,hq,hkv,d,page", [(8, 8, 8000, 32, 8, 128, 64), (8, 8, 7900, 32, 8, 64, 16), (3, 100, 6001, 8, 4, 128, 32), (40, 3, 2305, 16, 4, 64, 128),
+                                                      (2, 700, 5000, 12, 4, 128, 64), (1, 5, 60000, 6, 1, 128, 16), (1, 1000, 1000, 30, 10, 64, 32), (20, 40, 4100, 8, 8, 128, 256)])
+def test_many_queries_agree_with_single_tokens(hccs, B, q_len, kv, hq, hkv, d, page):
+    """At sizes beyond the oracle: a causal query is a single token of a sequence that ends with it, and sums are exact,
+    so both kernels give the same bits.  Repeated, since what could go wrong here are races."""
+    import torch
+    rng = np.random.default_rng(kv)
+    ctx = hccs.Context(0)
+    ctx.hccs_params_upload_wide(_theta(rng, hq, kv, True), kv)
+    g = torch.Generator(device="cuda").manual_seed(kv)
+    per = -(-kv // page)
+    kp, vp = (torch.randint(-128, 128, (B * per, hkv, page, d), device="cuda", generator=g).to(torch.int8) for _ in range(2))
+    table = torch.randperm(B * per, device="cuda", generator=g).to(torch.int32).reshape(B, per)
+    Q = torch.randint(-128, 128, (B * q_len, hq, d), device="cuda", generator=g).to(torch.int8)
+    mult, scale = np.full(hq, int(20 / (74.0 ** 2 * math.sqrt(d)) * (1 << 20)), np.int32), np.full(hq, 0.03, np.float32)
+    lens = torch.randint(q_len + (kv - q_len) // 2, kv + 1, (B,), device="cuda", generator=g).to(torch.int32)
+    lens[0] = kv
+    kw = dict(out_scale=scale, flags=hccs.HCCS_RECIP_REAL, max_kv=kv)
+    want = torch.empty((B * q_len, hq, d), device="cuda")
+    single = lens.repeat_interleave(q_len) - q_len + 1 + torch.arange(q_len, device="cuda", dtype=torch.int32).repeat(B)
+    ctx.hccs_attention_cached(Q, kp, vp, table.repeat_interleave(q_len, 0).contiguous(), torch.arange(B * q_len + 1, dtype=torch.int32, device="cuda"),
+                              single.to(torch.int32), want, mult, 20, max_q=1, **kw)
+    start = torch.arange(0, B * q_len + 1, q_len, dtype=torch.int32, device="cuda")
+    for _ in range(8):
+        got = torch.full_like(want, 7.0)
+        ctx.hccs_attention_cached(Q, kp, vp, table, start, lens, got, mult, 20, max_q=q_len, **kw)
+        assert ctx.hccs_device_status() == 0
+        assert torch.equal(got, want), f"{(got != want).sum().item()} of {got.numel()} differ"
+    ctx.close()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("d", [64, 128])
 def test_rows_that_see_nothing(hccs, d):
     """Tree rows without a bit and without a prefix, queries in front of the first key, sequences without keys."""
