@@ -20,6 +20,8 @@
 // changes no bit).  Row warps whose 32 rows lie behind the tile's last row do nothing.
 #include <cooperative_groups.h>
 
+#include <type_traits>
+
 #include "hccs_cached.cuh"
 #include "hccs_tcgen05.cuh"
 
@@ -38,6 +40,9 @@ constexpr int kMaxSlots = 12;
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kIdescQK = instr_desc(1, 1, 0, 128, 128);
 constexpr int kNone = -(1 << 30);                // below every accumulator
+
+using Yes = std::true_type;
+using No = std::false_type;
 
 struct TileBarriers {
     uint64_t o_full;
@@ -96,6 +101,8 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
     const int blocks = (n_tile + kTile - 1) / kTile;
     const int per = (blocks + split - 1) / split;
     const int kb0 = min(rank * per, blocks), nb = min(kb0 + per, blocks) - kb0;
+    // the leading blocks that every row sees whole (as long as no page is bad)
+    const int seen_first = min(a.tree_mask ? seq.prefix : seq.prefix + row0 / a.group + 1, seq.n);
     const int32_t *table = a.page_table + (int64_t)b * a.max_pages;
     volatile int *abortp = &abort_flag;
 
@@ -149,6 +156,7 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
     const uint32_t tmem = tmem_slot;
     const bool bad = any_bad != 0;
     if (bad && tid == 0) atomicOr(a.status, STATUS_BAD_PAGE);
+    const int nfull = bad ? 0 : min(max(seen_first / kTile - kb0, 0), nb);
     auto wait = [&](uint64_t *bar, uint32_t parity) { return mbar_wait(smem_u32(bar), parity, abortp, a.status, a.wait_cycles); };
 
     if (warp >= kCopyWarp && warp < kCopyWarp + kCopyWarps) {
@@ -270,7 +278,7 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
         Requant rq;
         int M = 0;
         int rsum = 0, count = 0;
-        int xmax = 0;
+        int xmax = 0, kb;
         // which of keys 64 * half + 32 * part ... of block kb the thread's row sees
         const int seen_all = !real ? 0 : min(a.tree_mask ? seq.prefix : seq.prefix + qi + 1, seq.n);
         const uint32_t *tree = a.tree_mask ? reinterpret_cast<const uint32_t *>(a.tree_mask) + ((int64_t)seq.s0 + qi) * a.tree_words : nullptr;
@@ -305,10 +313,10 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
             rq = make_requant(M, a.requant_shift);
             // ---- first pass: the largest accumulator
             int amax = kNone;
-            for (int kb = group; ok && kb < nb; kb += 2) {
+            auto first = [&](int kb, auto masked) {
                 const int sb = kb & 3;
                 ok = __all_sync(~0u, wait(&bars.m_full[sb], (kb >> 2) & 1));
-                if (!ok) break;
+                if (!ok) return;
                 tcgen05_fence_after();
 #pragma unroll
                 for (int part = 0; part < 2; ++part) {
@@ -318,16 +326,18 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
                         tcgen05_fence_before();
                         mbar_arrive(smem_u32(&bars.m_free[sb]));
                     }
-                    const uint32_t mask = mask_of(kb, part);
-                    if (mask != 0xffffffffu) {
+                    if constexpr (decltype(masked)::value) {
+                        const uint32_t mask = mask_of(kb, part);
 #pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (!((mask >> i) & 1)) acc[i] = (uint32_t)kNone;
+                        for (int i = 0; i < 32; ++i) acc[i] = (mask >> i) & 1 ? acc[i] : (uint32_t)kNone;
                     }
 #pragma unroll
                     for (int i = 0; i < 32; i += 2) amax = __vimax3_s32(amax, (int)acc[i], (int)acc[i + 1]);
                 }
-            }
+            };
+            kb = group;
+            for (; ok && kb < nfull; kb += 2) first(kb, No{});
+            for (; ok && kb < nb; kb += 2) first(kb, Yes{});
             mbar_arrive(smem_u32(&bars.m_done));
             part_max[grp][t] = amax;
             row_barrier();
@@ -359,11 +369,14 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
             const uint32_t row_off = (uint32_t)((t >> 3) * 1024 + (t & 7) * 128);
             // r and mask panels of this group's blocks: buffer `group` of each
             uint8_t *pr = g_r + group * kPanelBytes + row_off, *pw = g_w + group * kPanelBytes + row_off;
-            uint32_t held[2];                        // the masks whose bytes the mask panel holds, once `fresh` is false
-            bool fresh = true;
-            for (int kb = group; ok && kb < nb; kb += 2) {
+            auto panel16 = [&](uint8_t *panel, int part, const uint32_t (&w)[8]) {      // 32 bytes of the thread's row
+                const int c16 = 4 * half + 2 * part;
+                *reinterpret_cast<uint4 *>(panel + ((c16 ^ swz) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+                *reinterpret_cast<uint4 *>(panel + (((c16 + 1) ^ swz) << 4)) = make_uint4(w[4], w[5], w[6], w[7]);
+            };
+            auto second = [&](int kb, auto masked) {
                 ok = __all_sync(~0u, wait(&bars.s_full[group], (kb >> 1) & 1));
-                if (!ok) break;
+                if (!ok) return;
                 tcgen05_fence_after();
 #pragma unroll
                 for (int part = 0; part < 2; ++part) {
@@ -373,41 +386,43 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
                         tcgen05_fence_before();
                         mbar_arrive(smem_u32(&bars.s_free[group]));
                     }
-                    const uint32_t mask = mask_of(kb, part);
 #pragma unroll
                     for (int i = 0; i < 32; ++i) acc[i] = (uint32_t)__viaddmin_s32_relu((int)acc[i], neg_lo, span) * mk + ck;
-                    if (mask != 0xffffffffu) {
+                    uint32_t w[8], ones[8];
+                    if constexpr (decltype(masked)::value) {
+                        const uint32_t mask = mask_of(kb, part);
+                        count += __popc(mask);
 #pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (!((mask >> i) & 1)) acc[i] = 0u;
+                        for (int g = 0; g < 8; ++g) ones[g] = (((mask >> (4 * g)) & 15u) * 0x00204081u) & 0x01010101u;
                     }
-                    uint32_t w[8];
 #pragma unroll
                     for (int g = 0; g < 8; ++g) {
                         w[g] = __byte_perm(__byte_perm(acc[4 * g], acc[4 * g + 1], 0x0073), __byte_perm(acc[4 * g + 2], acc[4 * g + 3], 0x0073), 0x5410);
+                        if constexpr (decltype(masked)::value) w[g] &= ones[g] * 255u;
                         rsum = (int)__dp4a(w[g], 0x01010101u, (uint32_t)rsum);
                     }
-                    count += __popc(mask);
                     // the products of the buffer's previous block have read it
-                    if (part == 0 && kb >= 2) ok = __all_sync(~0u, wait(&bars.r_free[group], ((kb >> 1) - 1) & 1));
-                    const int c16 = 4 * half + 2 * part;
-                    *reinterpret_cast<uint4 *>(pr + ((c16 ^ swz) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
-                    *reinterpret_cast<uint4 *>(pr + (((c16 + 1) ^ swz) << 4)) = make_uint4(w[4], w[5], w[6], w[7]);
-                    // the mask's bytes are written only where they differ from what the panel holds: full blocks,
-                    // the common case, write them once
-                    if (fresh || held[part] != mask) {
-#pragma unroll
-                        for (int g = 0; g < 8; ++g) w[g] = (((mask >> (4 * g)) & 15u) * 0x00204081u) & 0x01010101u;
-                        *reinterpret_cast<uint4 *>(pw + ((c16 ^ swz) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
-                        *reinterpret_cast<uint4 *>(pw + (((c16 + 1) ^ swz) << 4)) = make_uint4(w[4], w[5], w[6], w[7]);
-                        held[part] = mask;
+                    if (part == 0 && kb >= 2) {
+                        ok = __all_sync(~0u, wait(&bars.r_free[group], ((kb >> 1) - 1) & 1));
+                        if (!ok) return;
                     }
+                    panel16(pr, part, w);
+                    if constexpr (decltype(masked)::value) panel16(pw, part, ones);
                 }
-                if (!ok) break;
-                fresh = false;
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 mbar_arrive(smem_u32(&bars.r_ready[group]));
+            };
+            kb = group;
+            if (kb < nfull) {      // full blocks find the mask panel full of ones
+                uint32_t ones[8];
+#pragma unroll
+                for (int g = 0; g < 8; ++g) ones[g] = 0x01010101u;
+                panel16(pw, 0, ones);
+                panel16(pw, 1, ones);
+                count = 64 * ((nfull - group + 1) >> 1);
             }
+            for (; ok && kb < nfull; kb += 2) second(kb, No{});
+            for (; ok && kb < nb; kb += 2) second(kb, Yes{});
             part_sum[grp][t] = rsum;
             part_cnt[grp][t] = count;
             row_barrier();
