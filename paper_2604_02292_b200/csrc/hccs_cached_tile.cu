@@ -6,8 +6,13 @@
 //     sum s V = F*sum V + S*sum r V
 // needs only r, which leaves the accumulators by one clamp, one multiply-add and a byte pick per logit; F and S
 // join at the end, where the sums are complete.  The clamp needs the row maximum first, so Q.K^T is computed
-// twice: once for the maximum of the raw accumulators (the requantisation is monotone), once for r.  sum V over
-// the keys a row sees is a contraction of its own, with the 0/1 bytes of the mask in the place of r.
+// twice: once for the maximum of the raw accumulators (the requantisation is monotone), once for r.
+//
+// sum V over the keys a row sees: over the blocks that every row sees whole it is the same for all rows, and a spare
+// row of ones beside the rows' r (tiles of 127 rows, or any tile that is not full) brings it with the product that is
+// computed anyway; over the others (the last ones, where a mask cuts) it is a contraction of its own with the 0/1 bytes
+// of the mask in the place of r.  (With that second product in every block, a prompt chunk took 215 us instead of
+// 184: tensor time, and the first product of the next block queued behind it.)
 //
 // Roles: sixteen row warps in two groups that take alternate blocks (two threads per row and group, 64 keys of a
 // block each; TMEM lane = row), two warps that issue the TMA loads of alternate tiles (a box per page, or per 128
@@ -63,7 +68,7 @@ template <int D> constexpr uint32_t kIdescPVOf = instr_desc(0, 1, 1, 128, D);   
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
 cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_constant__ CUtensorMap map_k,
-                   const __grid_constant__ CUtensorMap map_v, int split) {
+                   const __grid_constant__ CUtensorMap map_v, int split, int tile_rows) {
     // Q, K and V tiles are 128 rows of D bytes, swizzled over the whole row: K-major operands for Q and K, the
     // MN-major one for V as it is stored
     constexpr int kTileBytes = kTile * D;
@@ -80,7 +85,7 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
     __shared__ int abort_flag, any_bad;
     __shared__ int part_max[4][kTile], cta_max[kTile];
     __shared__ int part_sum[4][kTile], part_cnt[4][kTile];
-    __shared__ int cta_sum[kTile], cta_cnt[kTile];
+    __shared__ int cta_sum[kTile], cta_cnt[kTile], vsum[D];
 
     const int tid = threadIdx.x, lane = tid & 31;
     const int warp = __shfl_sync(~0u, tid >> 5, 0);                        // (uniform in the compiler's eyes too)
@@ -90,10 +95,11 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
     const SequenceAt seq = sequence_at(a, b);
     if (seq.cut && tid == 0 && blockIdx.x + blockIdx.y == 0) atomicOr(a.status, STATUS_BAD_LENGTH);
     const int queries = min(seq.nq, a.max_q);
-    const int row0 = rt * kTile;
-    const int vrows = min(kTile, queries * a.group - row0);
+    const int row0 = rt * tile_rows;
+    const int vrows = min(tile_rows, queries * a.group - row0);
     if (vrows <= 0) return;                                                // the whole cluster
-    const int quarters = (vrows + 31) >> 5;                                // TMEM lane quarters with rows
+    const bool spare = vrows < kTile;                                      // row number vrows is all ones
+    const int quarters = min((vrows + 32) >> 5, 4);                        // TMEM lane quarters with rows
     const int row_threads = quarters * 128;
     // key blocks of the tile (of its last query, where the rows are causal), and this CTA's share of them
     const int last_query = (row0 + vrows - 1) / a.group;
@@ -157,6 +163,7 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
     const bool bad = any_bad != 0;
     if (bad && tid == 0) atomicOr(a.status, STATUS_BAD_PAGE);
     const int nfull = bad ? 0 : min(max(seen_first / kTile - kb0, 0), nb);
+    const int w0 = spare ? nfull : 0;                                      // first block whose mask.V is computed
     auto wait = [&](uint64_t *bar, uint32_t parity) { return mbar_wait(smem_u32(bar), parity, abortp, a.status, a.wait_cycles); };
 
     if (warp >= kCopyWarp && warp < kCopyWarp + kCopyWarps) {
@@ -237,7 +244,7 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
                     if (ok) qk(slot, sb * 128, &bars.s_full[sb]);
                 }
             } else {
-                // O += r.V, W += mask.V
+                // O += r.V and, where a mask cuts, W += mask.V
                 const uint64_t dr = smem_desc(s_r, 16, 1024, kSwizzle128), dv = smem_desc(s_ring, 8 * D, 8 * D, kSwizzle);
                 const uint32_t dr_lo = (uint32_t)dr, dr_hi = (uint32_t)(dr >> 32), dv_lo = (uint32_t)dv, dv_hi = (uint32_t)(dv >> 32);
                 for (int kb = 0; ok && kb < nb; ++kb) {
@@ -249,11 +256,14 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
                     const uint32_t v_lo = dv_lo + ((uint32_t)(slot * kTileBytes) >> 4), r_lo = dr_lo + (uint32_t)(buf * kPanelBytes >> 4);
                     if (elect_one()) {
 #pragma unroll
-                        for (int w = 0; w < 2; ++w)
+                        for (int ks = 0; ks < 4; ++ks)
+                            tcgen05_mma_i8(tmem + kTmemO, make_u64(r_lo + 2 * ks, dr_hi), make_u64(v_lo + (ks * 32 * D >> 4), dv_hi), kIdescPV, (kb | ks) != 0);
+                        if (kb >= w0) {
 #pragma unroll
                             for (int ks = 0; ks < 4; ++ks)
-                                tcgen05_mma_i8(tmem + (w ? kTmemW : kTmemO), make_u64(r_lo + (2 * w * kPanelBytes >> 4) + 2 * ks, dr_hi),
-                                               make_u64(v_lo + (ks * 32 * D >> 4), dv_hi), kIdescPV, (kb | ks) != 0);
+                                tcgen05_mma_i8(tmem + kTmemW, make_u64(r_lo + (2 * kPanelBytes >> 4) + 2 * ks, dr_hi),
+                                               make_u64(v_lo + (ks * 32 * D >> 4), dv_hi), kIdescPV, ((kb - w0) | ks) != 0);
+                        }
                         tcgen05_commit(smem_u32(&bars.free[slot]));
                         tcgen05_commit(smem_u32(&bars.r_free[buf]));
                         if (kb == nb - 1) tcgen05_commit(smem_u32(&bars.o_full));
@@ -406,19 +416,21 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
                         ok = __all_sync(~0u, wait(&bars.r_free[group], ((kb >> 1) - 1) & 1));
                         if (!ok) return;
                     }
-                    panel16(pr, part, w);
+                    if (decltype(masked)::value || t != vrows) panel16(pr, part, w);     // (row vrows keeps its ones)
                     if constexpr (decltype(masked)::value) panel16(pw, part, ones);
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 mbar_arrive(smem_u32(&bars.r_ready[group]));
             };
             kb = group;
-            if (kb < nfull) {      // full blocks find the mask panel full of ones
+            if (kb < nfull) {      // full blocks find the spare row, or else the mask panel, full of ones
                 uint32_t ones[8];
 #pragma unroll
                 for (int g = 0; g < 8; ++g) ones[g] = 0x01010101u;
-                panel16(pw, 0, ones);
-                panel16(pw, 1, ones);
+                if (!spare || t == vrows) {
+                    panel16(spare ? pr : pw, 0, ones);
+                    panel16(spare ? pr : pw, 1, ones);
+                }
                 count = 64 * ((nfull - group + 1) >> 1);
             }
             for (; ok && kb < nfull; kb += 2) second(kb, No{});
@@ -434,26 +446,45 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
         // ---- join
         const int64_t at0 = ((int64_t)seq.s0 * a.Hq + (int64_t)kvh * a.group) * D;
         if (split == 1) {
-            if (active && ok) {
+            if (active) {
+                // the spare row's sums, for every row's thread of the same columns
+                uint32_t o[kCols / 16][16];
+#pragma unroll
+                for (int part = 0; part < kCols / 16; ++part) {
+                    if (nb > 0 && ok) {
+                        tmem_ld16(tmem + lane_addr + kTmemO + grp * kCols + 16 * part, o[part]);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) o[part][i] = 0u;
+                    }
+                    if (t == vrows) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) vsum[grp * kCols + 16 * part + i] = (int)o[part][i];
+                    }
+                }
+                row_barrier();
                 const int64_t F = th.B - th.S * th.D;
                 const RowFactor f = row_factor(a, F * count + (int64_t)th.S * rsum, a.scale[h]);
                 const int64_t at = at0 + ((int64_t)qi * a.Hq + (row - qi * a.group)) * D + grp * kCols;
 #pragma unroll
                 for (int part = 0; part < kCols / 16; ++part) {
-                    uint32_t o[16], w[16];
-                    if (nb > 0) {
-                        tmem_ld16(tmem + lane_addr + kTmemO + grp * kCols + 16 * part, o);
+                    uint32_t w[16];
+                    if (nb > w0 && ok) {
                         tmem_ld16(tmem + lane_addr + kTmemW + grp * kCols + 16 * part, w);
                     } else {
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) o[i] = w[i] = 0u;
+                        for (int i = 0; i < 16; ++i) w[i] = 0u;
                     }
-                    if (real) {
+                    if (spare) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) w[i] += (uint32_t)vsum[grp * kCols + 16 * part + i];
+                    }
+                    if (real && ok) {
 #pragma unroll
                         for (int g = 0; g < 4; ++g) {
                             int64_t num[4];
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) num[i] = F * (int)w[4 * g + i] + (int64_t)th.S * (int)o[4 * g + i];
+                            for (int i = 0; i < 4; ++i) num[i] = F * (int)w[4 * g + i] + (int64_t)th.S * (int)o[part][4 * g + i];
                             store_output4(a, at + 16 * part + 4 * g, num, f);
                         }
                     }
@@ -468,7 +499,7 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
                     const bool which = part >= kCols / 16;
                     const int col = grp * kCols + 16 * (part % (kCols / 16));
                     uint32_t v[16];
-                    if (nb > 0 && ok) {
+                    if (nb > (which ? w0 : 0) && ok) {
                         tmem_ld16(tmem + lane_addr + (which ? kTmemW : kTmemO) + col, v);
                     } else {
 #pragma unroll
@@ -488,7 +519,11 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
                 int o[4] = {0, 0, 0, 0}, w[4] = {0, 0, 0, 0}, rs = 0, cn = 0;
                 for (int c = 0; c < split; ++c) {
                     const int4 ov = *reinterpret_cast<const int4 *>(cluster.map_shared_rank(dump_o, c) + r * kDump + dim);
-                    const int4 wv = *reinterpret_cast<const int4 *>(cluster.map_shared_rank(dump_w, c) + r * kDump + dim);
+                    int4 wv = *reinterpret_cast<const int4 *>(cluster.map_shared_rank(dump_w, c) + r * kDump + dim);
+                    if (spare) {
+                        const int4 sv = *reinterpret_cast<const int4 *>(cluster.map_shared_rank(dump_o, c) + vrows * kDump + dim);
+                        wv.x += sv.x; wv.y += sv.y; wv.z += sv.z; wv.w += sv.w;
+                    }
                     o[0] += ov.x; o[1] += ov.y; o[2] += ov.z; o[3] += ov.w;
                     w[0] += wv.x; w[1] += wv.y; w[2] += wv.z; w[3] += wv.w;
                     rs += cluster.map_shared_rank(cta_sum, c)[r];
@@ -538,7 +573,11 @@ bool make_page_map(CUtensorMap *map, const void *pool, const CachedAttnArgs &a, 
 template <int D>
 cudaError_t launch_typed(const CachedAttnArgs &a, cudaStream_t stream) {
     const int64_t rows = (int64_t)a.max_q * a.group;
-    const int row_tiles = (int)((rows + kTile - 1) / kTile);
+    // Tiles of 127 rows leave room for the row of ones; full ones are taken where a row less would mean a tile more,
+    // unless there are many anyway (a second product per block costs a tile about 15 %)
+    const int64_t tiles127 = (rows + kTile - 2) / (kTile - 1), tiles128 = (rows + kTile - 1) / kTile;
+    const int tile_rows = tiles127 == tiles128 || tiles128 >= 8 ? kTile - 1 : kTile;
+    const int row_tiles = (int)(tile_rows == kTile ? tiles128 : tiles127);
     const int blocks = (a.max_kv + kTile - 1) / kTile;
     const int64_t ctas = (int64_t)row_tiles * a.Hkv * a.B;
     // Cluster size: waves of 148 CTAs times the blocks each walks over, plus about six blocks' time of set-up and join
@@ -569,7 +608,7 @@ cudaError_t launch_typed(const CachedAttnArgs &a, cudaStream_t stream) {
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, a, mk, mv, split);
+    return cudaLaunchKernelEx(&cfg, kernel, a, mk, mv, split, tile_rows);
 }
 
 }  // namespace
