@@ -345,42 +345,31 @@ class Context:
         some = q if q is not None else k
         if some is None:
             raise ValueError("q or k and v must be given")
-        T, _, d = some.shape
-        Hq = Hkv = pages = size = 0
-        strides = [0, 0, 0]
-        for n, (name, t) in enumerate((("q", q), ("k", k), ("v", v))):
-            if t is None:
-                continue
-            self._on_device(t, name)
-            if t.dtype != some.dtype or t.dim() != 3 or t.shape[0] != T or t.shape[2] != d:
-                raise ValueError(f"{name} must be [{T}, heads, {d}] of {some.dtype}, got {tuple(t.shape)} of {t.dtype}")
-            if t.numel() and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != d)):
-                raise ValueError(f"{name} must be contiguous inside a token")
-            strides[n] = t.stride(0)
-        if q is not None:
-            Hq = q.shape[1]
-            self._check(q8, "q8", 1, (T, Hq, d))
-            q_step = _floats(q_step, "q_step", Hq)
         if (k is None) != (v is None):
             raise ValueError("k and v go together")
+        T, _, d = some.shape
+        Hq = Hkv = pages = size = 0
+        qp = kp = vp = q8p = kpp = vpp = posp = slotp = qs = ks = vs = None
+        q_stride = k_stride = v_stride = 0
+        if q is not None:
+            Hq = q.shape[1]
+            q_stride = self._tokens(q, "q", some)
+            qp, q8p, qs = q.data_ptr(), self._check(q8, "q8", 1, (T, Hq, d)), _floats(q_step, "q_step", Hq)
         if k is not None:
             Hkv = k.shape[1]
-            pages, _, size, _ = k_pages.shape
+            k_stride, v_stride = self._tokens(k, "k", some), self._tokens(v, "v", some)
             if v.shape != k.shape:
                 raise ValueError("k and v must have one shape")
-            self._check(k_pages, "k_pages", 1, (pages, Hkv, size, d))
-            self._check(v_pages, "v_pages", 1, (pages, Hkv, size, d))
-            self._check(slots, "slots", 8, (T,))
-            k_step, v_step = _floats(k_step, "k_step", Hkv), _floats(v_step, "v_step", Hkv)
+            pages, _, size, _ = k_pages.shape
+            kp, vp = k.data_ptr(), v.data_ptr()
+            kpp, vpp = self._check(k_pages, "k_pages", 1, (pages, Hkv, size, d)), self._check(v_pages, "v_pages", 1, (pages, Hkv, size, d))
+            slotp = self._check(slots, "slots", 8, (T,))
+            ks, vs = _floats(k_step, "k_step", Hkv), _floats(v_step, "v_step", Hkv)
         if positions is not None:
-            self._check(positions, "positions", 4, (T,))
-        st = _lib.hccs_cache_write(
-            self._h, _ptr(q), _ptr(k), _ptr(v), _type_of(some), strides[0], strides[1], strides[2], _ptr(positions),
-            _ptr(slots) if k is not None else None, ctypes.byref(rope) if rope is not None else None,
-            _host(q_step) if q is not None else None, _host(k_step) if k is not None else None,
-            _host(v_step) if k is not None else None, _ptr(q8) if q is not None else None,
-            _ptr(k_pages) if k is not None else None, _ptr(v_pages) if k is not None else None,
-            T, Hq, Hkv, d, pages, size, self._stream(stream))
+            posp = self._check(positions, "positions", 4, (T,))
+        st = _lib.hccs_cache_write(self._h, qp, kp, vp, _type_of(some), q_stride, k_stride, v_stride, posp, slotp,
+                                   ctypes.byref(rope) if rope is not None else None, qs, ks, vs, q8p, kpp, vpp,
+                                   T, Hq, Hkv, d, pages, size, self._stream(stream))
         if st != HCCS_OK:
             raise HccsError(st, "hccs_cache_write")
 
@@ -395,19 +384,15 @@ class Context:
         if some is None:
             raise ValueError("k_out or v_out must be given")
         rows = some.shape[0]
-        self._check(k_pages, "k_pages", 1)
-        self._check(v_pages, "v_pages", 1, k_pages.shape)
-        self._check(page_table, "page_table", 4)
-        self._check(out_start, "out_start", 4, (B + 1,))
+        out = []
         for name, t in (("k_out", k_out), ("v_out", v_out)):
-            if t is not None:
-                self._check(t, name, some.element_size(), (rows, Hkv, d))
-                if t.dtype != some.dtype:
-                    raise ValueError("k_out and v_out must have one type")
-        st = _lib.hccs_cache_read(self._h, _ptr(k_pages), _ptr(v_pages), _ptr(page_table), _ptr(out_start),
-                                  _host(_floats(k_step, "k_step", Hkv)), _host(_floats(v_step, "v_step", Hkv)),
-                                  _ptr(k_out), _ptr(v_out), _type_of(some), B, max_pages, int(max_len), rows, Hkv, d, pages,
-                                  size, self._stream(stream))
+            if t is not None and t.dtype != some.dtype:
+                raise ValueError("k_out and v_out must have one type")
+            out.append(None if t is None else self._check(t, name, some.element_size(), (rows, Hkv, d)))
+        st = _lib.hccs_cache_read(self._h, self._check(k_pages, "k_pages", 1), self._check(v_pages, "v_pages", 1, k_pages.shape),
+                                  self._check(page_table, "page_table", 4), self._check(out_start, "out_start", 4, (B + 1,)),
+                                  _floats(k_step, "k_step", Hkv), _floats(v_step, "v_step", Hkv), out[0], out[1], _type_of(some),
+                                  B, max_pages, max_len, rows, Hkv, d, pages, size, self._stream(stream))
         if st != HCCS_OK:
             raise HccsError(st, "hccs_cache_read")
 
@@ -416,45 +401,52 @@ class Context:
                               max_q: int, max_kv: int, tree_mask=None, out_scale=None, flags: int = 0, stream=None) -> None:
         """HCCS attention of the new tokens Q [T,Hq,d] over the cache.  O [T,Hq,d] is int32 (no out_scale), or float32,
         bfloat16 or float16."""
-        T, Hq, d = Q.shape
-        pages, Hkv, size, dk = k_pages.shape
+        T, Hq, d = shape = Q.shape
+        pages, Hkv, size, dk = pool = k_pages.shape
         B, max_pages = page_table.shape
         if dk != d:
             raise ValueError(f"the cache holds heads of {dk}, Q of {d}")
-        self._check(Q, "Q", 1)
-        self._check(k_pages, "k_pages", 1)
-        self._check(v_pages, "v_pages", 1, k_pages.shape)
-        self._check(page_table, "page_table", 4)
-        self._check(q_start, "q_start", 4, (B + 1,))
-        self._check(kv_len, "kv_len", 4, (B,))
-        self._check(O, "O", O.element_size(), Q.shape)
-        words = 0
+        words, treep = 0, None
         if tree_mask is not None:
             words = tree_mask.shape[-1]
-            self._check(tree_mask, "tree_mask", 4, (T, words))
-        mult = _ints(requant_mult, "requant_mult", Hq)
-        scale = _floats(out_scale, "out_scale", Hq) if out_scale is not None else None
-        st = _lib.hccs_attention_cached(self._h, _ptr(Q), _ptr(k_pages), _ptr(v_pages), _ptr(page_table), _ptr(q_start),
-                                        _ptr(kv_len), _ptr(tree_mask), words, _host(mult), int(requant_shift),
-                                        _host(scale) if scale is not None else None, _ptr(O), _type_of(O), T, B, Hq, Hkv, d,
-                                        max_pages, pages, size, int(max_q), int(max_kv), int(flags), self._stream(stream))
+            treep = self._check(tree_mask, "tree_mask", 4, (T, words))
+        st = _lib.hccs_attention_cached(
+            self._h, self._check(Q, "Q", 1), self._check(k_pages, "k_pages", 1), self._check(v_pages, "v_pages", 1, pool),
+            self._check(page_table, "page_table", 4), self._check(q_start, "q_start", 4, (B + 1,)), self._check(kv_len, "kv_len", 4, (B,)),
+            treep, words, _ints(requant_mult, "requant_mult", Hq), requant_shift,
+            None if out_scale is None else _floats(out_scale, "out_scale", Hq), self._check(O, "O", O.element_size(), shape),
+            _type_of(O), T, B, Hq, Hkv, d, max_pages, pages, size, max_q, max_kv, flags, self._stream(stream))
         if st != HCCS_OK:
             raise HccsError(st, "hccs_attention_cached")
 
-    # The cache calls run on the context's device: its current stream, and tensors that live there.
+    # The cache calls run on the context's device: on its current stream, with tensors that live there.  They are made
+    # for every token of every layer, so their checks take the short way and build a message only where one is due.
     def _stream(self, stream):
         if stream is None:
-            import torch
-            return _vp(torch.cuda.current_stream(self.device).cuda_stream)
+            return _raw_stream()(self.device)
         return _stream_ptr(stream)
 
     def _on_device(self, t, name):
-        if t.device.type != "cuda" or t.device.index != self.device:
+        if t.get_device() != self.device:
             raise ValueError(f"{name} must live on cuda:{self.device}, not {t.device}")
 
-    def _check(self, t, name, itemsize, shape=None):
+    def _check(self, t, name, itemsize, shape=None) -> int:
+        """The address of a tensor that passes :func:`_check_tensor` on the context's device."""
+        if t.get_device() != self.device or not t.is_contiguous() or t.element_size() != itemsize or (shape is not None and t.shape != shape):
+            self._on_device(t, name)
+            _check_tensor(t, name, itemsize, shape)
+        return t.data_ptr()
+
+    def _tokens(self, t, name, some) -> int:
+        """Elements between the tokens of a [T, heads, d] view that is contiguous inside a token."""
         self._on_device(t, name)
-        _check_tensor(t, name, itemsize, shape)
+        T, heads, d = t.shape
+        if t.dtype != some.dtype or T != some.shape[0] or d != some.shape[2]:
+            raise ValueError(f"{name} must be [{some.shape[0]}, heads, {some.shape[2]}] of {some.dtype}, got {tuple(t.shape)} of {t.dtype}")
+        a, b, c = t.stride()
+        if T and heads and (c != 1 or (heads > 1 and b != d)):
+            raise ValueError(f"{name} must be contiguous inside a token")
+        return a if T > 1 else 0
 
     # -- hccs_device_status / hccs_last_cuda_error / hccs_launch_count
     def hccs_device_status(self, stream=None) -> int:
@@ -496,31 +488,50 @@ def hccs_forward_static_scratch(params, n_design: int, logits, probs, flags: int
     return int(word.value)
 
 
+_TORCH = []
+_TYPES = {}
+
+
+def _torch():
+    """torch, imported on first use (the host-only calls do without it)."""
+    if not _TORCH:
+        import torch
+        _TYPES.update({torch.int32: HCCS_I32, torch.float32: HCCS_F32, torch.bfloat16: HCCS_BF16, torch.float16: HCCS_F16})
+        _TORCH.append(torch)
+    return _TORCH[0]
+
+
+def _raw_stream():
+    """The function that gives the handle of a device's current stream: torch's own short way where it has one."""
+    if len(_TORCH) < 2:
+        torch = _torch()
+        short = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        _TORCH.append(short or (lambda device: torch.cuda.current_stream(device).cuda_stream))
+    return _TORCH[1]
+
+
 def _type_of(t) -> int:
-    import torch
-    kinds = {torch.int32: HCCS_I32, torch.float32: HCCS_F32, torch.bfloat16: HCCS_BF16, torch.float16: HCCS_F16}
-    if t.dtype not in kinds:
+    _torch()
+    kind = _TYPES.get(t.dtype)
+    if kind is None:
         raise ValueError(f"int32, float32, bfloat16 or float16 is wanted, got {t.dtype}")
-    return kinds[t.dtype]
+    return kind
 
 
-def _array(v, name, n, dtype):
-    arr = np.ascontiguousarray(v, dtype=dtype).reshape(-1)
+# Host arrays go to the library as the bytes of their values (it copies them before it returns).
+def _bytes(v, name, n, dtype) -> bytes:
+    arr = v if type(v) is np.ndarray and v.dtype == dtype else np.asarray(v, dtype=dtype)
     if arr.size != n:
         raise ValueError(f"{name} must have {n} entries, got {arr.size}")
-    return arr
+    return arr.tobytes()
 
 
-def _floats(v, name, n):
-    return _array(v, name, n, np.float32)
+def _floats(v, name, n) -> bytes:
+    return _bytes(v, name, n, np.float32)
 
 
-def _ints(v, name, n):
-    return _array(v, name, n, np.int32)
-
-
-def _host(arr):
-    return arr.__array_interface__["data"][0]
+def _ints(v, name, n) -> bytes:
+    return _bytes(v, name, n, np.int32)
 
 
 def _check_tensor(t, name, itemsize, shape=None, device="cuda"):

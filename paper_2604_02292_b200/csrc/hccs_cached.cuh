@@ -117,4 +117,16 @@ __device__ __forceinline__ void store_output4(const CachedAttnArgs &a, int64_t a
     }
 }
 
+// Raises a kernel's limits (dynamic shared memory, clusters of sixteen) once per kernel and device: `done` is the
+// kernel's own array of flags.
+inline cudaError_t raise_limits(const void *kernel, int smem, bool (&done)[64]) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess || (dev < 64 && done[dev])) return e;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e == cudaSuccess && dev < 64) done[dev] = true;
+    return e;
+}
+
 }  // namespace hccs

@@ -327,8 +327,8 @@ cudaError_t launch_typed(const CachedAttnArgs &a, cudaStream_t stream) {
     const int per = (tiles + split - 1) / split;
     const size_t smem = (size_t)per * tile_bytes;
     auto kernel = cached_decode_kernel<D, HI>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    static bool raised[64] = {};
+    const cudaError_t e = raise_limits((const void *)kernel, 160 * 1024, raised);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)split, (unsigned)(a.Hkv * row_tiles), (unsigned)a.B);

@@ -593,8 +593,8 @@ cudaError_t launch_typed(const CachedAttnArgs &a, cudaStream_t stream) {
     CUtensorMap mk, mv;
     if (!make_page_map(&mk, a.k_pages, a, D) || !make_page_map(&mv, a.v_pages, a, D)) return cudaErrorInvalidValue;
     auto kernel = cached_tile_kernel<D>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    static bool raised[64] = {};
+    const cudaError_t e = raise_limits((const void *)kernel, (int)smem, raised);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(row_tiles * split), (unsigned)a.Hkv, (unsigned)a.B);
