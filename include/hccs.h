@@ -269,7 +269,7 @@ hccs_status_t hccs_calibrate(const int8_t *logits, int32_t B, int32_t H, int32_t
 typedef struct {
     int32_t rot_dim;                          /* even, 0..d */
     int32_t interleaved;                      /* 0: halves, 1: neighbours */
-    double  scale;                            /* finite */
+    double  scale;                            /* magnitude 2^-64 .. 2^64 */
     double  freq[HCCS_MAX_ROT_DIM / 2];       /* radians per position, finite */
 } hccs_rope_t;
 
@@ -307,11 +307,11 @@ hccs_status_t hccs_rope_frequencies(hccs_rope_t *rope, int32_t rot_dim, int32_t 
  *                tokens); the others of one call must differ.  A slot at or beyond num_pages * page_size is
  *                skipped as well and reported (hccs_device_status).  May be NULL where k and v are
  *   rope         HOST, or NULL for none; applied to q and k
- *   *_step       HOST float [Hq], [Hkv], [Hkv], finite and > 0: the value of one code
+ *   *_step       HOST float [Hq], [Hkv], [Hkv], each in 2^-100 .. 2^100: the value of one code
  *   q8           device int8 [T, Hq, d];  k_pages, v_pages  the pools; 16-byte aligned
  * A code is clamp(round(y / step), -128, 127), the exact quotient rounded to nearest, ties to even: the
- * kernel works in fp32 and repeats in fp64 what lies next to a border, so the codes are those of a
- * computation in fp64.  NaN gives 0.  Nothing else in the pools is touched.
+ * kernel works in fp32 and repeats exactly (rotated dims: in fp64) what lies next to a border, so the codes
+ * are those of a computation in fp64.  NaN gives 0.  Nothing else in the pools is touched.
  */
 hccs_status_t hccs_cache_write(hccs_ctx_t *ctx, const void *q, const void *k, const void *v, hccs_type_t type,
                                int64_t q_stride, int64_t k_stride, int64_t v_stride,

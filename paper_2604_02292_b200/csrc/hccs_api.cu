@@ -518,7 +518,7 @@ static bool cache_shape(int32_t Hkv, int32_t d, int32_t num_pages, int32_t page_
 static bool steps_ok(const float *s, int32_t n) {
     if (!s) return false;
     for (int32_t i = 0; i < n; ++i)
-        if (!(s[i] > 0.0f) || !isfinite(s[i])) return false;
+        if (!(s[i] >= 0x1p-100f) || !(s[i] <= 0x1p100f)) return false;
     return true;
 }
 
@@ -585,7 +585,8 @@ hccs_status_t hccs_cache_write(hccs_ctx_t *ctx, const void *q, const void *k, co
     if (with_q && !steps_ok(q_step, Hq)) return HCCS_ERR_INVALID_ARG;
     if (with_kv && (!steps_ok(k_step, Hkv) || !steps_ok(v_step, Hkv))) return HCCS_ERR_INVALID_ARG;
     if (rope) {
-        if (rope->rot_dim < 0 || rope->rot_dim > d || (rope->rot_dim & 1) || !isfinite(rope->scale)) return HCCS_ERR_INVALID_ARG;
+        if (rope->rot_dim < 0 || rope->rot_dim > d || (rope->rot_dim & 1)) return HCCS_ERR_INVALID_ARG;
+        if (!(fabs(rope->scale) >= 0x1p-64) || !(fabs(rope->scale) <= 0x1p64)) return HCCS_ERR_INVALID_ARG;
         for (int32_t i = 0; i < rope->rot_dim / 2; ++i)
             if (!isfinite(rope->freq[i])) return HCCS_ERR_INVALID_ARG;
     }

@@ -343,6 +343,41 @@ def test_write_of_infinities_nan_and_the_largest_values(hccs, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("step", [0.03, 0.03125, 1.0, 0.3333333, 7e-3, 1e-6, 1e30, 2.0 ** -100, 2.0 ** 100, 3e30, 1.1754944e-38, 2.0 ** -140])
+def test_write_at_the_borders(hccs, dtype, step):
+    """Values on, just below and just above every border k + 1/2, and all 16-bit patterns of the type's range."""
+    import torch
+    s = np.float32(step)
+    k = np.arange(-130, 130)
+    v = ((k + 0.5) * np.float64(s)).astype(np.float32)
+    vals = np.concatenate([v, np.nextafter(v, np.float32(-np.inf)), np.nextafter(v, np.float32(np.inf)), (k * np.float64(s)).astype(np.float32)])
+    bits = torch.from_numpy(np.arange(0, 65536, 1, dtype=np.uint16).view(np.int16))
+    some = {"bf16": bits.view(torch.bfloat16), "f16": bits.view(torch.float16), "f32": bits.view(torch.bfloat16).float()}[dtype]
+    x = torch.cat([torch.from_numpy(vals).to(_torch_type(dtype)), some])
+    x = torch.cat([x, x[:-x.numel() % 64]]) if x.numel() % 64 else x
+    x = x.view(-1, 1, 64).cuda()
+    T = x.shape[0]
+    pages = -(-T // 16)
+    kp, vp = (torch.zeros((pages, 1, 16, 64), dtype=torch.int8, device="cuda") for _ in range(2))
+    q8 = torch.zeros((T, 1, 64), dtype=torch.int8, device="cuda")
+    ctx = hccs.Context(0)
+    args = (x, x, x, q8, kp, vp, torch.zeros(T, dtype=torch.int32, device="cuda"), torch.arange(T, device="cuda"), [s], [s], [s])
+    if step < 2.0 ** -100 or step > 2.0 ** 100:            # a reciprocal that fp32 cannot hold: refused
+        with pytest.raises(hccs.HccsError) as ei:
+            ctx.hccs_cache_write(*args)
+        assert ei.value.status == hccs.HCCS_ERR_INVALID_ARG
+        return
+    ctx.hccs_cache_write(*args, rope=hccs.Rope([1.0] * 16))                                    # position 0: turned by nothing
+    xs = x.float().cpu().numpy()
+    want = orc.quantise(xs.astype(np.longdouble), [s])
+    assert (vp.cpu().numpy().reshape(-1, 64)[:T] == want[:, 0]).all()
+    finite = np.isfinite(xs).all(axis=(1, 2))              # an infinity times a sine of zero is a NaN
+    assert (q8.cpu().numpy()[finite] == want[finite]).all() and (kp.cpu().numpy().reshape(-1, 64)[:T][finite] == want[finite][:, 0]).all()
+    ctx.close()
+
+
+@pytest.mark.gpu
 def test_write_parts_and_bad_slots(hccs):
     import torch
     ctx = hccs.Context(0)
