@@ -12,6 +12,7 @@
 
 #include "hccs_device.cuh"
 #include "hccs_internal.h"
+#include "hccs_tcgen05.cuh"
 
 namespace hccs {
 
@@ -115,6 +116,21 @@ __device__ __forceinline__ void store_output4(const CachedAttnArgs &a, int64_t a
         }
         *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.O) + at) = w;
     }
+}
+
+// A pool as [num_pages * Hkv][page_size][D] bytes, boxes of a page's rows (`most` at most), swizzled over the whole row.
+inline bool make_page_map(CUtensorMap *map, const void *pool, const CachedAttnArgs &a, int most) {
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    const cuuint64_t page = (cuuint64_t)1 << a.page_shift;
+    const int d = a.d;
+    const cuuint64_t dims[3] = {(cuuint64_t)d, page, (cuuint64_t)a.num_pages * a.Hkv};
+    const cuuint64_t strides[2] = {(cuuint64_t)d, page * d};
+    const cuuint32_t box[3] = {(cuuint32_t)d, page < (cuuint64_t)most ? (cuuint32_t)page : (cuuint32_t)most, 1};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void *>(pool), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              d == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // Raises a kernel's limits (dynamic shared memory, clusters of sixteen) once per kernel and device: `done` is the

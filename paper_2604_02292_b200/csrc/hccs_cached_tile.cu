@@ -556,20 +556,6 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
     }
 }
 
-// A pool as [num_pages * Hkv][page_size][D] bytes, boxes of a page's rows (128 at most), swizzled over the whole row.
-bool make_page_map(CUtensorMap *map, const void *pool, const CachedAttnArgs &a, int d) {
-    EncodeTiledFn fn = encode_tiled_fn();
-    if (!fn) return false;
-    const cuuint64_t page = (cuuint64_t)1 << a.page_shift;
-    const cuuint64_t dims[3] = {(cuuint64_t)d, page, (cuuint64_t)a.num_pages * a.Hkv};
-    const cuuint64_t strides[2] = {(cuuint64_t)d, page * d};
-    const cuuint32_t box[3] = {(cuuint32_t)d, page < kTile ? (cuuint32_t)page : (cuuint32_t)kTile, 1};
-    const cuuint32_t estr[3] = {1, 1, 1};
-    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void *>(pool), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-              d == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
-              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 template <int D>
 cudaError_t launch_typed(const CachedAttnArgs &a, cudaStream_t stream) {
     const int64_t rows = (int64_t)a.max_q * a.group;
@@ -591,7 +577,7 @@ cudaError_t launch_typed(const CachedAttnArgs &a, cudaStream_t stream) {
     constexpr size_t smem = 1024 + (size_t)(1 + kSlotsOf<D>) * kTile * D + 4 * kPanelBytes;
     static_assert(smem - 1024 >= 2 * sizeof(int) * kTile * (D + 4), "the joined sums fit the operands' place");
     CUtensorMap mk, mv;
-    if (!make_page_map(&mk, a.k_pages, a, D) || !make_page_map(&mv, a.v_pages, a, D)) return cudaErrorInvalidValue;
+    if (!make_page_map(&mk, a.k_pages, a, kTile) || !make_page_map(&mv, a.v_pages, a, kTile)) return cudaErrorInvalidValue;
     auto kernel = cached_tile_kernel<D>;
     static bool raised[64] = {};
     const cudaError_t e = raise_limits((const void *)kernel, (int)smem, raised);
