@@ -107,6 +107,10 @@ class Rope(ctypes.Structure):
         for i, f in enumerate(freq):
             self.freq[i] = f
 
+    @property
+    def _ref(self):
+        return ctypes.byref(self)
+
 
 class _RopeScaling(ctypes.Structure):
     _fields_ = [("kind", _i32), ("factor", ctypes.c_double), ("low", ctypes.c_double), ("high", ctypes.c_double),
@@ -332,7 +336,7 @@ class Context:
         arr = np.ascontiguousarray(params, dtype=np.int32).reshape(-1, 3)
         bad = _i32(-1)
         st = _lib.hccs_params_upload_wide(self._h, arr.ctypes.data_as(_vp), arr.shape[0], int(n_design),
-                                          ctypes.byref(bad), self._stream(stream))
+                                          ctypes.byref(bad), _raw_stream(self.device) if stream is None else _stream_ptr(stream))
         if st != HCCS_OK:
             raise HccsError(st, "hccs_params_upload_wide", f"(head {bad.value})" if bad.value >= 0 else "")
 
@@ -351,25 +355,35 @@ class Context:
         Hq = Hkv = pages = size = 0
         qp = kp = vp = q8p = kpp = vpp = posp = slotp = qs = ks = vs = None
         q_stride = k_stride = v_stride = 0
+        dev, dtype = self.device, some.dtype
         if q is not None:
             Hq = q.shape[1]
+            if q8.get_device() != dev or q8.shape != q.shape or q8.element_size() != 1 or not q8.is_contiguous():
+                self._explain(q8, "q8", 1, q.shape)
+            qp, q8p, qs = q.data_ptr(), q8.data_ptr(), _floats(q_step, "q_step", Hq)
             q_stride = self._tokens(q, "q", some)
-            qp, q8p, qs = q.data_ptr(), self._check(q8, "q8", 1, (T, Hq, d)), _floats(q_step, "q_step", Hq)
         if k is not None:
-            Hkv = k.shape[1]
+            shape = k.shape
+            Hkv = shape[1]
+            pages, _, size, _ = pool = k_pages.shape
+            if v.dtype != dtype or v.shape != shape:
+                raise ValueError("k and v must have one shape and type")
             k_stride, v_stride = self._tokens(k, "k", some), self._tokens(v, "v", some)
-            if v.shape != k.shape:
-                raise ValueError("k and v must have one shape")
-            pages, _, size, _ = k_pages.shape
-            kp, vp = k.data_ptr(), v.data_ptr()
-            kpp, vpp = self._check(k_pages, "k_pages", 1, (pages, Hkv, size, d)), self._check(v_pages, "v_pages", 1, (pages, Hkv, size, d))
-            slotp = self._check(slots, "slots", 8, (T,))
+            if (k_pages.get_device() != dev or v_pages.get_device() != dev or slots.get_device() != dev or pool[1] != Hkv or pool[3] != d
+                    or v_pages.shape != pool or k_pages.element_size() != 1 or v_pages.element_size() != 1 or slots.element_size() != 8
+                    or slots.shape != (T,) or not k_pages.is_contiguous() or not v_pages.is_contiguous() or not slots.is_contiguous()):
+                self._explain(k_pages, "k_pages", 1, (pages, Hkv, size, d))
+                self._explain(v_pages, "v_pages", 1, pool)
+                self._explain(slots, "slots", 8, (T,))
+            kp, vp, kpp, vpp, slotp = k.data_ptr(), v.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), slots.data_ptr()
             ks, vs = _floats(k_step, "k_step", Hkv), _floats(v_step, "v_step", Hkv)
         if positions is not None:
-            posp = self._check(positions, "positions", 4, (T,))
+            if positions.get_device() != dev or positions.element_size() != 4 or positions.shape != (T,) or not positions.is_contiguous():
+                self._explain(positions, "positions", 4, (T,))
+            posp = positions.data_ptr()
         st = _lib.hccs_cache_write(self._h, qp, kp, vp, _type_of(some), q_stride, k_stride, v_stride, posp, slotp,
-                                   ctypes.byref(rope) if rope is not None else None, qs, ks, vs, q8p, kpp, vpp,
-                                   T, Hq, Hkv, d, pages, size, self._stream(stream))
+                                   rope._ref if rope is not None else None, qs, ks, vs, q8p, kpp, vpp,
+                                   T, Hq, Hkv, d, pages, size, _raw_stream(dev) if stream is None else _stream_ptr(stream))
         if st != HCCS_OK:
             raise HccsError(st, "hccs_cache_write")
 
@@ -392,7 +406,8 @@ class Context:
         st = _lib.hccs_cache_read(self._h, self._check(k_pages, "k_pages", 1), self._check(v_pages, "v_pages", 1, k_pages.shape),
                                   self._check(page_table, "page_table", 4), self._check(out_start, "out_start", 4, (B + 1,)),
                                   _floats(k_step, "k_step", Hkv), _floats(v_step, "v_step", Hkv), out[0], out[1], _type_of(some),
-                                  B, max_pages, max_len, rows, Hkv, d, pages, size, self._stream(stream))
+                                  B, max_pages, max_len, rows, Hkv, d, pages, size,
+                                  _raw_stream(self.device) if stream is None else _stream_ptr(stream))
         if st != HCCS_OK:
             raise HccsError(st, "hccs_cache_read")
 
@@ -404,44 +419,57 @@ class Context:
         T, Hq, d = shape = Q.shape
         pages, Hkv, size, dk = pool = k_pages.shape
         B, max_pages = page_table.shape
+        dev = self.device
         if dk != d:
             raise ValueError(f"the cache holds heads of {dk}, Q of {d}")
+        if (Q.get_device() != dev or k_pages.get_device() != dev or v_pages.get_device() != dev or page_table.get_device() != dev
+                or q_start.get_device() != dev or kv_len.get_device() != dev or O.get_device() != dev or Q.element_size() != 1
+                or k_pages.element_size() != 1 or v_pages.element_size() != 1 or page_table.element_size() != 4
+                or q_start.element_size() != 4 or kv_len.element_size() != 4 or v_pages.shape != pool or O.shape != shape
+                or q_start.shape != (B + 1,) or kv_len.shape != (B,) or not Q.is_contiguous() or not k_pages.is_contiguous()
+                or not v_pages.is_contiguous() or not page_table.is_contiguous() or not q_start.is_contiguous()
+                or not kv_len.is_contiguous() or not O.is_contiguous()):
+            self._explain(Q, "Q", 1)
+            self._explain(k_pages, "k_pages", 1)
+            self._explain(v_pages, "v_pages", 1, pool)
+            self._explain(page_table, "page_table", 4)
+            self._explain(q_start, "q_start", 4, (B + 1,))
+            self._explain(kv_len, "kv_len", 4, (B,))
+            self._explain(O, "O", O.element_size(), shape)
         words, treep = 0, None
         if tree_mask is not None:
             words = tree_mask.shape[-1]
-            treep = self._check(tree_mask, "tree_mask", 4, (T, words))
+            if tree_mask.get_device() != dev or tree_mask.element_size() != 4 or tree_mask.shape != (T, words) or not tree_mask.is_contiguous():
+                self._explain(tree_mask, "tree_mask", 4, (T, words))
+            treep = tree_mask.data_ptr()
         st = _lib.hccs_attention_cached(
-            self._h, self._check(Q, "Q", 1), self._check(k_pages, "k_pages", 1), self._check(v_pages, "v_pages", 1, pool),
-            self._check(page_table, "page_table", 4), self._check(q_start, "q_start", 4, (B + 1,)), self._check(kv_len, "kv_len", 4, (B,)),
+            self._h, Q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(), q_start.data_ptr(), kv_len.data_ptr(),
             treep, words, _ints(requant_mult, "requant_mult", Hq), requant_shift,
-            None if out_scale is None else _floats(out_scale, "out_scale", Hq), self._check(O, "O", O.element_size(), shape),
-            _type_of(O), T, B, Hq, Hkv, d, max_pages, pages, size, max_q, max_kv, flags, self._stream(stream))
+            None if out_scale is None else _floats(out_scale, "out_scale", Hq), O.data_ptr(), _type_of(O), T, B, Hq, Hkv, d, max_pages,
+            pages, size, max_q, max_kv, flags, _raw_stream(dev) if stream is None else _stream_ptr(stream))
         if st != HCCS_OK:
             raise HccsError(st, "hccs_attention_cached")
 
     # The cache calls run on the context's device: on its current stream, with tensors that live there.  They are made
     # for every token of every layer, so their checks take the short way and build a message only where one is due.
-    def _stream(self, stream):
-        if stream is None:
-            return _raw_stream()(self.device)
-        return _stream_ptr(stream)
-
-    def _on_device(self, t, name):
+    def _explain(self, t, name, itemsize, shape=None):
+        """Raises with what is wrong with a tensor, if it is this one."""
         if t.get_device() != self.device:
             raise ValueError(f"{name} must live on cuda:{self.device}, not {t.device}")
+        _check_tensor(t, name, itemsize, shape)
 
     def _check(self, t, name, itemsize, shape=None) -> int:
-        """The address of a tensor that passes :func:`_check_tensor` on the context's device."""
+        """The address of a tensor of the context's device that passes."""
         if t.get_device() != self.device or not t.is_contiguous() or t.element_size() != itemsize or (shape is not None and t.shape != shape):
-            self._on_device(t, name)
-            _check_tensor(t, name, itemsize, shape)
+            self._explain(t, name, itemsize, shape)
         return t.data_ptr()
 
     def _tokens(self, t, name, some) -> int:
         """Elements between the tokens of a [T, heads, d] view that is contiguous inside a token."""
-        self._on_device(t, name)
+        if t.get_device() != self.device:
+            self._explain(t, name, t.element_size())
         T, heads, d = t.shape
-        if t.dtype != some.dtype or T != some.shape[0] or d != some.shape[2]:
+        if t is not some and (t.dtype != some.dtype or T != some.shape[0] or d != some.shape[2]):
             raise ValueError(f"{name} must be [{some.shape[0]}, heads, {some.shape[2]}] of {some.dtype}, got {tuple(t.shape)} of {t.dtype}")
         a, b, c = t.stride()
         if T and heads and (c != 1 or (heads > 1 and b != d)):
@@ -488,33 +516,26 @@ def hccs_forward_static_scratch(params, n_design: int, logits, probs, flags: int
     return int(word.value)
 
 
-_TORCH = []
 _TYPES = {}
 
 
-def _torch():
-    """torch, imported on first use (the host-only calls do without it)."""
-    if not _TORCH:
-        import torch
-        _TYPES.update({torch.int32: HCCS_I32, torch.float32: HCCS_F32, torch.bfloat16: HCCS_BF16, torch.float16: HCCS_F16})
-        _TORCH.append(torch)
-    return _TORCH[0]
-
-
-def _raw_stream():
-    """The function that gives the handle of a device's current stream: torch's own short way where it has one."""
-    if len(_TORCH) < 2:
-        torch = _torch()
-        short = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-        _TORCH.append(short or (lambda device: torch.cuda.current_stream(device).cuda_stream))
-    return _TORCH[1]
+# torch is imported on first use: the host-only calls do without it.
+def _raw_stream(device):
+    """The handle of a device's current stream (torch's own short way where it has one)."""
+    global _raw_stream
+    import torch
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+    return _raw_stream(device)
 
 
 def _type_of(t) -> int:
-    _torch()
     kind = _TYPES.get(t.dtype)
     if kind is None:
-        raise ValueError(f"int32, float32, bfloat16 or float16 is wanted, got {t.dtype}")
+        import torch
+        _TYPES.update({torch.int32: HCCS_I32, torch.float32: HCCS_F32, torch.bfloat16: HCCS_BF16, torch.float16: HCCS_F16})
+        if t.dtype not in _TYPES:
+            raise ValueError(f"int32, float32, bfloat16 or float16 is wanted, got {t.dtype}")
+        kind = _TYPES[t.dtype]
     return kind
 
 
