@@ -87,8 +87,8 @@ __device__ __forceinline__ RowFactor row_factor(const CachedAttnArgs &a, int64_t
     }
     return f;
 }
-// Four neighbouring values; `at` is the index of the first.
-__device__ __forceinline__ void store_output4(const CachedAttnArgs &a, int64_t at, const int64_t (&num)[4], const RowFactor &f) {
+// Four neighbouring values as they are stored, in the low `size` words (two or four).
+__device__ __forceinline__ uint4 output4(const CachedAttnArgs &a, const int64_t (&num)[4], const RowFactor &f) {
     int o[4];
     float y[4];
 #pragma unroll
@@ -101,21 +101,21 @@ __device__ __forceinline__ void store_output4(const CachedAttnArgs &a, int64_t a
             y[e] = (float)o[e] * f.scale;
         }
     }
-    if (a.out_type == HCCS_I32) {
-        *reinterpret_cast<int4 *>(static_cast<int32_t *>(a.O) + at) = make_int4(o[0], o[1], o[2], o[3]);
-    } else if (a.out_type == HCCS_F32) {
-        *reinterpret_cast<float4 *>(static_cast<float *>(a.O) + at) = make_float4(y[0], y[1], y[2], y[3]);
-    } else {
-        uint2 w;
-        if (a.out_type == HCCS_BF16) {
-            __nv_bfloat162 lo = __floats2bfloat162_rn(y[0], y[1]), hi = __floats2bfloat162_rn(y[2], y[3]);
-            w = make_uint2(*reinterpret_cast<uint32_t *>(&lo), *reinterpret_cast<uint32_t *>(&hi));
-        } else {
-            __half2 lo = __floats2half2_rn(y[0], y[1]), hi = __floats2half2_rn(y[2], y[3]);
-            w = make_uint2(*reinterpret_cast<uint32_t *>(&lo), *reinterpret_cast<uint32_t *>(&hi));
-        }
-        *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.O) + at) = w;
+    if (a.out_type == HCCS_I32) return make_uint4((uint32_t)o[0], (uint32_t)o[1], (uint32_t)o[2], (uint32_t)o[3]);
+    if (a.out_type == HCCS_F32) return make_uint4(__float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]), __float_as_uint(y[3]));
+    if (a.out_type == HCCS_BF16) {
+        const __nv_bfloat162 lo = __floats2bfloat162_rn(y[0], y[1]), hi = __floats2bfloat162_rn(y[2], y[3]);
+        return make_uint4(*reinterpret_cast<const uint32_t *>(&lo), *reinterpret_cast<const uint32_t *>(&hi), 0u, 0u);
     }
+    const __half2 lo = __floats2half2_rn(y[0], y[1]), hi = __floats2half2_rn(y[2], y[3]);
+    return make_uint4(*reinterpret_cast<const uint32_t *>(&lo), *reinterpret_cast<const uint32_t *>(&hi), 0u, 0u);
+}
+__device__ __forceinline__ bool output_is_wide(const CachedAttnArgs &a) { return a.out_type == HCCS_I32 || a.out_type == HCCS_F32; }
+// `at` is the index of the first of the four.
+__device__ __forceinline__ void store_output4(const CachedAttnArgs &a, int64_t at, const int64_t (&num)[4], const RowFactor &f) {
+    const uint4 v = output4(a, num, f);
+    if (output_is_wide(a)) *reinterpret_cast<uint4 *>(static_cast<uint32_t *>(a.O) + at) = v;
+    else *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.O) + at) = make_uint2(v.x, v.y);
 }
 
 // A pool as [num_pages * Hkv][page_size][D] bytes, boxes of a page's rows (`most` at most), swizzled over the whole row.

@@ -139,25 +139,28 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
     }
     tcgen05_fence_before();
     __syncthreads();
-    // pages outside the pools: a look at this CTA's part of the table tells whether the masks have to care
-    {
+    // (the copy warps are off to their loads; the others look at the pages and fetch Q first)
+    constexpr int kOthers = kThreads - 32 * kCopyWarps;
+    if (warp < kCopyWarp || warp >= kCopyWarp + kCopyWarps) {
+        const int i0 = warp < kCopyWarp ? tid : tid - 32 * kCopyWarps;
+        // pages outside the pools: a look at this CTA's part of the table tells whether the masks have to care
         const int key_end = min((kb0 + nb) * kTile, seq.n);
-        for (int p = (kb0 * kTile >> a.page_shift) + tid; (int64_t)p << a.page_shift < key_end; p += kThreads)
+        for (int p = (kb0 * kTile >> a.page_shift) + i0; (int64_t)p << a.page_shift < key_end; p += kOthers)
             if ((uint32_t)table[p] >= (uint32_t)a.num_pages) any_bad = 1;
-    }
-    // Q, swizzled by hand: the rows of a tile are (query, head) pairs, not a box of the tensor
-    constexpr int kChunks = D / 16;
-    for (int i = tid; i < kTile * kChunks; i += kThreads) {
-        const int r = i / kChunks, chunk = i % kChunks;
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (r < vrows) {
-            const int row = row0 + r, q = row / a.group;
-            v = *reinterpret_cast<const uint4 *>(a.Q + (((int64_t)seq.s0 + q) * a.Hq + kvh * a.group + (row - q * a.group)) * D + chunk * 16);
+        // Q, swizzled by hand: the rows of a tile are (query, head) pairs, not a box of the tensor
+        constexpr int kChunks = D / 16;
+        for (int i = i0; i < kTile * kChunks; i += kOthers) {
+            const int r = i / kChunks, chunk = i % kChunks;
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (r < vrows) {
+                const int row = row0 + r, q = row / a.group;
+                v = *reinterpret_cast<const uint4 *>(a.Q + (((int64_t)seq.s0 + q) * a.Hq + kvh * a.group + (row - q * a.group)) * D + chunk * 16);
+            }
+            *reinterpret_cast<uint4 *>(gen + r * D + ((chunk ^ (D == 128 ? r & 7 : (r >> 1) & 3)) << 4)) = v;
         }
-        *reinterpret_cast<uint4 *>(gen + r * D + ((chunk ^ (D == 128 ? r & 7 : (r >> 1) & 3)) << 4)) = v;
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        asm volatile("bar.sync 2, %0;" ::"n"(kOthers) : "memory");
     }
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    __syncthreads();
     tcgen05_fence_after();
     const uint32_t tmem = tmem_slot;
     const bool bad = any_bad != 0;
@@ -465,7 +468,11 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
                 row_barrier();
                 const int64_t F = th.B - th.S * th.D;
                 const RowFactor f = row_factor(a, F * count + (int64_t)th.S * rsum, a.scale[h]);
-                const int64_t at = at0 + ((int64_t)qi * a.Hq + (row - qi * a.group)) * D + grp * kCols;
+                // the tile's rows as they are stored go through shared memory (the operands' place: every product is
+                // complete), so that neighbouring lanes write neighbouring pieces of a row
+                const bool wide = output_is_wide(a);
+                const int pitch = D * (wide ? 4 : 2) + 16;
+                uint8_t *const stage = gen + t * pitch + grp * kCols * (wide ? 4 : 2);
 #pragma unroll
                 for (int part = 0; part < kCols / 16; ++part) {
                     uint32_t w[16];
@@ -479,16 +486,26 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
 #pragma unroll
                         for (int i = 0; i < 16; ++i) w[i] += (uint32_t)vsum[grp * kCols + 16 * part + i];
                     }
-                    if (real && ok) {
 #pragma unroll
-                        for (int g = 0; g < 4; ++g) {
-                            int64_t num[4];
+                    for (int g = 0; g < 4; ++g) {
+                        int64_t num[4];
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) num[i] = F * (int)w[4 * g + i] + (int64_t)th.S * (int)o[part][4 * g + i];
-                            store_output4(a, at + 16 * part + 4 * g, num, f);
-                        }
+                        for (int i = 0; i < 4; ++i) num[i] = F * (int)w[4 * g + i] + (int64_t)th.S * (int)o[part][4 * g + i];
+                        const uint4 v = output4(a, num, f);
+                        if (wide) *reinterpret_cast<uint4 *>(stage + (16 * part + 4 * g) * 4) = v;
+                        else *reinterpret_cast<uint2 *>(stage + (16 * part + 4 * g) * 2) = make_uint2(v.x, v.y);
                     }
                 }
+                row_barrier();
+                const int pieces = D * (wide ? 4 : 2) / 16;
+                const int me = (warp & 3) * 128 + grp * 32 + lane;        // of the row_threads that are active
+                if (ok)
+                    for (int i = me; i < vrows * pieces; i += row_threads) {
+                        const int r = i / pieces, piece = i - r * pieces, rr = row0 + r, q = rr / a.group;
+                        const int64_t at = at0 + ((int64_t)q * a.Hq + (rr - q * a.group)) * D;
+                        reinterpret_cast<uint4 *>(static_cast<uint8_t *>(a.O) + at * (wide ? 4 : 2))[piece] =
+                            *reinterpret_cast<const uint4 *>(gen + r * pitch + piece * 16);
+                    }
             }
         } else {
             // the CTA's sums go to shared memory (the operands' place: every product is complete)
