@@ -421,8 +421,10 @@ cudaError_t write_typed(const CacheWriteArgs &a, cudaStream_t stream) {
     const bool few = (int64_t)a.T * items < 148 * kWriteThreads;
     const int groups = (items + (few ? 128 : kWriteThreads) - 1) / (few ? 128 : kWriteThreads);
     const int threads = ((items + groups - 1) / groups + 31) / 32 * 32;
-    // as many tokens per CTA as leave four CTAs per SM, sixteen at most
-    int per_cta = (int)((int64_t)a.T * groups / (4 * 148));
+    // Tokens per CTA: sixteen at most, and as many as make the waves of CTAs (24 warps per SM) come out even
+    const int64_t slots = 148 * (2 * kWriteThreads / threads), all = (int64_t)a.T * groups;
+    const int64_t waves = (all + slots * kTokens - 1) / (slots * kTokens);
+    int per_cta = (int)((all + slots * waves - 1) / (slots * waves));
     per_cta = per_cta < 1 ? 1 : per_cta > kTokens ? kTokens : per_cta;
     cache_write_kernel<T><<<dim3((unsigned)((a.T + per_cta - 1) / per_cta), (unsigned)groups), threads, 0, stream>>>(a, items, shift, per_cta);
     return cudaGetLastError();
