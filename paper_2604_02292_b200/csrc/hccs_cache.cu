@@ -306,18 +306,57 @@ cache_write_kernel(const __grid_constant__ CacheWriteArgs a, int items, int per_
         slot = next_slot;
         raw_a = next_a; raw_b = next_b;
     }
-    // What was next to a border, a dim at a time.  Behind the loop: a call in it, however rare, costs its registers.
+    // What was next to a border, four pairs at a time (a dim at a time where items do not hold whole pairs).  Behind the loop: a
+    // call in it, however rare, costs its registers.
     src -= (int64_t)tokens * stride;
     q_dst -= (int64_t)tokens * a.Hq * a.d;
     while (redo) {
         const int bit = __ffs(redo) - 1, j = bit >> 1, g = bit & 1;
         redo &= redo - 1;
         int8_t *const dst = kind == 0 ? q_dst + (int64_t)j * a.Hq * a.d : place(a.slots[t0 + j]);
+        const T *const row = src + j * stride;
+        const Turn &tn = turn[j];
+        const double position = (double)a.positions[t0 + j];
+        if (!aligned) {
 #pragma unroll 1
-        for (int e = 0; e < 8; ++e) {
-            // in halves the four pairs of elements 4g ... of either chunk, else the eight elements of chunk g
-            const int dim = aligned && !inter ? (e < 4 ? dim_a : dim_b - 4) + 4 * g + e : (g ? dim_b : dim_a) + e;
-            dst[dim] = code_of(src + j * stride, dim, rot, inter, &turn[j], (double)a.positions[t0 + j], a.rope.freq, a.rope.scale, step);
+            for (int e = 0; e < 8; ++e) {
+                const int dim = (g ? dim_b : dim_a) + e;
+                dst[dim] = code_of(row, dim, rot, inter, &tn, position, a.rope.freq, a.rope.scale, step);
+            }
+            continue;
+        }
+        const int chunk_g = g ? dim_b : dim_a, at = g ? at_b : at_a, first = inter ? chunk_g >> 1 : dim_a + 4 * g;
+        float u[4], v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            u[i] = to_float(row[inter ? chunk_g + 2 * i : dim_a + 4 * g + i]);
+            v[i] = to_float(row[inter ? chunk_g + 2 * i + 1 : dim_b + 4 * g + i]);
+        }
+        int nu[4], nv[4];
+        uint32_t unsure = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float c = tn.c[at + i], s = tn.s[at + i], limit = fmaf(fabsf(u[i]) + fabsf(v[i]), bound, 0.5f);
+            const float du = nearest(__fmul_rn(fmaf(u[i], c, -__fmul_rn(v[i], s)), inv), nu[i]);
+            const float dv = nearest(__fmul_rn(fmaf(v[i], c, __fmul_rn(u[i], s)), inv), nv[i]);
+            unsure |= du < limit && dv < limit ? 0u : 1u << i;
+        }
+#pragma unroll 1
+        for (int i = 0; i < 4; ++i) {
+            if (!((unsure >> i) & 1)) continue;
+            const float x = i == 0 ? u[0] : i == 1 ? u[1] : i == 2 ? u[2] : u[3], y = i == 0 ? v[0] : i == 1 ? v[1] : i == 2 ? v[2] : v[3];
+            const uint32_t n2 = code_pair(x, y, position, a.rope.freq[first + i], a.rope.scale, step);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                nu[k] = k == i ? (int8_t)(n2 & 255) : nu[k];
+                nv[k] = k == i ? (int8_t)(n2 >> 8) : nv[k];
+            }
+        }
+        if (inter) {
+            *reinterpret_cast<uint2 *>(dst + chunk_g) = make_uint2(pack4(nu[0], nv[0], nu[1], nv[1]), pack4(nu[2], nv[2], nu[3], nv[3]));
+        } else {
+            *reinterpret_cast<uint32_t *>(dst + dim_a + 4 * g) = pack4(nu[0], nu[1], nu[2], nu[3]);
+            *reinterpret_cast<uint32_t *>(dst + dim_b + 4 * g) = pack4(nv[0], nv[1], nv[2], nv[3]);
         }
     }
 }
