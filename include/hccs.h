@@ -24,10 +24,11 @@
  *     stated otherwise.
  *   - Errors are return codes only.  On any error nothing is launched.
  *   - A context is not thread-safe: one host call at a time per context (different contexts, also
- *     on the same device, are independent).  On the GPU, hccs_forward, hccs_forward_keylen and
- *     hccs_forward_host calls of one context only read the context's parameter table and may
- *     overlap each other freely (different streams, back to back on one stream).  Calls that rewrite
- *     device memory the context owns do so on their own `cuda_stream`: hccs_params_upload (the
+ *     on the same device, are independent).  On the GPU, hccs_forward, hccs_forward_keylen,
+ *     hccs_forward_host and hccs_attention_cached calls of one context only read the context's parameter
+ *     table (hccs_cache_write and hccs_cache_read not even that) and may overlap each other freely
+ *     (different streams, back to back on one stream).  Calls that rewrite device memory the context
+ *     owns do so on their own `cuda_stream`: hccs_params_upload and hccs_params_upload_wide (the
  *     parameter table) and the hccs_attention_fused* calls (a small per-head multiplier table,
  *     rewritten only when the multipliers, the shift or the output scales differ from the previous
  *     fused call's).  Order such a call against other work of the same context that may still be
@@ -252,7 +253,8 @@ hccs_status_t hccs_calibrate(const int8_t *logits, int32_t B, int32_t H, int32_t
  * ---- Generation over an int8 key/value cache (not in the paper: its models are encoders) ----
  *
  * The cache is two pools of pages, int8 [num_pages, Hkv, page_size, d] each, one for keys and one for
- * values; page_size is a power of two from 16 to 65536, d is 64 or 128.  A sequence is a row of a page
+ * values; page_size is a power of two from 16 to 65536, d is 64 or 128,
+ * num_pages * Hkv is below 2^31.  A sequence is a row of a page
  * table: its token j lives in page table[j / page_size], at place j % page_size.  A slot is
  * page * page_size + place.  Codes stand for code * step with one step per head.  The pools, tables and
  * every workspace belong to the caller; nothing here allocates, copies from pageable memory or
@@ -304,7 +306,8 @@ hccs_status_t hccs_rope_frequencies(hccs_rope_t *rope, int32_t rot_dim, int32_t 
  *                (HCCS_ERR_UNSUPPORTED otherwise).  q may be NULL (Hq is then ignored), or both k and v
  *   positions    device int32 [T], any values; may be NULL without rope
  *   slots        device int64 [T]: where the token's key and value go; a negative slot skips them (padding
- *                tokens); the others of one call must differ.  A slot at or beyond num_pages * page_size is
+ *                tokens); the others of one call must differ (where two are
+ *                the same, the slot holds a mixture of both).  A slot at or beyond num_pages * page_size is
  *                skipped as well and reported (hccs_device_status).  May be NULL where k and v are
  *   rope         HOST, or NULL for none; applied to q and k
  *   *_step       HOST float [Hq], [Hkv], [Hkv], each in 2^-100 .. 2^100: the value of one code

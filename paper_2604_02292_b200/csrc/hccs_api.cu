@@ -509,7 +509,7 @@ hccs_status_t hccs_device_status(hccs_ctx_t *ctx, uint32_t *word, void *cuda_str
 
 static bool cache_shape(int32_t Hkv, int32_t d, int32_t num_pages, int32_t page_size, int32_t *page_shift) {
     if (Hkv < 1 || Hkv > HCCS_MAX_CACHE_HEADS || num_pages < 1 || page_size < 16 || page_size > 65536) return false;
-    if ((page_size & (page_size - 1)) != 0) return false;
+    if ((page_size & (page_size - 1)) != 0 || (int64_t)num_pages * Hkv >= (1ll << 31)) return false;
     *page_shift = 0;
     while ((1 << *page_shift) < page_size) ++*page_shift;
     return d == 64 || d == 128;

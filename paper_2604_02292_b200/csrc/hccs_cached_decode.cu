@@ -146,6 +146,8 @@ cached_decode_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_cons
     bool ok = true;
     auto landed = [&](int x) {
         ok = __all_sync(~0u, mbar_wait(smem_u32(&full[warp][x % kDepth]), (x / kDepth) & 1, &abort_flag, a.status, a.wait_cycles));
+        if (!ok)       // given up: the copies on their way (this one and the next) land before the CTA may leave, again with a limit
+            for (int y = x; y < min(x + kDepth, 2 * mine); ++y) mbar_wait_bounded(smem_u32(&full[warp][y % kDepth]), (y / kDepth) & 1, a.wait_cycles);
     };
     // Row r of a tile is swizzled over its D bytes: 16-byte chunk ch sits at ch ^ (r & 7), or ch ^ (r / 2 & 3) for D = 64.  Of K a
     // lane reads chunk c (and c + 4) of keys 16*half + 4*(nn/2) + 2*(t & 1) + (nn & 1), n tile t; of V, dims kDims*nn ... of
@@ -299,7 +301,7 @@ cached_decode_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_cons
 #pragma unroll
     for (int w = 0; w < (HI ? kDims : 1); ++w) vsum[w] = 0;
     int rs0 = 0, rs1 = 0, count = 0;
-    for (int i = 0; i < mine; ++i) {
+    for (int i = 0; ok && i < mine; ++i) {
         landed(mine + i);
         if (!ok) break;
         const uint32_t src = ring + ((mine + i) % kDepth) * S::kTileBytes;

@@ -51,6 +51,7 @@ using No = std::false_type;
 
 struct TileBarriers {
     uint64_t o_full;
+    uint64_t drained[2];                // a given-up CTA: the products of either issuer are through
     uint64_t m_done;                    // every row thread has read its last S block of the first pass
     uint64_t full[kMaxSlots], free[kMaxSlots];
     uint64_t m_full[4], m_free[4];      // S blocks of the first pass (all of tensor memory holds four)
@@ -121,6 +122,7 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
         abort_flag = 0;
         any_bad = 0;
         mbar_init(smem_u32(&bars.o_full), 1);
+        for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&bars.drained[i]), 1);
         mbar_init(smem_u32(&bars.m_done), row_threads);
         for (int i = 0; i < kSlots; ++i) { mbar_init(smem_u32(&bars.full[i]), 1); mbar_init(smem_u32(&bars.free[i]), 1); }
         for (int i = 0; i < 4; ++i) { mbar_init(smem_u32(&bars.m_full[i]), 1); mbar_init(smem_u32(&bars.m_free[i]), row_threads / 2); }
@@ -186,7 +188,7 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
             return page;
         };
         const int x0 = warp - kCopyWarp;
-        int page = x0 < loads ? page_of(x0) : -1;
+        int page = x0 < loads ? page_of(x0) : -1, sent = -1;
         for (int x = x0; ok && x < loads; x += kCopyWarps) {
             const bool values = x >= nb && ((x - nb) & 1);
             const bool there = (uint32_t)page < (uint32_t)a.num_pages;
@@ -201,7 +203,11 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
                 tma_load_3d(s_ring + (x % kSlots) * kTileBytes + lane * box * D, values ? &map_v : &map_k, 0,
                             (block_of(x) * kTile + kb0 * kTile + lane * box) & ((1 << a.page_shift) - 1), page * a.Hkv + kvh, bar);
             page = next;
+            sent = x;
         }
+        // (each slot's last copy has landed before the CTA may leave, whatever became of its readers; again with a limit)
+        for (int x = max(x0, sent - kSlots + kCopyWarps); x <= sent; x += kCopyWarps)
+            mbar_wait_bounded(smem_u32(&bars.full[x % kSlots]), (x / kSlots) & 1, a.wait_cycles);
     } else if (warp == kQkWarp || warp == kPvWarp) {
         // ===================================================== the products, issued by one thread of each warp.  The whole
         // warp walks through the loops and only the instructions themselves are the elected thread's: in a branch of one
@@ -273,6 +279,11 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
                     }
                     __syncwarp();
                 }
+            }
+            if (!ok) {
+                if (elect_one()) tcgen05_commit(smem_u32(&bars.drained[me]));
+                __syncwarp();
+                mbar_wait_bounded(smem_u32(&bars.drained[me]), 0, a.wait_cycles);
             }
         }
         __syncwarp();
