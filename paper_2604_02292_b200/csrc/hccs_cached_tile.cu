@@ -36,6 +36,12 @@ namespace {
 
 namespace cg = cooperative_groups;
 
+// of a whole warp: one try by all lanes is nearly always enough
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *abortp, uint32_t *status, long long limit) {
+    if (__all_sync(~0u, mbar_try_wait(bar, parity))) return true;
+    return __all_sync(~0u, mbar_wait(bar, parity, abortp, status, limit));
+}
+
 constexpr int kRowThreads = 512;
 constexpr int kCopyWarp = 16, kCopyWarps = 2, kQkWarp = 18, kPvWarp = 19;
 constexpr int kThreads = 640;                    // 20 warps: 96 registers a thread
@@ -169,7 +175,7 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
     if (bad && tid == 0) atomicOr(a.status, STATUS_BAD_PAGE);
     const int nfull = bad ? 0 : min(max(seen_first / kTile - kb0, 0), nb);
     const int w0 = spare ? nfull : 0;                                      // first block whose mask.V is computed
-    auto wait = [&](uint64_t *bar, uint32_t parity) { return mbar_wait(smem_u32(bar), parity, abortp, a.status, a.wait_cycles); };
+    auto wait = [&](uint64_t *bar, uint32_t parity) { return warp_wait(smem_u32(bar), parity, abortp, a.status, a.wait_cycles); };
 
     if (warp >= kCopyWarp && warp < kCopyWarp + kCopyWarps) {
         // ===================================================== copies: load number x by warp x % kCopyWarps (a thread
@@ -194,7 +200,7 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
             const bool there = (uint32_t)page < (uint32_t)a.num_pages;
             const int count = __popc(__ballot_sync(~0u, there));
             const int next = x + kCopyWarps < loads ? page_of(x + kCopyWarps) : -1;
-            if (x >= kSlots) ok = __all_sync(~0u, wait(&bars.free[x % kSlots], (x / kSlots - 1) & 1));
+            if (x >= kSlots) ok = wait(&bars.free[x % kSlots], (x / kSlots - 1) & 1);
             if (!ok) break;
             const uint32_t bar = smem_u32(&bars.full[x % kSlots]);
             if (lane == 0) mbar_expect_tx(bar, (uint32_t)(count * box * D));
@@ -217,7 +223,7 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
             const int me = warp == kQkWarp ? 0 : 1;
             bool ok = true;
             auto wait = [&](uint64_t *bar, uint32_t parity) -> bool {
-                return __all_sync(~0u, mbar_wait(smem_u32(bar), parity, abortp, a.status, a.wait_cycles));
+                return warp_wait(smem_u32(bar), parity, abortp, a.status, a.wait_cycles);
             };
             const uint64_t dq = smem_desc(s_q, 16, 8 * D, kSwizzle), dk = smem_desc(s_ring, 16, 8 * D, kSwizzle);
             const uint32_t dq_lo = (uint32_t)dq, dq_hi = (uint32_t)(dq >> 32), dk_lo = (uint32_t)dk, dk_hi = (uint32_t)(dk >> 32);
@@ -339,7 +345,7 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
             int amax = kNone;
             auto first = [&](int kb, auto masked) {
                 const int sb = kb & 3;
-                ok = __all_sync(~0u, wait(&bars.m_full[sb], (kb >> 2) & 1));
+                ok = wait(&bars.m_full[sb], (kb >> 2) & 1);
                 if (!ok) return;
                 tcgen05_fence_after();
 #pragma unroll
@@ -399,7 +405,7 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
                 *reinterpret_cast<uint4 *>(panel + (((c16 + 1) ^ swz) << 4)) = make_uint4(w[4], w[5], w[6], w[7]);
             };
             auto second = [&](int kb, auto masked) {
-                ok = __all_sync(~0u, wait(&bars.s_full[group], (kb >> 1) & 1));
+                ok = wait(&bars.s_full[group], (kb >> 1) & 1);
                 if (!ok) return;
                 tcgen05_fence_after();
 #pragma unroll
@@ -427,7 +433,7 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
                     }
                     // the products of the buffer's previous block have read it
                     if (part == 0 && kb >= 2) {
-                        ok = __all_sync(~0u, wait(&bars.r_free[group], ((kb >> 1) - 1) & 1));
+                        ok = wait(&bars.r_free[group], ((kb >> 1) - 1) & 1);
                         if (!ok) return;
                     }
                     if (decltype(masked)::value || t != vrows) panel16(pr, part, w);     // (row vrows keeps its ones)
@@ -454,7 +460,7 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
             row_barrier();
             rsum = part_sum[0][t] + part_sum[1][t] + part_sum[2][t] + part_sum[3][t];
             count = part_cnt[0][t] + part_cnt[1][t] + part_cnt[2][t] + part_cnt[3][t];
-            if (ok && nb > 0) ok = __all_sync(~0u, wait(&bars.o_full, 0));
+            if (ok && nb > 0) ok = wait(&bars.o_full, 0);
             tcgen05_fence_after();
         }
         // ---- join
