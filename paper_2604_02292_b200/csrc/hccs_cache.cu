@@ -166,8 +166,14 @@ cache_write_kernel(const __grid_constant__ CacheWriteArgs a, int items, int per_
     const bool aligned = (rot & 15) == 0;                     // rotated items hold eight whole pairs
 
     const int item = blockIdx.y * blockDim.x + threadIdx.x;
-    int head = item >> per_head_shift;
-    const int chunk = item & ((1 << per_head_shift) - 1);
+    int head = item >> per_head_shift, chunk = item & ((1 << per_head_shift) - 1);
+    const int all = 1 << per_head_shift, some = (rot + 15) >> 4;              // items of a head, and those with rotated dims
+    if (some != 0 && some != all) {
+        // the rotated items of all heads first, then the others: a warp with both kinds would take both branches below
+        const int rotated = (a.Hq + a.Hkv) * some, i = item - rotated;
+        if (i < 0) { head = item / some; chunk = item - head * some; }
+        else if (i < (a.Hq + a.Hkv) * (all - some)) { head = i / (all - some); chunk = some + i - head * (all - some); }
+    }
     const int kind = head < a.Hq ? 0 : head < a.Hq + a.Hkv ? 1 : 2;            // query, key, value
     head -= kind == 0 ? 0 : kind == 1 ? a.Hq : a.Hq + a.Hkv;
     const bool mine = item < items;
