@@ -358,7 +358,7 @@ class Context:
         dev, dtype = self.device, some.dtype
         if q is not None:
             Hq = q.shape[1]
-            if q8.get_device() != dev or q8.shape != q.shape or q8.element_size() != 1 or not q8.is_contiguous():
+            if q8.get_device() != dev or q8.shape != q.shape or q8.element_size() != 1 or not q8.is_contiguous() or q8.is_floating_point():
                 self._explain(q8, "q8", 1, q.shape)
             qp, q8p, qs = q.data_ptr(), q8.data_ptr(), _floats(q_step, "q_step", Hq)
             q_stride = self._tokens(q, "q", some)
@@ -371,14 +371,15 @@ class Context:
             k_stride, v_stride = self._tokens(k, "k", some), self._tokens(v, "v", some)
             if (k_pages.get_device() != dev or v_pages.get_device() != dev or slots.get_device() != dev or pool[1] != Hkv or pool[3] != d
                     or v_pages.shape != pool or k_pages.element_size() != 1 or v_pages.element_size() != 1 or slots.element_size() != 8
-                    or slots.shape != (T,) or not k_pages.is_contiguous() or not v_pages.is_contiguous() or not slots.is_contiguous()):
+                    or slots.shape != (T,) or not k_pages.is_contiguous() or not v_pages.is_contiguous() or not slots.is_contiguous()
+                    or k_pages.is_floating_point() or v_pages.is_floating_point() or slots.is_floating_point()):
                 self._explain(k_pages, "k_pages", 1, (pages, Hkv, size, d))
                 self._explain(v_pages, "v_pages", 1, pool)
                 self._explain(slots, "slots", 8, (T,))
             kp, vp, kpp, vpp, slotp = k.data_ptr(), v.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), slots.data_ptr()
             ks, vs = _floats(k_step, "k_step", Hkv), _floats(v_step, "v_step", Hkv)
         if positions is not None:
-            if positions.get_device() != dev or positions.element_size() != 4 or positions.shape != (T,) or not positions.is_contiguous():
+            if positions.get_device() != dev or positions.element_size() != 4 or positions.shape != (T,) or not positions.is_contiguous() or positions.is_floating_point():
                 self._explain(positions, "positions", 4, (T,))
             posp = positions.data_ptr()
         st = _lib.hccs_cache_write(self._h, qp, kp, vp, _type_of(some), q_stride, k_stride, v_stride, posp, slotp,
@@ -402,7 +403,7 @@ class Context:
         for name, t in (("k_out", k_out), ("v_out", v_out)):
             if t is not None and t.dtype != some.dtype:
                 raise ValueError("k_out and v_out must have one type")
-            out.append(None if t is None else self._check(t, name, some.element_size(), (rows, Hkv, d)))
+            out.append(None if t is None else self._output(t, name, (rows, Hkv, d)))
         st = _lib.hccs_cache_read(self._h, self._check(k_pages, "k_pages", 1), self._check(v_pages, "v_pages", 1, k_pages.shape),
                                   self._check(page_table, "page_table", 4), self._check(out_start, "out_start", 4, (B + 1,)),
                                   _floats(k_step, "k_step", Hkv), _floats(v_step, "v_step", Hkv), out[0], out[1], _type_of(some),
@@ -428,18 +429,19 @@ class Context:
                 or q_start.element_size() != 4 or kv_len.element_size() != 4 or v_pages.shape != pool or O.shape != shape
                 or q_start.shape != (B + 1,) or kv_len.shape != (B,) or not Q.is_contiguous() or not k_pages.is_contiguous()
                 or not v_pages.is_contiguous() or not page_table.is_contiguous() or not q_start.is_contiguous()
-                or not kv_len.is_contiguous() or not O.is_contiguous()):
+                or not kv_len.is_contiguous() or not O.is_contiguous() or Q.is_floating_point() or k_pages.is_floating_point()
+                or v_pages.is_floating_point() or page_table.is_floating_point() or q_start.is_floating_point() or kv_len.is_floating_point()):
             self._explain(Q, "Q", 1)
             self._explain(k_pages, "k_pages", 1)
             self._explain(v_pages, "v_pages", 1, pool)
             self._explain(page_table, "page_table", 4)
             self._explain(q_start, "q_start", 4, (B + 1,))
             self._explain(kv_len, "kv_len", 4, (B,))
-            self._explain(O, "O", O.element_size(), shape)
+            self._output(O, "O", shape)
         words, treep = 0, None
         if tree_mask is not None:
             words = tree_mask.shape[-1]
-            if tree_mask.get_device() != dev or tree_mask.element_size() != 4 or tree_mask.shape != (T, words) or not tree_mask.is_contiguous():
+            if tree_mask.get_device() != dev or tree_mask.element_size() != 4 or tree_mask.shape != (T, words) or not tree_mask.is_contiguous() or tree_mask.is_floating_point():
                 self._explain(tree_mask, "tree_mask", 4, (T, words))
             treep = tree_mask.data_ptr()
         st = _lib.hccs_attention_cached(
@@ -457,11 +459,21 @@ class Context:
         if t.get_device() != self.device:
             raise ValueError(f"{name} must live on cuda:{self.device}, not {t.device}")
         _check_tensor(t, name, itemsize, shape)
+        if t.is_floating_point():
+            raise ValueError(f"{name} must hold integers, not {t.dtype}")
 
     def _check(self, t, name, itemsize, shape=None) -> int:
-        """The address of a tensor of the context's device that passes."""
-        if t.get_device() != self.device or not t.is_contiguous() or t.element_size() != itemsize or (shape is not None and t.shape != shape):
+        """The address of a tensor of integers of the context's device that passes."""
+        if (t.get_device() != self.device or not t.is_contiguous() or t.element_size() != itemsize or t.is_floating_point()
+                or (shape is not None and t.shape != shape)):
             self._explain(t, name, itemsize, shape)
+        return t.data_ptr()
+
+    def _output(self, t, name, shape) -> int:
+        """The address of an output tensor (its type goes to the library, which knows which it takes)."""
+        if t.get_device() != self.device:
+            raise ValueError(f"{name} must live on cuda:{self.device}, not {t.device}")
+        _check_tensor(t, name, t.element_size(), shape)
         return t.data_ptr()
 
     def _tokens(self, t, name, some) -> int:

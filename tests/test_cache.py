@@ -890,3 +890,36 @@ def test_a_run_of_steps(hccs):
         want = np.concatenate([orc.sequence(pool, tab[b], n) for b, n in enumerate(lens)]).astype(np.float32) * st[None, :, None]
         assert (got.cpu().numpy() == want).all()
     ctx.close()
+
+
+@pytest.mark.gpu
+def test_tensors_of_other_kinds_are_refused(hccs):
+    """Floats where whole numbers belong, whole numbers where values belong: refused before anything is launched."""
+    import torch
+    dev = "cuda"
+    ctx = hccs.Context(0)
+    ctx.hccs_params_upload([(300, 3, 85)] * 2, 64)                        # (a table of the integer modes)
+    i8 = lambda *s: torch.zeros(s, dtype=torch.int8, device=dev)          # noqa: E731
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32, device=dev)        # noqa: E731
+    x, step = torch.zeros((3, 2, 64), device=dev), np.ones(2, np.float32)
+    write = dict(q=x, k=x, v=x, q8=i8(3, 2, 64), k_pages=i8(2, 2, 16, 64), v_pages=i8(2, 2, 16, 64), positions=i32(3),
+                 slots=torch.arange(3, device=dev), q_step=step, k_step=step, v_step=step)
+    read = dict(k_pages=i8(2, 2, 16, 64), v_pages=i8(2, 2, 16, 64), page_table=i32(1, 1), out_start=i32(2), k_out=x.clone(), v_out=x.clone(),
+                k_step=step, v_step=step, max_len=3)
+    attend = dict(Q=i8(3, 2, 64), k_pages=i8(2, 2, 16, 64), v_pages=i8(2, 2, 16, 64), page_table=i32(1, 1), q_start=i32(2), kv_len=i32(1),
+                  O=i32(3, 2, 64), requant_mult=np.ones(2, np.int32), requant_shift=8, max_q=3, max_kv=16, tree_mask=i32(3, 1))
+    torch.cuda.synchronize()
+    before = ctx.hccs_launch_count()
+    f8 = torch.float8_e4m3fn
+    for call, args, wrong in [(ctx.hccs_cache_write, write, {"q8": f8, "k_pages": f8, "v_pages": f8, "positions": torch.float32, "slots": torch.float64, "k": torch.float16, "q": torch.int32}),
+                              (ctx.hccs_cache_read, read, {"k_pages": f8, "v_pages": f8, "page_table": torch.float32, "out_start": torch.float32, "k_out": torch.int32, "v_out": torch.int16}),
+                              (ctx.hccs_attention_cached, attend, {"Q": f8, "k_pages": f8, "v_pages": f8, "page_table": torch.float32, "q_start": torch.float32, "kv_len": torch.float32,
+                                                                   "tree_mask": torch.float32, "O": torch.int64})]:
+        for name, dtype in wrong.items():
+            with pytest.raises((ValueError, hccs.HccsError)):
+                call(**{**args, name: args[name].to(dtype)})
+    assert ctx.hccs_launch_count() == before
+    ctx.hccs_cache_write(**write)
+    ctx.hccs_attention_cached(**attend)
+    assert ctx.hccs_launch_count() == before + 2
+    ctx.close()
