@@ -1,7 +1,9 @@
 // The int8 key/value cache: tokens rotated, quantised and written to their slots, and sequences read back.
 //
-// Both are bound by HBM: every element is read once and written once (2 or 4 bytes in and one out, or the
-// reverse).
+// Every element is read once and written once (2 or 4 bytes in and one out, or the reverse).  Reading back is bound by
+// HBM: 8 sequences of 8192 tokens (8 heads of 128, to bf16) in 65 us, 6.2 TB/s.  Writing is bound by instructions, about
+// twenty per element with the margins below (issue slots 70 % busy, DRAM 45 %): 16384 tokens (32 + 8 + 8 heads of 128,
+// bf16, all of a head rotated) in 75 us, 4.0 TB/s; without rotation 60 us, 5.1 TB/s.
 //
 // Exactness of the codes.  A code is the exact quotient y / step rounded to nearest; a border decides a whole
 // step, so the value next to it needs more than fp32.  Computed in fp32,

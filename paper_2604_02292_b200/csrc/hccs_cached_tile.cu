@@ -20,6 +20,13 @@
 // in the first pass, where there are none, every second Q.K^T).  K blocks of the first pass, then K and V blocks
 // in turn, stream through one ring; load number x uses slot x % kSlots.
 //
+// Bound: the chain of a block, tensor product -> tensor memory -> registers -> r -> tensor product, in turns of two
+// groups: tensor pipe and integer pipe are both half busy.  2048 new tokens on each of two caches of 8192 keys (16 query
+// heads on 4 of 128): 179 us, 0.40 of the int8 rate counting the formula's two products; 8 trees of 48 on
+// 8000 keys (32 heads on 8): 53 us.  Tried and slower or no faster: r (and Q) as operands in tensor memory (185 us), a
+// third S buffer in the second pass (208), four groups (222), 64 columns per tensor-memory load (191), all sequences' longest
+// tiles first (185; with caches beyond L2 up to half slower), one issuer for both products (263).
+//
 // Few rows and many keys: the key blocks of a row tile are split over the CTAs of a cluster, which exchange row
 // maxima between the passes and sums at the end through distributed shared memory (exact integers: the split
 // changes no bit).  Row warps whose 32 rows lie behind the tile's last row do nothing.
