@@ -5,6 +5,8 @@
 // hold exactly in integers: sum r V is an int8 x int8 contraction that never leaves int32
 // (127 * 128 * 131072 < 2^31), whatever the table, and sums of parts join without rounding.
 #pragma once
+#include <atomic>
+
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -135,14 +137,47 @@ inline bool make_page_map(CUtensorMap *map, const void *pool, const CachedAttnAr
 
 // Raises a kernel's limits (dynamic shared memory, clusters of sixteen) once per kernel and device: `done` is the
 // kernel's own array of flags.
-inline cudaError_t raise_limits(const void *kernel, int smem, bool (&done)[64]) {
+inline cudaError_t raise_limits(const void *kernel, int smem, std::atomic<bool> (&done)[64]) {
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess || (dev < 64 && done[dev])) return e;
+    if (e != cudaSuccess || (dev < 64 && done[dev].load(std::memory_order_acquire))) return e;
     e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-    if (e == cudaSuccess && dev < 64) done[dev] = true;
+    if (e == cudaSuccess && dev < 64) done[dev].store(true, std::memory_order_release);
     return e;
+}
+
+constexpr int kMaxSplit = 16;              // CTAs per cluster
+
+// Clusters of 1 .. 16 CTAs of one kernel that the current device holds at a time, with all of an SM's shared memory per CTA
+// (how many depends on how the device's SMs are grouped; asked once per kernel and device).
+struct Active { int n[kMaxSplit + 1]; std::atomic<bool> known; };
+template <typename K>
+cudaError_t active_clusters(K kernel, int threads, size_t smem, Active (&all)[64], const Active **out) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    Active &a = all[dev < 64 ? dev : 63];
+    if (!a.known.load(std::memory_order_acquire) || dev >= 63) {
+        for (int s = 1; s <= kMaxSplit; ++s) {
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3((unsigned)s, 64, 1);
+            cfg.blockDim = dim3((unsigned)threads);
+            cfg.dynamicSmemBytes = smem;
+            cudaLaunchAttribute attr[1];
+            attr[0].id = cudaLaunchAttributeClusterDimension;
+            attr[0].val.clusterDim.x = (unsigned)s;
+            attr[0].val.clusterDim.y = 1;
+            attr[0].val.clusterDim.z = 1;
+            cfg.attrs = attr;
+            cfg.numAttrs = 1;
+            e = cudaOccupancyMaxActiveClusters(&a.n[s], kernel, &cfg);
+            if (e != cudaSuccess) return e;
+        }
+        a.known.store(true, std::memory_order_release);
+    }
+    *out = &a;
+    return cudaSuccess;
 }
 
 }  // namespace hccs

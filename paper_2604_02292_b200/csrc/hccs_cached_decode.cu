@@ -72,7 +72,6 @@ struct Sizes {
     }
 };
 
-constexpr int kMaxSplit = 16;              // CTAs per cluster
 
 // D: head dim.  HI: more than 8 rows (the fragments' rows 8..15 are rows too; otherwise row 8 is all ones and
 // collects sum V for nothing).  tiles_per_warp bounds what shared memory holds.
@@ -438,37 +437,6 @@ cached_decode_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_cons
         }
 }
 
-// Clusters of 1 .. 16 CTAs of one kernel that the current device holds at a time, with all of an SM's shared memory per CTA
-// (how many depends on how the device's SMs are grouped; asked once per kernel and device).
-struct Active { int n[kMaxSplit + 1]; bool known; };
-template <typename K>
-cudaError_t active_clusters(K kernel, int threads, size_t smem, Active (&all)[64], const Active **out) {
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return e;
-    Active &a = all[dev < 64 ? dev : 63];
-    if (!a.known || dev >= 63) {
-        for (int s = 1; s <= kMaxSplit; ++s) {
-            cudaLaunchConfig_t cfg = {};
-            cfg.gridDim = dim3((unsigned)s, 64, 1);
-            cfg.blockDim = dim3((unsigned)threads);
-            cfg.dynamicSmemBytes = smem;
-            cudaLaunchAttribute attr[1];
-            attr[0].id = cudaLaunchAttributeClusterDimension;
-            attr[0].val.clusterDim.x = (unsigned)s;
-            attr[0].val.clusterDim.y = 1;
-            attr[0].val.clusterDim.z = 1;
-            cfg.attrs = attr;
-            cfg.numAttrs = 1;
-            e = cudaOccupancyMaxActiveClusters(&a.n[s], kernel, &cfg);
-            if (e != cudaSuccess) return e;
-        }
-        a.known = true;
-    }
-    *out = &a;
-    return cudaSuccess;
-}
-
 constexpr size_t kMaxSmem = 210 * 1024;    // dynamic; the kernel's own arrays take up to 16 KB more
 constexpr size_t kHalfSmem = 98 * 1024;    // two CTAs per SM
 
@@ -482,8 +450,8 @@ struct Plan { int split, per_warp; double cost; };
 template <int D, bool HI, int W>
 cudaError_t plan_for(const CachedAttnArgs &a, int64_t groups, Plan &best) {
     using S = Sizes<D, HI, W>;
-    static Active known[64] = {};
-    static bool raised[64] = {};
+    static Active known[64];
+    static std::atomic<bool> raised[64];
     auto kernel = cached_decode_kernel<D, HI, W>;
     cudaError_t e = raise_limits((const void *)kernel, (int)kMaxSmem, raised);
     const Active *active = nullptr;

@@ -607,22 +607,30 @@ cudaError_t launch_typed(const CachedAttnArgs &a, cudaStream_t stream) {
     const int row_tiles = (int)(tile_rows == kTile ? tiles128 : tiles127);
     const int blocks = (a.max_kv + kTile - 1) / kTile;
     const int64_t ctas = (int64_t)row_tiles * a.Hkv * a.B;
-    // Cluster size: waves of 148 CTAs times the blocks each walks over, plus about six blocks' time of set-up and join
-    int split = 1;
-    int64_t best = -1;
-    for (int s = 1; s <= 16 && (s == 1 || blocks >= 2 * s); s *= 2) {
-        const int64_t cost = ((ctas * s + 147) / 148) * ((blocks + s - 1) / s + 6 + (s > 1 ? 4 : 0));
-        if (best < 0 || cost < best) { best = cost; split = s; }
-    }
-    if ((int64_t)row_tiles * split > 0x7fffffff) return cudaErrorInvalidValue;
     constexpr size_t smem = 1024 + (size_t)(1 + kSlotsOf<D>) * kTile * D + 4 * kPanelBytes;
     static_assert(smem - 1024 >= 2 * sizeof(int) * kTile * (D + 4), "the joined sums fit the operands' place");
+    auto kernel = cached_tile_kernel<D>;
+    static std::atomic<bool> raised[64];
+    static Active known[64];
+    const Active *active = nullptr;
+    cudaError_t e = raise_limits((const void *)kernel, (int)smem, raised);
+    if (e == cudaSuccess) e = active_clusters(kernel, kThreads, smem, known, &active);
+    if (e != cudaSuccess) return e;
+    // Cluster size: waves of as many CTAs as the device holds in clusters of that size, times the blocks each walks over, plus
+    // about six blocks' time of set-up and join, ten with an exchange.  (One cache of 100000 keys, 8 kv heads, 8 new tokens: clusters of
+    // sixteen, of which seven run at a time, 105 us; of eight 81.)
+    int split = 1;
+    int64_t best = -1;
+    for (int s = 1; s <= kMaxSplit && (s == 1 || blocks >= 2 * s); s *= 2) {
+        if (active->n[s] < 1) continue;
+        const int64_t slots = (int64_t)active->n[s] * s;
+        const int64_t cost = ((ctas * s + slots - 1) / slots) * ((blocks + s - 1) / s + (s > 1 ? 10 : 6));
+        if (best < 0 || cost < best) { best = cost; split = s; }
+    }
+    if (best < 0) return cudaErrorInvalidConfiguration;
+    if ((int64_t)row_tiles * split > 0x7fffffff) return cudaErrorInvalidValue;
     CUtensorMap mk, mv;
     if (!make_page_map(&mk, a.k_pages, a, kTile) || !make_page_map(&mv, a.v_pages, a, kTile)) return cudaErrorInvalidValue;
-    auto kernel = cached_tile_kernel<D>;
-    static bool raised[64] = {};
-    const cudaError_t e = raise_limits((const void *)kernel, (int)smem, raised);
-    if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(row_tiles * split), (unsigned)a.Hkv, (unsigned)a.B);
     cfg.blockDim = dim3(kThreads);
