@@ -13,7 +13,8 @@
 // rounding and its product, for the product and the sum, for 1/step, and half for the distance from the border, where X
 // is at least a half.  With margin = X * 8 * 2^-24, a z that is further than margin from every border k + 1/2 has the
 // right code; the few pairs with any other (one in five thousand on usual data) are computed in fp64 by the
-// definition.  NaN and infinities fail the comparison too.  Dims that are not rotated need no fp64: see
+// definition.  NaN and infinities fail the comparison too, and the turn of an angle beyond 2^24 is made NaN: its
+// reduction would be off by more than that share.  Dims that are not rotated need no fp64: see
 // code_of_quotient.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -145,7 +146,7 @@ __device__ __noinline__ int8_t code_of(const T *head, int dim, int rot, bool int
     const float s = turn->s[skew(pair)];
     const float z = __fmul_rn(fmaf(x, turn->c[skew(pair)], __fmul_rn(p, first ? -s : s)), inv);
     int n;
-    if (fmaf(fabsf(x) + fabsf(p), fabsf((float)scale) * inv * 0x1p-21f, nearest(z, n)) < 0.5f) return (int8_t)max(min(n, 127), -128);
+    if (fmaf(fabsf(x) + fabsf(p), fmaxf(fabsf((float)scale) * inv * 0x1p-21f, 0x1p-125f), nearest(z, n)) < 0.5f) return (int8_t)max(min(n, 127), -128);
     const uint32_t two = first ? code_pair(x, p, position, freq[pair], scale, step) : code_pair(p, x, position, freq[pair], scale, step) >> 8;
     return (int8_t)(two & 255);
 }
@@ -193,12 +194,14 @@ cache_write_kernel(const __grid_constant__ CacheWriteArgs a, int items, int per_
         for (int i = threadIdx.x; i < tokens * half; i += blockDim.x) {
             const int tok = i / half, pair = i - tok * half;
             // the angle as the definition rounds it, in turns, less the whole ones: exact but for 2^-53 of the turns
-            const double turns = __dmul_rn(__dmul_rn((double)a.positions[t0 + tok], a.rope.freq[pair]), 0.15915494309189533577);
+            const double angle = __dmul_rn((double)a.positions[t0 + tok], a.rope.freq[pair]), turns = __dmul_rn(angle, 0.15915494309189533577);
             const double part = turns - rint(turns);
             const float hi = (float)part, lo = (float)(part - (double)hi) * 6.2831853f;
             float s, c;
             sincospif(2.0f * hi, &s, &c);
             const float scale = (float)a.rope.scale;
+            // beyond 2^24 radians the turns are no longer good to the margin's share (2^-27): NaN sends all codes to fp64
+            if (!(fabs(angle) < 0x1p24)) c = s = __int_as_float(0x7fffffff);
             turn[tok].c[skew(pair)] = (c - lo * s) * scale;
             turn[tok].s[skew(pair)] = (s + lo * c) * scale;
             turn[tok].ns[skew(pair)] = -turn[tok].s[skew(pair)];
@@ -208,7 +211,8 @@ cache_write_kernel(const __grid_constant__ CacheWriteArgs a, int items, int per_
     if (!mine) return;
     const float step = a.step[kind * HCCS_MAX_CACHE_HEADS + head], inv = 1.0f / step;
     const F2 inv2 = f2(inv, inv), neg_inv2 = f2(-inv, -inv);
-    const float bound = (turned ? fabsf((float)a.rope.scale) : 1.0f) * inv * -0x1p-21f;
+    // (never so small that it loses digits below the normal range: values near 2^128 with steps near 2^100)
+    const float bound = -fmaxf((turned ? fabsf((float)a.rope.scale) : 1.0f) * inv * 0x1p-21f, 0x1p-125f);
     const F2 bound2 = f2(bound, bound), half2 = f2(0.5f, 0.5f), magic2 = f2(12582912.0f, 12582912.0f), unmagic2 = f2(-12582912.0f, -12582912.0f);
     // nearest integers of w * (1/step) for two values; `sure` stays if both are further than their margins from a border
     auto nearest2 = [&](F2 w, F2 limit, int &n0, int &n1, bool &sure) {

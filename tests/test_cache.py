@@ -923,3 +923,27 @@ def test_tensors_of_other_kinds_are_refused(hccs):
     ctx.hccs_attention_cached(**attend)
     assert ctx.hccs_launch_count() == before + 2
     ctx.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rot,interleaved", [(64, False), (32, True), (20, False)])
+def test_write_of_far_positions(hccs, rot, interleaved):
+    """Angles of up to 2^51 radians: the codes are still those of the angle as it rounds to fp64."""
+    import torch
+    rng = np.random.default_rng(rot)
+    T, d = 257, 64
+    x = torch.from_numpy(rng.standard_normal((T, 4, d)).astype(np.float32)).cuda()
+    pos = np.concatenate([rng.integers(-2 ** 31, 2 ** 31, T - 6), [2 ** 31 - 1, -2 ** 31, 2 ** 24, 2 ** 24 + 1, 2 ** 24 - 1, 0]]).astype(np.int32)
+    freq = [[1.0, 1e6, 0.37, 1000.0, 1e-3][i % 5] * 1.07 ** i for i in range(rot // 2)]
+    q8 = torch.zeros((T, 2, d), dtype=torch.int8, device="cuda")
+    kp, vp = (torch.zeros((20, 1, 16, d), dtype=torch.int8, device="cuda") for _ in range(2))
+    step = [0.02, 0.003]
+    ctx = hccs.Context(0)
+    ctx.hccs_cache_write(x[:, :2], x[:, 2:3], x[:, 3:], q8, kp, vp, torch.from_numpy(pos).cuda(), torch.arange(T, device="cuda"), step, [0.02], [0.02],
+                         rope=hccs.Rope(freq, interleaved=interleaved))
+    xs = x.cpu().numpy()
+    assert (q8.cpu().numpy() == orc.quantise(orc.rotate(xs[:, :2], pos, freq, interleaved, 1.0), step)).all()
+    got = kp.cpu().numpy().transpose(0, 2, 1, 3).reshape(-1, 1, d)[:T]
+    assert (got == orc.quantise(orc.rotate(xs[:, 2:3], pos, freq, interleaved, 1.0), [0.02])).all()
+    assert ctx.hccs_device_status() == 0
+    ctx.close()
