@@ -3,7 +3,7 @@
 // Every element is read once and written once (2 or 4 bytes in and one out, or the reverse).  Reading back is bound by
 // HBM: 8 sequences of 8192 tokens (8 heads of 128, to bf16) in 65 us, 6.2 TB/s.  Writing is bound by instructions, about
 // twenty per element with the margins below (issue slots 70 % busy, DRAM 45 %): 16384 tokens (32 + 8 + 8 heads of 128,
-// bf16, all of a head rotated) in 75 us, 4.0 TB/s; without rotation 60 us, 5.1 TB/s.
+// bf16, all of a head rotated) in 74 us, 4.1 TB/s; without rotation 60 us, 5.0 TB/s.
 //
 // Exactness of the codes.  A code is the exact quotient y / step rounded to nearest; a border decides a whole
 // step, so the value next to it needs more than fp32.  Computed in fp32,
@@ -191,20 +191,27 @@ cache_write_kernel(const __grid_constant__ CacheWriteArgs a, int items, int per_
     if (mine && tokens > 0) { raw_a = load_raw(src + dim_a); raw_b = load_raw(src + dim_b); }
 
     if (rot > 0) {
-        for (int i = threadIdx.x; i < tokens * half; i += blockDim.x) {
-            const int tok = i / half, pair = i - tok * half;
-            // the angle as the definition rounds it, in turns, less the whole ones: exact but for 2^-53 of the turns
-            const double angle = __dmul_rn((double)a.positions[t0 + tok], a.rope.freq[pair]), turns = __dmul_rn(angle, 0.15915494309189533577);
-            const double part = turns - rint(turns);
-            const float hi = (float)part, lo = (float)(part - (double)hi) * 6.2831853f;
-            float s, c;
-            sincospif(2.0f * hi, &s, &c);
+        // a thread stays with one pair (two in a CTA of 32 threads): the next power of two of pairs side by side, several
+        // tokens abreast (with pairs and tokens in turn, and a division for each, a prompt took 2.5 us more)
+        const int wide = min(1 << (32 - __clz(half - 1)), (int)blockDim.x), abreast = (int)blockDim.x / wide;
+        const int tok0 = (int)threadIdx.x / wide;
+        for (int pair = (int)threadIdx.x & (wide - 1); pair < half && tok0 < abreast; pair += wide) {
+            const double freq = a.rope.freq[pair];
             const float scale = (float)a.rope.scale;
-            // beyond 2^24 radians the turns are no longer good to the margin's share (2^-27): NaN sends all codes to fp64
-            if (!(fabs(angle) < 0x1p24)) c = s = __int_as_float(0x7fffffff);
-            turn[tok].c[skew(pair)] = (c - lo * s) * scale;
-            turn[tok].s[skew(pair)] = (s + lo * c) * scale;
-            turn[tok].ns[skew(pair)] = -turn[tok].s[skew(pair)];
+            for (int tok = tok0; tok < tokens; tok += abreast) {
+                // the angle as the definition rounds it, in turns, less the whole ones: exact but for 2^-53 of the turns
+                const double angle = __dmul_rn((double)a.positions[t0 + tok], freq), turns = __dmul_rn(angle, 0.15915494309189533577);
+                const double part = turns - rint(turns);
+                const float hi = (float)part, lo = (float)(part - (double)hi) * 6.2831853f;
+                float s, c;
+                sincospif(2.0f * hi, &s, &c);
+                // beyond 2^24 radians the turns are no longer good to the margin's share (2^-27): NaN sends all codes to fp64
+                if (!(fabs(angle) < 0x1p24)) c = s = __int_as_float(0x7fffffff);
+                const float ss = (s + lo * c) * scale;
+                turn[tok].c[skew(pair)] = (c - lo * s) * scale;
+                turn[tok].s[skew(pair)] = ss;
+                turn[tok].ns[skew(pair)] = -ss;
+            }
         }
         __syncthreads();
     }

@@ -947,3 +947,29 @@ def test_write_of_far_positions(hccs, rot, interleaved):
     assert (got == orc.quantise(orc.rotate(xs[:, 2:3], pos, freq, interleaved, 1.0), [0.02])).all()
     assert ctx.hccs_device_status() == 0
     ctx.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hq,hkv,d,rot,T", [(1, 0, 128, 128, 5), (1, 0, 64, 64, 3), (0, 1, 128, 128, 2), (3, 0, 128, 96, 17), (1, 1, 64, 2, 33), (0, 2, 64, 34, 9)])
+def test_write_of_a_few_heads(hccs, hq, hkv, d, rot, T):
+    """Calls so small that a CTA has fewer threads than a head has pairs; queries alone, keys and values alone."""
+    import torch
+    rng = np.random.default_rng(hq + 10 * hkv + rot)
+    x = torch.from_numpy(rng.standard_normal((T, max(hq, 1) + 2 * max(hkv, 1), d)).astype(np.float32)).cuda()
+    q, k, v = (x[:, :hq].contiguous() if hq else None), (x[:, hq:hq + hkv].contiguous() if hkv else None), (x[:, hq + hkv:hq + 2 * hkv].contiguous() if hkv else None)
+    pos = rng.integers(0, 5000, T).astype(np.int32)
+    freq = [10000.0 ** (-2.0 * i / rot) for i in range(rot // 2)]
+    q8 = torch.zeros((T, hq, d), dtype=torch.int8, device="cuda") if hq else None
+    kp, vp = ((torch.zeros((3, hkv, 16, d), dtype=torch.int8, device="cuda") for _ in range(2)) if hkv else (None, None))
+    ctx = hccs.Context(0)
+    ctx.hccs_cache_write(q, k, v, q8, kp, vp, torch.from_numpy(pos).cuda(), torch.arange(T, device="cuda") if hkv else None,
+                         [0.03] * hq if hq else None, [0.03] * hkv if hkv else None, [0.04] * hkv if hkv else None, rope=hccs.Rope(freq))
+    xs = x.cpu().numpy()
+    if hq:
+        assert (q8.cpu().numpy() == orc.quantise(orc.rotate(xs[:, :hq], pos, freq, False, 1.0), [0.03] * hq)).all()
+    if hkv:
+        back = lambda p: p.cpu().numpy().transpose(0, 2, 1, 3).reshape(-1, hkv, d)[:T]          # noqa: E731
+        assert (back(kp) == orc.quantise(orc.rotate(xs[:, hq:hq + hkv], pos, freq, False, 1.0), [0.03] * hkv)).all()
+        assert (back(vp) == orc.quantise(xs[:, hq + hkv:hq + 2 * hkv].astype(np.longdouble), [0.04] * hkv)).all()
+    assert ctx.hccs_device_status() == 0
+    ctx.close()
