@@ -31,7 +31,6 @@ namespace hccs {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kItem = 16;                  // codes per thread and step
 
 // Eight neighbouring elements as they are loaded.
 template <typename T> struct Raw { uint4 w[sizeof(T) / 2]; };
