@@ -358,7 +358,7 @@ class Context:
         dev, dtype = self.device, some.dtype
         if q is not None:
             Hq = q.shape[1]
-            if q8.get_device() != dev or q8.shape != q.shape or q8.element_size() != 1 or not q8.is_contiguous() or q8.is_floating_point():
+            if q8.get_device() != dev or q8.shape != q.shape or q8.dtype not in _I8 or not q8.is_contiguous():
                 self._explain(q8, "q8", 1, q.shape)
             qp, q8p, qs = q.data_ptr(), q8.data_ptr(), _floats(q_step, "q_step", Hq)
             q_stride = self._tokens(q, "q", some)
@@ -370,16 +370,15 @@ class Context:
                 raise ValueError("k and v must have one shape and type")
             k_stride, v_stride = self._tokens(k, "k", some), self._tokens(v, "v", some)
             if (k_pages.get_device() != dev or v_pages.get_device() != dev or slots.get_device() != dev or pool[1] != Hkv or pool[3] != d
-                    or v_pages.shape != pool or k_pages.element_size() != 1 or v_pages.element_size() != 1 or slots.element_size() != 8
-                    or slots.shape != (T,) or not k_pages.is_contiguous() or not v_pages.is_contiguous() or not slots.is_contiguous()
-                    or k_pages.is_floating_point() or v_pages.is_floating_point() or slots.is_floating_point()):
+                    or v_pages.shape != pool or k_pages.dtype not in _I8 or v_pages.dtype not in _I8 or slots.dtype not in _I64
+                    or slots.shape != (T,) or not k_pages.is_contiguous() or not v_pages.is_contiguous() or not slots.is_contiguous()):
                 self._explain(k_pages, "k_pages", 1, (pages, Hkv, size, d))
                 self._explain(v_pages, "v_pages", 1, pool)
                 self._explain(slots, "slots", 8, (T,))
             kp, vp, kpp, vpp, slotp = k.data_ptr(), v.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), slots.data_ptr()
             ks, vs = _floats(k_step, "k_step", Hkv), _floats(v_step, "v_step", Hkv)
         if positions is not None:
-            if positions.get_device() != dev or positions.element_size() != 4 or positions.shape != (T,) or not positions.is_contiguous() or positions.is_floating_point():
+            if positions.get_device() != dev or positions.dtype not in _I32 or positions.shape != (T,) or not positions.is_contiguous():
                 self._explain(positions, "positions", 4, (T,))
             posp = positions.data_ptr()
         st = _lib.hccs_cache_write(self._h, qp, kp, vp, _type_of(some), q_stride, k_stride, v_stride, posp, slotp,
@@ -424,13 +423,12 @@ class Context:
         if dk != d:
             raise ValueError(f"the cache holds heads of {dk}, Q of {d}")
         if (Q.get_device() != dev or k_pages.get_device() != dev or v_pages.get_device() != dev or page_table.get_device() != dev
-                or q_start.get_device() != dev or kv_len.get_device() != dev or O.get_device() != dev or Q.element_size() != 1
-                or k_pages.element_size() != 1 or v_pages.element_size() != 1 or page_table.element_size() != 4
-                or q_start.element_size() != 4 or kv_len.element_size() != 4 or v_pages.shape != pool or O.shape != shape
+                or q_start.get_device() != dev or kv_len.get_device() != dev or O.get_device() != dev or Q.dtype not in _I8
+                or k_pages.dtype not in _I8 or v_pages.dtype not in _I8 or page_table.dtype not in _I32
+                or q_start.dtype not in _I32 or kv_len.dtype not in _I32 or v_pages.shape != pool or O.shape != shape
                 or q_start.shape != (B + 1,) or kv_len.shape != (B,) or not Q.is_contiguous() or not k_pages.is_contiguous()
                 or not v_pages.is_contiguous() or not page_table.is_contiguous() or not q_start.is_contiguous()
-                or not kv_len.is_contiguous() or not O.is_contiguous() or Q.is_floating_point() or k_pages.is_floating_point()
-                or v_pages.is_floating_point() or page_table.is_floating_point() or q_start.is_floating_point() or kv_len.is_floating_point()):
+                or not kv_len.is_contiguous() or not O.is_contiguous()):
             self._explain(Q, "Q", 1)
             self._explain(k_pages, "k_pages", 1)
             self._explain(v_pages, "v_pages", 1, pool)
@@ -441,7 +439,7 @@ class Context:
         words, treep = 0, None
         if tree_mask is not None:
             words = tree_mask.shape[-1]
-            if tree_mask.get_device() != dev or tree_mask.element_size() != 4 or tree_mask.shape != (T, words) or not tree_mask.is_contiguous() or tree_mask.is_floating_point():
+            if tree_mask.get_device() != dev or tree_mask.dtype not in _I32 or tree_mask.shape != (T, words) or not tree_mask.is_contiguous():
                 self._explain(tree_mask, "tree_mask", 4, (T, words))
             treep = tree_mask.data_ptr()
         st = _lib.hccs_attention_cached(
@@ -459,13 +457,17 @@ class Context:
         if t.get_device() != self.device:
             raise ValueError(f"{name} must live on cuda:{self.device}, not {t.device}")
         _check_tensor(t, name, itemsize, shape)
-        if t.is_floating_point():
+        if not _I8:
+            import torch
+            _I8.update((torch.int8, torch.uint8))
+            _I32.update((torch.int32, torch.uint32))
+            _I64.update((torch.int64, torch.uint64))
+        if t.dtype not in _WHOLE[itemsize]:
             raise ValueError(f"{name} must hold integers, not {t.dtype}")
 
     def _check(self, t, name, itemsize, shape=None) -> int:
         """The address of a tensor of integers of the context's device that passes."""
-        if (t.get_device() != self.device or not t.is_contiguous() or t.element_size() != itemsize or t.is_floating_point()
-                or (shape is not None and t.shape != shape)):
+        if t.get_device() != self.device or not t.is_contiguous() or t.dtype not in _WHOLE[itemsize] or (shape is not None and t.shape != shape):
             self._explain(t, name, itemsize, shape)
         return t.data_ptr()
 
@@ -479,7 +481,7 @@ class Context:
     def _tokens(self, t, name, some) -> int:
         """Elements between the tokens of a [T, heads, d] view that is contiguous inside a token."""
         if t.get_device() != self.device:
-            self._explain(t, name, t.element_size())
+            raise ValueError(f"{name} must live on cuda:{self.device}, not {t.device}")
         T, heads, d = t.shape
         if t is not some and (t.dtype != some.dtype or T != some.shape[0] or d != some.shape[2]):
             raise ValueError(f"{name} must be [{some.shape[0]}, heads, {some.shape[2]}] of {some.dtype}, got {tuple(t.shape)} of {t.dtype}")
@@ -529,6 +531,8 @@ def hccs_forward_static_scratch(params, n_design: int, logits, probs, flags: int
 
 
 _TYPES = {}
+_I8, _I32, _I64 = set(), set(), set()      # integer types by their size, filled on first use
+_WHOLE = {1: _I8, 4: _I32, 8: _I64}
 
 
 # torch is imported on first use: the host-only calls do without it.
