@@ -17,6 +17,8 @@
 // The CTAs of a cluster take tiles in turn, push their row maxima to each other between the passes and their sums to
 // the CTA that finishes a dim at the end, through distributed shared memory: one launch, no workspace, and exact
 // integers, so the split changes no bit.
+#include <math.h>
+
 #include "hccs_cached.cuh"
 
 namespace hccs {
@@ -440,7 +442,7 @@ cached_decode_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_cons
 constexpr size_t kMaxSmem = 210 * 1024;    // dynamic; the kernel's own arrays take up to 16 KB more
 constexpr size_t kHalfSmem = 98 * 1024;    // two CTAs per SM
 
-struct Plan { int split, per_warp; double cost; };
+struct Plan { int split, per_warp; double cost; };      // cost: infinite where no cluster size has the shared memory
 
 // What a launch with W warps per CTA and clusters of `s` costs, in microseconds: waves of clusters, each the time of a CTA's
 // share of a kv head's codes at a CTA's rate (measured 42 GB/s with eight warps, 53 with sixteen or for two CTAs of eight on one
@@ -457,7 +459,7 @@ cudaError_t plan_for(const CachedAttnArgs &a, int64_t groups, Plan &best) {
     const Active *active = nullptr;
     if (e == cudaSuccess) e = active_clusters(kernel, 32 * W, kMaxSmem, known, &active);
     if (e != cudaSuccess) return e;
-    best.cost = -1;
+    best.cost = HUGE_VAL;
     const int tiles = (a.max_kv + kTileKeys - 1) / kTileKeys;
     const double bytes = 2.0 * a.max_kv * D;
     for (int s = 1; s <= kMaxSplit; ++s) {
@@ -472,9 +474,9 @@ cudaError_t plan_for(const CachedAttnArgs &a, int64_t groups, Plan &best) {
         double waves = (double)((groups + at_a_time - 1) / at_a_time);
         if (waves > 2) waves = (double)groups / at_a_time + 0.5;
         const double cost = waves * (4.5 + (s > 1 ? 0.5 + 0.1 * s : 0.0) + bytes / s / rate);
-        if (best.cost < 0 || cost < best.cost) { best.cost = cost; best.split = s; best.per_warp = per; }
+        if (cost < best.cost) { best.cost = cost; best.split = s; best.per_warp = per; }
     }
-    return best.cost < 0 ? cudaErrorInvalidConfiguration : cudaSuccess;
+    return cudaSuccess;
 }
 
 template <int D, bool HI, int W>
@@ -505,6 +507,9 @@ cudaError_t launch_typed(const CachedAttnArgs &a, cudaStream_t stream) {
     cudaError_t e = plan_for<D, HI, 8>(a, groups, p8);
     if (e == cudaSuccess) e = plan_for<D, HI, 16>(a, groups, p16);
     if (e != cudaSuccess) return e;
+    // (sixteen warps' rings leave no room for the logits of many rows of long caches: d = 128, 16 rows, more than 81920 keys;
+    // eight warps in clusters of sixteen hold all that is allowed)
+    if (p8.cost == HUGE_VAL && p16.cost == HUGE_VAL) return cudaErrorInvalidConfiguration;
     return p16.cost < p8.cost ? launch_plan<D, HI, 16>(a, p16, row_tiles, stream) : launch_plan<D, HI, 8>(a, p8, row_tiles, stream);
 }
 

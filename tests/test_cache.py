@@ -973,3 +973,51 @@ def test_write_of_a_few_heads(hccs, hq, hkv, d, rot, T):
         assert (back(vp) == orc.quantise(xs[:, hq + hkv:hq + 2 * hkv].astype(np.longdouble), [0.04] * hkv)).all()
     assert ctx.hccs_device_status() == 0
     ctx.close()
+
+
+def _sums_in_64_bits(q, k, v, theta, mult, shift):
+    """sum s V and Z of one head's queries q [rows, d] over keys k, v [n, d], exact integers in float64 on the GPU."""
+    import torch
+    acc = q.double() @ k.double().T
+    x = torch.floor((acc * float(mult) + 2.0 ** (shift - 1)) / 2.0 ** shift).clamp(-128, 127)
+    big, slope, reach = (float(c) for c in theta)
+    s = big - slope * (x.amax(1, keepdim=True) - x).clamp(max=reach)
+    return s @ v.double(), s.sum(1, keepdim=True)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("group", [9, 11, 12, 16, 17])
+@pytest.mark.parametrize("n", [81952, 100000, 131072])
+def test_large_head_groups_on_long_caches(hccs, d, group, n):
+    """Single tokens with more than eight query heads per kv head and many keys: against float64, which holds every sum exactly, and bit for
+    bit against the kernel for several tokens.  Short sequences under the same bound too."""
+    import torch
+    rng = np.random.default_rng(n + group)
+    page, shift = 64, 20
+    ctx = hccs.Context(0)
+    theta = _theta(rng, group, n, True)
+    ctx.hccs_params_upload_wide(theta, n)
+    g = torch.Generator(device="cuda").manual_seed(n + group)
+    per = -(-n // page)
+    kp, vp = (torch.randint(-128, 128, (per, 1, page, d), device="cuda", generator=g).to(torch.int8) for _ in range(2))
+    lens = [n, 300, n // 3, 1]
+    table = torch.stack([torch.randperm(per, device="cuda", generator=g) for _ in lens]).to(torch.int32)
+    Q = torch.randint(-128, 128, (len(lens), group, d), device="cuda", generator=g).to(torch.int8)
+    mult, scale = np.full(group, int(20 / (74.0 ** 2 * math.sqrt(d)) * (1 << shift)), np.int32), rng.uniform(0.01, 0.05, group).astype(np.float32)
+    start, kv = torch.arange(len(lens) + 1, dtype=torch.int32, device="cuda"), torch.tensor(lens, dtype=torch.int32, device="cuda")
+    got = []
+    for max_q in (1, 2):
+        out = torch.full((len(lens), group, d), 7.0, device="cuda")
+        ctx.hccs_attention_cached(Q, kp, vp, table, start, kv, out, mult, shift, max_q=max_q, max_kv=n, out_scale=scale, flags=hccs.HCCS_RECIP_REAL)
+        assert ctx.hccs_device_status() == 0
+        got.append(out)
+    assert torch.equal(*got)
+    for b, length in enumerate(lens):
+        pages = table[b, :-(-length // page)].long()
+        k, v = (p[pages, 0].reshape(-1, d)[:length] for p in (kp, vp))
+        for h in range(group):
+            num, z = _sums_in_64_bits(Q[b, h:h + 1], k, v, theta[h], mult[h], shift)
+            want = num / z * float(scale[h])
+            assert bool(((got[0][b, h].double() - want[0]).abs() <= 4 * 2.0 ** -24 * want[0].abs()).all()), (b, h)
+    ctx.close()
