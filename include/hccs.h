@@ -105,8 +105,11 @@ hccs_status_t hccs_destroy(hccs_ctx_t *ctx);
  * single int8 multiply-accumulate, so S is kept an int8 operand).  On a violation nothing is
  * uploaded and the previous table stays in force.
  * The table is copied from an internal pinned staging buffer on `cuda_stream`; `params` may be
- * reused as soon as the call returns.  The first upload (or one with more heads than before)
- * allocates device memory and therefore synchronises the device.
+ * reused as soon as the call returns.  The first upload makes room for 256 heads; it, and one with more
+ * heads than there is room for, allocates device memory and therefore synchronises the device.
+ * Uploads do not belong into a stream capture.  Captured launches read the table that is in force when they
+ * are replayed; one that is uploaded meanwhile has to have as many heads.  An upload that needs more room
+ * moves the table: graphs captured before it must not be replayed any more.
  */
 hccs_status_t hccs_params_upload(hccs_ctx_t *ctx, const hccs_head_params_t *params,
                                  int32_t num_heads, int32_t n_design, int32_t out_shift,
@@ -257,8 +260,10 @@ hccs_status_t hccs_calibrate(const int8_t *logits, int32_t B, int32_t H, int32_t
  * num_pages * Hkv is below 2^31.  A sequence is a row of a page
  * table: its token j lives in page table[j / page_size], at place j % page_size.  A slot is
  * page * page_size + place.  Codes stand for code * step with one step per head.  The pools, tables and
- * every workspace belong to the caller; nothing here allocates, copies from pageable memory or
- * synchronises, so all of it can be captured into a CUDA graph (host arrays are taken by value).
+ * every workspace belong to the caller.  hccs_cache_write, hccs_cache_read and hccs_attention_cached do not
+ * allocate, copy from pageable memory or synchronise, so they can be captured into a CUDA graph (host
+ * arrays are taken by value).  hccs_params_upload_wide allocates and synchronises like hccs_params_upload:
+ * it comes before a capture.  No upload that these calls can use moves the table that they read.
  * At most HCCS_MAX_CACHE_HEADS query heads and HCCS_MAX_CACHE_KEYS keys per sequence.
  */
 #define HCCS_MAX_CACHE_HEADS 256

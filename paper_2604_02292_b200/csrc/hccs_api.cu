@@ -104,7 +104,8 @@ hccs_status_t ensure_capacity(hccs_ctx *ctx, int32_t heads) {
     ctx->d_table = nullptr; ctx->h_table = nullptr; ctx->d_mult = nullptr; ctx->h_mult = nullptr;
     ctx->mult_last = nullptr; ctx->mult_last_heads = 0;
     ctx->capacity = 0;
-    int32_t cap = heads < 64 ? 64 : heads;
+    // room for every count of heads that the cache calls take, so that captured launches of theirs never lose their table
+    int32_t cap = heads < HCCS_MAX_CACHE_HEADS ? HCCS_MAX_CACHE_HEADS : heads;
     HCCS_CUDA(ctx, cudaMalloc(&ctx->d_table, sizeof(hccs::HeadEntry) * cap));
     HCCS_CUDA(ctx, cudaHostAlloc(&ctx->h_table, sizeof(hccs::HeadEntry) * cap, cudaHostAllocDefault));
     HCCS_CUDA(ctx, cudaMalloc(&ctx->d_mult, sizeof(int32_t) * 8 * cap));

@@ -1021,3 +1021,33 @@ def test_large_head_groups_on_long_caches(hccs, d, group, n):
             want = num / z * float(scale[h])
             assert bool(((got[0][b, h].double() - want[0]).abs() <= 4 * 2.0 ** -24 * want[0].abs()).all()), (b, h)
     ctx.close()
+
+
+@pytest.mark.gpu
+def test_captured_calls_outlive_larger_tables(hccs):
+    """Uploads of up to 256 heads leave the table where captured launches look for it."""
+    import torch
+    rng = np.random.default_rng(41)
+    ctx = hccs.Context(0)
+    runs = []
+    theta = _theta(rng, 4, 300, False)
+    for q_lens in ([1, 1], [5, 2]):
+        out, _, (args, kw, _) = attend(hccs, ctx, rng, q_lens, [300, 40], 4, 2, 64, 16, "real", "f32", n_design=300, theta=theta)
+        runs.append((args, kw, out, out.clone()))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for args, kw, _, _ in runs:
+            ctx.hccs_attention_cached(*args, **kw)
+    for heads in (65, 128, 256):
+        ctx.hccs_params_upload_wide([(16000, 1, 127)] * heads, 300)
+        ctx.hccs_params_upload([(109, 0, 1)] * heads, 300)
+    filler = [torch.full((n,), -1, dtype=torch.int32, device="cuda") for n in (256, 1024, 4096)]     # takes what was given back
+    ctx.hccs_params_upload(theta, 300)
+    for _, _, out, want in runs:
+        out.fill_(77)
+    graph.replay()
+    torch.cuda.synchronize()
+    for _, _, out, want in runs:
+        assert torch.equal(out, want)
+    assert ctx.hccs_device_status() == 0 and all((t == -1).all() for t in filler)
+    ctx.close()
