@@ -457,13 +457,13 @@ class Context:
         if t.get_device() != self.device:
             raise ValueError(f"{name} must live on cuda:{self.device}, not {t.device}")
         _check_tensor(t, name, itemsize, shape)
-        if not _I8:
-            import torch
+        if t.dtype not in _WHOLE[itemsize]:
+            import torch                       # whoever misses a type fills the sets before it judges: threads do not wait for each other
             _I8.update((torch.int8, torch.uint8))
             _I32.update((torch.int32, torch.uint32))
             _I64.update((torch.int64, torch.uint64))
-        if t.dtype not in _WHOLE[itemsize]:
-            raise ValueError(f"{name} must hold integers, not {t.dtype}")
+            if t.dtype not in _WHOLE[itemsize]:
+                raise ValueError(f"{name} must hold integers, not {t.dtype}")
 
     def _check(self, t, name, itemsize, shape=None) -> int:
         """The address of a tensor of integers of the context's device that passes."""

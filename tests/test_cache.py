@@ -1051,3 +1051,75 @@ def test_captured_calls_outlive_larger_tables(hccs):
         assert torch.equal(out, want)
     assert ctx.hccs_device_status() == 0 and all((t == -1).all() for t in filler)
     ctx.close()
+
+
+def test_first_calls_of_two_threads(binding):
+    """The table of integer types is filled on first use: whatever line of that another thread's first call falls on, a right tensor passes.
+    For each line of the first look at a tensor, a fresh process in which a second thread makes the same look just before that line."""
+    import subprocess
+    import sys
+    code = """
+import os, sys, threading
+import torch
+from paper_2604_02292_b200 import binding as b
+
+class Fake:                                  # what the binding asks of a tensor on the context's device
+    device = torch.device("cuda", 0)
+    shape = (4,)
+    def __init__(self, dtype): self.dtype = dtype
+    def get_device(self): return 0
+    def is_contiguous(self): return True
+    def element_size(self): return self.dtype.itemsize
+    def data_ptr(self): return 4096
+
+ctx = b.Context.__new__(b.Context)
+ctx._h, ctx.device = None, 0
+failed = []
+def look():
+    for dtype in (torch.int8, torch.int32, torch.int64):
+        try:
+            ctx._check(Fake(dtype), "t", dtype.itemsize, (4,))
+        except ValueError as e:
+            failed.append(str(e))
+def first_look(line):
+    threads, seen = [], [0]
+    def trace(frame, event, arg):
+        if not frame.f_code.co_filename.endswith("binding.py"):
+            return None
+        if event == "line":
+            if seen[0] == line:
+                threads.append(threading.Thread(target=look))
+                threads[0].start()
+                threads[0].join(0.1)         # (it may have to wait for this thread)
+            seen[0] += 1
+        return trace
+    sys.settrace(trace)
+    look()
+    sys.settrace(None)
+    for t in threads:
+        t.join()
+    return 1 if failed else 0 if threads else 2
+line = 0
+while True:
+    child = os.fork()
+    if child == 0:
+        os._exit(first_look(line))
+    result = os.waitstatus_to_exitcode(os.waitpid(child, 0)[1])
+    if result == 2:
+        break
+    assert result == 0, f"a look before line {line} of the first one was refused"
+    line += 1
+assert line > 0
+for dtype, size in ((torch.float32, 4), (torch.bool, 1), (torch.float64, 8)):
+    try:
+        ctx._check(Fake(dtype), "t", size, (4,))
+    except ValueError as e:
+        assert "integers" in str(e)
+    else:
+        raise AssertionError(dtype)
+print("passed")
+"""
+    import os
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    done = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=240)
+    assert done.returncode == 0 and "passed" in done.stdout, done.stderr[-2000:]
