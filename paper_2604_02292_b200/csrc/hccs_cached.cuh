@@ -70,18 +70,23 @@ __device__ __forceinline__ uint32_t requant_top(const Requant &q, int acc) {
 }
 
 // One output value from num = sum s V and the row's Z (0: the row sees nothing): the integer of the int16
-// path, or its product with the scale, or num * (scale / Z); each step rounded once to fp32.
+// path, or its product with the scale, or num * (scale / Z); each step rounded once to fp32.  Scales below 2^-60 are divided
+// 2^64 times as large, since with Z up to 2^32 the quotient would lose bits below the normal range.
 struct RowFactor {
     float scale;       // real: scale / Z; integer modes: the scale
+    float unit;        // real: 1, or 2^-64 for a scale that was taken 2^64 times as large
     int rho;           // integer modes
 };
 __device__ __forceinline__ RowFactor row_factor(const CachedAttnArgs &a, int64_t Z, float scale) {
     RowFactor f;
     f.rho = 0;
     f.scale = 0.0f;
+    f.unit = 1.0f;
     if (Z > 0) {
         if (a.recip == HCCS_RECIP_REAL) {
-            f.scale = scale / (float)Z;
+            const bool tiny = fabsf(scale) < 0x1p-60f;
+            f.scale = (tiny ? scale * 0x1p64f : scale) / (float)Z;
+            f.unit = tiny ? 0x1p-64f : 1.0f;
         } else {
             f.rho = (int)(a.recip == HCCS_RECIP_CLB ? reciprocal<true, true>((uint32_t)Z) : reciprocal<true, false>((uint32_t)Z));
             f.scale = scale;
@@ -97,7 +102,7 @@ __device__ __forceinline__ uint4 output4(const CachedAttnArgs &a, const int64_t 
     for (int e = 0; e < 4; ++e) {
         if (a.recip == HCCS_RECIP_REAL) {
             o[e] = 0;
-            y[e] = (float)num[e] * f.scale;
+            y[e] = (float)num[e] * f.scale * f.unit;
         } else {
             o[e] = (int)num[e] * f.rho;
             y[e] = (float)o[e] * f.scale;

@@ -1123,3 +1123,24 @@ print("passed")
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     done = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=240)
     assert done.returncode == 0 and "passed" in done.stdout, done.stderr[-2000:]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("q_len", [1, 4])
+def test_scales_of_any_size(hccs, q_len):
+    """The real quotient with scales down to the smallest float, and sums Z of 2^26: num and Z to fp32, their quotient with the scale and the
+    product round by 2^-24 each; what is subnormal is off by half of its step, 2^-150, besides."""
+    rng = np.random.default_rng(51)
+    ctx = hccs.Context(0)
+    scales = np.array([0.03, 1e-28, -1e-33, 1e-36, 1.1754944e-38, -3e-39, 7e-43, 2.0 ** -149, 2e36, 2.0 ** -60, 2.0 ** -61, 0.0], np.float32)
+    hq, n = len(scales), 3001
+    theta = np.array([(32767 - 9 * h, int(rng.integers(1, 128)), int(rng.integers(1, 128))) for h in range(hq)], np.int32)
+    out, c, (args, kw, _) = attend(hccs, ctx, rng, [q_len], [n], hq, 2, 64, 16, "real", "f32", wide=True, theta=theta, check=False)
+    ctx.hccs_attention_cached(*args, **{**kw, "out_scale": scales})
+    assert ctx.hccs_device_status() == 0
+    num, zs, cnt = orc.attend(args[0][:q_len].cpu().numpy(), c.k, c.v, c.table, [0, q_len], [n], theta, args[7], args[8])
+    assert zs.max() > 2 ** 26
+    want = num / zs[..., None] * scales.astype(np.float64)[None, :, None]
+    off = np.abs(_values(out[:q_len]) - want) - (4.01 * 2.0 ** -24 * np.abs(want) + 2.0 ** -150)
+    assert (off <= 0).all(), [(float(scales[h]), float(off[:, h].max())) for h in range(hq) if off[:, h].max() > 0]
+    ctx.close()
