@@ -441,6 +441,8 @@ class Context:
             words = tree_mask.shape[-1]
             if tree_mask.get_device() != dev or tree_mask.dtype not in _I32 or tree_mask.shape != (T, words) or not tree_mask.is_contiguous():
                 self._explain(tree_mask, "tree_mask", 4, (T, words))
+            if words < 1:                      # (an empty tensor has no address, and none means causal)
+                raise ValueError("tree_mask must have a word or more per token")
             treep = tree_mask.data_ptr()
         st = _lib.hccs_attention_cached(
             self._h, Q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(), q_start.data_ptr(), kv_len.data_ptr(),

@@ -1144,3 +1144,20 @@ def test_scales_of_any_size(hccs, q_len):
     off = np.abs(_values(out[:q_len]) - want) - (4.01 * 2.0 ** -24 * np.abs(want) + 2.0 ** -150)
     assert (off <= 0).all(), [(float(scales[h]), float(off[:, h].max())) for h in range(hq) if off[:, h].max() > 0]
     ctx.close()
+
+
+@pytest.mark.gpu
+def test_a_tree_mask_without_words_is_refused(hccs):
+    """An empty tensor has no address: it must not pass for no mask, which means causal."""
+    import torch
+    ctx = hccs.Context(0)
+    rng = np.random.default_rng(61)
+    for q_len in (1, 3):
+        out, _, (args, kw, _) = attend(hccs, ctx, rng, [q_len], [40], 2, 1, 64, 16, "div", "i32")
+        out.fill_(77)
+        before = ctx.hccs_launch_count()
+        with pytest.raises(ValueError, match="tree_mask"):
+            ctx.hccs_attention_cached(*args, **{**kw, "tree_mask": torch.empty((out.shape[0], 0), dtype=torch.int32, device="cuda")})
+        torch.cuda.synchronize()
+        assert ctx.hccs_launch_count() == before and (out == 77).all()
+    ctx.close()
