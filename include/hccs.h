@@ -331,7 +331,7 @@ hccs_status_t hccs_cache_write(hccs_ctx_t *ctx, const void *q, const void *k, co
 
 /*
  * Reads sequences back: token j of sequence b goes to row out_start[b] + j of the outputs.
- *   page_table   device int32 [B, max_pages]
+ *   page_table   device int32 [B, max_pages]; may be NULL where max_pages is 0
  *   out_start    device int32 [B+1], not falling; sequence b has out_start[b+1] - out_start[b] tokens, at
  *                most max_len (host) and max_pages * page_size of which are read; more is reported, and so
  *                is a page outside 0..num_pages-1, whose rows become zeros
@@ -368,7 +368,7 @@ hccs_status_t hccs_params_upload_wide(hccs_ctx_t *ctx, const hccs_head_params_t 
  * tree_mask, those whose bit is set: bit j % 32 of word j / 32 of row i for the j-th new key of the
  * sequence (a tree of drafted tokens: itself and its ancestors).  A query that sees no key gives zeros.
  *   Q            device int8 [T, Hq, d], 16-byte aligned
- *   page_table   device int32 [B, max_pages];  q_start  device int32 [B+1], not falling;  kv_len  device int32 [B]
+ *   page_table   device int32 [B, max_pages] (may be NULL where max_pages is 0);  q_start  device int32 [B+1], not falling;  kv_len  device int32 [B]
  *   tree_mask    device int32 [T, tree_words], or NULL
  *   requant_mult HOST int32 [Hq], each in [0, 2^13) and below 2^(shift-1) (HCCS_ERR_UNSUPPORTED beyond);
  *                requant_shift in 1..24

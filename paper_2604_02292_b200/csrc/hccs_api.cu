@@ -634,7 +634,7 @@ hccs_status_t hccs_cache_read(hccs_ctx_t *ctx, const int8_t *k_pages, const int8
     if ((k_out && (!k_pages || !steps_ok(k_step, Hkv))) || (v_out && (!v_pages || !steps_ok(v_step, Hkv)))) return HCCS_ERR_INVALID_ARG;
     if (B > 65535) return HCCS_ERR_UNSUPPORTED;
     if (B == 0 || max_len == 0 || rows == 0 || (!k_out && !v_out)) return ctx ? HCCS_OK : HCCS_ERR_INVALID_ARG;
-    if (!page_table || !out_start) return HCCS_ERR_INVALID_ARG;
+    if ((!page_table && max_pages > 0) || !out_start) return HCCS_ERR_INVALID_ARG;
     if (!aligned16(k_pages) || !aligned16(v_pages) || !aligned16(k_out) || !aligned16(v_out)) return HCCS_ERR_UNSUPPORTED;
     if (!ctx) return HCCS_ERR_INVALID_ARG;
     DeviceGuard g(ctx->device);
@@ -681,7 +681,7 @@ hccs_status_t hccs_attention_cached(hccs_ctx_t *ctx, const int8_t *Q, const int8
             if (!isfinite(out_scale[h])) return HCCS_ERR_INVALID_ARG;
     if (tree_mask && (tree_words < 1 || (int64_t)tree_words * 32 < max_q)) return HCCS_ERR_INVALID_ARG;
     const bool empty = T == 0 || B == 0 || max_q == 0;
-    if (!empty && (!Q || !k_pages || !v_pages || !page_table || !q_start || !kv_len || !O)) return HCCS_ERR_INVALID_ARG;
+    if (!empty && (!Q || !k_pages || !v_pages || (!page_table && max_pages > 0) || !q_start || !kv_len || !O)) return HCCS_ERR_INVALID_ARG;
     if (!aligned16(Q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(O)) return HCCS_ERR_UNSUPPORTED;
     if (!ctx) return HCCS_ERR_INVALID_ARG;
     if (ctx->num_heads == 0) return HCCS_ERR_NOT_UPLOADED;

@@ -1161,3 +1161,26 @@ def test_a_tree_mask_without_words_is_refused(hccs):
         torch.cuda.synchronize()
         assert ctx.hccs_launch_count() == before and (out == 77).all()
     ctx.close()
+
+
+@pytest.mark.gpu
+def test_page_tables_without_pages(hccs):
+    """max_pages of zero, whose table has no address: sequences without keys, and lengths that are cut to none."""
+    import torch
+    ctx = hccs.Context(0)
+    ctx.hccs_params_upload([(300, 3, 85)] * 4, 64)
+    pool = torch.full((2, 2, 16, 64), 5, dtype=torch.int8, device="cuda")
+    table = torch.empty((2, 0), dtype=torch.int32, device="cuda")
+    for nq in (1, 3):
+        Q = torch.ones((2 * nq, 4, 64), dtype=torch.int8, device="cuda")
+        start = torch.tensor([0, nq, 2 * nq], dtype=torch.int32, device="cuda")
+        for length, word in ((0, 0), (9, 16)):
+            kv = torch.full((2,), length, dtype=torch.int32, device="cuda")
+            out = torch.full((2 * nq, 4, 64), 7, dtype=torch.int32, device="cuda")
+            ctx.hccs_attention_cached(Q, pool, pool, table, start, kv, out, [100] * 4, 20, max_q=nq, max_kv=64)
+            assert ctx.hccs_device_status() == word and not out.any()
+    for starts, word in (([0, 0, 0], 0), ([0, 2, 5], 16)):
+        back = [torch.full((6, 2, 64), 7.0, device="cuda") for _ in range(2)]
+        ctx.hccs_cache_read(pool, pool, table, torch.tensor(starts, dtype=torch.int32, device="cuda"), *back, [0.1] * 2, [0.1] * 2, 16)
+        assert ctx.hccs_device_status() == word and all((t == 7).all() for t in back)
+    ctx.close()
