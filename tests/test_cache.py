@@ -1184,3 +1184,85 @@ def test_page_tables_without_pages(hccs):
         ctx.hccs_cache_read(pool, pool, table, torch.tensor(starts, dtype=torch.int32, device="cuda"), *back, [0.1] * 2, [0.1] * 2, 16)
         assert ctx.hccs_device_status() == word and all((t == 7).all() for t in back)
     ctx.close()
+
+
+def _attend_seen(q, c, row, theta, mult, shift, seen):
+    """As the oracle, for one sequence and any pattern: seen [queries, keys]."""
+    k, v = (orc.sequence(p, c.table[row], seen.shape[1]).astype(np.int64) for p in (c.k, c.v))
+    T, hq, d = q.shape
+    num, zs, cnt = np.zeros((T, hq, d), np.int64), np.zeros((T, hq), np.int64), np.zeros((T, hq), np.int64)
+    for t in range(T):
+        w = seen[t]
+        if not w.any():
+            continue
+        for h in range(hq):
+            kh = h // (hq // k.shape[1])
+            x = np.clip((k[w, kh] @ q[t, h].astype(np.int64) * int(mult[h]) + (1 << (shift - 1))) >> shift, -128, 127)
+            s = theta[h][0] - theta[h][1] * np.minimum(x.max() - x, theta[h][2])
+            num[t, h], zs[t, h], cnt[t, h] = s @ v[w, kh], s.sum(), w.sum()
+    return num, zs, cnt
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("q_len", [1, 5, 40])
+@pytest.mark.parametrize("tree", [False, True])
+def test_bounds_below_the_lengths(hccs, d, q_len, tree):
+    """max_kv and max_q below what the sequence has: what is cut is not seen and not computed, the rest is as ever, and both are reported."""
+    import torch
+    rng = np.random.default_rng(71)
+    ctx = hccs.Context(0)
+    n = 700
+    mask = None
+    if tree:                                               # any bits, those of nodes beyond the bounds among them
+        mask = rng.integers(0, 2 ** 32, (q_len, 2), dtype=np.uint64).astype(np.uint32).view(np.int32)
+    out, c, (args, kw, theta) = attend(hccs, ctx, rng, [q_len], [n], 4, 2, d, 16, "div", "i32", n_design=n, tree=mask)
+    q = args[0][:q_len].cpu().numpy()
+
+    def check(max_q, max_kv):
+        rows = min(q_len, max_q)
+        seen = np.zeros((rows, n), bool)
+        for t in range(rows):
+            for j in range(min(n, max_kv)):
+                new = j - (n - q_len)
+                seen[t, j] = new < 0 or (new <= t if mask is None else new < max_q and bool((int(mask[t, new // 32]) >> (new % 32)) & 1))
+        out.fill_(77)
+        ctx.hccs_attention_cached(*args, **{**kw, "max_q": max_q, "max_kv": max_kv})
+        assert ctx.hccs_device_status() == (16 if max_kv < n or max_q < q_len else 0), (max_q, max_kv)
+        compare(out[:rows], *_attend_seen(q[:rows], c, 0, theta, args[7], args[8], seen), "div", "i32", None)
+        assert (out[rows:] == 77).all()
+    for max_kv in (0, 1, 16, 127, 128, 129, 500, n - q_len, n - 1, n):
+        check(q_len, max_kv)
+    for max_q in (1, 2, 4, 31, 32, 33):
+        if max_q < q_len:
+            check(max_q, n)
+            check(max_q, n - q_len + 1)
+    ctx.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("max_q", [1, 4])
+def test_starts_that_fall_or_leave_the_tokens(hccs, max_q):
+    """q_start is cut to the tokens; a sequence whose start lies behind its end has none."""
+    import torch
+    rng = np.random.default_rng(81)
+    ctx = hccs.Context(0)
+    T, lens = 8, [50, 40, 30, 20]
+    out, c, (args, kw, theta) = attend(hccs, ctx, rng, [2] * 4, lens, 4, 2, 64, 16, "real", "f32")
+    for starts, owners in (([5, 3, 6, 99, 99], {1: (3, 6), 2: (6, 8)}), ([-9, 2, 2, 7, 2 ** 31 - 1], {0: (0, 2), 2: (2, 7), 3: (7, 8)}),
+                           ([-2 ** 31, -1, 0, 1, 0], {2: (0, 1)})):
+        big = torch.full((T + 6, 4, 64), 77.0, device="cuda")
+        o = big[3:3 + T]
+        a = list(args)
+        a[0], a[4], a[6] = args[0][:T], torch.tensor(starts, dtype=torch.int32, device="cuda"), o
+        ctx.hccs_attention_cached(*a, **{**kw, "max_q": max_q})
+        ctx.hccs_device_status()
+        done = np.zeros(T, bool)
+        for b, (s0, s1) in owners.items():
+            rows = min(s1 - s0, max_q)
+            seen = np.arange(lens[b])[None, :] <= (lens[b] - (s1 - s0)) + np.arange(rows)[:, None]
+            sums = _attend_seen(args[0][s0:s0 + rows].cpu().numpy(), c, b, theta, args[7], args[8], seen)
+            compare(o[s0:s0 + rows], *sums, "real", "f32", kw["out_scale"])
+            done[s0:s0 + rows] = True
+        assert (o[torch.from_numpy(~done).cuda()] == 77).all() and (big[:3] == 77).all() and (big[3 + T:] == 77).all()
+    ctx.close()
