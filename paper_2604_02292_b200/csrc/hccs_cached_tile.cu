@@ -50,7 +50,7 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatil
 }
 
 constexpr int kRowThreads = 512;
-constexpr int kCopyWarp = 16, kCopyWarps = 2, kQkWarp = 18, kPvWarp = 19;
+constexpr int kCopyWarp = 16, kCopyWarps = 2, kQkWarp = 18, kPvWarp = kQkWarp + 1;
 constexpr int kThreads = 640;                    // 20 warps: 96 registers a thread
 constexpr int kTile = 128;
 constexpr int kPanelBytes = kTile * 128;         // 128 rows x 128 keys, 128-byte swizzle
@@ -292,11 +292,6 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
                     }
                     __syncwarp();
                 }
-            }
-            if (!ok) {
-                if (elect_one()) tcgen05_commit(smem_u32(&bars.drained[me]));
-                __syncwarp();
-                mbar_wait_bounded(smem_u32(&bars.drained[me]), 0, a.wait_cycles);
             }
         }
         __syncwarp();
@@ -591,6 +586,17 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
     }
     tcgen05_fence_before();
     __syncthreads();
+    if (*abortp) {
+        // Some wait has run out, so the products may not all have been waited for; neither tensor memory nor shared memory goes
+        // before they are through (again with a limit).  Nobody waits any more: the flag is the same for all.
+        if (warp == kQkWarp || warp == kPvWarp) {
+            uint64_t *const bar = &bars.drained[warp - kQkWarp];
+            if (elect_one()) tcgen05_commit(smem_u32(bar));
+            __syncwarp();
+            mbar_wait_bounded(smem_u32(bar), 0, a.wait_cycles);
+        }
+        __syncthreads();
+    }
     if (warp == kPvWarp) {
         tcgen05_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
