@@ -375,7 +375,8 @@ hccs_status_t hccs_params_upload_wide(hccs_ctx_t *ctx, const hccs_head_params_t 
  *   out_scale    HOST float [Hq]; NULL for HCCS_I32 output, whose O is the exact integer
  *   O            device [T, Hq, d] of out_type; float types hold the fp32 product with out_scale[h], rounded
  *                once more to the type; HCCS_I32 goes with DIV and CLB only.  16-byte aligned
- *   max_q, max_kv (host)  bounds of the lengths of this call, which choose kernel and grid: queries beyond
+ *   max_q, max_kv (host)  bounds of the lengths of this call, which choose kernel and grid for all its
+ *                sequences (chunks and single tokens are faster in calls of their own): queries beyond
  *                max_q are not computed (nor are their keys seen by a tree), and keys beyond max_kv are not seen, both reported.  max_kv beyond
  *                n_design is HCCS_ERR_CONSTRAINT, beyond HCCS_MAX_CACHE_KEYS HCCS_ERR_UNSUPPORTED
  *   flags        one HCCS_RECIP_*; nothing else
@@ -394,7 +395,8 @@ hccs_status_t hccs_attention_cached(hccs_ctx_t *ctx, const int8_t *Q, const int8
 /* Reads (and clears) the device status word: 0 = no kernel gave up a bounded wait or met an index out of
  * range.  Synchronises `cuda_stream`.  Returns HCCS_ERR_DEVICE_TIMEOUT when a wait was given up (bits 0
  * and 1), else HCCS_ERR_DEVICE_INDEX when the word was non-zero (bit 2: slot, bit 3: page, bit 4: length);
- * *word (may be NULL) receives it. */
+ * *word (may be NULL) receives it.  A launch that gave up a wait leaves its output incomplete: some rows as
+ * they were, some from part of their sums; none of it is to be used. */
 hccs_status_t hccs_device_status(hccs_ctx_t *ctx, uint32_t *word, void *cuda_stream);
 
 /*

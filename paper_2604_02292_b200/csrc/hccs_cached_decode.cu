@@ -4,7 +4,9 @@
 // Bound: HBM.  Every key and value code is read once, 2*D bytes per key and kv head; a code takes part in at most
 // 16 multiply-adds, which mma.sync (m16n8k32, int8) does while the loads are in flight.  64 sequences of 8192 keys (32
 // query heads on 8 of 128): 162 us, 6.6 TB/s; 32 of 4096: 45 us, 6.0 TB/s.  One sequence of 131072 keys (8 kv heads):
-// 61 us, 4.4 TB/s, on 128 CTAs, as a cluster has sixteen at most and the two passes need all of a row's maxima.
+// 60 us, 4.5 TB/s, on 80 CTAs of sixteen warps: the two passes need all of a row's maxima, so a kv head has one cluster,
+// and of clusters of more than ten CTAs the device does not hold eight at a time.  Groups of more than 16 query heads read
+// the codes once per 16: 64 sequences of 8192 keys, one kv head, 16, 32, 64, 128 query heads: 36, 63, 120, 211 us.
 //
 // Two passes, because the clamp of the distance needs the row maximum first: over K (the logits stay in shared
 // memory, one byte each), then over V.  A warp takes tiles of 32 keys; the order of the keys inside a tile is
@@ -447,8 +449,9 @@ struct Plan { int split, per_warp; double cost; };      // cost: infinite where 
 // What a launch with W warps per CTA and clusters of `s` costs, in microseconds: waves of clusters, each the time of a CTA's
 // share of a kv head's codes at a CTA's rate (measured 42 GB/s with eight warps, 53 with sixteen or for two CTAs of eight on one
 // SM, as long as the wave's CTAs do not ask for more than the 6.4 TB/s of the memory) plus about 4.5 us for the chain of loads at the start, the exchanges and the join.  Measured, 256 kv
-// heads x 4096 keys: s = 1, 2, 4: 44, 53, 66 us (the formula: 46, 57, 65); 8 kv heads x 131072 keys, eight warps, s = 16 (seven
-// clusters at a time): 102; 512 x 8192: sixteen warps, s = 1: 174; eight warps, s = 1, 2, 4: 198, 181, 205.
+// heads x 4096 keys: s = 1, 2, 4: 44, 53, 66 us (the formula: 46, 59, 71); 8 kv heads x 131072 keys: eight warps, s = 8, 10, 16: 100,
+// 81, 72 (106, 86, 86), sixteen warps, s = 8, 9, 10, 11: 71, 65, 60, 108 (85, 76, 69, 127; from eleven on the device holds seven
+// clusters at a time); 512 x 8192: sixteen warps, s = 1: 174; eight warps, s = 1, 2, 4: 198, 181, 205 (210; 203, 213, 223).
 template <int D, bool HI, int W>
 cudaError_t plan_for(const CachedAttnArgs &a, int64_t groups, Plan &best) {
     using S = Sizes<D, HI, W>;

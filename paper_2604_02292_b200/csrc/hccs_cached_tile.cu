@@ -22,8 +22,8 @@
 //
 // Bound: the chain of a block, tensor product -> tensor memory -> registers -> r -> tensor product, in turns of two
 // groups: tensor pipe and integer pipe are both half busy.  2048 new tokens on each of two caches of 8192 keys (16 query
-// heads on 4 of 128): 179 us, 0.40 of the int8 rate counting the formula's two products; 8 trees of 48 on
-// 8000 keys (32 heads on 8): 53 us.  Tried and slower or no faster: r (and Q) as operands in tensor memory (185 us), a
+// heads on 4 of 128), the caches in L2: 180 us, 0.40 of the int8 rate counting the formula's two products (inputs and caches
+// new to L2: 196, 0.37); 8 trees of 48 on 8000 keys (32 heads on 8): 53 us.  Tried and slower or no faster: r (and Q) as operands in tensor memory (185 us), a
 // third S buffer in the second pass (208), four groups (222), 64 columns per tensor-memory load (191), all sequences' longest
 // tiles first (185; with caches beyond L2 up to half slower), one issuer for both products (263).
 //

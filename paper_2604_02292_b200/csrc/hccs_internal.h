@@ -41,7 +41,7 @@ struct RowArgs {
 // Bits of the device status word.
 enum : uint32_t {
     STATUS_ROW_TMA_TIMEOUT = 1u,     // CTA-per-row kernel: a bulk copy never completed
-    STATUS_FUSED_TIMEOUT = 2u,       // fused kernel: an mbarrier wait gave up
+    STATUS_FUSED_TIMEOUT = 2u,       // fused kernel and the cached attention kernels: an mbarrier wait gave up
     STATUS_BAD_SLOT = 4u,            // cache write: a slot beyond the pools
     STATUS_BAD_PAGE = 8u,            // cache read and cached attention: a page outside the pools
     STATUS_BAD_LENGTH = 16u,         // cache read and cached attention: a length beyond its bound
