@@ -109,7 +109,8 @@ hccs_status_t hccs_destroy(hccs_ctx_t *ctx);
  * heads than there is room for, allocates device memory and therefore synchronises the device.
  * Uploads do not belong into a stream capture.  Captured launches read the table that is in force when they
  * are replayed; one that is uploaded meanwhile has to have as many heads.  An upload that needs more room
- * moves the table: graphs captured before it must not be replayed any more.
+ * moves the table: graphs captured before it must not be replayed any more.  Should that allocation
+ * fail, the context has no table (HCCS_ERR_NOT_UPLOADED) until an upload succeeds.
  */
 hccs_status_t hccs_params_upload(hccs_ctx_t *ctx, const hccs_head_params_t *params,
                                  int32_t num_heads, int32_t n_design, int32_t out_shift,

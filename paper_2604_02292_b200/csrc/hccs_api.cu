@@ -104,6 +104,7 @@ hccs_status_t ensure_capacity(hccs_ctx *ctx, int32_t heads) {
     ctx->d_table = nullptr; ctx->h_table = nullptr; ctx->d_mult = nullptr; ctx->h_mult = nullptr;
     ctx->mult_last = nullptr; ctx->mult_last_heads = 0;
     ctx->capacity = 0;
+    ctx->num_heads = 0;                     // should an allocation fail, no call launches without a table
     // room for every count of heads that the cache calls take, so that captured launches of theirs never lose their table
     int32_t cap = heads < HCCS_MAX_CACHE_HEADS ? HCCS_MAX_CACHE_HEADS : heads;
     HCCS_CUDA(ctx, cudaMalloc(&ctx->d_table, sizeof(hccs::HeadEntry) * cap));
