@@ -25,8 +25,8 @@
  *   - Errors are return codes only.  On any error nothing is launched.
  *   - A context is not thread-safe: one host call at a time per context (different contexts, also
  *     on the same device, are independent).  On the GPU, hccs_forward, hccs_forward_keylen,
- *     hccs_forward_host and hccs_attention_cached calls of one context only read the context's parameter
- *     table (hccs_cache_write and hccs_cache_read not even that) and may overlap each other freely
+ *     hccs_forward_host, hccs_attention_cached and hccs_attention_cross calls of one context only read the context's parameter
+ *     table (hccs_cache_write, hccs_cache_write_axes, hccs_states_write and hccs_cache_read not even that) and may overlap each other freely
  *     (different streams, back to back on one stream).  Calls that rewrite device memory the context
  *     owns do so on their own `cuda_stream`: hccs_params_upload and hccs_params_upload_wide (the
  *     parameter table) and the hccs_attention_fused* calls (a small per-head multiplier table,
@@ -73,7 +73,7 @@ enum {
     HCCS_CAUSAL    = 4    /* key j of query i takes part iff j <= i + (Lk - Lq); others give 0  */
 };
 
-/* a further reciprocal, of hccs_attention_cached only: the scores are divided by their sum as real numbers */
+/* a further reciprocal, of hccs_attention_cached and hccs_attention_cross only: the scores are divided by their sum as real numbers */
 enum { HCCS_RECIP_REAL = 8 };
 
 /* element types of the cache entry points */
@@ -261,7 +261,7 @@ hccs_status_t hccs_calibrate(const int8_t *logits, int32_t B, int32_t H, int32_t
  * num_pages * Hkv is below 2^31.  A sequence is a row of a page
  * table: its token j lives in page table[j / page_size], at place j % page_size.  A slot is
  * page * page_size + place.  Codes stand for code * step with one step per head.  The pools, tables and
- * every workspace belong to the caller.  hccs_cache_write, hccs_cache_read and hccs_attention_cached do not
+ * every workspace belong to the caller.  hccs_cache_write, hccs_cache_write_axes, hccs_states_write, hccs_cache_read and hccs_attention_cached do not
  * allocate, copy from pageable memory or synchronise, so they can be captured into a CUDA graph (host
  * arrays are taken by value).  hccs_params_upload_wide allocates and synchronises like hccs_params_upload:
  * it comes before a capture.  No upload that these calls can use moves the table that they read.
@@ -330,6 +330,57 @@ hccs_status_t hccs_cache_write(hccs_ctx_t *ctx, const void *q, const void *k, co
                                int32_t T, int32_t Hq, int32_t Hkv, int32_t d,
                                int32_t num_pages, int32_t page_size, void *cuda_stream);
 
+/* Rotary positions with several axes (time, rows and columns of a video, rows and columns of an image): pair i turns
+ * by positions of axis[i] alone, t = position[axis[i]] * freq[i]; the rest as in hccs_rope_t. */
+#define HCCS_MAX_AXES 4
+typedef struct {
+    hccs_rope_t rope;
+    int32_t num_axes;                         /* 1..HCCS_MAX_AXES */
+    uint8_t axis[HCCS_MAX_ROT_DIM / 2];       /* of each pair, below num_axes */
+} hccs_rope_axes_t;
+
+/* How the pairs are dealt out: the first pairs[0] of them to axis 0, the next pairs[1] to axis 1, and so on; or
+ * one to each axis in turn, axes that have theirs being left out. */
+enum { HCCS_AXES_SECTIONS = 0, HCCS_AXES_TURNS = 1 };
+
+/* Fills *axes (host only, no CUDA call).  pairs[x] >= 0 is the number of pairs of axis x; they sum to rot_dim / 2.
+ * Frequencies are those of hccs_rope_frequencies for rot_dim, or, with `restart`, each axis has those for its own
+ * 2 * pairs[x] dims, from the fastest on.  HCCS_ERR_INVALID_ARG as there, for a NULL axes or pairs, num_axes outside
+ * 1..HCCS_MAX_AXES, an order that is none, or pairs that do not sum up. */
+hccs_status_t hccs_rope_axes(hccs_rope_axes_t *axes, int32_t rot_dim, int32_t interleaved, double base,
+                             const hccs_rope_scaling_t *scaling, const int32_t *pairs, int32_t num_axes,
+                             int32_t order, int32_t restart);
+
+/*
+ * hccs_cache_write with positions of several axes: that of token t on axis x is
+ * positions[x*axis_stride + t*token_stride] (device int32, any values; strides in elements, of any sign).  `axes` is a
+ * HOST pointer or NULL for no rotation.  All else as there.
+ */
+hccs_status_t hccs_cache_write_axes(hccs_ctx_t *ctx, const void *q, const void *k, const void *v, hccs_type_t type,
+                                    int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                                    const int32_t *positions, int64_t axis_stride, int64_t token_stride,
+                                    const int64_t *slots, const hccs_rope_axes_t *axes,
+                                    const float *q_step, const float *k_step, const float *v_step,
+                                    int8_t *q8, int8_t *k_pages, int8_t *v_pages,
+                                    int32_t T, int32_t Hq, int32_t Hkv, int32_t d,
+                                    int32_t num_pages, int32_t page_size, void *cuda_stream);
+
+/*
+ * The same into dense tensors, for states that are no cache: an encoder's own (hccs_attention_fused reads
+ * [B, H, L, d]) or those that a decoder looks at (hccs_attention_cross reads [T, Hkv, d]).
+ *   q8, k8, v8   device int8 [T/L, Hq | Hkv, L, d]: token t is number t % L of entry t / L.  L = 1 makes it [T, Hq | Hkv, d].
+ *                L in 1..T divides T (HCCS_ERR_INVALID_ARG otherwise).  16-byte aligned
+ * q may be NULL (with q8 and q_step; Hq is then ignored), or both k and v.  Codes, types, strides, positions and steps as in
+ * hccs_cache_write_axes.
+ */
+hccs_status_t hccs_states_write(hccs_ctx_t *ctx, const void *q, const void *k, const void *v, hccs_type_t type,
+                                int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                                const int32_t *positions, int64_t axis_stride, int64_t token_stride,
+                                const hccs_rope_axes_t *axes,
+                                const float *q_step, const float *k_step, const float *v_step,
+                                int8_t *q8, int8_t *k8, int8_t *v8,
+                                int32_t T, int32_t L, int32_t Hq, int32_t Hkv, int32_t d, void *cuda_stream);
+
 /*
  * Reads sequences back: token j of sequence b goes to row out_start[b] + j of the outputs.
  *   page_table   device int32 [B, max_pages]; may be NULL where max_pages is 0
@@ -350,7 +401,7 @@ hccs_status_t hccs_cache_read(hccs_ctx_t *ctx, const int8_t *k_pages, const int8
 /*
  * hccs_params_upload for caches longer than the paper's int16 row sums allow (n*B <= 32767 leaves a table
  * of constants at 16384 keys): Dmax in 1..127, S in 0..127, 1 <= B <= 32767, B - S*Dmax >= 0, n_design in
- * 1..HCCS_MAX_CACHE_KEYS.  Such a table serves hccs_attention_cached with HCCS_RECIP_REAL alone; the other
+ * 1..HCCS_MAX_CACHE_KEYS.  Such a table serves hccs_attention_cached and hccs_attention_cross with HCCS_RECIP_REAL alone; the other
  * calls return HCCS_ERR_CONSTRAINT until hccs_params_upload puts an ordinary table in its place.
  */
 hccs_status_t hccs_params_upload_wide(hccs_ctx_t *ctx, const hccs_head_params_t *params, int32_t num_heads,
@@ -392,6 +443,32 @@ hccs_status_t hccs_attention_cached(hccs_ctx_t *ctx, const int8_t *Q, const int8
                                     int32_t T, int32_t B, int32_t Hq, int32_t Hkv, int32_t d, int32_t max_pages,
                                     int32_t num_pages, int32_t page_size, int32_t max_q, int32_t max_kv,
                                     uint32_t flags, void *cuda_stream);
+
+/*
+ * HCCS attention of queries to states of another length (cross attention: an encoder's states, an image's, a
+ * video's).  Sequence b has the queries q_start[b] .. q_start[b+1] - 1 and the keys k_start[b] .. k_start[b] + k_len[b] - 1
+ * (sequences may share states, in whole or in part).  A query sees all keys of its sequence, or with key_range those
+ * numbered key_range[t][0] .. key_range[t][1] - 1 of them (cut to the sequence's; the image that a token follows, for
+ * instance).  Logits, scores, normalisation and outputs as in hccs_attention_cached; a query that sees no key gives
+ * zeros.  Does not allocate or synchronise, and can be captured.
+ *   Q            device int8 [T, Hq, d], 16-byte aligned
+ *   K, V         device int8 [S, Hkv, d]; heads and dims are contiguous, keys are k_stride, v_stride BYTES apart: multiples of 16,
+ *                Hkv*d or more, below 2^36 (halves of one tensor, for instance); 16-byte aligned.  May be NULL where S is 0
+ *   q_start      device int32 [B+1], not falling;  k_start, k_len  device int32 [B]
+ *   key_range    device int32 [T, 2], 8-byte aligned, or NULL
+ *   requant_mult, requant_shift, out_scale, O, out_type, flags   as in hccs_attention_cached
+ *   max_q, max_kv (host)  bounds of the lengths of this call, which choose kernel and grid: queries beyond max_q are not
+ *                computed and keys beyond max_kv are not seen, both reported.  max_kv beyond n_design is
+ *                HCCS_ERR_CONSTRAINT, beyond HCCS_MAX_CACHE_KEYS HCCS_ERR_UNSUPPORTED
+ * Keys outside 0..S-1 are not seen and reported (bit 4 of the status word); q_start is cut to 0..T.  Rows no sequence has are left as they are.
+ */
+hccs_status_t hccs_attention_cross(hccs_ctx_t *ctx, const int8_t *Q, const int8_t *K, const int8_t *V,
+                                   int64_t k_stride, int64_t v_stride, const int32_t *q_start,
+                                   const int32_t *k_start, const int32_t *k_len, const int32_t *key_range,
+                                   const int32_t *requant_mult, int32_t requant_shift, const float *out_scale,
+                                   void *O, hccs_type_t out_type,
+                                   int32_t T, int32_t S, int32_t B, int32_t Hq, int32_t Hkv, int32_t d,
+                                   int32_t max_q, int32_t max_kv, uint32_t flags, void *cuda_stream);
 
 /* Reads (and clears) the device status word: 0 = no kernel gave up a bounded wait or met an index out of
  * range.  Synchronises `cuda_stream`.  Returns HCCS_ERR_DEVICE_TIMEOUT when a wait was given up (bits 0

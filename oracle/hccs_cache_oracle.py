@@ -90,3 +90,37 @@ def integer_output(num, zs, cnt, clb):
             if cnt[t, h]:
                 out[t, h] = num[t, h] * rho16(zs[t, h], clb)
     return out
+
+
+def rotate_axes(x, pos, freq, axis, interleaved, scale):
+    """``rotate`` with positions [axes, tokens]: pair i turns by those of its axis alone."""
+    y = np.asarray(x, dtype=np.longdouble).copy()
+    half = len(freq)
+    for i in range(half):
+        ia, ib = (2 * i, 2 * i + 1) if interleaved else (i, i + half)
+        pair = np.stack([np.asarray(x)[..., ia], np.asarray(x)[..., ib]], axis=-1)
+        y[..., [ia, ib]] = rotate(pair, pos[axis[i]], [freq[i]], False, scale)
+    return y
+
+
+def cross(q, k, v, q_start, k_start, k_len, theta, mult, shift, ranges=None):
+    """``attend`` for queries on states k, v [S, Hkv, d]: query t sees keys ranges[t][0] .. ranges[t][1] - 1 of its sequence, or all."""
+    T, hq, d = q.shape
+    g = hq // k.shape[1]
+    num, zs, cnt = np.zeros((T, hq, d), np.int64), np.zeros((T, hq), np.int64), np.zeros((T, hq), np.int64)
+    for b in range(len(k_len)):
+        s0, s1, k0, n = int(q_start[b]), int(q_start[b + 1]), int(k_start[b]), int(k_len[b])
+        if s1 <= s0 or n <= 0:
+            continue
+        seen = np.ones((s1 - s0, n), dtype=bool)
+        if ranges is not None:
+            r = np.asarray(ranges)[s0:s1]
+            seen = (np.arange(n)[None] >= r[:, :1]) & (np.arange(n)[None] < r[:, 1:])
+        for h in range(hq):
+            big, slope, reach = (int(c) for c in theta[h])
+            kk, vv = k[k0:k0 + n, h // g].astype(np.int64), v[k0:k0 + n, h // g].astype(np.int64)
+            x = np.clip((q[s0:s1, h].astype(np.int64) @ kk.T * int(mult[h]) + (1 << (shift - 1))) >> shift, -128, 127)
+            m = np.where(seen, x, -1000).max(axis=1, keepdims=True)
+            s = np.where(seen, big - slope * np.minimum(m - x, reach), 0)
+            num[s0:s1, h], zs[s0:s1, h], cnt[s0:s1, h] = s @ vv, s.sum(axis=1), seen.sum(axis=1)
+    return num, zs, cnt

@@ -42,12 +42,15 @@ HCCS_ROPE_NONE, HCCS_ROPE_LINEAR, HCCS_ROPE_BASE, HCCS_ROPE_WAVELENGTH, HCCS_ROP
 HCCS_MAX_CACHE_HEADS = 256
 HCCS_MAX_CACHE_KEYS = 131072
 HCCS_MAX_ROT_DIM = 128
+HCCS_MAX_AXES = 4
+HCCS_AXES_SECTIONS, HCCS_AXES_TURNS = 0, 1
 
 EXPORTS = ("hccs_create", "hccs_destroy", "hccs_params_check", "hccs_params_upload", "hccs_forward",
            "hccs_forward_keylen", "hccs_forward_host",
            "hccs_attention_fused", "hccs_attention_fused_keylen", "hccs_attention_fused_f32", "hccs_attention_fused_i8", "hccs_device_status", "hccs_last_cuda_error", "hccs_status_string",
            "hccs_launch_count", "hccs_forward_static_scratch", "hccs_calibrate", "hccs_debug_wait_timeout",
-           "hccs_rope_frequencies", "hccs_cache_write", "hccs_cache_read", "hccs_params_upload_wide", "hccs_attention_cached")
+           "hccs_rope_frequencies", "hccs_cache_write", "hccs_cache_read", "hccs_params_upload_wide", "hccs_attention_cached",
+           "hccs_rope_axes", "hccs_cache_write_axes", "hccs_states_write", "hccs_attention_cross")
 
 _vp, _i32, _u32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint32
 
@@ -112,6 +115,26 @@ class Rope(ctypes.Structure):
         return ctypes.byref(self)
 
 
+class RopeAxes(ctypes.Structure):
+    """``hccs_rope_axes_t``: frequencies and, per pair of rotated dims, the axis whose positions turn it."""
+    _fields_ = [("rope", Rope), ("num_axes", _i32), ("axis", ctypes.c_uint8 * (HCCS_MAX_ROT_DIM // 2))]
+
+    def __init__(self, freq=(), axis=(), interleaved: bool = False, scale: float = 1.0, num_axes: int | None = None):
+        axis = [int(x) for x in axis]
+        if len(axis) != len(freq):
+            raise ValueError(f"{len(freq)} frequencies and {len(axis)} axes: there is one of each per pair")
+        count = max(axis, default=0) + 1 if num_axes is None else int(num_axes)
+        if not 1 <= count <= HCCS_MAX_AXES or any(not 0 <= x < count for x in axis):
+            raise ValueError(f"axes are numbered 0 to {HCCS_MAX_AXES - 1} at most")
+        super().__init__(Rope(freq, interleaved, scale), count)
+        for i, x in enumerate(axis):
+            self.axis[i] = x
+
+    @property
+    def _ref(self):
+        return ctypes.byref(self)
+
+
 class _RopeScaling(ctypes.Structure):
     _fields_ = [("kind", _i32), ("factor", ctypes.c_double), ("low", ctypes.c_double), ("high", ctypes.c_double),
                 ("original_len", ctypes.c_double)]
@@ -142,6 +165,34 @@ def hccs_rope_frequencies(rot_dim: int, base: float = 10000.0, interleaved: bool
     if st != HCCS_OK:
         raise HccsError(st, "hccs_rope_frequencies")
     return rope
+
+
+_lib.hccs_rope_axes.argtypes = [ctypes.POINTER(RopeAxes), _i32, _i32, ctypes.c_double, ctypes.POINTER(_RopeScaling), _vp, _i32, _i32, _i32]
+_lib.hccs_rope_axes.restype = ctypes.c_int
+_lib.hccs_cache_write_axes.argtypes = [_vp, _vp, _vp, _vp, ctypes.c_int, _i64, _i64, _i64, _vp, _i64, _i64, _vp, _vp, _vp, _vp, _vp,
+                                       _vp, _vp, _vp, _i32, _i32, _i32, _i32, _i32, _i32, _vp]
+_lib.hccs_cache_write_axes.restype = ctypes.c_int
+_lib.hccs_states_write.argtypes = [_vp, _vp, _vp, _vp, ctypes.c_int, _i64, _i64, _i64, _vp, _i64, _i64, _vp, _vp, _vp, _vp,
+                                   _vp, _vp, _vp, _i32, _i32, _i32, _i32, _i32, _vp]
+_lib.hccs_states_write.restype = ctypes.c_int
+_lib.hccs_attention_cross.argtypes = [_vp, _vp, _vp, _vp, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _i32, _vp, _vp, ctypes.c_int,
+                                      _i32, _i32, _i32, _i32, _i32, _i32, _i32, _i32, _u32, _vp]
+_lib.hccs_attention_cross.restype = ctypes.c_int
+
+
+def hccs_rope_axes(rot_dim: int, pairs, base: float = 10000.0, interleaved: bool = False, order: int = HCCS_AXES_SECTIONS,
+                   restart: bool = False, kind: int = HCCS_ROPE_NONE, factor: float = 1.0, low: float = 1.0, high: float = 4.0,
+                   original_len: float = 8192.0) -> RopeAxes:
+    """A :class:`RopeAxes` whose axis x has ``pairs[x]`` of the rot_dim / 2 pairs, dealt out in sections or in turns, with the
+    frequencies of :func:`hccs_rope_frequencies` over all pairs, or (``restart``) over each axis's own."""
+    axes = RopeAxes()
+    count = np.ascontiguousarray(pairs, dtype=np.int32).reshape(-1)
+    sc = _RopeScaling(int(kind), float(factor), float(low), float(high), float(original_len))
+    st = _lib.hccs_rope_axes(ctypes.byref(axes), int(rot_dim), int(bool(interleaved)), float(base), ctypes.byref(sc),
+                             count.ctypes.data_as(_vp), count.size, int(order), int(bool(restart)))
+    if st != HCCS_OK:
+        raise HccsError(st, "hccs_rope_axes")
+    return axes
 
 
 class _CalibGrid(ctypes.Structure):
@@ -346,6 +397,34 @@ class Context:
         """Rotates and quantises tokens: q [T,Hq,d] to q8, k and v [T,Hkv,d] into the pools at ``slots``.  q (with q8 and
         q_step) may be None, or k and v (with the pools, the slots and their steps).  q, k and v may be views whose tokens
         are any multiple of 16 bytes apart."""
+        (some, T, d, Hq, Hkv, pages, size, qp, kp, vp, q8p, kpp, vpp, slotp, qs, ks, vs, q_stride, k_stride,
+         v_stride) = self._paged_tokens(q, k, v, q8, k_pages, v_pages, slots, q_step, k_step, v_step)
+        dev, posp = self.device, None
+        if positions is not None:
+            if positions.get_device() != dev or positions.dtype not in _I32 or positions.shape != (T,) or not positions.is_contiguous():
+                self._explain(positions, "positions", 4, (T,))
+            posp = positions.data_ptr()
+        st = _lib.hccs_cache_write(self._h, qp, kp, vp, _type_of(some), q_stride, k_stride, v_stride, posp, slotp,
+                                   rope._ref if rope is not None else None, qs, ks, vs, q8p, kpp, vpp,
+                                   T, Hq, Hkv, d, pages, size, _raw_stream(dev) if stream is None else _stream_ptr(stream))
+        if st != HCCS_OK:
+            raise HccsError(st, "hccs_cache_write")
+
+    # -- hccs_cache_write_axes
+    def hccs_cache_write_axes(self, q, k, v, q8, k_pages, v_pages, positions, slots, q_step, k_step, v_step,
+                              rope: RopeAxes | None = None, stream=None) -> None:
+        """:meth:`hccs_cache_write` with positions [axes,T] (int32, any strides: the transpose of [T,axes] as well)."""
+        (some, T, d, Hq, Hkv, pages, size, qp, kp, vp, q8p, kpp, vpp, slotp, qs, ks, vs, q_stride, k_stride,
+         v_stride) = self._paged_tokens(q, k, v, q8, k_pages, v_pages, slots, q_step, k_step, v_step)
+        posp, axis_stride, token_stride = self._axes(positions, rope, T)
+        st = _lib.hccs_cache_write_axes(self._h, qp, kp, vp, _type_of(some), q_stride, k_stride, v_stride, posp, axis_stride, token_stride,
+                                        slotp, rope._ref if rope is not None else None, qs, ks, vs, q8p, kpp, vpp, T, Hq, Hkv, d, pages,
+                                        size, _raw_stream(self.device) if stream is None else _stream_ptr(stream))
+        if st != HCCS_OK:
+            raise HccsError(st, "hccs_cache_write_axes")
+
+    def _paged_tokens(self, q, k, v, q8, k_pages, v_pages, slots, q_step, k_step, v_step):
+        """What the two cache writes hand to the library."""
         some = q if q is not None else k
         if some is None:
             raise ValueError("q or k and v must be given")
@@ -353,7 +432,7 @@ class Context:
             raise ValueError("k and v go together")
         T, _, d = some.shape
         Hq = Hkv = pages = size = 0
-        qp = kp = vp = q8p = kpp = vpp = posp = slotp = qs = ks = vs = None
+        qp = kp = vp = q8p = kpp = vpp = slotp = qs = ks = vs = None
         q_stride = k_stride = v_stride = 0
         dev, dtype = self.device, some.dtype
         if q is not None:
@@ -377,15 +456,61 @@ class Context:
                 self._explain(slots, "slots", 8, (T,))
             kp, vp, kpp, vpp, slotp = k.data_ptr(), v.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), slots.data_ptr()
             ks, vs = _floats(k_step, "k_step", Hkv), _floats(v_step, "v_step", Hkv)
-        if positions is not None:
-            if positions.get_device() != dev or positions.dtype not in _I32 or positions.shape != (T,) or not positions.is_contiguous():
-                self._explain(positions, "positions", 4, (T,))
-            posp = positions.data_ptr()
-        st = _lib.hccs_cache_write(self._h, qp, kp, vp, _type_of(some), q_stride, k_stride, v_stride, posp, slotp,
-                                   rope._ref if rope is not None else None, qs, ks, vs, q8p, kpp, vpp,
-                                   T, Hq, Hkv, d, pages, size, _raw_stream(dev) if stream is None else _stream_ptr(stream))
+        return (some, T, d, Hq, Hkv, pages, size, qp, kp, vp, q8p, kpp, vpp, slotp, qs, ks, vs, q_stride, k_stride, v_stride)
+
+    def _axes(self, positions, rope, T):
+        """(address, stride of the axes, stride of the tokens) of positions [axes,T]."""
+        if positions is None:
+            return None, 0, 0
+        if positions.get_device() != self.device or positions.dtype not in _I32 or positions.ndim != 2 or positions.shape[1] != T:
+            if positions.get_device() == self.device:
+                self._explain(positions.contiguous(), "positions", 4, (positions.shape[0], T))
+            self._explain(positions, "positions", 4)
+        if rope is not None and positions.shape[0] < rope.num_axes:
+            raise ValueError(f"positions have {positions.shape[0]} axes, the rotation {rope.num_axes}")
+        return positions.data_ptr(), positions.stride(0), positions.stride(1)
+
+    # -- hccs_states_write
+    def hccs_states_write(self, q, k, v, q8, k8, v8, positions, q_step, k_step, v_step, rope: RopeAxes | None = None, stream=None) -> None:
+        """Rotates (by positions [axes,T], any strides) and quantises tokens q [T,Hq,d], k and v [T,Hkv,d] into dense tensors:
+        q8, k8 and v8 are [T,heads,d], or [B,heads,L,d] with B*L = T (as ``hccs_attention_fused`` reads them).  q (with q8
+        and q_step) may be None, or k and v (with theirs)."""
+        some, out = (q, q8) if q is not None else (k, k8)
+        if some is None:
+            raise ValueError("q or k and v must be given")
+        if (k is None) != (v is None):
+            raise ValueError("k and v go together")
+        T, _, d = some.shape
+        heads_first = out.ndim == 4
+        L = out.shape[2] if heads_first else 1
+        if heads_first and out.shape[0] * L != T:
+            raise ValueError(f"[B,heads,L,d] of {tuple(out.shape)} does not hold {T} tokens")
+
+        def dense(t, name, heads):
+            shape = (T // L if L else 0, heads, L, d) if heads_first else (T, heads, d)
+            if t.get_device() != self.device or t.shape != shape or t.dtype not in _I8 or not t.is_contiguous():
+                self._explain(t, name, 1, shape)
+            return t.data_ptr()
+
+        Hq = Hkv = 0
+        qp = kp = vp = q8p = k8p = v8p = qs = ks = vs = None
+        q_stride = k_stride = v_stride = 0
+        if q is not None:
+            Hq = q.shape[1]
+            qp, q8p, qs, q_stride = q.data_ptr(), dense(q8, "q8", Hq), _floats(q_step, "q_step", Hq), self._tokens(q, "q", some)
+        if k is not None:
+            Hkv = k.shape[1]
+            if v.dtype != some.dtype or v.shape != k.shape:
+                raise ValueError("k and v must have one shape and type")
+            k_stride, v_stride = self._tokens(k, "k", some), self._tokens(v, "v", some)
+            kp, vp, k8p, v8p = k.data_ptr(), v.data_ptr(), dense(k8, "k8", Hkv), dense(v8, "v8", Hkv)
+            ks, vs = _floats(k_step, "k_step", Hkv), _floats(v_step, "v_step", Hkv)
+        posp, axis_stride, token_stride = self._axes(positions, rope, T)
+        st = _lib.hccs_states_write(self._h, qp, kp, vp, _type_of(some), q_stride, k_stride, v_stride, posp, axis_stride, token_stride,
+                                    rope._ref if rope is not None else None, qs, ks, vs, q8p, k8p, v8p, T, max(L, 1), Hq, Hkv, d,
+                                    _raw_stream(self.device) if stream is None else _stream_ptr(stream))
         if st != HCCS_OK:
-            raise HccsError(st, "hccs_cache_write")
+            raise HccsError(st, "hccs_states_write")
 
     # -- hccs_cache_read
     def hccs_cache_read(self, k_pages, v_pages, page_table, out_start, k_out, v_out, k_step, v_step, max_len: int,
@@ -452,6 +577,40 @@ class Context:
         if st != HCCS_OK:
             raise HccsError(st, "hccs_attention_cached")
 
+    # -- hccs_attention_cross
+    def hccs_attention_cross(self, Q, K, V, q_start, k_start, k_len, O, requant_mult, requant_shift: int, max_q: int, max_kv: int,
+                             key_range=None, out_scale=None, flags: int = 0, stream=None) -> None:
+        """HCCS attention of the queries Q [T,Hq,d] to the states K and V [S,Hkv,d] (int8; views whose keys are a multiple of 16
+        bytes apart as well).  O [T,Hq,d] is int32 (no out_scale), or float32, bfloat16 or float16."""
+        T, Hq, d = shape = Q.shape
+        S, Hkv, dk = K.shape
+        B = k_len.shape[0]
+        dev = self.device
+        if dk != d:
+            raise ValueError(f"the states have heads of {dk}, Q of {d}")
+        if (Q.get_device() != dev or q_start.get_device() != dev or k_start.get_device() != dev or k_len.get_device() != dev
+                or O.get_device() != dev or Q.dtype not in _I8 or q_start.dtype not in _I32 or k_start.dtype not in _I32
+                or k_len.dtype not in _I32 or O.shape != shape or q_start.shape != (B + 1,) or k_start.shape != (B,) or k_len.shape != (B,)
+                or not Q.is_contiguous() or not q_start.is_contiguous() or not k_start.is_contiguous() or not k_len.is_contiguous()
+                or not O.is_contiguous()):
+            self._explain(Q, "Q", 1)
+            self._explain(q_start, "q_start", 4, (B + 1,))
+            self._explain(k_start, "k_start", 4, (B,))
+            self._explain(k_len, "k_len", 4, (B,))
+            self._output(O, "O", shape)
+        k_stride, v_stride = self._states(K, "K", K), self._states(V, "V", K)
+        rangep = None
+        if key_range is not None:
+            if key_range.get_device() != dev or key_range.dtype not in _I32 or key_range.shape != (T, 2) or not key_range.is_contiguous():
+                self._explain(key_range, "key_range", 4, (T, 2))
+            rangep = key_range.data_ptr()
+        st = _lib.hccs_attention_cross(
+            self._h, Q.data_ptr(), K.data_ptr(), V.data_ptr(), k_stride, v_stride, q_start.data_ptr(), k_start.data_ptr(), k_len.data_ptr(),
+            rangep, _ints(requant_mult, "requant_mult", Hq), requant_shift, None if out_scale is None else _floats(out_scale, "out_scale", Hq),
+            O.data_ptr(), _type_of(O), T, S, B, Hq, Hkv, d, max_q, max_kv, flags, _raw_stream(dev) if stream is None else _stream_ptr(stream))
+        if st != HCCS_OK:
+            raise HccsError(st, "hccs_attention_cross")
+
     # The cache calls run on the context's device: on its current stream, with tensors that live there.  They are made
     # for every token of every layer, so their checks take the short way and build a message only where one is due.
     def _explain(self, t, name, itemsize, shape=None):
@@ -491,6 +650,16 @@ class Context:
         if T and heads and (c != 1 or (heads > 1 and b != d)):
             raise ValueError(f"{name} must be contiguous inside a token")
         return a if T > 1 else 0
+
+    def _states(self, t, name, like) -> int:
+        """Bytes between the keys of int8 states [S, heads, d] that are contiguous inside a key."""
+        if t.get_device() != self.device or t.dtype not in _I8 or t.shape != like.shape:
+            self._explain(t if t.get_device() != self.device or t.is_contiguous() else t.contiguous(), name, 1, like.shape)
+        S, heads, d = t.shape
+        a, b, c = t.stride()
+        if S and heads and (c != 1 or (heads > 1 and b != d)):
+            raise ValueError(f"{name} must be contiguous inside a key")
+        return a if S > 1 else heads * d
 
     # -- hccs_device_status / hccs_last_cuda_error / hccs_launch_count
     def hccs_device_status(self, stream=None) -> int:

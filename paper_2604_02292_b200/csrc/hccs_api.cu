@@ -569,6 +569,116 @@ hccs_status_t hccs_rope_frequencies(hccs_rope_t *rope, int32_t rot_dim, int32_t 
     return HCCS_OK;
 }
 
+hccs_status_t hccs_rope_axes(hccs_rope_axes_t *axes, int32_t rot_dim, int32_t interleaved, double base,
+                             const hccs_rope_scaling_t *scaling, const int32_t *pairs, int32_t num_axes,
+                             int32_t order, int32_t restart) {
+    if (!axes || !pairs || num_axes < 1 || num_axes > HCCS_MAX_AXES) return HCCS_ERR_INVALID_ARG;
+    if (order != HCCS_AXES_SECTIONS && order != HCCS_AXES_TURNS) return HCCS_ERR_INVALID_ARG;
+    hccs_rope_axes_t got;
+    memset(&got, 0, sizeof(got));
+    hccs_status_t st = hccs_rope_frequencies(&got.rope, rot_dim, interleaved, base, scaling);
+    if (st != HCCS_OK) return st;
+    int64_t sum = 0;
+    for (int32_t x = 0; x < num_axes; ++x) {
+        if (pairs[x] < 0) return HCCS_ERR_INVALID_ARG;
+        sum += pairs[x];
+    }
+    if (sum != rot_dim / 2) return HCCS_ERR_INVALID_ARG;
+    got.num_axes = num_axes;
+    hccs_rope_t own[HCCS_MAX_AXES];
+    int32_t dealt[HCCS_MAX_AXES] = {0, 0, 0, 0};
+    if (restart)
+        for (int32_t x = 0; x < num_axes; ++x) {
+            if (pairs[x] == 0) continue;
+            st = hccs_rope_frequencies(&own[x], 2 * pairs[x], interleaved, base, scaling);
+            if (st != HCCS_OK) return st;
+        }
+    for (int32_t i = 0, x = 0; i < rot_dim / 2; ++i) {
+        while (dealt[x] == pairs[x]) x = (x + 1) % num_axes;
+        got.axis[i] = (uint8_t)x;
+        if (restart) got.rope.freq[i] = own[x].freq[dealt[x]];
+        ++dealt[x];
+        if (order == HCCS_AXES_TURNS) x = (x + 1) % num_axes;
+    }
+    *axes = got;
+    return HCCS_OK;
+}
+
+// Where the new tokens of a write come from and go to, besides the kernel's own arguments.
+struct WriteCall {
+    const void *q, *k, *v;
+    hccs_type_t type;
+    int64_t q_stride, k_stride, v_stride;
+    const int32_t *positions;
+    int64_t axis_stride, token_stride;
+    const int64_t *slots;
+    const hccs_rope_t *rope;
+    const hccs_rope_axes_t *axes;               // NULL: one axis
+    const float *q_step, *k_step, *v_step;
+    int8_t *q8, *k8, *v8;
+    int32_t T, L, Hq, Hkv, d;                   // L: 0 for pages
+    int32_t num_pages, page_size;
+};
+
+static hccs_status_t write_tokens(hccs_ctx_t *ctx, const WriteCall &w, void *cuda_stream) {
+    const int32_t T = w.T, d = w.d;
+    const hccs_rope_t *rope = w.rope;
+    if (T < 0) return HCCS_ERR_INVALID_ARG;
+    if (w.type != HCCS_F32 && w.type != HCCS_BF16 && w.type != HCCS_F16) return HCCS_ERR_INVALID_ARG;
+    const bool with_q = w.q != nullptr, with_kv = w.k != nullptr, paged = w.L == 0;
+    if ((w.k == nullptr) != (w.v == nullptr)) return HCCS_ERR_INVALID_ARG;
+    int32_t page_shift = 0;
+    if (d != 64 && d != 128) return HCCS_ERR_UNSUPPORTED;
+    if (with_kv && (paged ? !cache_shape(w.Hkv, d, w.num_pages, w.page_size, &page_shift) : w.Hkv < 1 || w.Hkv > HCCS_MAX_CACHE_HEADS))
+        return HCCS_ERR_INVALID_ARG;
+    if (with_q && (w.Hq < 1 || w.Hq > HCCS_MAX_CACHE_HEADS)) return HCCS_ERR_INVALID_ARG;
+    if (with_q && !steps_ok(w.q_step, w.Hq)) return HCCS_ERR_INVALID_ARG;
+    if (with_kv && (!steps_ok(w.k_step, w.Hkv) || !steps_ok(w.v_step, w.Hkv))) return HCCS_ERR_INVALID_ARG;
+    if (rope) {
+        if (rope->rot_dim < 0 || rope->rot_dim > d || (rope->rot_dim & 1)) return HCCS_ERR_INVALID_ARG;
+        if (!(fabs(rope->scale) >= 0x1p-64) || !(fabs(rope->scale) <= 0x1p64)) return HCCS_ERR_INVALID_ARG;
+        for (int32_t i = 0; i < rope->rot_dim / 2; ++i)
+            if (!isfinite(rope->freq[i])) return HCCS_ERR_INVALID_ARG;
+    }
+    if (w.axes) {
+        if (w.axes->num_axes < 1 || w.axes->num_axes > HCCS_MAX_AXES) return HCCS_ERR_INVALID_ARG;
+        for (int32_t i = 0; i < rope->rot_dim / 2; ++i)
+            if (w.axes->axis[i] >= w.axes->num_axes) return HCCS_ERR_INVALID_ARG;
+    }
+    const bool turns = rope && rope->rot_dim > 0;
+    if (T == 0 || (!with_q && !with_kv)) return ctx ? HCCS_OK : HCCS_ERR_INVALID_ARG;
+    if (!paged && (w.L < 1 || T % w.L != 0)) return HCCS_ERR_INVALID_ARG;
+    if ((turns && !w.positions) || (with_q && !w.q8) || (with_kv && ((paged && !w.slots) || !w.k8 || !w.v8))) return HCCS_ERR_INVALID_ARG;
+    const int64_t esz = w.type == HCCS_F32 ? 4 : 2;
+    if (with_q && (!aligned16(w.q) || !aligned16(w.q8) || (w.q_stride * esz) % 16 != 0)) return HCCS_ERR_UNSUPPORTED;
+    if (with_kv && (!aligned16(w.k) || !aligned16(w.v) || !aligned16(w.k8) || !aligned16(w.v8) ||
+                    (w.k_stride * esz) % 16 != 0 || (w.v_stride * esz) % 16 != 0))
+        return HCCS_ERR_UNSUPPORTED;
+    if (!ctx) return HCCS_ERR_INVALID_ARG;
+    DeviceGuard g(ctx->device);
+    if (!g.ok) return cuda_fail(ctx, cudaErrorInvalidDevice);
+    hccs::CacheWriteArgs a;
+    memset(&a, 0, sizeof(a));
+    a.q = w.q; a.k = w.k; a.v = w.v;
+    a.q_stride = w.q_stride; a.k_stride = w.k_stride; a.v_stride = w.v_stride;
+    a.positions = w.positions; a.axis_stride = w.axis_stride; a.token_stride = w.token_stride;
+    a.slots = w.slots;
+    a.q8 = w.q8; a.k_pages = w.k8; a.v_pages = w.v8;
+    a.status = ctx->d_status;
+    a.num_slots = with_kv && paged ? (int64_t)w.num_pages * w.page_size : 0;
+    a.T = T; a.Hq = with_q ? w.Hq : 0; a.Hkv = with_kv ? w.Hkv : 0; a.d = d; a.page_shift = page_shift;
+    a.dense_len = w.L;
+    if (turns) a.rope = *rope;
+    if (turns && w.axes) memcpy(a.axis, w.axes->axis, sizeof(a.axis));
+    if (with_q) memcpy(a.step, w.q_step, sizeof(float) * w.Hq);
+    if (with_kv) {
+        memcpy(a.step + HCCS_MAX_CACHE_HEADS, w.k_step, sizeof(float) * w.Hkv);
+        memcpy(a.step + 2 * HCCS_MAX_CACHE_HEADS, w.v_step, sizeof(float) * w.Hkv);
+    }
+    HCCS_CUDA(ctx, hccs::launch_cache_write(a, w.type, (cudaStream_t)cuda_stream, &ctx->launches));
+    return HCCS_OK;
+}
+
 hccs_status_t hccs_cache_write(hccs_ctx_t *ctx, const void *q, const void *k, const void *v, hccs_type_t type,
                                int64_t q_stride, int64_t k_stride, int64_t v_stride,
                                const int32_t *positions, const int64_t *slots, const hccs_rope_t *rope,
@@ -576,50 +686,34 @@ hccs_status_t hccs_cache_write(hccs_ctx_t *ctx, const void *q, const void *k, co
                                int8_t *q8, int8_t *k_pages, int8_t *v_pages,
                                int32_t T, int32_t Hq, int32_t Hkv, int32_t d,
                                int32_t num_pages, int32_t page_size, void *cuda_stream) {
-    if (T < 0) return HCCS_ERR_INVALID_ARG;
-    if (type != HCCS_F32 && type != HCCS_BF16 && type != HCCS_F16) return HCCS_ERR_INVALID_ARG;
-    const bool with_q = q != nullptr, with_kv = k != nullptr;
-    if ((k == nullptr) != (v == nullptr)) return HCCS_ERR_INVALID_ARG;
-    int32_t page_shift = 0;
-    if (d != 64 && d != 128) return HCCS_ERR_UNSUPPORTED;
-    if (with_kv && !cache_shape(Hkv, d, num_pages, page_size, &page_shift)) return HCCS_ERR_INVALID_ARG;
-    if (with_q && (Hq < 1 || Hq > HCCS_MAX_CACHE_HEADS)) return HCCS_ERR_INVALID_ARG;
-    if (with_q && !steps_ok(q_step, Hq)) return HCCS_ERR_INVALID_ARG;
-    if (with_kv && (!steps_ok(k_step, Hkv) || !steps_ok(v_step, Hkv))) return HCCS_ERR_INVALID_ARG;
-    if (rope) {
-        if (rope->rot_dim < 0 || rope->rot_dim > d || (rope->rot_dim & 1)) return HCCS_ERR_INVALID_ARG;
-        if (!(fabs(rope->scale) >= 0x1p-64) || !(fabs(rope->scale) <= 0x1p64)) return HCCS_ERR_INVALID_ARG;
-        for (int32_t i = 0; i < rope->rot_dim / 2; ++i)
-            if (!isfinite(rope->freq[i])) return HCCS_ERR_INVALID_ARG;
-    }
-    const bool turns = rope && rope->rot_dim > 0;
-    if (T == 0 || (!with_q && !with_kv)) return ctx ? HCCS_OK : HCCS_ERR_INVALID_ARG;
-    if ((turns && !positions) || (with_q && !q8) || (with_kv && (!slots || !k_pages || !v_pages))) return HCCS_ERR_INVALID_ARG;
-    const int64_t esz = type == HCCS_F32 ? 4 : 2;
-    if (with_q && (!aligned16(q) || !aligned16(q8) || (q_stride * esz) % 16 != 0)) return HCCS_ERR_UNSUPPORTED;
-    if (with_kv && (!aligned16(k) || !aligned16(v) || !aligned16(k_pages) || !aligned16(v_pages) ||
-                    (k_stride * esz) % 16 != 0 || (v_stride * esz) % 16 != 0))
-        return HCCS_ERR_UNSUPPORTED;
-    if (!ctx) return HCCS_ERR_INVALID_ARG;
-    DeviceGuard g(ctx->device);
-    if (!g.ok) return cuda_fail(ctx, cudaErrorInvalidDevice);
-    hccs::CacheWriteArgs a;
-    memset(&a, 0, sizeof(a));
-    a.q = q; a.k = k; a.v = v;
-    a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride;
-    a.positions = positions; a.slots = slots;
-    a.q8 = q8; a.k_pages = k_pages; a.v_pages = v_pages;
-    a.status = ctx->d_status;
-    a.num_slots = with_kv ? (int64_t)num_pages * page_size : 0;
-    a.T = T; a.Hq = with_q ? Hq : 0; a.Hkv = with_kv ? Hkv : 0; a.d = d; a.page_shift = page_shift;
-    if (turns) a.rope = *rope;
-    if (with_q) memcpy(a.step, q_step, sizeof(float) * Hq);
-    if (with_kv) {
-        memcpy(a.step + HCCS_MAX_CACHE_HEADS, k_step, sizeof(float) * Hkv);
-        memcpy(a.step + 2 * HCCS_MAX_CACHE_HEADS, v_step, sizeof(float) * Hkv);
-    }
-    HCCS_CUDA(ctx, hccs::launch_cache_write(a, type, (cudaStream_t)cuda_stream, &ctx->launches));
-    return HCCS_OK;
+    return write_tokens(ctx, {q, k, v, type, q_stride, k_stride, v_stride, positions, 0, 1, slots, rope, nullptr, q_step, k_step, v_step,
+                              q8, k_pages, v_pages, T, 0, Hq, Hkv, d, num_pages, page_size}, cuda_stream);
+}
+
+hccs_status_t hccs_cache_write_axes(hccs_ctx_t *ctx, const void *q, const void *k, const void *v, hccs_type_t type,
+                                    int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                                    const int32_t *positions, int64_t axis_stride, int64_t token_stride,
+                                    const int64_t *slots, const hccs_rope_axes_t *axes,
+                                    const float *q_step, const float *k_step, const float *v_step,
+                                    int8_t *q8, int8_t *k_pages, int8_t *v_pages,
+                                    int32_t T, int32_t Hq, int32_t Hkv, int32_t d,
+                                    int32_t num_pages, int32_t page_size, void *cuda_stream) {
+    return write_tokens(ctx, {q, k, v, type, q_stride, k_stride, v_stride, positions, axis_stride, token_stride, slots,
+                              axes ? &axes->rope : nullptr, axes, q_step, k_step, v_step,
+                              q8, k_pages, v_pages, T, 0, Hq, Hkv, d, num_pages, page_size}, cuda_stream);
+}
+
+hccs_status_t hccs_states_write(hccs_ctx_t *ctx, const void *q, const void *k, const void *v, hccs_type_t type,
+                                int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                                const int32_t *positions, int64_t axis_stride, int64_t token_stride,
+                                const hccs_rope_axes_t *axes,
+                                const float *q_step, const float *k_step, const float *v_step,
+                                int8_t *q8, int8_t *k8, int8_t *v8,
+                                int32_t T, int32_t L, int32_t Hq, int32_t Hkv, int32_t d, void *cuda_stream) {
+    if (L < 1) return HCCS_ERR_INVALID_ARG;
+    return write_tokens(ctx, {q, k, v, type, q_stride, k_stride, v_stride, positions, axis_stride, token_stride, nullptr,
+                              axes ? &axes->rope : nullptr, axes, q_step, k_step, v_step,
+                              q8, k8, v8, T, L, Hq, Hkv, d, 0, 0}, cuda_stream);
 }
 
 hccs_status_t hccs_cache_read(hccs_ctx_t *ctx, const int8_t *k_pages, const int8_t *v_pages,
@@ -654,22 +748,9 @@ hccs_status_t hccs_cache_read(hccs_ctx_t *ctx, const int8_t *k_pages, const int8
     return HCCS_OK;
 }
 
-hccs_status_t hccs_attention_cached(hccs_ctx_t *ctx, const int8_t *Q, const int8_t *k_pages, const int8_t *v_pages,
-                                    const int32_t *page_table, const int32_t *q_start, const int32_t *kv_len,
-                                    const int32_t *tree_mask, int32_t tree_words,
-                                    const int32_t *requant_mult, int32_t requant_shift, const float *out_scale,
-                                    void *O, hccs_type_t out_type,
-                                    int32_t T, int32_t B, int32_t Hq, int32_t Hkv, int32_t d, int32_t max_pages,
-                                    int32_t num_pages, int32_t page_size, int32_t max_q, int32_t max_kv,
-                                    uint32_t flags, void *cuda_stream) {
-    // what needs no context first
-    if (T < 0 || B < 0 || max_pages < 0 || max_q < 0 || max_kv < 0) return HCCS_ERR_INVALID_ARG;
-    if (flags != HCCS_RECIP_DIV && flags != HCCS_RECIP_CLB && flags != HCCS_RECIP_REAL) return HCCS_ERR_INVALID_ARG;
-    if (out_type != HCCS_I32 && out_type != HCCS_F32 && out_type != HCCS_BF16 && out_type != HCCS_F16) return HCCS_ERR_INVALID_ARG;
-    if (out_type == HCCS_I32 ? (flags == HCCS_RECIP_REAL || out_scale) : !out_scale) return HCCS_ERR_INVALID_ARG;
-    if (d != 64 && d != 128) return HCCS_ERR_UNSUPPORTED;
-    int32_t page_shift = 0;
-    if (!requant_mult || Hq < 1 || !cache_shape(Hkv, d, num_pages, page_size, &page_shift) || Hq % Hkv != 0) return HCCS_ERR_INVALID_ARG;
+// What the two calls of attention to int8 states check alike: first what needs no context, then the context.
+static hccs_status_t states_attention_shape(const int32_t *requant_mult, int32_t requant_shift, const float *out_scale, int32_t B, int32_t Hq,
+                                            int32_t Hkv, int32_t max_q, int32_t max_kv) {
     if (Hq > HCCS_MAX_CACHE_HEADS || B > 65535 || max_kv > HCCS_MAX_CACHE_KEYS) return HCCS_ERR_UNSUPPORTED;
     if ((int64_t)max_q * (Hq / Hkv) > (1ll << 30)) return HCCS_ERR_UNSUPPORTED;
     if (requant_shift < 1 || requant_shift > 24) return HCCS_ERR_INVALID_ARG;
@@ -680,34 +761,102 @@ hccs_status_t hccs_attention_cached(hccs_ctx_t *ctx, const int8_t *Q, const int8
     if (out_scale)
         for (int32_t h = 0; h < Hq; ++h)
             if (!isfinite(out_scale[h])) return HCCS_ERR_INVALID_ARG;
-    if (tree_mask && (tree_words < 1 || (int64_t)tree_words * 32 < max_q)) return HCCS_ERR_INVALID_ARG;
-    const bool empty = T == 0 || B == 0 || max_q == 0;
-    if (!empty && (!Q || !k_pages || !v_pages || (!page_table && max_pages > 0) || !q_start || !kv_len || !O)) return HCCS_ERR_INVALID_ARG;
-    if (!aligned16(Q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(O)) return HCCS_ERR_UNSUPPORTED;
+    return HCCS_OK;
+}
+static hccs_status_t states_attention_context(const hccs_ctx_t *ctx, int32_t Hq, int32_t max_kv, uint32_t flags) {
     if (!ctx) return HCCS_ERR_INVALID_ARG;
     if (ctx->num_heads == 0) return HCCS_ERR_NOT_UPLOADED;
     if (Hq != ctx->num_heads) return HCCS_ERR_INVALID_ARG;
     if ((ctx->wide && flags != HCCS_RECIP_REAL) || max_kv > ctx->n_design) return HCCS_ERR_CONSTRAINT;
-    if (empty) return HCCS_OK;
-    DeviceGuard g(ctx->device);
-    if (!g.ok) return cuda_fail(ctx, cudaErrorInvalidDevice);
-    hccs::CachedAttnArgs a;
-    memset(&a, 0, sizeof(a));
-    a.Q = Q; a.k_pages = k_pages; a.v_pages = v_pages;
-    a.page_table = page_table; a.q_start = q_start; a.kv_len = kv_len; a.tree_mask = tree_mask;
-    a.O = O;
+    return HCCS_OK;
+}
+static bool states_attention_types(hccs_type_t out_type, const float *out_scale, uint32_t flags) {
+    if (flags != HCCS_RECIP_DIV && flags != HCCS_RECIP_CLB && flags != HCCS_RECIP_REAL) return false;
+    if (out_type != HCCS_I32 && out_type != HCCS_F32 && out_type != HCCS_BF16 && out_type != HCCS_F16) return false;
+    return out_type == HCCS_I32 ? flags != HCCS_RECIP_REAL && !out_scale : out_scale != nullptr;
+}
+static void states_attention_args(hccs::CachedAttnArgs &a, const hccs_ctx_t *ctx, const int32_t *requant_mult, int32_t requant_shift,
+                                  const float *out_scale, hccs_type_t out_type, int32_t T, int32_t B, int32_t Hq, int32_t Hkv, int32_t d,
+                                  int32_t max_q, int32_t max_kv, uint32_t flags) {
     a.table = ctx->d_table;
     a.status = ctx->d_status;
     a.wait_cycles = hccs::kDefaultWaitCycles;
-    a.tree_words = tree_words; a.out_type = out_type; a.recip = (int32_t)flags;
+    a.out_type = out_type; a.recip = (int32_t)flags;
     a.T = T; a.B = B; a.Hq = Hq; a.Hkv = Hkv; a.group = Hq / Hkv; a.d = d;
-    a.max_pages = max_pages; a.num_pages = num_pages; a.page_shift = page_shift;
     a.max_q = max_q; a.max_kv = max_kv; a.requant_shift = requant_shift;
     for (int32_t h = 0; h < Hq; ++h) {
         a.mult[h] = (uint16_t)requant_mult[h];
         a.scale[h] = out_scale ? out_scale[h] : 1.0f;
     }
+}
+
+hccs_status_t hccs_attention_cached(hccs_ctx_t *ctx, const int8_t *Q, const int8_t *k_pages, const int8_t *v_pages,
+                                    const int32_t *page_table, const int32_t *q_start, const int32_t *kv_len,
+                                    const int32_t *tree_mask, int32_t tree_words,
+                                    const int32_t *requant_mult, int32_t requant_shift, const float *out_scale,
+                                    void *O, hccs_type_t out_type,
+                                    int32_t T, int32_t B, int32_t Hq, int32_t Hkv, int32_t d, int32_t max_pages,
+                                    int32_t num_pages, int32_t page_size, int32_t max_q, int32_t max_kv,
+                                    uint32_t flags, void *cuda_stream) {
+    // what needs no context first
+    if (T < 0 || B < 0 || max_pages < 0 || max_q < 0 || max_kv < 0) return HCCS_ERR_INVALID_ARG;
+    if (!states_attention_types(out_type, out_scale, flags)) return HCCS_ERR_INVALID_ARG;
+    if (d != 64 && d != 128) return HCCS_ERR_UNSUPPORTED;
+    int32_t page_shift = 0;
+    if (!requant_mult || Hq < 1 || !cache_shape(Hkv, d, num_pages, page_size, &page_shift) || Hq % Hkv != 0) return HCCS_ERR_INVALID_ARG;
+    hccs_status_t st = states_attention_shape(requant_mult, requant_shift, out_scale, B, Hq, Hkv, max_q, max_kv);
+    if (st != HCCS_OK) return st;
+    if (tree_mask && (tree_words < 1 || (int64_t)tree_words * 32 < max_q)) return HCCS_ERR_INVALID_ARG;
+    const bool empty = T == 0 || B == 0 || max_q == 0;
+    if (!empty && (!Q || !k_pages || !v_pages || (!page_table && max_pages > 0) || !q_start || !kv_len || !O)) return HCCS_ERR_INVALID_ARG;
+    if (!aligned16(Q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(O)) return HCCS_ERR_UNSUPPORTED;
+    st = states_attention_context(ctx, Hq, max_kv, flags);
+    if (st != HCCS_OK || empty) return st;
+    DeviceGuard g(ctx->device);
+    if (!g.ok) return cuda_fail(ctx, cudaErrorInvalidDevice);
+    hccs::CachedAttnArgs a;
+    memset(&a, 0, sizeof(a));
+    states_attention_args(a, ctx, requant_mult, requant_shift, out_scale, out_type, T, B, Hq, Hkv, d, max_q, max_kv, flags);
+    a.Q = Q; a.k_pages = k_pages; a.v_pages = v_pages;
+    a.page_table = page_table; a.q_start = q_start; a.kv_len = kv_len; a.tree_mask = tree_mask;
+    a.O = O;
+    a.tree_words = tree_words;
+    a.max_pages = max_pages; a.num_pages = num_pages; a.page_shift = page_shift;
     HCCS_CUDA(ctx, hccs::launch_cached_attention(a, (cudaStream_t)cuda_stream, &ctx->launches));
+    return HCCS_OK;
+}
+
+hccs_status_t hccs_attention_cross(hccs_ctx_t *ctx, const int8_t *Q, const int8_t *K, const int8_t *V,
+                                   int64_t k_stride, int64_t v_stride, const int32_t *q_start,
+                                   const int32_t *k_start, const int32_t *k_len, const int32_t *key_range,
+                                   const int32_t *requant_mult, int32_t requant_shift, const float *out_scale,
+                                   void *O, hccs_type_t out_type,
+                                   int32_t T, int32_t S, int32_t B, int32_t Hq, int32_t Hkv, int32_t d,
+                                   int32_t max_q, int32_t max_kv, uint32_t flags, void *cuda_stream) {
+    if (T < 0 || S < 0 || B < 0 || max_q < 0 || max_kv < 0) return HCCS_ERR_INVALID_ARG;
+    if (!states_attention_types(out_type, out_scale, flags)) return HCCS_ERR_INVALID_ARG;
+    if (d != 64 && d != 128) return HCCS_ERR_UNSUPPORTED;
+    if (!requant_mult || Hq < 1 || Hkv < 1 || Hkv > HCCS_MAX_CACHE_HEADS || Hq % Hkv != 0) return HCCS_ERR_INVALID_ARG;
+    hccs_status_t st = states_attention_shape(requant_mult, requant_shift, out_scale, B, Hq, Hkv, max_q, max_kv);
+    if (st != HCCS_OK) return st;
+    const bool empty = T == 0 || B == 0 || max_q == 0;
+    if (!empty && (!Q || (S > 0 && (!K || !V)) || !q_start || !k_start || !k_len || !O)) return HCCS_ERR_INVALID_ARG;
+    if (S > 0 && (k_stride < (int64_t)Hkv * d || v_stride < (int64_t)Hkv * d)) return HCCS_ERR_INVALID_ARG;
+    if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(O) || ((uintptr_t)key_range & 7u) != 0) return HCCS_ERR_UNSUPPORTED;
+    if (S > 0 && (k_stride % 16 != 0 || v_stride % 16 != 0 || k_stride >= (1ll << 36) || v_stride >= (1ll << 36))) return HCCS_ERR_UNSUPPORTED;
+    st = states_attention_context(ctx, Hq, max_kv, flags);
+    if (st != HCCS_OK || empty) return st;
+    DeviceGuard g(ctx->device);
+    if (!g.ok) return cuda_fail(ctx, cudaErrorInvalidDevice);
+    hccs::CachedAttnArgs a;
+    memset(&a, 0, sizeof(a));
+    states_attention_args(a, ctx, requant_mult, requant_shift, out_scale, out_type, T, B, Hq, Hkv, d, max_q, max_kv, flags);
+    a.Q = Q; a.k_pages = K; a.v_pages = V;
+    a.k_stride = k_stride; a.v_stride = v_stride;
+    a.q_start = q_start; a.k_start = k_start; a.kv_len = k_len; a.key_range = key_range;
+    a.states = S;
+    a.O = O;
+    HCCS_CUDA(ctx, hccs::launch_cross_attention(a, (cudaStream_t)cuda_stream, &ctx->launches));
     return HCCS_OK;
 }
 

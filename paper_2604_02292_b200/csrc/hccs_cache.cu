@@ -1,4 +1,5 @@
-// The int8 key/value cache: tokens rotated, quantised and written to their slots, and sequences read back.
+// The int8 key/value cache: tokens rotated, quantised and written to their slots (or, as an encoder's states, to dense
+// tensors), and sequences read back.
 //
 // Every element is read once and written once (2 or 4 bytes in and one out, or the reverse).  Reading back is bound by
 // HBM: 8 sequences of 8192 tokens (8 heads of 128, to bf16) in 65 us, 6.2 TB/s.  Writing is bound by instructions, about
@@ -132,10 +133,16 @@ __device__ __noinline__ uint32_t code_pair(float a, float b, double position, do
     return (uint32_t)(m & 255) | (uint32_t)(n & 255) << 8;
 }
 
+// The position that turns a pair of token t: every pair goes by one axis.
+__device__ __forceinline__ double position_of(const CacheWriteArgs &a, int t, int pair) {
+    return (double)a.positions[a.axis[pair] * a.axis_stride + t * a.token_stride];
+}
+
 // Items of heads whose rotated part is no multiple of 16 dims: a dim at a time, in fp32 where that is sure.
 template <typename T>
-__device__ __noinline__ int8_t code_of(const T *head, int dim, int rot, bool inter, const Turn *turn, double position, const double *freq,
-                                       double scale, float step) {
+__device__ __noinline__ int8_t code_of(const T *head, int dim, const CacheWriteArgs &a, const Turn *turn, int t, float step) {
+    const int rot = a.rope.rot_dim;
+    const bool inter = a.rope.interleaved != 0;
     const float x = to_float(head[dim]), inv = 1.0f / step;
     if (dim >= rot) return (int8_t)max(min(code_of_quotient(x, step, inv), 127), -128);
     const int half = rot >> 1;
@@ -145,8 +152,9 @@ __device__ __noinline__ int8_t code_of(const T *head, int dim, int rot, bool int
     const float s = turn->s[skew(pair)];
     const float z = __fmul_rn(fmaf(x, turn->c[skew(pair)], __fmul_rn(p, first ? -s : s)), inv);
     int n;
-    if (fmaf(fabsf(x) + fabsf(p), fmaxf(fabsf((float)scale) * inv * 0x1p-21f, 0x1p-125f), nearest(z, n)) < 0.5f) return (int8_t)max(min(n, 127), -128);
-    const uint32_t two = first ? code_pair(x, p, position, freq[pair], scale, step) : code_pair(p, x, position, freq[pair], scale, step) >> 8;
+    if (fmaf(fabsf(x) + fabsf(p), fmaxf(fabsf((float)a.rope.scale) * inv * 0x1p-21f, 0x1p-125f), nearest(z, n)) < 0.5f) return (int8_t)max(min(n, 127), -128);
+    const double position = position_of(a, t, pair), freq = a.rope.freq[pair];
+    const uint32_t two = first ? code_pair(x, p, position, freq, a.rope.scale, step) : code_pair(p, x, position, freq, a.rope.scale, step) >> 8;
     return (int8_t)(two & 255);
 }
 
@@ -157,7 +165,8 @@ __device__ __noinline__ int8_t code_of(const T *head, int dim, int rot, bool int
 constexpr int kWriteThreads = 384;         // most threads per CTA: all items of a token where they fit, so that its angles are computed once
 constexpr int kTokens = 16;                // most tokens per CTA
 
-template <typename T>
+// DENSE: codes of all three kinds go to tensors [T/L, heads, L, d], L tokens of a head together (L = 1: [T, heads, d]).
+template <typename T, bool DENSE>
 __global__ void __launch_bounds__(kWriteThreads, 2)
 cache_write_kernel(const __grid_constant__ CacheWriteArgs a, int items, int per_head_shift, int per_cta) {
     __shared__ Turn turn[kTokens];
@@ -197,9 +206,10 @@ cache_write_kernel(const __grid_constant__ CacheWriteArgs a, int items, int per_
         for (int pair = (int)threadIdx.x & (wide - 1); pair < half && tok0 < abreast; pair += wide) {
             const double freq = a.rope.freq[pair];
             const float scale = (float)a.rope.scale;
+            const int32_t *const positions = a.positions + a.axis[pair] * a.axis_stride;
             for (int tok = tok0; tok < tokens; tok += abreast) {
                 // the angle as the definition rounds it, in turns, less the whole ones: exact but for 2^-53 of the turns
-                const double angle = __dmul_rn((double)a.positions[t0 + tok], freq), turns = __dmul_rn(angle, 0.15915494309189533577);
+                const double angle = __dmul_rn((double)positions[(t0 + tok) * a.token_stride], freq), turns = __dmul_rn(angle, 0.15915494309189533577);
                 const double part = turns - rint(turns);
                 const float hi = (float)part, lo = (float)(part - (double)hi) * 6.2831853f;
                 float s, c;
@@ -233,9 +243,17 @@ cache_write_kernel(const __grid_constant__ CacheWriteArgs a, int items, int per_
         sure = sure & (fabsf(d0) < l0) & (fabsf(d1) < l1);
     };
     const int at_a = skew(inter ? dim_a >> 1 : dim_a), at_b = skew(inter ? dim_b >> 1 : dim_a + 4);
-    int8_t *q_dst = a.q8 + ((int64_t)t0 * a.Hq + head) * a.d;
-    int8_t *const pool = kind == 1 ? a.k_pages : a.v_pages;
-    int64_t slot = kind != 0 ? a.slots[t0] : 0;
+    // rows of the dense outputs (queries alone, where keys and values go to pages)
+    const bool dense = DENSE || kind == 0;
+    int8_t *const pool = kind == 0 ? a.q8 : kind == 1 ? a.k_pages : a.v_pages;
+    const int heads = kind == 0 ? a.Hq : a.Hkv, run = DENSE ? a.dense_len : 1;     // tokens of a head together
+    auto row_at = [&](int t) -> int8_t * {
+        const int entry = DENSE ? t / run : t;
+        return pool + (((int64_t)entry * heads + head) * run + (t - entry * run)) * a.d;
+    };
+    int in_run = DENSE ? t0 % run : 0;
+    int8_t *q_dst = row_at(t0);
+    int64_t slot = dense ? 0 : a.slots[t0];
     auto place = [&](int64_t at) -> int8_t * {
         if (at >= a.num_slots) atomicOr(a.status, STATUS_BAD_SLOT);
         if (at < 0 || at >= a.num_slots) return nullptr;
@@ -246,8 +264,8 @@ cache_write_kernel(const __grid_constant__ CacheWriteArgs a, int items, int per_
     for (int j = 0; j < tokens; ++j) {
         Raw<T> next_a, next_b;
         if (j + 1 < tokens) { next_a = load_raw(src + stride + dim_a); next_b = load_raw(src + stride + dim_b); }
-        const int64_t next_slot = kind != 0 && j + 1 < tokens ? a.slots[t0 + j + 1] : 0;
-        int8_t *const dst = kind == 0 ? q_dst : place(slot);  // the head
+        const int64_t next_slot = !dense && j + 1 < tokens ? a.slots[t0 + j + 1] : 0;
+        int8_t *const dst = dense ? q_dst : place(slot);      // the head
         if (dst) {
             const Turn &tn = turn[j];
             uint32_t wa[2], wb[2];                            // the codes of the two chunks
@@ -320,26 +338,29 @@ cache_write_kernel(const __grid_constant__ CacheWriteArgs a, int items, int per_
             }
         }
         src += stride;
-        q_dst += (int64_t)a.Hq * a.d;
+        if constexpr (DENSE) {
+            q_dst += a.d;
+            if (++in_run == run) { in_run = 0; q_dst += (int64_t)(heads - 1) * run * a.d; }
+        } else {
+            q_dst += (int64_t)a.Hq * a.d;
+        }
         slot = next_slot;
         raw_a = next_a; raw_b = next_b;
     }
     // What was next to a border, four pairs at a time (a dim at a time where items do not hold whole pairs).  Behind the loop: a
     // call in it, however rare, costs its registers.
     src -= (int64_t)tokens * stride;
-    q_dst -= (int64_t)tokens * a.Hq * a.d;
     while (redo) {
         const int bit = __ffs(redo) - 1, j = bit >> 1, g = bit & 1;
         redo &= redo - 1;
-        int8_t *const dst = kind == 0 ? q_dst + (int64_t)j * a.Hq * a.d : place(a.slots[t0 + j]);
+        int8_t *const dst = dense ? row_at(t0 + j) : place(a.slots[t0 + j]);
         const T *const row = src + j * stride;
         const Turn &tn = turn[j];
-        const double position = (double)a.positions[t0 + j];
         if (!aligned) {
 #pragma unroll 1
             for (int e = 0; e < 8; ++e) {
                 const int dim = (g ? dim_b : dim_a) + e;
-                dst[dim] = code_of(row, dim, rot, inter, &tn, position, a.rope.freq, a.rope.scale, step);
+                dst[dim] = code_of(row, dim, a, &tn, t0 + j, step);
             }
             continue;
         }
@@ -363,7 +384,7 @@ cache_write_kernel(const __grid_constant__ CacheWriteArgs a, int items, int per_
         for (int i = 0; i < 4; ++i) {
             if (!((unsure >> i) & 1)) continue;
             const float x = i == 0 ? u[0] : i == 1 ? u[1] : i == 2 ? u[2] : u[3], y = i == 0 ? v[0] : i == 1 ? v[1] : i == 2 ? v[2] : v[3];
-            const uint32_t n2 = code_pair(x, y, position, a.rope.freq[first + i], a.rope.scale, step);
+            const uint32_t n2 = code_pair(x, y, position_of(a, t0 + j, first + i), a.rope.freq[first + i], a.rope.scale, step);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 nu[k] = k == i ? (int8_t)(n2 & 255) : nu[k];
@@ -483,7 +504,9 @@ cudaError_t write_typed(const CacheWriteArgs &a, cudaStream_t stream) {
     const int64_t waves = (all + slots * kTokens - 1) / (slots * kTokens);
     int per_cta = (int)((all + slots * waves - 1) / (slots * waves));
     per_cta = per_cta < 1 ? 1 : per_cta > kTokens ? kTokens : per_cta;
-    cache_write_kernel<T><<<dim3((unsigned)((a.T + per_cta - 1) / per_cta), (unsigned)groups), threads, 0, stream>>>(a, items, shift, per_cta);
+    const dim3 grid((unsigned)((a.T + per_cta - 1) / per_cta), (unsigned)groups);
+    if (a.dense_len) cache_write_kernel<T, true><<<grid, threads, 0, stream>>>(a, items, shift, per_cta);
+    else cache_write_kernel<T, false><<<grid, threads, 0, stream>>>(a, items, shift, per_cta);
     return cudaGetLastError();
 }
 

@@ -1,4 +1,4 @@
-// What the kernels of HCCS attention over the int8 cache share.
+// What the kernels of HCCS attention over the int8 cache share (they serve attention to an encoder's states as well: CROSS).
 //
 // With r_j = max(x_j + D - m, 0) in 0..127 a score is s_j = F + S*r_j, F = B - S*D >= 0, so that
 //     Z = F*count + S*sum r,   sum s V = F*sum V + S*sum r V
@@ -22,13 +22,26 @@ namespace hccs {
 struct SequenceAt {
     int s0, nq;        // first token, number of queries (those beyond max_q are not computed)
     int n;             // keys that may be seen
-    int prefix;        // keys before the new ones (negative where there are fewer keys than queries)
+    int prefix;        // keys before the new ones (negative where there are fewer keys than queries); cross: all of them
+    int k0;            // cross: the first key's place among the states
     bool cut;          // a length was beyond its bound
 };
+template <bool CROSS = false>
 __device__ __forceinline__ SequenceAt sequence_at(const CachedAttnArgs &a, int b) {
     SequenceAt q;
     const int s0 = min(max(a.q_start[b], 0), a.T), s1 = min(max(a.q_start[b + 1], s0), a.T);
     const int kv = a.kv_len[b];
+    if constexpr (CROSS) {
+        const int k0 = a.k_start[b];
+        q.s0 = s0;
+        q.nq = s1 - s0;
+        q.k0 = k0;
+        q.n = k0 < 0 || k0 > a.states ? 0 : max(min(min(kv, a.states - k0), a.max_kv), 0);
+        q.prefix = q.n;
+        q.cut = q.n != kv || k0 < 0 || k0 > a.states || q.nq > a.max_q;
+        return q;
+    }
+    q.k0 = 0;
     const int pos = (int)max(min((int64_t)kv, (int64_t)a.max_pages << a.page_shift), (int64_t)0);
     q.s0 = s0;
     q.nq = s1 - s0;
@@ -138,6 +151,21 @@ inline bool make_page_map(CUtensorMap *map, const void *pool, const CachedAttnAr
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void *>(pool), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
               d == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Keys or values of an encoder's states, [states][Hkv][D] bytes, boxes of `most` keys of one head, swizzled over the whole row.
+inline bool make_states_map(CUtensorMap *map, const void *states, int64_t stride, const CachedAttnArgs &a, int most) {
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    const int d = a.d;
+    const bool none = a.states == 0;           // (no load is ever issued then, but a map has an address and an extent)
+    const cuuint64_t dims[3] = {(cuuint64_t)d, (cuuint64_t)a.Hkv, (cuuint64_t)(none ? 1 : a.states)};
+    const cuuint64_t strides[2] = {(cuuint64_t)d, (cuuint64_t)(none ? (int64_t)a.Hkv * d : stride)};
+    const cuuint32_t box[3] = {(cuuint32_t)d, 1, (cuuint32_t)most};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void *>(none ? (const void *)a.Q : states), dims, strides, box, estr,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, d == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // Raises a kernel's limits (dynamic shared memory, clusters of sixteen) once per kernel and device: `done` is the

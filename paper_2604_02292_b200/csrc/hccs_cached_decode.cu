@@ -79,7 +79,9 @@ struct Sizes {
 
 // D: head dim.  HI: more than 8 rows (the fragments' rows 8..15 are rows too; otherwise row 8 is all ones and
 // collects sum V for nothing).  tiles_per_warp bounds what shared memory holds.
-template <int D, bool HI, int W>
+// CROSS: queries on an encoder's states.  The rows of a kv head are its (query, head) pairs, all of which see the same keys:
+// those of the sequence, or where max_q is 1 those of the query's key range.
+template <int D, bool HI, int W, bool CROSS>
 __global__ void __launch_bounds__(32 * W, 16 / W)
 cached_decode_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_constant__ CUtensorMap map_k,
                      const __grid_constant__ CUtensorMap map_v, int row_tiles, int tiles_per_warp) {
@@ -105,25 +107,36 @@ cached_decode_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_cons
     uint8_t *const smem = smem_raw + (((smem_u32(smem_raw) + 1023u) & ~1023u) - smem_u32(smem_raw));      // (the swizzles count from there)
     if (tid == 0) abort_flag = 0;
     if (split > 1) cluster_arrive();           // the other CTAs run: waited for before the first push
-    const int32_t *table = a.page_table + (int64_t)b * a.max_pages;
+    const int32_t *table = CROSS ? nullptr : a.page_table + (int64_t)b * a.max_pages;
     // tiles in turn to the warps of the cluster: the first does not depend on the length
     const int first = rank * kWarps + warp, stride = kWarps * split;
-    auto page_at = [&](int key) -> int { return (key >> a.page_shift) < a.max_pages ? __ldg(table + (key >> a.page_shift)) : -1; };
+    auto page_at = [&](int key) -> int {
+        if constexpr (CROSS) return 0;
+        return (key >> a.page_shift) < a.max_pages ? __ldg(table + (key >> a.page_shift)) : -1;
+    };
     int page[2] = {page_at(first * kTileKeys), page_at(first * kTileKeys + 16)};
-    const SequenceAt seq = sequence_at(a, b);
-    const int rows = min(kRows, a.group - row0);
+    const SequenceAt seq = sequence_at<CROSS>(a, b);
+    const int rows = CROSS ? min(kRows, min(seq.nq, a.max_q) * a.group - row0) : min(kRows, a.group - row0);
     const int head0 = kvh * a.group + row0;
+    auto query_of = [&](int row) -> int { return CROSS ? (row0 + row) / a.group : 0; };
+    auto head_of = [&](int row) -> int { return CROSS ? kvh * a.group + (row0 + row) % a.group : head0 + row; };
     if (seq.cut && tid == 0 && blockIdx.x + blockIdx.y == 0) atomicOr(a.status, STATUS_BAD_LENGTH);
     // the new token sees the keys before it and, unless a tree mask hides it, itself
     int self = 1;
     if (a.tree_mask && seq.nq > 0) self = a.tree_mask[(int64_t)seq.s0 * a.tree_words] & 1;
-    const int n = min(max(seq.prefix + self, 0), seq.n);
-    const int tiles = seq.nq > 0 ? (n + kTileKeys - 1) / kTileKeys : 0;
+    int n = CROSS ? seq.n : min(max(seq.prefix + self, 0), seq.n), k0 = seq.k0;
+    if (CROSS && a.key_range && seq.nq > 0) {
+        const int2 r = reinterpret_cast<const int2 *>(a.key_range)[seq.s0];
+        const int x = max(r.x, 0);
+        n = max(min(r.y, n) - x, 0);
+        k0 += n > 0 ? x : 0;
+    }
+    const int tiles = seq.nq > 0 && rows > 0 ? (n + kTileKeys - 1) / kTileKeys : 0;
     const int mine = min(first < tiles ? (tiles - first + stride - 1) / stride : 0, tiles_per_warp);
 
     const uint32_t ring = smem_u32(smem) + (uint32_t)(warp * kDepth * S::kTileBytes);
     // logits of a tile: [half of its keys][row, four words of four keys each]; a lane whose row is none has no place
-    const int max_rows = min(kRows, a.group), x_half = 4 * max_rows, x_tile = 2 * x_half;
+    const int max_rows = min(kRows, CROSS ? a.max_q * a.group : a.group), x_half = 4 * max_rows, x_tile = 2 * x_half;
     uint32_t *const xs = reinterpret_cast<uint32_t *>(smem + S::kRing) + warp * x_tile + lane;               // + tile * kWarps * x_tile
     uint32_t *const seen_s = reinterpret_cast<uint32_t *>(smem + S::kRing) + (size_t)tiles_per_warp * kWarps * x_tile + warp;   // + tile * kWarps
     const bool has0 = nn < max_rows, has1 = HI && nn + 8 < max_rows;
@@ -136,13 +149,18 @@ cached_decode_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_cons
     __syncwarp();
     // Copy number x of this warp: K tiles 0 .. mine-1, then V tiles; a box per 16 or 32 keys, those that are not there or whose
     // page is not left out (what the place held is finite, and their logits are masked).
-    const int boxes = a.page_shift < 5 ? 2 : 1;
+    const int boxes = !CROSS && a.page_shift < 5 ? 2 : 1;
     auto copy = [&](int x) {
         if (lane != 0) return;
         const bool values = x >= mine;
         const int key = (first + (values ? x - mine : x) * stride) * kTileKeys;
         const uint32_t dst = ring + (x % kDepth) * S::kTileBytes, bar = smem_u32(&full[warp][x % kDepth]);
         const CUtensorMap *map = values ? &map_v : &map_k;
+        if constexpr (CROSS) {                 // (keys behind the last one seen are some other's, or zeros behind all of them)
+            mbar_expect_tx(bar, (uint32_t)S::kTileBytes);
+            tma_load_3d(dst, map, 0, kvh, k0 + key, bar);
+            return;
+        }
         const bool r0 = (uint32_t)page[0] < (uint32_t)a.num_pages, r1 = boxes == 2 && key + 16 < n && (uint32_t)page[1] < (uint32_t)a.num_pages;
         mbar_expect_tx(bar, (uint32_t)((r0 ? 1 : 0) + (r1 ? 1 : 0)) * (S::kTileBytes / boxes));
         if (r0) tma_load_3d(dst, map, 0, key & ((1 << a.page_shift) - 1), page[0] * a.Hkv + kvh, bar);
@@ -173,7 +191,7 @@ cached_decode_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_cons
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
             int v = min(max(n - key - 16 * hf, 0), 16);
-            if (v > 0 && (uint32_t)page[hf] >= (uint32_t)a.num_pages) {
+            if (!CROSS && v > 0 && (uint32_t)page[hf] >= (uint32_t)a.num_pages) {
                 if (lane == 0) atomicOr(a.status, STATUS_BAD_PAGE);
                 v = 0;
             }
@@ -195,17 +213,17 @@ cached_decode_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_cons
     if (tid < kRows) {
         row_max[tid] = kNone;
         row_sum[tid] = 0;
-        rq_s[tid] = make_requant(tid < rows ? a.mult[head0 + tid] : 0, a.requant_shift);
+        rq_s[tid] = make_requant(tid < rows ? a.mult[head_of(tid)] : 0, a.requant_shift);
     }
     // Q as A fragments: lane (nn, c) holds chunk c (and c + 4) of rows nn and nn + 8
     uint32_t qf[2 * kChunks][4];
     {
-        const int8_t *q = a.Q + ((int64_t)seq.s0 * a.Hq + head0) * D;
+        auto q = [&](int row) -> const int8_t * { return a.Q + (((int64_t)seq.s0 + query_of(row)) * a.Hq + head_of(row)) * D; };
 #pragma unroll
         for (int ch = 0; ch < kChunks; ++ch) {
             uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
-            if (nn < rows && mine > 0) lo = *reinterpret_cast<const uint4 *>(q + nn * D + ch * 64 + c * 16);
-            if (HI && nn + 8 < rows && mine > 0) hi = *reinterpret_cast<const uint4 *>(q + (nn + 8) * D + ch * 64 + c * 16);
+            if (nn < rows && mine > 0) lo = *reinterpret_cast<const uint4 *>(q(nn) + ch * 64 + c * 16);
+            if (HI && nn + 8 < rows && mine > 0) hi = *reinterpret_cast<const uint4 *>(q(nn + 8) + ch * 64 + c * 16);
             qf[2 * ch][0] = lo.x; qf[2 * ch][1] = hi.x; qf[2 * ch][2] = lo.y; qf[2 * ch][3] = hi.y;
             qf[2 * ch + 1][0] = lo.z; qf[2 * ch + 1][1] = hi.z; qf[2 * ch + 1][2] = lo.w; qf[2 * ch + 1][3] = hi.w;
         }
@@ -293,7 +311,7 @@ cached_decode_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_cons
     // c = m + 128 - D per row, negated, in both 16-bit lanes
     auto neg_c = [&](const Requant &rq, int m, int row) -> uint32_t {
         const int top = ((int)requant_top(rq, m) >> 24) + 128;
-        const int v = (row < rows ? a.table[head0 + row].D : 0) - top;
+        const int v = (row < rows ? a.table[head_of(row)].D : 0) - top;
         return prmt((uint32_t)v, 0, 0x1010);
     };
     const uint32_t c0 = neg_c(rq0, m0, nn), c1 = HI ? neg_c(rq1, m1, nn + 8) : 0u;
@@ -431,13 +449,13 @@ cached_decode_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_cons
                 rs += all_sum[r][row];
                 keys += all_sum[r][kRows];
             }
-            const int h = head0 + row;
+            const int h = head_of(row);
             const HeadEntry th = a.table[h];
             const int64_t F = th.B - th.S * th.D;
             int64_t num[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) num[e] = F * vs[e] + (int64_t)th.S * rv[e];
-            store_output4(a, ((int64_t)seq.s0 * a.Hq + h) * D + 4 * (q * split + rank), num, row_factor(a, F * keys + (int64_t)th.S * rs, a.scale[h]));
+            store_output4(a, (((int64_t)seq.s0 + query_of(row)) * a.Hq + h) * D + 4 * (q * split + rank), num, row_factor(a, F * keys + (int64_t)th.S * rs, a.scale[h]));
         }
 }
 
@@ -452,12 +470,12 @@ struct Plan { int split, per_warp; double cost; };      // cost: infinite where 
 // heads x 4096 keys: s = 1, 2, 4: 44, 53, 66 us (the formula: 46, 59, 71); 8 kv heads x 131072 keys: eight warps, s = 8, 10, 16: 100,
 // 81, 72 (106, 86, 86), sixteen warps, s = 8, 9, 10, 11: 71, 65, 60, 108 (85, 76, 69, 127; from eleven on the device holds seven
 // clusters at a time); 512 x 8192: sixteen warps, s = 1: 174; eight warps, s = 1, 2, 4: 198, 181, 205 (210; 203, 213, 223).
-template <int D, bool HI, int W>
-cudaError_t plan_for(const CachedAttnArgs &a, int64_t groups, Plan &best) {
+template <int D, bool HI, int W, bool CROSS>
+cudaError_t plan_for(const CachedAttnArgs &a, int64_t groups, int rows, Plan &best) {
     using S = Sizes<D, HI, W>;
     static Active known[64];
     static std::atomic<bool> raised[64];
-    auto kernel = cached_decode_kernel<D, HI, W>;
+    auto kernel = cached_decode_kernel<D, HI, W, CROSS>;
     cudaError_t e = raise_limits((const void *)kernel, (int)kMaxSmem, raised);
     const Active *active = nullptr;
     if (e == cudaSuccess) e = active_clusters(kernel, 32 * W, kMaxSmem, known, &active);
@@ -467,7 +485,7 @@ cudaError_t plan_for(const CachedAttnArgs &a, int64_t groups, Plan &best) {
     const double bytes = 2.0 * a.max_kv * D;
     for (int s = 1; s <= kMaxSplit; ++s) {
         const int per = (tiles + s * W - 1) / (s * W);
-        const size_t smem = S::smem(per * W, a.group);
+        const size_t smem = S::smem(per * W, rows);
         if (smem > kMaxSmem || active->n[s] < 1) continue;
         if (s > 1 && per < 2 && (tiles + (s - 1) * W - 1) / ((s - 1) * W) == per) break;      // no warp has less to do
         const int64_t at_a_time = (int64_t)active->n[s] * (W == 8 && smem <= kHalfSmem ? 2 : 1);
@@ -482,14 +500,16 @@ cudaError_t plan_for(const CachedAttnArgs &a, int64_t groups, Plan &best) {
     return cudaSuccess;
 }
 
-template <int D, bool HI, int W>
-cudaError_t launch_plan(const CachedAttnArgs &a, const Plan &p, int row_tiles, cudaStream_t stream) {
+template <int D, bool HI, int W, bool CROSS>
+cudaError_t launch_plan(const CachedAttnArgs &a, const Plan &p, int rows, int row_tiles, cudaStream_t stream) {
     CUtensorMap mk, mv;
-    if (!make_page_map(&mk, a.k_pages, a, kTileKeys) || !make_page_map(&mv, a.v_pages, a, kTileKeys)) return cudaErrorInvalidValue;
+    if (CROSS ? !make_states_map(&mk, a.k_pages, a.k_stride, a, kTileKeys) || !make_states_map(&mv, a.v_pages, a.v_stride, a, kTileKeys)
+              : !make_page_map(&mk, a.k_pages, a, kTileKeys) || !make_page_map(&mv, a.v_pages, a, kTileKeys))
+        return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)p.split, (unsigned)(a.Hkv * row_tiles), (unsigned)a.B);
     cfg.blockDim = dim3(32 * W);
-    cfg.dynamicSmemBytes = Sizes<D, HI, W>::smem(p.per_warp * W, a.group);
+    cfg.dynamicSmemBytes = Sizes<D, HI, W>::smem(p.per_warp * W, rows);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -498,29 +518,37 @@ cudaError_t launch_plan(const CachedAttnArgs &a, const Plan &p, int row_tiles, c
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, cached_decode_kernel<D, HI, W>, a, mk, mv, row_tiles, p.per_warp);
+    return cudaLaunchKernelEx(&cfg, cached_decode_kernel<D, HI, W, CROSS>, a, mk, mv, row_tiles, p.per_warp);
 }
 
-template <int D, bool HI>
+template <int D, bool HI, bool CROSS>
 cudaError_t launch_typed(const CachedAttnArgs &a, cudaStream_t stream) {
     constexpr int kRows = Sizes<D, HI, 8>::kRows;
-    const int row_tiles = (a.group + kRows - 1) / kRows;
+    const int rows = CROSS ? a.max_q * a.group : a.group;           // of a kv head
+    const int row_tiles = (rows + kRows - 1) / kRows;
     const int64_t groups = (int64_t)a.B * a.Hkv * row_tiles;
     Plan p8, p16;
-    cudaError_t e = plan_for<D, HI, 8>(a, groups, p8);
-    if (e == cudaSuccess) e = plan_for<D, HI, 16>(a, groups, p16);
+    cudaError_t e = plan_for<D, HI, 8, CROSS>(a, groups, rows, p8);
+    if (e == cudaSuccess) e = plan_for<D, HI, 16, CROSS>(a, groups, rows, p16);
     if (e != cudaSuccess) return e;
     // (sixteen warps' rings leave no room for the logits of many rows of long caches: d = 128, 16 rows, more than 81920 keys;
     // eight warps in clusters of sixteen hold all that is allowed)
     if (p8.cost == HUGE_VAL && p16.cost == HUGE_VAL) return cudaErrorInvalidConfiguration;
-    return p16.cost < p8.cost ? launch_plan<D, HI, 16>(a, p16, row_tiles, stream) : launch_plan<D, HI, 8>(a, p8, row_tiles, stream);
+    return p16.cost < p8.cost ? launch_plan<D, HI, 16, CROSS>(a, p16, rows, row_tiles, stream)
+                              : launch_plan<D, HI, 8, CROSS>(a, p8, rows, row_tiles, stream);
+}
+
+template <bool CROSS>
+cudaError_t launch_rows_of_kv_heads(const CachedAttnArgs &a, int rows, cudaStream_t stream) {
+    if (a.d == 128) return rows > 8 ? launch_typed<128, true, CROSS>(a, stream) : launch_typed<128, false, CROSS>(a, stream);
+    return rows > 8 ? launch_typed<64, true, CROSS>(a, stream) : launch_typed<64, false, CROSS>(a, stream);
 }
 
 }  // namespace
 
-cudaError_t launch_cached_decode(const CachedAttnArgs &a, cudaStream_t stream) {
-    if (a.d == 128) return a.group > 8 ? launch_typed<128, true>(a, stream) : launch_typed<128, false>(a, stream);
-    return a.group > 8 ? launch_typed<64, true>(a, stream) : launch_typed<64, false>(a, stream);
+cudaError_t launch_cached_decode(const CachedAttnArgs &a, cudaStream_t stream) { return launch_rows_of_kv_heads<false>(a, a.group, stream); }
+cudaError_t launch_cross_decode(const CachedAttnArgs &a, cudaStream_t stream) {
+    return launch_rows_of_kv_heads<true>(a, a.max_q * a.group, stream);
 }
 
 }  // namespace hccs

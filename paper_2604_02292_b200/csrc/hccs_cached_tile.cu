@@ -74,12 +74,22 @@ struct TileBarriers {
 
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+// Keys [x, y) that query q of a sequence sees of an encoder's states: x = y = 0 where none.
+__device__ __forceinline__ int2 range_of(const CachedAttnArgs &a, const SequenceAt &seq, int q) {
+    if (!a.key_range) return make_int2(0, seq.n);
+    const int2 r = reinterpret_cast<const int2 *>(a.key_range)[(int64_t)seq.s0 + q];
+    const int x = max(r.x, 0), y = min(r.y, seq.n);
+    return x < y ? make_int2(x, y) : make_int2(0, 0);
+}
 __device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; }
 
 template <int D> constexpr int kSlotsOf = D == 128 ? 8 : kMaxSlots;
 template <int D> constexpr uint32_t kIdescPVOf = instr_desc(0, 1, 1, 128, D);   // r.V and mask.V: uint8 x int8, V MN-major
 
-template <int D>
+// CROSS: queries on an encoder's states.  A row sees keys [first, end) of its sequence, all of them where there are no key
+// ranges; the blocks that every row of the tile sees whole come first, then the others (the order of blocks is free:
+// the sums are exact).
+template <int D, bool CROSS>
 __global__ void __launch_bounds__(kThreads, 1)
 cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_constant__ CUtensorMap map_k,
                    const __grid_constant__ CUtensorMap map_v, int split, int tile_rows) {
@@ -106,7 +116,7 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
     const int b = blockIdx.z, kvh = blockIdx.y;
     const int rank = (int)blockIdx.x % split;
     const int rt = (int)(gridDim.x / split - 1 - blockIdx.x / split);      // the tiles with the most keys first
-    const SequenceAt seq = sequence_at(a, b);
+    const SequenceAt seq = sequence_at<CROSS>(a, b);
     if (seq.cut && tid == 0 && blockIdx.x + blockIdx.y == 0) atomicOr(a.status, STATUS_BAD_LENGTH);
     const int queries = min(seq.nq, a.max_q);
     const int row0 = rt * tile_rows;
@@ -118,12 +128,29 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
     // key blocks of the tile (of its last query, where the rows are causal), and this CTA's share of them
     const int last_query = (row0 + vrows - 1) / a.group;
     const int n_tile = a.tree_mask ? seq.n : min(max(seq.prefix + last_query + 1, 0), seq.n);
-    const int blocks = (n_tile + kTile - 1) / kTile;
+    int first_any = 0, first_all = 0, end_any = n_tile, end_all = n_tile;  // CROSS: keys that some row sees, that all rows see
+    if constexpr (CROSS) {
+        if (a.key_range) {
+            __shared__ int seen[4];
+            if (tid == 0) { seen[0] = seq.n; seen[1] = 0; seen[2] = 0; seen[3] = seq.n; }
+            __syncthreads();
+            for (int q = row0 / a.group + tid; q <= last_query; q += kThreads) {
+                const int2 r = range_of(a, seq, q);
+                if (r.x < r.y) { atomicMin(&seen[0], r.x); atomicMax(&seen[2], r.y); }
+                atomicMax(&seen[1], r.x);
+                atomicMin(&seen[3], r.y);
+            }
+            __syncthreads();
+            first_any = seen[0]; first_all = seen[1]; end_any = seen[2]; end_all = seen[3];
+        }
+    }
+    const int blocks_from = CROSS ? min(first_any, end_any) / kTile : 0;
+    const int blocks = CROSS && first_any >= end_any ? 0 : (end_any + kTile - 1) / kTile - blocks_from;
     const int per = (blocks + split - 1) / split;
-    const int kb0 = min(rank * per, blocks), nb = min(kb0 + per, blocks) - kb0;
+    const int kb0 = blocks_from + min(rank * per, blocks), nb = min(min(rank * per, blocks) + per, blocks) - min(rank * per, blocks);
     // the leading blocks that every row sees whole (as long as no page is bad)
     const int seen_first = min(a.tree_mask ? seq.prefix : seq.prefix + row0 / a.group + 1, seq.n);
-    const int32_t *table = a.page_table + (int64_t)b * a.max_pages;
+    const int32_t *table = CROSS ? nullptr : a.page_table + (int64_t)b * a.max_pages;
     volatile int *abortp = &abort_flag;
 
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -159,9 +186,11 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
     if (warp < kCopyWarp || warp >= kCopyWarp + kCopyWarps) {
         const int i0 = warp < kCopyWarp ? tid : tid - 32 * kCopyWarps;
         // pages outside the pools: a look at this CTA's part of the table tells whether the masks have to care
-        const int key_end = min((kb0 + nb) * kTile, seq.n);
-        for (int p = (kb0 * kTile >> a.page_shift) + i0; (int64_t)p << a.page_shift < key_end; p += kOthers)
-            if ((uint32_t)table[p] >= (uint32_t)a.num_pages) any_bad = 1;
+        if constexpr (!CROSS) {
+            const int key_end = min((kb0 + nb) * kTile, seq.n);
+            for (int p = (kb0 * kTile >> a.page_shift) + i0; (int64_t)p << a.page_shift < key_end; p += kOthers)
+                if ((uint32_t)table[p] >= (uint32_t)a.num_pages) any_bad = 1;
+        }
         // Q, swizzled by hand: the rows of a tile are (query, head) pairs, not a box of the tensor
         constexpr int kChunks = D / 16;
         for (int i = i0; i < kTile * kChunks; i += kOthers) {
@@ -180,7 +209,14 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
     const uint32_t tmem = tmem_slot;
     const bool bad = any_bad != 0;
     if (bad && tid == 0) atomicOr(a.status, STATUS_BAD_PAGE);
-    const int nfull = bad ? 0 : min(max(seen_first / kTile - kb0, 0), nb);
+    // whole blocks of this CTA's share, number full0 of it on: the first of the share, or CROSS, taken first all the same
+    const int full0 = CROSS ? min(max((first_all + kTile - 1) / kTile - kb0, 0), nb) : 0;
+    const int nfull = CROSS ? max(min(end_all / kTile - kb0, nb) - full0, 0) : bad ? 0 : min(max(seen_first / kTile - kb0, 0), nb);
+    // the first key of block number kb in the order in which they are taken
+    auto key_of = [&](int kb) -> int {
+        if constexpr (CROSS) kb = kb < nfull ? full0 + kb : kb - nfull < full0 ? kb - nfull : kb;
+        return (kb0 + kb) * kTile;
+    };
     const int w0 = spare ? nfull : 0;                                      // first block whose mask.V is computed
     auto wait = [&](uint64_t *bar, uint32_t parity) { return warp_wait(smem_u32(bar), parity, abortp, a.status, a.wait_cycles); };
 
@@ -188,14 +224,15 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
         // ===================================================== copies: load number x by warp x % kCopyWarps (a thread
         // gets through one TMA copy per several hundred cycles, the copies of different warps and lanes overlap)
         if (split > 1) cluster_arrive();
-        const int box = min(1 << a.page_shift, kTile), boxes = kTile / box;
+        const int box = CROSS ? kTile : min(1 << a.page_shift, kTile), boxes = kTile / box;
         const int loads = 3 * nb;
         bool ok = true;
         // lane l of `boxes` copies keys l * box ... of the block; keys that are not there, or whose page is not, are left
         // out (their masks are clear and what the slot held is finite).  The page of the next load is looked up early.
         auto block_of = [&](int x) { return x < nb ? x : (x - nb) >> 1; };
         auto page_of = [&](int x) -> int {
-            const int key = (kb0 + block_of(x)) * kTile + lane * box;
+            if constexpr (CROSS) return lane == 0 ? 0 : -1;               // (a block that some row sees has keys)
+            const int key = key_of(block_of(x)) + lane * box;
             int page = -1;
             if (lane < boxes && key < seq.n) page = __ldg(table + (key >> a.page_shift));
             return page;
@@ -204,7 +241,7 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
         int page = x0 < loads ? page_of(x0) : -1, sent = -1;
         for (int x = x0; ok && x < loads; x += kCopyWarps) {
             const bool values = x >= nb && ((x - nb) & 1);
-            const bool there = (uint32_t)page < (uint32_t)a.num_pages;
+            const bool there = CROSS ? page == 0 : (uint32_t)page < (uint32_t)a.num_pages;
             const int count = __popc(__ballot_sync(~0u, there));
             const int next = x + kCopyWarps < loads ? page_of(x + kCopyWarps) : -1;
             if (x >= kSlots) ok = wait(&bars.free[x % kSlots], (x / kSlots - 1) & 1);
@@ -212,9 +249,13 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
             const uint32_t bar = smem_u32(&bars.full[x % kSlots]);
             if (lane == 0) mbar_expect_tx(bar, (uint32_t)(count * box * D));
             __syncwarp();
-            if (there)
-                tma_load_3d(s_ring + (x % kSlots) * kTileBytes + lane * box * D, values ? &map_v : &map_k, 0,
-                            (block_of(x) * kTile + kb0 * kTile + lane * box) & ((1 << a.page_shift) - 1), page * a.Hkv + kvh, bar);
+            if (there) {
+                const int key = key_of(block_of(x)) + lane * box;
+                const uint32_t dst = s_ring + (x % kSlots) * kTileBytes + lane * box * D;
+                // (keys behind the sequence's last are some other's, or zeros behind all of them; their masks are clear)
+                if constexpr (CROSS) tma_load_3d(dst, values ? &map_v : &map_k, 0, kvh, seq.k0 + key, bar);
+                else tma_load_3d(dst, values ? &map_v : &map_k, 0, key & ((1 << a.page_shift) - 1), page * a.Hkv + kvh, bar);
+            }
             page = next;
             sent = x;
         }
@@ -312,11 +353,13 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
         int rsum = 0, count = 0;
         int xmax = 0, kb;
         // which of keys 64 * half + 32 * part ... of block kb the thread's row sees
-        const int seen_all = !real ? 0 : min(a.tree_mask ? seq.prefix : seq.prefix + qi + 1, seq.n);
+        const int2 range = !CROSS || !real ? make_int2(0, 0) : range_of(a, seq, qi);
+        const int seen_all = !real ? 0 : CROSS ? range.y : min(a.tree_mask ? seq.prefix : seq.prefix + qi + 1, seq.n);
         const uint32_t *tree = a.tree_mask ? reinterpret_cast<const uint32_t *>(a.tree_mask) + ((int64_t)seq.s0 + qi) * a.tree_words : nullptr;
         auto mask_of = [&](int kb, int part) -> uint32_t {
-            const int c0 = (kb0 + kb) * kTile + half * 64 + part * 32;
+            const int c0 = key_of(kb) + half * 64 + part * 32;
             uint32_t m = low_bits(seen_all - c0);
+            if constexpr (CROSS) return m & ~low_bits(range.x - c0);
             if (tree && real && m != 0xffffffffu) {
                 // new key number j0 + k sits at bit k; words beyond max_q's last are never read
                 const int j0 = c0 - seq.prefix;
@@ -603,7 +646,7 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
     }
 }
 
-template <int D>
+template <int D, bool CROSS>
 cudaError_t launch_typed(const CachedAttnArgs &a, cudaStream_t stream) {
     const int64_t rows = (int64_t)a.max_q * a.group;
     // Tiles of 127 rows leave room for the row of ones; full ones are taken where a row less would mean a tile more,
@@ -615,7 +658,7 @@ cudaError_t launch_typed(const CachedAttnArgs &a, cudaStream_t stream) {
     const int64_t ctas = (int64_t)row_tiles * a.Hkv * a.B;
     constexpr size_t smem = 1024 + (size_t)(1 + kSlotsOf<D>) * kTile * D + 4 * kPanelBytes;
     static_assert(smem - 1024 >= 2 * sizeof(int) * kTile * (D + 4), "the joined sums fit the operands' place");
-    auto kernel = cached_tile_kernel<D>;
+    auto kernel = cached_tile_kernel<D, CROSS>;
     static std::atomic<bool> raised[64];
     static Active known[64];
     const Active *active = nullptr;
@@ -636,7 +679,9 @@ cudaError_t launch_typed(const CachedAttnArgs &a, cudaStream_t stream) {
     if (best < 0) return cudaErrorInvalidConfiguration;
     if ((int64_t)row_tiles * split > 0x7fffffff) return cudaErrorInvalidValue;
     CUtensorMap mk, mv;
-    if (!make_page_map(&mk, a.k_pages, a, kTile) || !make_page_map(&mv, a.v_pages, a, kTile)) return cudaErrorInvalidValue;
+    if (CROSS ? !make_states_map(&mk, a.k_pages, a.k_stride, a, kTile) || !make_states_map(&mv, a.v_pages, a.v_stride, a, kTile)
+              : !make_page_map(&mk, a.k_pages, a, kTile) || !make_page_map(&mv, a.v_pages, a, kTile))
+        return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(row_tiles * split), (unsigned)a.Hkv, (unsigned)a.B);
     cfg.blockDim = dim3(kThreads);
@@ -656,7 +701,16 @@ cudaError_t launch_typed(const CachedAttnArgs &a, cudaStream_t stream) {
 
 cudaError_t launch_cached_attention(const CachedAttnArgs &a, cudaStream_t stream, uint64_t *launches) {
     const cudaError_t e = a.max_q == 1 ? launch_cached_decode(a, stream)
-                          : a.d == 128 ? launch_typed<128>(a, stream) : launch_typed<64>(a, stream);
+                          : a.d == 128 ? launch_typed<128, false>(a, stream) : launch_typed<64, false>(a, stream);
+    if (e == cudaSuccess && launches) ++*launches;
+    return e;
+}
+
+cudaError_t launch_cross_attention(const CachedAttnArgs &a, cudaStream_t stream, uint64_t *launches) {
+    // up to sixteen rows of a kv head, all of which see the same keys, go through the kernel that is bound by HBM
+    const bool few = a.max_q == 1 || (!a.key_range && (int64_t)a.max_q * a.group <= 16);
+    const cudaError_t e = few ? launch_cross_decode(a, stream)
+                          : a.d == 128 ? launch_typed<128, true>(a, stream) : launch_typed<64, true>(a, stream);
     if (e == cudaSuccess && launches) ++*launches;
     return e;
 }

@@ -68,13 +68,16 @@ struct FusedArgs {
 struct CacheWriteArgs {
     const void *q, *k, *v;
     int64_t q_stride, k_stride, v_stride;       // elements between tokens
-    const int32_t *positions;
+    const int32_t *positions;                   // of token t on axis x: positions[x * axis_stride + t * token_stride]
+    int64_t axis_stride, token_stride;
     const int64_t *slots;
-    int8_t *q8, *k_pages, *v_pages;
+    int8_t *q8, *k_pages, *v_pages;             // (dense: k_pages and v_pages are tensors like q8)
     uint32_t *status;
     int64_t num_slots;                          // num_pages * page_size
     int32_t T, Hq, Hkv, d, page_shift;
+    int32_t dense_len;                          // 0: pages; L: tensors [T/L, heads, L, d]
     hccs_rope_t rope;                           // rot_dim 0: none
+    uint8_t axis[HCCS_MAX_ROT_DIM / 2];         // of pair i
     float step[3 * HCCS_MAX_CACHE_HEADS];       // q, k and v, HCCS_MAX_CACHE_HEADS apart
 };
 
@@ -87,13 +90,18 @@ struct CacheReadArgs {
     float step[2 * HCCS_MAX_CACHE_HEADS];       // k and v
 };
 
+// Attention of new tokens over the cache, and of queries to an encoder's states (cross), where k_pages and v_pages are
+// [states, Hkv, d] with keys k_stride and v_stride bytes apart, and kv_len the keys of a sequence from k_start on.
 struct CachedAttnArgs {
     const int8_t *Q, *k_pages, *v_pages;
     const int32_t *page_table, *q_start, *kv_len, *tree_mask;
     void *O;
+    const int32_t *k_start, *key_range;         // cross
+    int64_t k_stride, v_stride;                 // cross
     const HeadEntry *table;
     uint32_t *status;
     long long wait_cycles;
+    int32_t states;                             // cross
     int32_t tree_words, out_type, recip;        // recip: HCCS_RECIP_*
     int32_t T, B, Hq, Hkv, group, d, max_pages, num_pages, page_shift, max_q, max_kv, requant_shift;
     uint16_t mult[HCCS_MAX_CACHE_HEADS];
@@ -104,6 +112,8 @@ cudaError_t launch_cache_write(const CacheWriteArgs &a, int type, cudaStream_t s
 cudaError_t launch_cache_read(const CacheReadArgs &a, int type, cudaStream_t stream, uint64_t *launches);
 cudaError_t launch_cached_decode(const CachedAttnArgs &a, cudaStream_t stream);      // max_q == 1
 cudaError_t launch_cached_attention(const CachedAttnArgs &a, cudaStream_t stream, uint64_t *launches);
+cudaError_t launch_cross_decode(const CachedAttnArgs &a, cudaStream_t stream);       // few rows per kv head; max_q == 1 with key ranges
+cudaError_t launch_cross_attention(const CachedAttnArgs &a, cudaStream_t stream, uint64_t *launches);
 
 // Launchers.  Each returns the CUDA error of the launch and adds to *launches.
 cudaError_t launch_rows(const int8_t *logits, void *probs, const RowArgs &a, uint32_t flags,

@@ -1,0 +1,434 @@
+"""Rotary positions with several axes, written to a cache or to dense states, and HCCS attention to states of another length.
+
+Codes and integer outputs are compared for equality, float outputs with the tolerances of test_cache.compare: one product
+of an exact integer with a rounded factor.
+"""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+
+from oracle import hccs_cache_oracle as orc
+from test_cache import _f, _theta, _torch_type, _values, compare
+
+TYPES = ("bf16", "f16", "f32")
+
+
+# ------------------------------------------------------------------------------------------- host only
+@pytest.fixture(scope="module")
+def binding():
+    from paper_2604_02292_b200 import build
+    build.build()
+    from paper_2604_02292_b200 import binding as b
+    return b
+
+
+@pytest.mark.parametrize("pairs", [(16, 24, 24), (64,), (1, 62, 1), (16, 16), (0, 8, 8), (5, 0, 3, 24), (24, 20, 20), (7, 9)])
+@pytest.mark.parametrize("restart", [False, True])
+def test_rope_axes_by_their_definition(binding, pairs, restart):
+    b = binding
+    half = sum(pairs)
+    sections = [x for x, n in enumerate(pairs) for _ in range(n)]
+    left, turns, x = list(pairs), [], 0
+    while len(turns) < half:
+        if left[x]:
+            turns.append(x)
+            left[x] -= 1
+        x = (x + 1) % len(pairs)
+    for order, want in ((b.HCCS_AXES_SECTIONS, sections), (b.HCCS_AXES_TURNS, turns)):
+        r = b.hccs_rope_axes(2 * half, pairs, base=500.0, interleaved=True, order=order, restart=restart, kind=b.HCCS_ROPE_LINEAR, factor=3.0)
+        assert r.num_axes == len(pairs) and r.rope.rot_dim == 2 * half and r.rope.interleaved == 1 and r.rope.scale == 1.0
+        assert list(r.axis)[:half] == want and not any(list(r.axis)[half:])
+        seen = [0] * len(pairs)
+        for i, a in enumerate(want):
+            f = 500.0 ** (-seen[a] / pairs[a]) if restart else 500.0 ** (-i / half)
+            assert math.isclose(r.rope.freq[i], f / 3, rel_tol=1e-13), (i, a)
+            seen[a] += 1
+    one = b.hccs_rope_frequencies(2 * half, 500.0)
+    r = b.hccs_rope_axes(2 * half, (half,), base=500.0, restart=restart)
+    assert list(r.rope.freq) == list(one.freq)             # one axis is the plain call
+
+
+def test_rope_axes_refusals(binding):
+    b = binding
+    for kw in (dict(rot_dim=0, pairs=(0,)), dict(rot_dim=63, pairs=(31,)), dict(pairs=(16, 17)), dict(pairs=(16, 15)), dict(pairs=(-1, 33)),
+               dict(pairs=()), dict(pairs=(8, 8, 8, 4, 4)), dict(order=2), dict(order=-1), dict(base=1.0), dict(kind=9),
+               dict(pairs=(1, 31), restart=True, kind=2, factor=2.0)):
+        args = dict(rot_dim=64, pairs=(16, 16))
+        args.update(kw)
+        with pytest.raises(b.HccsError) as ei:
+            b.hccs_rope_axes(**args)
+        assert ei.value.status == b.HCCS_ERR_INVALID_ARG, kw
+    lib = b.raw()
+    assert lib.hccs_rope_axes(None, 64, 0, 1e4, None, ctypes.byref((ctypes.c_int32 * 1)(32)), 1, 0, 0) == b.HCCS_ERR_INVALID_ARG
+    assert lib.hccs_rope_axes(ctypes.byref(b.RopeAxes()), 64, 0, 1e4, None, None, 1, 0, 0) == b.HCCS_ERR_INVALID_ARG
+    for args in (([1.0], [0, 1]), ([1.0], [4]), ([1.0], [-1]), ([1.0] * 65, [0] * 65)):
+        with pytest.raises(ValueError):
+            b.RopeAxes(*args)
+    with pytest.raises(ValueError):
+        b.RopeAxes([1.0, 1.0], [0, 1], num_axes=1)
+
+
+def test_write_refusals_without_a_gpu(binding):
+    """Argument checks that need no context come first; what passes them all ends at the NULL context."""
+    b, lib = binding, binding.raw()
+    P = 4096                                               # an aligned address that is never read
+    two = _f(0.1, 0.1)
+    good = b.RopeAxes([1.0] * 8, [0, 1, 2, 0, 1, 2, 0, 1])
+    bad_axis, no_axes, many = (b.RopeAxes([1.0] * 8, [0, 1, 2, 0, 1, 2, 0, 1]) for _ in range(3))
+    bad_axis.axis[7] = 3
+    no_axes.num_axes = 0
+    many.num_axes = 5
+
+    def call(paged, **kw):
+        a = dict(q=P, k=P, v=P, type=b.HCCS_F32, qs=64, ks=64, vs=64, pos=P, slots=P, rope=good, q_step=two, k_step=two, v_step=two, q8=P,
+                 k8=P, v8=P, T=6, L=3, Hq=2, Hkv=2, d=64, pages=4, size=16)
+        a.update(kw)
+        ptr = {n: (a[n].ctypes.data if a[n] is not None else None) for n in ("q_step", "k_step", "v_step")}
+        head = (None, a["q"], a["k"], a["v"], a["type"], a["qs"], a["ks"], a["vs"], a["pos"], 6, 1)
+        rope = ctypes.byref(a["rope"]) if a["rope"] else None
+        tail = (rope, ptr["q_step"], ptr["k_step"], ptr["v_step"], a["q8"], a["k8"], a["v8"], a["T"])
+        if paged:
+            return lib.hccs_cache_write_axes(*head, a["slots"], *tail, a["Hq"], a["Hkv"], a["d"], a["pages"], a["size"], None)
+        return lib.hccs_states_write(*head, *tail, a["L"], a["Hq"], a["Hkv"], a["d"], None)
+    I, U = b.HCCS_ERR_INVALID_ARG, b.HCCS_ERR_UNSUPPORTED
+    for paged in (True, False):
+        assert call(paged) == I                            # the NULL context
+        for kw in (dict(T=-1), dict(type=0), dict(type=9), dict(k=None), dict(v=None), dict(Hkv=0), dict(Hkv=257), dict(Hq=0), dict(Hq=257),
+                   dict(q_step=None), dict(k_step=_f(0.1, 0.0)), dict(v_step=_f(0.1, np.nan)), dict(rope=bad_axis), dict(rope=no_axes),
+                   dict(rope=many), dict(rope=b.RopeAxes([1.0] * 33, [0] * 33)), dict(rope=b.RopeAxes([np.inf], [0])), dict(pos=None),
+                   dict(q8=None), dict(k8=None), dict(v8=None)):
+            assert call(paged, **kw) == I, kw
+        for kw in (dict(d=32), dict(q=P + 8), dict(k=P + 4), dict(q8=P + 1), dict(k8=P + 8), dict(v8=P + 8), dict(qs=65), dict(vs=67),
+                   dict(type=b.HCCS_BF16, qs=68)):
+            assert call(paged, **kw) == U, kw
+    for kw in (dict(slots=None), dict(size=24), dict(pages=0)):
+        assert call(True, **kw) == I, kw
+    for kw in (dict(L=0), dict(L=-3), dict(L=4), dict(L=7)):
+        assert call(False, **kw) == I, kw
+
+
+def test_cross_refusals_without_a_gpu(binding):
+    b, lib = binding, binding.raw()
+    P = 4096
+    I, U = b.HCCS_ERR_INVALID_ARG, b.HCCS_ERR_UNSUPPORTED
+
+    def call(**kw):
+        a = dict(Q=P, K=P, V=P, ks=128, vs=128, qs=P, k0=P, kl=P, kr=None, mult=np.array([100, 100], np.int32), shift=20, scale=_f(1, 1),
+                 O=P, type=b.HCCS_F32, T=3, S=50, B=2, Hq=2, Hkv=2, d=64, mq=2, mkv=40, flags=0)
+        a.update(kw)
+        return lib.hccs_attention_cross(None, a["Q"], a["K"], a["V"], a["ks"], a["vs"], a["qs"], a["k0"], a["kl"], a["kr"],
+                                        a["mult"].ctypes.data if a["mult"] is not None else None, a["shift"],
+                                        a["scale"].ctypes.data if a["scale"] is not None else None, a["O"], a["type"], a["T"], a["S"], a["B"],
+                                        a["Hq"], a["Hkv"], a["d"], a["mq"], a["mkv"], a["flags"], None)
+    assert call() == I                                     # the NULL context
+    for kw in (dict(T=-1), dict(S=-1), dict(B=-1), dict(mq=-1), dict(mkv=-1), dict(flags=1), dict(flags=4), dict(flags=10), dict(type=7),
+               dict(scale=None), dict(type=b.HCCS_I32), dict(type=b.HCCS_I32, scale=None, flags=b.HCCS_RECIP_REAL),
+               dict(scale=_f(1, np.inf)), dict(mult=None), dict(Hq=3), dict(Hq=0), dict(Hkv=0), dict(Hkv=-1), dict(shift=0), dict(shift=25),
+               dict(mult=np.array([-1, 0], np.int32)), dict(mult=np.array([1 << 13, 0], np.int32)), dict(Q=None), dict(K=None), dict(V=None),
+               dict(qs=None), dict(k0=None), dict(kl=None), dict(O=None), dict(ks=112), dict(vs=0), dict(ks=-128)):
+        assert call(**kw) == I, kw
+    for kw in (dict(d=80), dict(B=65536), dict(mkv=131073), dict(Hq=258), dict(shift=5), dict(Q=P + 1), dict(K=P + 8), dict(V=P + 8),
+               dict(O=P + 4), dict(kr=P + 4), dict(ks=136), dict(vs=1 << 36), dict(mq=(1 << 30) + 1)):
+        assert call(**kw) == U, kw
+
+
+def test_oracle_of_cross_attention_agrees_with_that_of_the_cache():
+    """Queries whose keys are all before them: the same states in pages, or in a row."""
+    rng = np.random.default_rng(11)
+    n, d, hq, hkv = 48, 64, 4, 2
+    q = rng.integers(-64, 64, (3, hq, d), dtype=np.int8)
+    k, v = (rng.integers(-64, 64, (5, hkv, 16, d), dtype=np.int8) for _ in range(2))
+    table = np.array([[3, 1, 4]])
+    theta, mult = _theta(rng, hq, n, False), [2000] * hq
+    seq = [orc.sequence(p, table[0], n) for p in (k, v)]
+    for t in range(3):
+        want = orc.attend(q[t:t + 1], k, v, table, [0, 1], [n], theta, mult, 20)
+        got = orc.cross(q[t:t + 1], *seq, [0, 1], [0], [n], theta, mult, 20)
+        sliced = orc.cross(q[t:t + 1], *seq, [0, 1], [0], [n], theta, mult, 20, [[10, 31]])
+        shifted = orc.cross(q[t:t + 1], *seq, [0, 1], [10], [21], theta, mult, 20)
+        for a, c in zip(want, got):
+            assert (a == c).all()
+        for a, c in zip(sliced, shifted):
+            assert (a == c).all()
+
+
+# ------------------------------------------------------------------------------------------- rotary positions with several axes
+def _tokens(rng, T, hq, hkv, d, dtype):
+    import torch
+    x = torch.from_numpy(rng.standard_normal((T, (hq + 2 * hkv) * d + 16)).astype(np.float32)).to("cuda", _torch_type(dtype))
+    return [x[:, a * d:b * d].unflatten(1, (b - a, d)) for a, b in ((0, hq), (hq, hq + hkv), (hq + hkv, hq + 2 * hkv))]
+
+
+WRITES = [  # hq, hkv, d, pairs, order, restart, interleaved, T
+    (4, 2, 64, (8, 12, 12), 0, False, False, 1), (4, 2, 128, (24, 20, 20), 1, False, False, 37), (3, 3, 64, (8, 8), 0, True, True, 50),
+    (5, 1, 128, (16, 16, 16, 16), 1, True, True, 33), (2, 2, 64, (3, 7), 0, False, False, 20), (8, 2, 128, (1, 1, 1), 1, False, True, 19),
+    (6, 3, 64, (9, 2, 1), 0, True, False, 23), (7, 7, 128, (48,), 0, False, False, 40), (16, 4, 64, (1, 31), 0, False, True, 300)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("hq,hkv,d,pairs,order,restart,interleaved,T", WRITES)
+def test_cache_write_axes(hccs, dtype, hq, hkv, d, pairs, order, restart, interleaved, T):
+    import torch
+    rng = np.random.default_rng(hq * 1000 + d + T)
+    page = 16
+    pages = -(-T // page) + 2
+    q, k, v = _tokens(rng, T, hq, hkv, d, dtype)
+    pos = rng.integers(-50, 131072, (len(pairs), T)).astype(np.int32)
+    slots = rng.permutation(pages * page)[:T].astype(np.int64)
+    if T > 3:
+        slots[2] = -1
+    steps = [rng.uniform(0.005, 0.05, n).astype(np.float32) for n in (hq, hkv, hkv)]
+    steps[0][0] = 0.03125                                  # a power of two: exact ties
+    rope = hccs.hccs_rope_axes(2 * sum(pairs), pairs, interleaved=interleaved, order=order, restart=restart)
+    rope.rope.scale = 1.0 if T % 2 else 1.23
+    half = sum(pairs)
+    freq, axis, scale = list(rope.rope.freq)[:half], list(rope.axis)[:half], rope.rope.scale
+    kp, vp = (rng.integers(-128, 128, (pages, hkv, page, d), dtype=np.int8) for _ in range(2))
+    xq, xk, xv = (t.float().cpu().numpy() for t in (q, k, v))
+    want_q = orc.quantise(orc.rotate_axes(xq, pos, freq, axis, interleaved, scale), steps[0])
+    want_k = orc.write(kp, orc.quantise(orc.rotate_axes(xk, pos, freq, axis, interleaved, scale), steps[1]), slots)
+    want_v = orc.write(vp, orc.quantise(xv, steps[2]), slots)
+    ctx = hccs.Context(0)
+    for positions in (torch.from_numpy(pos).cuda(), torch.from_numpy(np.ascontiguousarray(pos.T)).cuda().t()):       # [axes,T] and [T,axes]
+        q8 = torch.full((T, hq, d), 99, dtype=torch.int8, device="cuda")
+        dk, dv = torch.from_numpy(kp).cuda(), torch.from_numpy(vp).cuda()
+        ctx.hccs_cache_write_axes(q, k, v, q8, dk, dv, positions, torch.from_numpy(slots).cuda(), *steps, rope=rope)
+        assert ctx.hccs_device_status() == 0
+        for name, got, want in (("q", q8, want_q), ("k", dk, want_k), ("v", dv, want_v)):
+            assert (got.cpu().numpy() == want).all(), name
+    if len(pairs) == 1:                                    # one axis: the plain call
+        q9, dk9, dv9 = torch.empty_like(q8), torch.from_numpy(kp).cuda(), torch.from_numpy(vp).cuda()
+        ctx.hccs_cache_write(q, k, v, q9, dk9, dv9, torch.from_numpy(pos[0]).cuda(), torch.from_numpy(slots).cuda(), *steps, rope=rope.rope)
+        assert torch.equal(q9, q8) and torch.equal(dk9, dk) and torch.equal(dv9, dv)
+    ctx.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("batch", [1, 3])
+@pytest.mark.parametrize("hq,hkv,d,pairs,order,restart,interleaved,T", WRITES)
+def test_states_write(hccs, dtype, batch, hq, hkv, d, pairs, order, restart, interleaved, T):
+    """Both layouts, with and without queries, with and without rotation; what lies around the outputs stays."""
+    import torch
+    rng = np.random.default_rng(hq * 1000 + d + T + batch)
+    T = min(T, 60)
+    n = T * batch
+    q, k, v = _tokens(rng, n, hq, hkv, d, dtype)
+    pos = rng.integers(0, 4096, (len(pairs), n)).astype(np.int32)
+    steps = [rng.uniform(0.005, 0.05, m).astype(np.float32) for m in (hq, hkv, hkv)]
+    steps[1][0] = 2.0 ** -5
+    rope = hccs.hccs_rope_axes(2 * sum(pairs), pairs, interleaved=interleaved, order=order, restart=restart)
+    half = sum(pairs)
+    freq, axis = list(rope.rope.freq)[:half], list(rope.axis)[:half]
+    xq, xk, xv = (t.float().cpu().numpy() for t in (q, k, v))
+    turned = [orc.quantise(orc.rotate_axes(x, pos, freq, axis, interleaved, 1.0), s) for x, s in ((xq, steps[0]), (xk, steps[1]))]
+    plain = [orc.quantise(x, s) for x, s in ((xq, steps[0]), (xk, steps[1]), (xv, steps[2]))]
+    ctx = hccs.Context(0)
+    positions = torch.from_numpy(pos).cuda()
+    for heads_first in (False, True):
+        def out(heads):
+            flat = torch.full((n * heads * d + 64,), 77, dtype=torch.int8, device="cuda")
+            shape = (batch, heads, T, d) if heads_first else (n, heads, d)
+            return flat, flat[32:-32].view(shape)
+
+        def tokens_first(t):
+            return (t.transpose(1, 2).reshape(n, -1, d) if heads_first else t).cpu().numpy()
+        for with_q, with_kv, turn in ((True, True, True), (True, False, True), (False, True, True), (True, True, False)):
+            fq, q8 = out(hq)
+            fk, k8 = out(hkv)
+            fv, v8 = out(hkv)
+            ctx.hccs_states_write(q if with_q else None, k if with_kv else None, v if with_kv else None, q8, k8, v8,
+                                  positions if turn else None, *steps, rope=rope if turn else None)
+            assert ctx.hccs_device_status() == 0
+            want = (turned if turn else plain[:2]) + plain[2:]
+            for name, flat, got, w, there in (("q", fq, q8, want[0], with_q), ("k", fk, k8, want[1], with_kv), ("v", fv, v8, want[2], with_kv)):
+                assert (tokens_first(got) == (w if there else 77)).all(), name
+                assert (flat[:32] == 77).all() and (flat[-32:] == 77).all(), name
+    ctx.close()
+
+
+@pytest.mark.gpu
+def test_write_axes_of_far_positions_infinities_and_nan(hccs):
+    """Angles beyond 2^24 radians on one axis alone, values that are none: the pair's own axis decides."""
+    import torch
+    rng = np.random.default_rng(3)
+    d, T, hq = 64, 40, 3
+    x = rng.standard_normal((T, hq, d)).astype(np.float32)
+    x[0, 0, 3], x[1, 1, 40], x[2, 2, ::5] = np.nan, np.inf, -np.inf
+    freq = [1.0] * 8 + [1000.0 ** (-i / 24) for i in range(24)]
+    axis = [1] * 8 + [0] * 24
+    pos = np.stack([np.arange(T), rng.integers(-2**31, 2**31 - 1, T)]).astype(np.int32)
+    step = np.array([0.03, 0.03125, 0.01], np.float32)
+    ctx = hccs.Context(0)
+    q8 = torch.empty((T, hq, d), dtype=torch.int8, device="cuda")
+    ctx.hccs_states_write(torch.from_numpy(x).cuda(), None, None, q8, None, None, torch.from_numpy(pos).cuda(), step, None, None,
+                          rope=hccs.RopeAxes(freq, axis))
+    assert (q8.cpu().numpy() == orc.quantise(orc.rotate_axes(x, pos, freq, axis, False, 1.0), step)).all()
+    ctx.close()
+
+
+@pytest.mark.gpu
+def test_write_refusals_of_the_binding(hccs):
+    import torch
+    ctx = hccs.Context(0)
+    dev = "cuda"
+    q, k = torch.zeros((6, 4, 64), device=dev), torch.zeros((6, 2, 64), device=dev)
+    q8, k8, v8 = (torch.zeros((6, h, 64), dtype=torch.int8, device=dev) for h in (4, 2, 2))
+    pos = torch.zeros((3, 6), dtype=torch.int32, device=dev)
+    rope = hccs.hccs_rope_axes(64, (8, 12, 12))
+    steps = [np.full(h, 0.1, np.float32) for h in (4, 2, 2)]
+
+    def call(**kw):
+        a = dict(q=q, k=k, v=k, q8=q8, k8=k8, v8=v8, pos=pos, rope=rope)
+        a.update(kw)
+        ctx.hccs_states_write(a["q"], a["k"], a["v"], a["q8"], a["k8"], a["v8"], a["pos"], *steps, rope=a["rope"])
+    call()
+    for kw in (dict(pos=pos[:2]), dict(pos=pos[0]), dict(pos=pos[:, :5]), dict(pos=pos.float()), dict(pos=pos.long()), dict(pos=pos.cpu()),
+               dict(q8=q8[:5]), dict(k8=k8.float()), dict(v8=v8.cpu()), dict(q=None, k=None, v=None), dict(v=None), dict(v=k.half()),
+               dict(q8=torch.zeros((2, 4, 2, 64), dtype=torch.int8, device=dev)), dict(k8=torch.zeros((2, 2, 3, 64), dtype=torch.int8, device=dev))):
+        with pytest.raises(ValueError):
+            call(**kw)
+    with pytest.raises(hccs.HccsError):
+        call(pos=None)
+    # nothing to do
+    none = torch.zeros((0, 4, 64), device=dev)
+    ctx.hccs_states_write(none, None, None, q8[:0], None, None, None, steps[0], None, None)
+    ctx.close()
+
+
+# ------------------------------------------------------------------------------------------- cross attention
+def cross(pkg, ctx, rng, q_lens, k_lens, hq, hkv, d, norm="real", dtype="f32", ranges=None, wide=False, shift=20, mult=None, spread=24.0,
+          fused=False, share=None, gap=3, n_design=None, theta=None, q=None, kv=None, max_q=None, check=True, stream=None):
+    """One call and its comparison with the oracle.  gap: states between the sequences' own; share: sequence whose states are read."""
+    import torch
+    T = sum(q_lens)
+    start = np.concatenate([[0], np.cumsum(q_lens)]).astype(np.int32)
+    k_start, at = [], gap
+    for b, n in enumerate(k_lens):
+        if share and share[b] != b:
+            k_start.append(k_start[share[b]])
+        else:
+            k_start.append(at)
+            at += n + gap
+    S = at
+    kv = rng.integers(-128, 128, (S, 2 * hkv, d), dtype=np.int8) if kv is None else kv
+    q = rng.integers(-128, 128, (T, hq, d), dtype=np.int8) if q is None else q
+    n = n_design or max(max(k_lens), 1)
+    theta = _theta(rng, hq, n, wide) if theta is None else theta
+    if mult is None:
+        sigma = 74.0 ** 2 * math.sqrt(d)
+        mult = np.array([min(8191, (1 << (shift - 1)) - 1, int(spread * rng.uniform(0.3, 1.5) / sigma * (1 << shift))) for _ in range(hq)], np.int32)
+    (ctx.hccs_params_upload_wide if wide else ctx.hccs_params_upload)(theta, n)
+    scale = rng.uniform(0.01, 0.05, hq).astype(np.float32)
+    dev = "cuda"
+    out = torch.full((T + 2, hq, d), 77, dtype=_torch_type(dtype), device=dev)         # two rows behind the last sequence
+    Q = torch.full((T + 2, hq, d), 3, dtype=torch.int8, device=dev)
+    Q[:T] = torch.from_numpy(q).to(dev)
+    states = torch.from_numpy(kv).to(dev)
+    K, V = states[:, :hkv], states[:, hkv:]
+    if not fused:
+        K, V = K.contiguous(), V.contiguous()
+    R = None
+    if ranges is not None:
+        R = torch.zeros((T + 2, 2), dtype=torch.int32, device=dev)
+        R[:T] = torch.from_numpy(np.asarray(ranges, np.int32).reshape(T, 2)).to(dev)
+    args = (Q, K, V, torch.from_numpy(start).to(dev), torch.tensor(k_start, dtype=torch.int32, device=dev),
+            torch.tensor(k_lens, dtype=torch.int32, device=dev), out, mult, shift)
+    flags = {"real": pkg.HCCS_RECIP_REAL, "div": 0, "clb": pkg.HCCS_RECIP_CLB}[norm]
+    kw = dict(max_q=max_q or max(max(q_lens), 1), max_kv=max(max(k_lens), 1), key_range=R, out_scale=None if dtype == "i32" else scale, flags=flags)
+    ctx.hccs_attention_cross(*args, **kw)
+    torch.cuda.synchronize()
+    assert (_values(out[T:]) == 77).all(), "rows behind the last sequence were written"
+    if check:
+        num, zs, cnt = orc.cross(q, kv[:, :hkv], kv[:, hkv:], start, k_start, k_lens, theta, mult, shift, ranges)
+        compare(out[:T], num, zs, cnt, norm, dtype, scale)
+        assert ctx.hccs_device_status() == 0
+    return out, (args, kw, theta)
+
+
+@pytest.fixture
+def ctx(hccs):
+    c = hccs.Context(0)
+    yield c
+    c.close()
+
+
+# single queries, few rows: lengths around tiles of 32 keys, heads in groups of every kind
+@pytest.mark.gpu
+@pytest.mark.parametrize("hq,hkv,d", [(1, 1, 64), (3, 3, 128), (8, 2, 64), (7, 1, 128), (16, 1, 64), (12, 1, 128), (40, 2, 128)])
+@pytest.mark.parametrize("norm,dtype", [("div", "i32"), ("clb", "i32"), ("real", "f32"), ("real", "bf16"), ("div", "f16"), ("clb", "bf16")])
+def test_single_queries(hccs, ctx, hq, hkv, d, norm, dtype):
+    rng = np.random.default_rng(hq + d)
+    cross(hccs, ctx, rng, [1, 1, 0, 1, 1, 1], [1, 31, 7, 0, 64, 77], hq, hkv, d, norm, dtype, fused=hq % 2 == 0)
+    cross(hccs, ctx, rng, [1, 1], [333, 2], hq, hkv, d, norm, dtype)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hq,hkv,d,queries", [(1, 1, 64, 16), (2, 2, 128, 9), (4, 2, 64, 5), (3, 1, 128, 5), (8, 2, 128, 4), (5, 1, 64, 3), (8, 1, 64, 2)])
+@pytest.mark.parametrize("norm,dtype", [("div", "i32"), ("real", "f32"), ("real", "f16")])
+def test_few_rows(hccs, ctx, hq, hkv, d, queries, norm, dtype):
+    """Up to sixteen (query, head) rows of a kv head."""
+    rng = np.random.default_rng(hq + d + queries)
+    cross(hccs, ctx, rng, [queries, 1, 0, queries - 1], [150, 33, 20, 1], hq, hkv, d, norm, dtype)
+    cross(hccs, ctx, rng, [queries], [1203], hq, hkv, d, norm, dtype, fused=True)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hq,hkv,d", [(1, 1, 64), (2, 2, 128), (8, 2, 128), (6, 2, 64), (7, 1, 128), (12, 1, 64), (32, 1, 64)])
+@pytest.mark.parametrize("k_lens", [(1, 16, 31, 0, 32), (33, 77, 64, 2, 96), (127, 128, 129, 100, 1), (255, 256, 224, 250, 192), (257, 500, 384, 3, 300)])
+@pytest.mark.parametrize("norm,dtype", [("div", "i32"), ("clb", "f32"), ("real", "f32"), ("real", "bf16")])
+def test_many_queries(hccs, ctx, hq, hkv, d, k_lens, norm, dtype):
+    """Lengths around blocks of 32 and 128 keys, tiles of 128 rows cut by the sequences' ends, sequences without queries or keys."""
+    rng = np.random.default_rng(hq + d + sum(k_lens))
+    cross(hccs, ctx, rng, [129, 40, 0, 17, 300 // hq + 18], k_lens, hq, hkv, d, norm, dtype, fused=hq % 2 == 0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f16", "i32"])
+@pytest.mark.parametrize("d,hq,hkv,length", [(64, 4, 4, 50), (128, 4, 1, 200), (128, 8, 8, 700), (64, 16, 2, 1500)])
+def test_shared_states(hccs, ctx, d, hq, hkv, length, dtype):
+    rng = np.random.default_rng(length)
+    for queries in (1, 30):
+        cross(hccs, ctx, rng, [queries, queries, 2, queries], [length, length, 9, length], hq, hkv, d, "div", dtype, share=[0, 0, 2, 0])
+
+
+def _some_ranges(rng, q_lens, k_lens):
+    out = []
+    for nq, n in zip(q_lens, k_lens):
+        for i in range(nq):
+            kind = rng.integers(0, 6)
+            a, b = sorted(int(v) for v in rng.integers(-3, n + 4, 2))
+            out.append([(0, 0), (0, n), (a, b), (b, a), (a, a + 1), (0, 1 << 30)][kind])
+    return out
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hq,hkv,d", [(2, 2, 64), (8, 2, 128), (5, 1, 128)])
+@pytest.mark.parametrize("norm,dtype", [("div", "i32"), ("real", "f32")])
+@pytest.mark.parametrize("q_lens,k_lens", [((1, 1, 1, 1, 0), (40, 1, 300, 0, 9)), ((20, 3, 1), (500, 30, 0)), ((150, 60), (700, 129))])
+def test_key_ranges(hccs, ctx, hq, hkv, d, norm, dtype, q_lens, k_lens):
+    """Every query its own keys: none, all, one, some in the middle, bounds outside the sequence or in the wrong order."""
+    rng = np.random.default_rng(hq + d + sum(k_lens))
+    for _ in range(3):
+        cross(hccs, ctx, rng, q_lens, k_lens, hq, hkv, d, norm, dtype, ranges=_some_ranges(rng, q_lens, k_lens))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+def test_key_ranges_of_images(hccs, ctx, d):
+    """Texts that see the image they follow: tiles whose rows see one image, two, or none, with whole blocks in the middle."""
+    rng = np.random.default_rng(d)
+    q_lens, k_lens, per = [500, 200], [2404, 1803], 601
+    ranges = []
+    for nq, n in zip(q_lens, k_lens):
+        at = sorted(int(v) for v in rng.integers(0, nq, n // per))
+        for i in range(nq):
+            last = sum(a <= i for a in at) - 1
+            ranges.append((last * per, last * per + per) if last >= 0 else (0, 0))
+    cross(hccs, ctx, rng, q_lens, k_lens, 4, 2, d, "real", "f32", ranges=ranges, wide=True)
+    none = [(0, 0)] * 700
+    out, _ = cross(hccs, ctx, rng, q_lens, k_lens, 4, 2, d, "real", "f32", ranges=none, wide=True)
+    assert (out[:700] == 0).all()
