@@ -18,6 +18,16 @@
 
 namespace hccs {
 
+constexpr int kNone = -(1 << 30);          // below every accumulator
+
+// of a whole warp: one try by all lanes is nearly always enough
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *abortp, uint32_t *status, long long limit) {
+    if (__all_sync(~0u, mbar_try_wait(bar, parity))) return true;
+    return __all_sync(~0u, mbar_wait(bar, parity, abortp, status, limit));
+}
+
+__device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; }
+
 // Where the new tokens and the keys of a sequence are.
 struct SequenceAt {
     int s0, nq;        // first token, number of queries (those beyond max_q are not computed)
@@ -26,21 +36,22 @@ struct SequenceAt {
     int k0;            // cross: the first key's place among the states
     bool cut;          // a length was beyond its bound
 };
+__device__ __forceinline__ SequenceAt cross_sequence(const CachedAttnArgs &a, int q0, int q1, int k0, int kv) {
+    SequenceAt q;
+    q.s0 = min(max(q0, 0), a.T);
+    q.nq = min(max(q1, q.s0), a.T) - q.s0;
+    q.k0 = k0;
+    q.n = k0 < 0 || k0 > a.states ? 0 : max(min(min(kv, a.states - k0), a.max_kv), 0);
+    q.prefix = q.n;
+    q.cut = q.n != kv || k0 < 0 || k0 > a.states || q.nq > a.max_q;
+    return q;
+}
 template <bool CROSS = false>
 __device__ __forceinline__ SequenceAt sequence_at(const CachedAttnArgs &a, int b) {
+    if constexpr (CROSS) return cross_sequence(a, a.q_start[b], a.q_start[b + 1], a.k_start[b], a.kv_len[b]);
     SequenceAt q;
     const int s0 = min(max(a.q_start[b], 0), a.T), s1 = min(max(a.q_start[b + 1], s0), a.T);
     const int kv = a.kv_len[b];
-    if constexpr (CROSS) {
-        const int k0 = a.k_start[b];
-        q.s0 = s0;
-        q.nq = s1 - s0;
-        q.k0 = k0;
-        q.n = k0 < 0 || k0 > a.states ? 0 : max(min(min(kv, a.states - k0), a.max_kv), 0);
-        q.prefix = q.n;
-        q.cut = q.n != kv || k0 < 0 || k0 > a.states || q.nq > a.max_q;
-        return q;
-    }
     q.k0 = 0;
     const int pos = (int)max(min((int64_t)kv, (int64_t)a.max_pages << a.page_shift), (int64_t)0);
     q.s0 = s0;
@@ -108,7 +119,8 @@ __device__ __forceinline__ RowFactor row_factor(const CachedAttnArgs &a, int64_t
     return f;
 }
 // Four neighbouring values as they are stored, in the low `size` words (two or four).
-__device__ __forceinline__ uint4 output4(const CachedAttnArgs &a, const int64_t (&num)[4], const RowFactor &f) {
+template <typename Int>
+__device__ __forceinline__ uint4 output4(const CachedAttnArgs &a, const Int (&num)[4], const RowFactor &f) {
     int o[4];
     float y[4];
 #pragma unroll

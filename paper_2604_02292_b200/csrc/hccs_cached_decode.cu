@@ -29,7 +29,6 @@ namespace {
 
 constexpr int kTileKeys = 32;
 constexpr int kDepth = 2;                  // tiles on their way per warp
-constexpr int kNone = -(1 << 30);          // below every accumulator
 
 __device__ __forceinline__ void mma_s8(int (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"

@@ -43,12 +43,6 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-// of a whole warp: one try by all lanes is nearly always enough
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *abortp, uint32_t *status, long long limit) {
-    if (__all_sync(~0u, mbar_try_wait(bar, parity))) return true;
-    return __all_sync(~0u, mbar_wait(bar, parity, abortp, status, limit));
-}
-
 constexpr int kRowThreads = 512;
 constexpr int kCopyWarp = 16, kCopyWarps = 2, kQkWarp = 18, kPvWarp = kQkWarp + 1;
 constexpr int kThreads = 640;                    // 20 warps: 96 registers a thread
@@ -57,7 +51,6 @@ constexpr int kPanelBytes = kTile * 128;         // 128 rows x 128 keys, 128-byt
 constexpr int kMaxSlots = 12;
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kIdescQK = instr_desc(1, 1, 0, 128, 128);
-constexpr int kNone = -(1 << 30);                // below every accumulator
 
 using Yes = std::true_type;
 using No = std::false_type;
@@ -81,7 +74,6 @@ __device__ __forceinline__ int2 range_of(const CachedAttnArgs &a, const Sequence
     const int x = max(r.x, 0), y = min(r.y, seq.n);
     return x < y ? make_int2(x, y) : make_int2(0, 0);
 }
-__device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; }
 
 template <int D> constexpr int kSlotsOf = D == 128 ? 8 : kMaxSlots;
 template <int D> constexpr uint32_t kIdescPVOf = instr_desc(0, 1, 1, 128, D);   // r.V and mask.V: uint8 x int8, V MN-major
@@ -709,7 +701,7 @@ cudaError_t launch_cached_attention(const CachedAttnArgs &a, cudaStream_t stream
 cudaError_t launch_cross_attention(const CachedAttnArgs &a, cudaStream_t stream, uint64_t *launches) {
     // up to sixteen rows of a kv head, all of which see the same keys, go through the kernel that is bound by HBM
     const bool few = a.max_q == 1 || (!a.key_range && (int64_t)a.max_q * a.group <= 16);
-    const cudaError_t e = few ? launch_cross_decode(a, stream)
+    const cudaError_t e = few ? launch_cross_decode(a, stream) : cross_short_fits(a) ? launch_cross_short(a, stream)
                           : a.d == 128 ? launch_typed<128, true>(a, stream) : launch_typed<64, true>(a, stream);
     if (e == cudaSuccess && launches) ++*launches;
     return e;

@@ -113,6 +113,8 @@ cudaError_t launch_cache_read(const CacheReadArgs &a, int type, cudaStream_t str
 cudaError_t launch_cached_decode(const CachedAttnArgs &a, cudaStream_t stream);      // max_q == 1
 cudaError_t launch_cached_attention(const CachedAttnArgs &a, cudaStream_t stream, uint64_t *launches);
 cudaError_t launch_cross_decode(const CachedAttnArgs &a, cudaStream_t stream);       // few rows per kv head; max_q == 1 with key ranges
+cudaError_t launch_cross_short(const CachedAttnArgs &a, cudaStream_t stream);        // cross_short_fits
+bool cross_short_fits(const CachedAttnArgs &a);
 cudaError_t launch_cross_attention(const CachedAttnArgs &a, cudaStream_t stream, uint64_t *launches);
 
 // Launchers.  Each returns the CUDA error of the launch and adds to *launches.
