@@ -7,13 +7,14 @@
 // K and V stay in shared memory for all tiles of a chunk.  sum V is the same for every row: a warp of its own adds V up once per
 // chunk.  All sums fit int32: |sum r V| < 2^22, S < 2^7, F < 2^15, |sum V| <= 2^15.
 //
-// CTAs are persistent and take chunks (up to `per_chunk` tiles of one sequence and kv head) in turn.  Two stages, each with half
+// CTAs are persistent.  The tiles that the sequences really have are counted at the start and shared out evenly, in order, so a CTA
+// walks through few (sequence, kv head) pairs: chunks of tiles with one K and V.  Two stages, each with half
 // of tensor memory, a Q tile, a panel of r and eight row warps, take the tiles alternately: while one waits for a product or
 // stores its rows, the other has the integer pipe.  O takes columns of its own in the stage's half where the keys leave room,
 // else those of S (all of whose logits have been read twice by then).
 //
-// Roles: sixteen row warps (two threads per row, half of the keys and of the dims each), a warp each for the copies of Q, the
-// copies of K and V, Q.K^T, r.V, and the sums of V.
+// Roles: sixteen row warps (two threads per row, half of the keys and of the dims each), a warp each for the copies, Q.K^T, r.V, and
+// the sums of V.
 #include "hccs_cached.cuh"
 #include "hccs_tcgen05.cuh"
 
@@ -21,8 +22,8 @@ namespace hccs {
 
 namespace {
 
-constexpr int kRowWarps = 16, kQWarp = 16, kKvWarp = 17, kQkWarp = 18, kPvWarp = 19, kSumWarp = 20;
-constexpr int kThreads = 672;                    // 21 warps: 96 registers a thread
+constexpr int kRowWarps = 16, kCopyWarp = 16, kQkWarp = 17, kPvWarp = 18, kSumWarp = 19;
+constexpr int kThreads = 640;                    // 20 warps: 96 registers a thread
 constexpr int kTile = 128;
 constexpr int kStage = 256;                      // threads and tensor-memory columns of a stage
 constexpr int kMaxKeys = 256;
@@ -41,22 +42,142 @@ struct ShortBarriers {
     uint64_t drained[2];                         // a given-up CTA: the products of either issuer are through
 };
 
-// A chunk, the same for every role: up to per_chunk tiles of one sequence and kv head.  What has to be read for it is fetched a
-// chunk ahead.
-struct ChunkRaw { int q0, q1, k0, kv; };
+// A chunk, the same for every role: tiles of one sequence and kv head.
 struct Chunk {
-    int kvh, tile0, tiles;                       // tiles: with rows
+    int kvh, tile0, tiles;
     SequenceAt seq;
 };
 
 struct ShortPlan {
-    int per_chunk, chunks_per, chunks;           // tiles of a chunk, chunks of a (sequence, kv head), all of them
     int keys;                                    // of the K and V tiles: a multiple of 32
     int v_slots;
     int queries;                                 // per tile
 };
 
-template <int D>
+__device__ __forceinline__ int tiles_of(const CachedAttnArgs &a, const SequenceAt &seq, const ShortPlan &plan) {
+    return (min(seq.nq, a.max_q) + plan.queries - 1) / plan.queries;
+}
+
+// The chunks of a CTA, walked through by whole warps: tiles are in the order (sequence, kv head, tile).  A lane holds one of 32
+// neighbouring sequences, so that their lengths are read together and those without queries are skipped together.
+struct Walk {
+    int q0, q1, k0, kv, first;                   // this lane's sequence, number first + lane
+    int b, kvh, tile;
+    int64_t left;                                // tiles still to come
+
+    __device__ __forceinline__ void window(const CachedAttnArgs &a, int from) {
+        const int mine = from + (int)(threadIdx.x & 31);
+        first = from;
+        q0 = q1 = k0 = kv = 0;
+        if (mine < a.B) {
+            q0 = __ldg(a.q_start + mine);
+            q1 = __ldg(a.q_start + mine + 1);
+            k0 = __ldg(a.k_start + mine);
+            kv = __ldg(a.kv_len + mine);
+        }
+    }
+    // false: no more
+    __device__ __forceinline__ bool next(const CachedAttnArgs &a, const ShortPlan &plan, Chunk &k) {
+        if (left <= 0) return false;
+        for (;;) {
+            const SequenceAt mine = cross_sequence(a, q0, q1, k0, kv);
+            const uint32_t some = __ballot_sync(~0u, mine.nq > 0) & ~low_bits(b - first);
+            if (some != 0) {
+                const int from = __ffs(some) - 1;
+                if (first + from != b) { b = first + from; kvh = 0; tile = 0; }
+                break;
+            }
+            b = first + 32;
+            kvh = tile = 0;
+            if (b >= a.B) return false;
+            window(a, b);
+        }
+        const int from = b - first;
+        k.seq = cross_sequence(a, __shfl_sync(~0u, q0, from), __shfl_sync(~0u, q1, from), __shfl_sync(~0u, k0, from), __shfl_sync(~0u, kv, from));
+        const int all = tiles_of(a, k.seq, plan);
+        k.kvh = kvh;
+        k.tile0 = tile;
+        k.tiles = (int)min((int64_t)(all - tile), left);
+        left -= k.tiles;
+        tile = 0;
+        if (++kvh == a.Hkv) { kvh = 0; ++b; }
+        return true;
+    }
+};
+
+// Where a CTA's walk starts, found by one warp: a lane counts the tiles of its share of the sequences.
+__device__ __forceinline__ void find_start(const CachedAttnArgs &a, const ShortPlan &plan, int *start, int64_t *count) {
+    const int lane = threadIdx.x & 31, share = (a.B + 31) / 32, b0 = min(lane * share, a.B), b1 = min(b0 + share, a.B);
+    int64_t mine = 0;
+    bool cut = false;
+#pragma unroll 4
+    for (int b = b0; b < b1; ++b) {
+        const SequenceAt seq = sequence_at<true>(a, b);
+        mine += tiles_of(a, seq, plan);
+        cut |= seq.cut;
+    }
+    if (cut && blockIdx.x == 0) atomicOr(a.status, STATUS_BAD_LENGTH);
+    int64_t upto = mine;                         // of this lane's share and those before it
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t v = __shfl_up_sync(~0u, upto, o);
+        if (lane >= o) upto += v;
+    }
+    const int64_t all = __shfl_sync(~0u, upto, 31) * a.Hkv, per = all / gridDim.x, more = all % gridDim.x;
+    const int64_t from = blockIdx.x * per + min((int64_t)blockIdx.x, more);
+    if (lane == 0) { start[0] = start[1] = start[2] = 0; *count = per + ((int64_t)blockIdx.x < more ? 1 : 0); }
+    __syncwarp();
+    int64_t before = (upto - mine) * a.Hkv;
+    if (from >= before && from < upto * a.Hkv) {
+        for (int b = b0; b < b1; ++b) {
+            const int n = tiles_of(a, sequence_at<true>(a, b), plan);
+            if (from < before + (int64_t)n * a.Hkv) {
+                const int64_t off = from - before;
+                start[0] = b;
+                start[1] = (int)(off / n);
+                start[2] = (int)(off % n);
+                break;
+            }
+            before += (int64_t)n * a.Hkv;
+        }
+    }
+}
+
+// Requantisation of a head (see Requant) without fp64: a quotient of num = c * 2^(sh-1) - less by M is estimated in fp32, off by less than one
+// where it is below 2^22, and put right by its remainder; beyond that it is cut to the accumulators' range.
+struct HeadRequant {
+    uint32_t mk, ck;
+    int lo, hi, M, sh;
+    float unit;                                  // 2^(sh-1) / M
+};
+__device__ __forceinline__ int whole_quotient(const HeadRequant &q, int c, int less) {      // floor((c * 2^(sh-1) - less) / M)
+    int v = (int)floorf(fminf(fmaxf((float)c * q.unit, -0x1p22f), 0x1p22f));
+    const int rest = (int)(((uint32_t)c << (q.sh - 1)) - (uint32_t)less - (uint32_t)v * (uint32_t)q.M);
+    v += rest >= q.M ? 1 : rest < 0 ? -1 : 0;
+    return min(max(v, -kAccLimit), kAccLimit);
+}
+__device__ __forceinline__ HeadRequant head_requant(int M, int sh) {
+    HeadRequant q;
+    q.M = M;
+    q.sh = sh;
+    q.unit = M > 0 ? (float)(1 << (sh - 1)) / (float)M : 0.0f;
+    q.lo = M > 0 ? -whole_quotient(q, 257, 0) : -kAccLimit;
+    q.hi = M > 0 ? whole_quotient(q, 255, 1) : kAccLimit;
+    q.mk = (uint32_t)M << (24 - sh);
+    q.ck = ((uint32_t)q.lo * (uint32_t)M + (1u << (sh - 1))) << (24 - sh);
+    return q;
+}
+
+// N columns of tensor memory (load and wait in one statement)
+__device__ __forceinline__ void tmem_ld(uint32_t at, uint32_t (&r)[16]) { tmem_ld16(at, r); }
+__device__ __forceinline__ void tmem_ld(uint32_t at, uint32_t (&r)[32]) { tmem_ld32(at, r); }
+
+// Values and their products with a factor, two at a time.
+__device__ __forceinline__ void scale2(float &x, float &y, float by) {
+    asm("{\n\t.reg .b64 v, w;\n\tmov.b64 v, {%0, %1};\n\tmov.b64 w, {%2, %2};\n\tmul.rn.f32x2 v, v, w;\n\tmov.b64 {%0, %1}, v;\n\t}" : "+f"(x), "+f"(y) : "f"(by));
+}
+
+template <int D, int OUT>
 __global__ void __launch_bounds__(kThreads, 1)
 cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                    const __grid_constant__ CUtensorMap map_v, const ShortPlan plan) {
@@ -69,7 +190,8 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
     __shared__ int abort_flag;
     __shared__ int part_max[2][2][kTile], part_sum[2][2][kTile];   // [stage][half][row]
     __shared__ __align__(16) int vsum[2][D];
-    __shared__ int row_at[kTile];                                  // where a row of a tile lies in Q and O
+    __shared__ int start[3];                                       // of the walk: sequence, kv head, tile
+    __shared__ int64_t count;
 
     const int tid = threadIdx.x, lane = tid & 31;
     const int warp = __shfl_sync(~0u, tid >> 5, 0);                // (uniform in the compiler's eyes too)
@@ -102,7 +224,7 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    if (tid < kTile) row_at[tid] = (tid / a.group * a.Hq + tid % a.group) * D;
+    if (warp == 0) find_start(a, plan, start, &count);
     if (warp == kPvWarp) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(kTmemCols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -113,81 +235,46 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
     const uint32_t tmem = tmem_slot;
     auto wait = [&](uint64_t *bar, uint32_t parity) -> bool { return warp_wait(smem_u32(bar), parity, abortp, a.status, a.wait_cycles); };
 
-    auto fetch = [&](int c) -> ChunkRaw {
-        ChunkRaw r = {0, 0, 0, 0};
-        if (c < plan.chunks) {
-            const int b = c / (plan.chunks_per * a.Hkv);
-            r.q0 = __ldg(a.q_start + b);
-            r.q1 = __ldg(a.q_start + b + 1);
-            r.k0 = __ldg(a.k_start + b);
-            r.kv = __ldg(a.kv_len + b);
-        }
-        return r;
-    };
-    auto chunk_of = [&](int c, const ChunkRaw &r) -> Chunk {
-        Chunk k;
-        const int pair = c / plan.chunks_per;
-        k.kvh = pair % a.Hkv;
-        k.seq = cross_sequence(a, r.q0, r.q1, r.k0, r.kv);
-        k.tile0 = (c - pair * plan.chunks_per) * plan.per_chunk;
-        const int all = (min(k.seq.nq, a.max_q) + plan.queries - 1) / plan.queries;
-        k.tiles = max(min(all - k.tile0, plan.per_chunk), 0);
-        return k;
-    };
-    const int step = gridDim.x;
+    Walk walk;
+    walk.b = start[0]; walk.kvh = start[1]; walk.tile = start[2]; walk.left = count;
+    walk.window(a, walk.b);
+    Chunk k;
 
-    if (warp == kQWarp) {
-        // ===================================================== copies of Q: tile number `it` of the CTA into stage it & 1
-        int it = 0;
+    if (warp == kCopyWarp) {
+        // ===================================================== copies: K and V of a chunk and the Q of its tiles, in the order in which they
+        // are needed; tile number `it` of the CTA goes into stage it & 1, chunk number kc into slot kc & 1 (or, V, the only one)
+        int it = 0, kc = 0, sent_v = 0;
         bool ok = true;
-        const uint32_t bytes = (uint32_t)(plan.queries * a.group * D);
-        ChunkRaw raw = fetch(blockIdx.x);
-        for (int c = blockIdx.x; ok && c < plan.chunks; c += step) {
-            const Chunk k = chunk_of(c, raw);
-            raw = fetch(c + step);
-            if (k.seq.cut && k.tile0 == 0 && k.kvh == 0 && lane == 0) atomicOr(a.status, STATUS_BAD_LENGTH);
+        const uint32_t q_bytes = (uint32_t)(plan.queries * a.group * D);
+        auto copy = [&](uint32_t dst, const CUtensorMap *map, int y, int z, uint64_t *full, uint32_t bytes) {
+            if (lane == 0) {
+                mbar_expect_tx(smem_u32(full), bytes);
+                tma_load_3d(dst, map, 0, y, z, smem_u32(full));
+            }
+            __syncwarp();
+        };
+        while (ok && walk.next(a, plan, k)) {
             if (k.seq.n == 0) continue;
+            const int ks = kc & 1, vs = plan.v_slots == 2 ? kc & 1 : 0, vround = plan.v_slots == 2 ? kc >> 1 : kc;
+            if (kc >= 2) ok = wait(&bars.k_free[ks], ((kc >> 1) - 1) & 1);
+            if (!ok) break;
+            copy(s_k + ks * kv_bytes, &map_k, k.kvh, k.seq.k0, &bars.k_full[ks], (uint32_t)kv_bytes);
+            ++kc;
             for (int t = 0; t < k.tiles; ++t, ++it) {
                 const int st = it & 1;
                 if (it >= 2) ok = wait(&bars.q_free[st], ((it >> 1) - 1) & 1);
                 if (!ok) break;
-                if (lane == 0) {
-                    mbar_expect_tx(smem_u32(&bars.q_full[st]), bytes);
-                    tma_load_3d(s_q + st * kTileBytes, &map_q, 0, k.kvh * a.group, k.seq.s0 + (k.tile0 + t) * plan.queries, smem_u32(&bars.q_full[st]));
+                copy(s_q + st * kTileBytes, &map_q, k.kvh * a.group, k.seq.s0 + (k.tile0 + t) * plan.queries, &bars.q_full[st], q_bytes);
+                if (t == 0) {
+                    if (vround >= 1) ok = wait(&bars.v_free[vs], (vround - 1) & 1);
+                    if (!ok) { ++it; break; }
+                    copy(s_v + vs * kv_bytes, &map_v, k.kvh, k.seq.k0, &bars.v_full[vs], (uint32_t)kv_bytes);
+                    ++sent_v;
                 }
-                __syncwarp();
             }
         }
-        // (the last copy of each stage has landed before the CTA may leave, whatever became of its readers; again with a limit)
+        // (the last copy into each place has landed before the CTA may leave, whatever became of its readers; again with a limit)
         for (int x = max(it - 2, 0); x < it; ++x) mbar_wait_bounded(smem_u32(&bars.q_full[x & 1]), (x >> 1) & 1, a.wait_cycles);
-    } else if (warp == kKvWarp) {
-        // ===================================================== copies of K and V, a chunk ahead where there is a slot
-        int kc = 0;
-        bool ok = true;
-        int sent_v = 0;
-        ChunkRaw raw = fetch(blockIdx.x);
-        for (int c = blockIdx.x; ok && c < plan.chunks; c += step) {
-            const Chunk k = chunk_of(c, raw);
-            raw = fetch(c + step);
-            if (k.seq.n == 0 || k.tiles == 0) continue;
-            const int ks = kc & 1, vs = plan.v_slots == 2 ? kc & 1 : 0, vround = plan.v_slots == 2 ? kc >> 1 : kc;
-            if (kc >= 2) ok = wait(&bars.k_free[ks], ((kc >> 1) - 1) & 1);
-            if (!ok) break;
-            if (lane == 0) {
-                mbar_expect_tx(smem_u32(&bars.k_full[ks]), (uint32_t)kv_bytes);
-                tma_load_3d(s_k + ks * kv_bytes, &map_k, 0, k.kvh, k.seq.k0, smem_u32(&bars.k_full[ks]));
-            }
-            __syncwarp();
-            ++kc;
-            if (vround >= 1) ok = wait(&bars.v_free[vs], (vround - 1) & 1);
-            if (!ok) break;
-            if (lane == 0) {
-                mbar_expect_tx(smem_u32(&bars.v_full[vs]), (uint32_t)kv_bytes);
-                tma_load_3d(s_v + vs * kv_bytes, &map_v, 0, k.kvh, k.seq.k0, smem_u32(&bars.v_full[vs]));
-            }
-            __syncwarp();
-            ++sent_v;
-        }
         for (int x = max(kc - 2, 0); x < kc; ++x) mbar_wait_bounded(smem_u32(&bars.k_full[x & 1]), (x >> 1) & 1, a.wait_cycles);
         for (int x = max(sent_v - plan.v_slots, 0); x < sent_v; ++x)
             mbar_wait_bounded(smem_u32(&bars.v_full[x % plan.v_slots]), (x / plan.v_slots) & 1, a.wait_cycles);
@@ -197,11 +284,8 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
         const uint32_t idesc = kIdescQK | (uint32_t)(nk >> 3) << 17;
         int it = 0, kc = 0;
         bool ok = true;
-        ChunkRaw raw = fetch(blockIdx.x);
-        for (int c = blockIdx.x; ok && c < plan.chunks; c += step) {
-            const Chunk k = chunk_of(c, raw);
-            raw = fetch(c + step);
-            if (k.seq.n == 0 || k.tiles == 0) continue;
+        while (ok && walk.next(a, plan, k)) {
+            if (k.seq.n == 0) continue;
             const int ks = kc & 1;
             ok = wait(&bars.k_full[ks], (kc >> 1) & 1);
             const uint32_t k_lo = (uint32_t)dk + ((uint32_t)(ks * kv_bytes) >> 4);
@@ -229,11 +313,8 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
         const uint64_t dr = smem_desc(s_r, 16, 1024, kSwizzle128), dv = smem_desc(s_v, 8 * D, 8 * D, kSwizzle);
         int it = 0, kc = 0;
         bool ok = true;
-        ChunkRaw raw = fetch(blockIdx.x);
-        for (int c = blockIdx.x; ok && c < plan.chunks; c += step) {
-            const Chunk k = chunk_of(c, raw);
-            raw = fetch(c + step);
-            if (k.seq.n == 0 || k.tiles == 0) continue;
+        while (ok && walk.next(a, plan, k)) {
+            if (k.seq.n == 0) continue;
             const int vs = plan.v_slots == 2 ? kc & 1 : 0, vround = plan.v_slots == 2 ? kc >> 1 : kc;
             ok = wait(&bars.v_full[vs], vround & 1);
             const uint32_t v_lo = (uint32_t)dv + ((uint32_t)(vs * kv_bytes) >> 4);
@@ -260,11 +341,8 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
         const int piece = lane % kPieces, first = lane / kPieces;
         int kc = 0;
         bool ok = true;
-        ChunkRaw raw = fetch(blockIdx.x);
-        for (int c = blockIdx.x; ok && c < plan.chunks; c += step) {
-            const Chunk k = chunk_of(c, raw);
-            raw = fetch(c + step);
-            if (k.seq.n == 0 || k.tiles == 0) continue;
+        while (ok && walk.next(a, plan, k)) {
+            if (k.seq.n == 0) continue;
             const int vs = plan.v_slots == 2 ? kc & 1 : 0, vround = plan.v_slots == 2 ? kc >> 1 : kc;
             if (kc >= 2) ok = wait(&bars.sum_free[kc & 1], ((kc >> 1) - 1) & 1);
             if (ok) ok = wait(&bars.v_full[vs], vround & 1);
@@ -305,43 +383,41 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
         const int width = nk >> 1, key0 = half * width;            // a multiple of 16
         uint8_t *const panel = gen + (s_r - base) + stage * panel_bytes;
         uint8_t *const staged = panel + (warp & 7) * (32 * kStageRow);      // (taken when the tile's products are through)
-        const bool wide = output_is_wide(a);
-        const int elem = wide ? 4 : 2;
+        constexpr bool kWide = OUT == HCCS_I32 || OUT == HCCS_F32;
+        constexpr int kElem = kWide ? 4 : 2, kDimsAtATime = kStageRow / kElem;
+        // a lane of the stores takes piece lane % 4 of rows lane / 4, + 8, ... of the warp's 32: where they lie in O (16-byte units)
+        int store_at[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int row = quarter * 32 + i * 8 + (lane >> 2);
+            store_at[i] = (row / a.group * a.Hq + row % a.group) * (D * kElem / 16) + (lane & 3);
+        }
         auto stage_barrier = [&]() { asm volatile("bar.sync %0, %1;" ::"r"(stage + 1), "n"(kStage) : "memory"); };
         int it = 0, kc = 0;
         bool ok = true;          // a wait given up: the rest is walked through for the stage's barriers alone
-        ChunkRaw raw = fetch(blockIdx.x);
-        for (int c = blockIdx.x; c < plan.chunks; c += step) {
-            const Chunk k = chunk_of(c, raw);
-            raw = fetch(c + step);
-            if (k.tiles == 0) continue;
+        while (walk.next(a, plan, k)) {
             const int rows_left = min(k.seq.nq, a.max_q) * a.group;
-            const int64_t o0 = ((int64_t)k.seq.s0 * a.Hq + (int64_t)k.kvh * a.group) * D + half * (D / 2);
-            // a lane of the stores takes piece lane % 4 of rows lane / 4, + 8, ... of the warp's 32
             auto store_rows = [&](int tile, int at_dim, bool zeros) {
-                const int left = rows_left - tile * plan.queries * a.group;
-                uint8_t *const out = static_cast<uint8_t *>(a.O) + (o0 + (int64_t)tile * plan.queries * a.Hq * D + at_dim) * elem + (lane & 3) * 16;
+                const int left = min(rows_left - tile * plan.queries * a.group, plan.queries * a.group) - quarter * 32 - (lane >> 2);
+                uint4 *const out = reinterpret_cast<uint4 *>(static_cast<uint8_t *>(a.O) +
+                    ((((int64_t)k.seq.s0 + (int64_t)tile * plan.queries) * a.Hq + (int64_t)k.kvh * a.group) * D + half * (D / 2) + at_dim) * kElem);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int r = i * 8 + (lane >> 2), row = quarter * 32 + r;
+                    const int r = i * 8 + (lane >> 2);
                     uint4 v = make_uint4(0, 0, 0, 0);
                     if (!zeros) v = *reinterpret_cast<const uint4 *>(staged + r * kStageRow + (((lane & 3) ^ ((r >> 1) & 3)) << 4));
-                    if (row < min(left, plan.queries * a.group)) *reinterpret_cast<uint4 *>(out + (int64_t)row_at[row] * elem) = v;
+                    if (i * 8 < left) out[store_at[i]] = v;
                 }
             };
-            const int dims_at_a_time = kStageRow / elem;
             if (k.seq.n == 0) {                                    // nothing to see: zeros
                 for (int x = stage; x < k.tiles; x += 2)
-                    for (int dim = 0; dim < D / 2; dim += dims_at_a_time) store_rows(k.tile0 + x, dim, true);
+                    for (int dim = 0; dim < D / 2; dim += kDimsAtATime) store_rows(k.tile0 + x, dim, true);
                 continue;
             }
             const int h = k.kvh * a.group + t % a.group;
             const int4 e = *reinterpret_cast<const int4 *>(a.table + h);
-            const int M = a.mult[h], sh = a.requant_shift, shl = 24 - sh;
-            const Requant rq = make_requant(M, sh);
-            const double inv = M > 0 ? 1.0 / (double)M : 0.0;
+            const HeadRequant rq = head_requant(a.mult[h], a.requant_shift);
             const int F = e.x - e.y * e.z, n = k.seq.n;
-            const int lo = -rq.neg_lo, hi = lo + rq.span;
             const float scale = a.scale[h];
             bool sums = false;                                     // sum V of the chunk has been waited for
             for (int x = 0; x < k.tiles; ++x, ++it) {
@@ -377,15 +453,11 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
                 amax = max(amax, part_max[stage][half ^ 1][t]);
                 // ---- r: with u = m - D, accumulators are clamped to [lo_u, hi], lo_u the smallest whose logit reaches max(u, -128); then
                 // clamp(acc - lo_u, 0, hi - lo_u)*(M << shl) + (((lo_u*M + R) << shl) - (u << 24)) has r as its top byte
-                const int u = ((int)requant_top(rq, amax) >> 24) - e.z;
-                int lo_u = lo;
-                if (M > 0) {
-                    // ceil of num / M, |num| < 2^33 and M < 2^13: num * inv is off by less than 2^-19, a fraction is 2^-13 or more
-                    const double q = ceil(((double)u * (double)(1 << sh) - (double)(1 << (sh - 1))) * inv - 0x1p-15);
-                    lo_u = (int)fmin(fmax(q, (double)lo), (double)hi);
-                }
-                const int neg_lo = -lo_u, span = hi - lo_u;
-                const uint32_t mk = rq.mk, ck = (((uint32_t)lo_u * (uint32_t)M + (1u << (sh - 1))) << shl) - ((uint32_t)u << 24);
+                const int u = ((int)((uint32_t)__viaddmin_s32_relu(amax, -rq.lo, rq.hi - rq.lo) * rq.mk + rq.ck) >> 24) - e.z;
+                // the smallest accumulator with acc*M >= u*2^sh - R
+                const int lo_u = rq.M > 0 ? min(max(whole_quotient(rq, 2 * u - 1, 1) + 1, rq.lo), rq.hi) : rq.lo;
+                const int neg_lo = -lo_u, span = rq.hi - lo_u;
+                const uint32_t mk = rq.mk, ck = (((uint32_t)lo_u * (uint32_t)rq.M + (1u << (rq.sh - 1))) << (24 - rq.sh)) - ((uint32_t)u << 24);
                 int rsum = 0;
                 auto bytes4 = [&](const uint32_t *acc) -> uint32_t {
                     uint32_t y[4];
@@ -447,35 +519,48 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
                 if (ok) ok = wait(&bars.o_full[stage], phase);
                 if (!ok) continue;
                 tcgen05_fence_after();
-                // ---- the rows' outputs, 64 bytes of each at a time, through the warp's part of the panel: four lanes store a row's piece
-                const int steps = D / 2 * elem / kStageRow;
-                for (int y = 0; y < steps; ++y) {
-                    auto quad = [&](int dim, const uint32_t *o) -> uint4 {
-                        const int4 vs = *reinterpret_cast<const int4 *>(&vsum[kc & 1][half * (D / 2) + dim]);
-                        const int num[4] = {e.y * (int)o[0] + F * vs.x, e.y * (int)o[1] + F * vs.y, e.y * (int)o[2] + F * vs.z, e.y * (int)o[3] + F * vs.w};
-                        return output4(a, num, f);
-                    };
-                    auto put = [&](int p, const uint4 &v) { *reinterpret_cast<uint4 *>(staged + lane * kStageRow + ((p ^ ((lane >> 1) & 3)) << 4)) = v; };
-                    if (wide) {
-                        uint32_t o[16];
-                        tmem_ld16(o_at + y * 16, o);
+                // ---- the rows' outputs, 64 bytes of each at a time, through the warp's part of the panel: four lanes store a row's piece.
+                // In the integer modes rho goes into the factors (what it multiplies out to fits int32).
+                const int rho = OUT != HCCS_I32 && a.recip == HCCS_RECIP_REAL ? 1 : f.rho, by_r = e.y * rho, by_v = F * rho;
+                const bool tiny = OUT != HCCS_I32 && __any_sync(~0u, f.unit != 1.0f);
+                for (int y = 0; y < D / 2 * kElem / kStageRow; ++y) {
+                    uint32_t o[kDimsAtATime];
+                    tmem_ld(o_at + y * kDimsAtATime, o);
 #pragma unroll
-                        for (int p = 0; p < 4; ++p) put(p, quad(y * 16 + 4 * p, o + 4 * p));
-                    } else {
-                        uint32_t o[32];
-                        tmem_ld32(o_at + y * 32, o);
+                    for (int i = 0; i < kDimsAtATime; i += 4) {
+                        const int4 vs = *reinterpret_cast<const int4 *>(&vsum[kc & 1][half * (D / 2) + y * kDimsAtATime + i]);
+                        o[i] = (uint32_t)(by_r * (int)o[i] + by_v * vs.x);
+                        o[i + 1] = (uint32_t)(by_r * (int)o[i + 1] + by_v * vs.y);
+                        o[i + 2] = (uint32_t)(by_r * (int)o[i + 2] + by_v * vs.z);
+                        o[i + 3] = (uint32_t)(by_r * (int)o[i + 3] + by_v * vs.w);
+                    }
+                    if constexpr (OUT != HCCS_I32) {
 #pragma unroll
-                        for (int p = 0; p < 4; ++p) {
-                            const uint4 v0 = quad(y * 32 + 8 * p, o + 8 * p), v1 = quad(y * 32 + 8 * p + 4, o + 8 * p + 4);
-                            put(p, make_uint4(v0.x, v0.y, v1.x, v1.y));
+                        for (int i = 0; i < kDimsAtATime; i += 2) {
+                            float v = (float)(int)o[i], w = (float)(int)o[i + 1];
+                            scale2(v, w, f.scale);
+                            if (tiny) scale2(v, w, f.unit);
+                            if constexpr (OUT == HCCS_F32) {
+                                o[i] = __float_as_uint(v);
+                                o[i + 1] = __float_as_uint(w);
+                            } else if constexpr (OUT == HCCS_BF16) {
+                                const __nv_bfloat162 b2 = __floats2bfloat162_rn(v, w);
+                                o[i >> 1] = *reinterpret_cast<const uint32_t *>(&b2);
+                            } else {
+                                const __half2 h2 = __floats2half2_rn(v, w);
+                                o[i >> 1] = *reinterpret_cast<const uint32_t *>(&h2);
+                            }
                         }
                     }
-                    if (y == steps - 1) {
+#pragma unroll
+                    for (int p = 0; p < 4; ++p)
+                        *reinterpret_cast<uint4 *>(staged + lane * kStageRow + ((p ^ ((lane >> 1) & 3)) << 4)) = make_uint4(o[4 * p], o[4 * p + 1], o[4 * p + 2], o[4 * p + 3]);
+                    if (y == D / 2 * kElem / kStageRow - 1) {
                         tcgen05_fence_before();
                         if (!apart) mbar_arrive(smem_u32(&bars.s_free[stage]));
                     }
                     __syncwarp();
-                    store_rows(k.tile0 + x, y * dims_at_a_time, false);
+                    store_rows(k.tile0 + x, y * kDimsAtATime, false);
                     __syncwarp();
                 }
             }
@@ -521,9 +606,9 @@ bool make_query_map(CUtensorMap *map, const CachedAttnArgs &a, int queries) {
 
 constexpr size_t kMaxSmem = 219 * 1024;    // dynamic; the kernel's own arrays take up to 6 KB more
 
-template <int D>
+template <int D, int OUT>
 cudaError_t launch_typed(const CachedAttnArgs &a, cudaStream_t stream) {
-    auto kernel = cross_short_kernel<D>;
+    auto kernel = cross_short_kernel<D, OUT>;
     static std::atomic<bool> raised[64];
     cudaError_t e = raise_limits((const void *)kernel, (int)kMaxSmem, raised);
     int dev = 0, sms = 0;
@@ -536,24 +621,22 @@ cudaError_t launch_typed(const CachedAttnArgs &a, cudaStream_t stream) {
     const size_t fixed = 1024 + 2 * (size_t)kTile * D + 2 * (size_t)((p.keys + 127) / 128) * kTile * 128, kv = (size_t)p.keys * D;
     p.v_slots = fixed + 4 * kv <= kMaxSmem ? 2 : 1;
     const size_t smem = fixed + (2 + p.v_slots) * kv;
-    // Tiles per chunk: the rounds of chunks that a CTA goes through, each as long as its tiles and about half a tile's time for the
-    // chunk's own
-    const int64_t pairs = (int64_t)a.B * a.Hkv, tiles = ((int64_t)a.max_q + p.queries - 1) / p.queries;
-    int64_t best = -1;
-    for (int64_t per = 1; per <= 64 && per <= tiles; ++per) {
-        const int64_t chunks = pairs * ((tiles + per - 1) / per);
-        if (chunks > 0x7fffffff - 1024) continue;
-        const int64_t cost = (chunks + sms - 1) / sms * (2 * per + 1);
-        if (best < 0 || cost < best) { best = cost; p.per_chunk = (int)per; }
-    }
-    if (best < 0) return cudaErrorInvalidConfiguration;
-    p.chunks_per = (int)((tiles + p.per_chunk - 1) / p.per_chunk);
-    p.chunks = (int)(pairs * p.chunks_per);
     CUtensorMap mq, mk, mv;
     if (!make_query_map(&mq, a, p.queries) || !make_states_map(&mk, a.k_pages, a.k_stride, a, p.keys) || !make_states_map(&mv, a.v_pages, a.v_stride, a, p.keys))
         return cudaErrorInvalidValue;
-    kernel<<<p.chunks < sms ? p.chunks : sms, kThreads, smem, stream>>>(a, mq, mk, mv, p);
+    const int64_t most = (int64_t)a.B * a.Hkv * (((int64_t)a.max_q + p.queries - 1) / p.queries);      // tiles
+    kernel<<<(unsigned)(most < sms ? most : sms), kThreads, smem, stream>>>(a, mq, mk, mv, p);
     return cudaGetLastError();
+}
+
+template <int D>
+cudaError_t launch_head_dim(const CachedAttnArgs &a, cudaStream_t stream) {
+    switch (a.out_type) {
+        case HCCS_I32: return launch_typed<D, HCCS_I32>(a, stream);
+        case HCCS_F32: return launch_typed<D, HCCS_F32>(a, stream);
+        case HCCS_BF16: return launch_typed<D, HCCS_BF16>(a, stream);
+        default: return launch_typed<D, HCCS_F16>(a, stream);
+    }
 }
 
 }  // namespace
@@ -561,7 +644,7 @@ cudaError_t launch_typed(const CachedAttnArgs &a, cudaStream_t stream) {
 bool cross_short_fits(const CachedAttnArgs &a) { return !a.key_range && a.max_kv <= kMaxKeys && a.group <= kTile; }
 
 cudaError_t launch_cross_short(const CachedAttnArgs &a, cudaStream_t stream) {
-    return a.d == 128 ? launch_typed<128>(a, stream) : launch_typed<64>(a, stream);
+    return a.d == 128 ? launch_head_dim<128>(a, stream) : launch_head_dim<64>(a, stream);
 }
 
 }  // namespace hccs
