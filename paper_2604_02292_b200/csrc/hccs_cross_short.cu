@@ -8,12 +8,12 @@
 // chunk.  All sums fit int32: |sum r V| < 2^22, S < 2^7, F < 2^15, |sum V| <= 2^15.
 //
 // CTAs are persistent.  The tiles that the sequences really have are counted at the start and shared out evenly, in order, so a CTA
-// walks through few (sequence, kv head) pairs: chunks of tiles with one K and V.  Two stages, each with half
-// of tensor memory, a Q tile, a panel of r and eight row warps, take the tiles alternately: while one waits for a product or
-// stores its rows, the other has the integer pipe.  O takes columns of its own in the stage's half where the keys leave room,
+// walks through few (sequence, kv head) pairs: chunks of tiles with one K and V.  Stages, each with its part
+// of tensor memory, a Q tile, a panel of r and its row warps, take the tiles in turn: while one waits for a product or
+// stores its rows, the others have the integer pipe.  O takes columns of its own in the stage's part where the keys leave room,
 // else those of S (all of whose logits have been read twice by then).
 //
-// Roles: sixteen row warps (two threads per row, half of the keys and of the dims each), a warp each for the copies, Q.K^T, r.V, and
+// Roles: sixteen row warps, a warp each for the copies, Q.K^T, r.V, and
 // the sums of V.
 #include "hccs_cached.cuh"
 #include "hccs_tcgen05.cuh"
@@ -25,7 +25,7 @@ namespace {
 constexpr int kRowWarps = 16, kCopyWarp = 16, kQkWarp = 17, kPvWarp = 18, kSumWarp = 19;
 constexpr int kThreads = 640;                    // 20 warps: 96 registers a thread
 constexpr int kTile = 128;
-constexpr int kStage = 256;                      // threads and tensor-memory columns of a stage
+constexpr int kMaxStages = 4;
 constexpr int kMaxKeys = 256;
 constexpr uint32_t kTmemCols = 512;
 constexpr int kStageRow = 64;                    // bytes of a row that a warp stages at a time for its stores
@@ -34,9 +34,9 @@ constexpr uint32_t kIdescQK = instr_desc(1, 1, 0, 128, 0);                      
 template <int D> constexpr uint32_t kIdescPVOf = instr_desc(0, 1, 1, 128, D);   // r.V: uint8 x int8, V MN-major
 
 struct ShortBarriers {
-    uint64_t q_full[2], q_free[2];               // a stage's Q tile
-    uint64_t s_full[2], s_free[2];               // its logits
-    uint64_t r_ready[2], o_full[2];
+    uint64_t q_full[kMaxStages], q_free[kMaxStages];               // a stage's Q tile
+    uint64_t s_full[kMaxStages], s_free[kMaxStages];               // its logits
+    uint64_t r_ready[kMaxStages], o_full[kMaxStages];
     uint64_t k_full[2], k_free[2], v_full[2], v_free[2];      // by chunk
     uint64_t sum_full[2], sum_free[2];           // sum V, by chunk
     uint64_t drained[2];                         // a given-up CTA: the products of either issuer are through
@@ -177,18 +177,22 @@ __device__ __forceinline__ void scale2(float &x, float &y, float by) {
     asm("{\n\t.reg .b64 v, w;\n\tmov.b64 v, {%0, %1};\n\tmov.b64 w, {%2, %2};\n\tmul.rn.f32x2 v, v, w;\n\tmov.b64 {%0, %1}, v;\n\t}" : "+f"(x), "+f"(y) : "f"(by));
 }
 
-template <int D, int OUT>
+// WIDE: more than 128 keys: two stages, two threads per row.  Else four stages and a thread per row, which has nobody to wait for.
+template <int D, int OUT, bool WIDE>
 __global__ void __launch_bounds__(kThreads, 1)
 cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                    const __grid_constant__ CUtensorMap map_v, const ShortPlan plan) {
     constexpr int kTileBytes = kTile * D;
+    constexpr int kStages = WIDE ? 2 : 4, kHalves = WIDE ? 2 : 1, kShift = WIDE ? 1 : 2;
+    constexpr int kCols = (int)kTmemCols / kStages;                // tensor-memory columns of a stage
+    constexpr int kStageThreads = 128 * kHalves, kDims = D / kHalves;
     constexpr uint64_t kSwizzle = D == 128 ? kSwizzle128 : kSwizzle64;
     constexpr uint32_t kIdescPV = kIdescPVOf<D>;
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) ShortBarriers bars;
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
-    __shared__ int part_max[2][2][kTile], part_sum[2][2][kTile];   // [stage][half][row]
+    __shared__ int part_max[kStages][kHalves][WIDE ? kTile : 1], part_sum[kStages][kHalves][WIDE ? kTile : 1];   // [stage][half][row]
     __shared__ __align__(16) int vsum[2][D];
     __shared__ int start[3];                                       // of the walk: sequence, kv head, tile
     __shared__ int64_t count;
@@ -200,19 +204,21 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t *gen = smem_raw + (base - smem_u32(smem_raw));
     const int panel_bytes = ((nk + 127) >> 7) * kTile * 128;       // r of a stage: 128 rows x 128 keys, 128-byte swizzle, once or twice
-    const uint32_t s_q = base, s_k = s_q + 2 * kTileBytes, s_v = s_k + 2 * kv_bytes, s_r = s_v + plan.v_slots * kv_bytes;
-    const uint32_t o_col = nk + D <= kStage ? kStage - D : 0;      // O's columns in its stage's half
+    const uint32_t s_q = base, s_k = s_q + kStages * kTileBytes, s_v = s_k + 2 * kv_bytes, s_r = s_v + plan.v_slots * kv_bytes;
+    const uint32_t o_col = nk + D <= kCols ? kCols - D : 0;        // O's columns in its stage's part
     const bool apart = o_col != 0;
 
     if (tid == 0) {
         abort_flag = 0;
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < kStages; ++i) {
             mbar_init(smem_u32(&bars.q_full[i]), 1);
             mbar_init(smem_u32(&bars.q_free[i]), 1);
             mbar_init(smem_u32(&bars.s_full[i]), 1);
-            mbar_init(smem_u32(&bars.s_free[i]), kStage);
-            mbar_init(smem_u32(&bars.r_ready[i]), kStage);
+            mbar_init(smem_u32(&bars.s_free[i]), kStageThreads);
+            mbar_init(smem_u32(&bars.r_ready[i]), kStageThreads);
             mbar_init(smem_u32(&bars.o_full[i]), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&bars.k_full[i]), 1);
             mbar_init(smem_u32(&bars.k_free[i]), 1);
             mbar_init(smem_u32(&bars.v_full[i]), 1);
@@ -242,7 +248,7 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
 
     if (warp == kCopyWarp) {
         // ===================================================== copies: K and V of a chunk and the Q of its tiles, in the order in which they
-        // are needed; tile number `it` of the CTA goes into stage it & 1, chunk number kc into slot kc & 1 (or, V, the only one)
+        // are needed; tile number `it` of the CTA goes into stage it % kStages, chunk number kc into slot kc & 1 (or, V, the only one)
         int it = 0, kc = 0, sent_v = 0;
         bool ok = true;
         const uint32_t q_bytes = (uint32_t)(plan.queries * a.group * D);
@@ -261,8 +267,8 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
             copy(s_k + ks * kv_bytes, &map_k, k.kvh, k.seq.k0, &bars.k_full[ks], (uint32_t)kv_bytes);
             ++kc;
             for (int t = 0; t < k.tiles; ++t, ++it) {
-                const int st = it & 1;
-                if (it >= 2) ok = wait(&bars.q_free[st], ((it >> 1) - 1) & 1);
+                const int st = it & (kStages - 1);
+                if (it >= kStages) ok = wait(&bars.q_free[st], ((it >> kShift) - 1) & 1);
                 if (!ok) break;
                 copy(s_q + st * kTileBytes, &map_q, k.kvh * a.group, k.seq.s0 + (k.tile0 + t) * plan.queries, &bars.q_full[st], q_bytes);
                 if (t == 0) {
@@ -274,7 +280,7 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
             }
         }
         // (the last copy into each place has landed before the CTA may leave, whatever became of its readers; again with a limit)
-        for (int x = max(it - 2, 0); x < it; ++x) mbar_wait_bounded(smem_u32(&bars.q_full[x & 1]), (x >> 1) & 1, a.wait_cycles);
+        for (int x = max(it - kStages, 0); x < it; ++x) mbar_wait_bounded(smem_u32(&bars.q_full[x & (kStages - 1)]), (x >> kShift) & 1, a.wait_cycles);
         for (int x = max(kc - 2, 0); x < kc; ++x) mbar_wait_bounded(smem_u32(&bars.k_full[x & 1]), (x >> 1) & 1, a.wait_cycles);
         for (int x = max(sent_v - plan.v_slots, 0); x < sent_v; ++x)
             mbar_wait_bounded(smem_u32(&bars.v_full[x % plan.v_slots]), (x / plan.v_slots) & 1, a.wait_cycles);
@@ -290,16 +296,16 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
             ok = wait(&bars.k_full[ks], (kc >> 1) & 1);
             const uint32_t k_lo = (uint32_t)dk + ((uint32_t)(ks * kv_bytes) >> 4);
             for (int t = 0; ok && t < k.tiles; ++t, ++it) {
-                const int st = it & 1;
-                if (it >= 2) ok = wait(&bars.s_free[st], ((it >> 1) - 1) & 1);
-                if (ok) ok = wait(&bars.q_full[st], (it >> 1) & 1);
+                const int st = it & (kStages - 1);
+                if (it >= kStages) ok = wait(&bars.s_free[st], ((it >> kShift) - 1) & 1);
+                if (ok) ok = wait(&bars.q_full[st], (it >> kShift) & 1);
                 if (!ok) break;
                 tcgen05_fence_after();
                 const uint32_t q_lo = (uint32_t)dq + ((uint32_t)(st * kTileBytes) >> 4);
                 if (elect_one()) {
 #pragma unroll
                     for (int x = 0; x < D / 32; ++x)
-                        tcgen05_mma_i8(tmem + st * kStage, make_u64(q_lo + 2 * x, (uint32_t)(dq >> 32)), make_u64(k_lo + 2 * x, (uint32_t)(dk >> 32)), idesc, x != 0);
+                        tcgen05_mma_i8(tmem + st * kCols, make_u64(q_lo + 2 * x, (uint32_t)(dq >> 32)), make_u64(k_lo + 2 * x, (uint32_t)(dk >> 32)), idesc, x != 0);
                     tcgen05_commit(smem_u32(&bars.s_full[st]));
                     tcgen05_commit(smem_u32(&bars.q_free[st]));
                     if (t == k.tiles - 1) tcgen05_commit(smem_u32(&bars.k_free[ks]));
@@ -319,14 +325,14 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
             ok = wait(&bars.v_full[vs], vround & 1);
             const uint32_t v_lo = (uint32_t)dv + ((uint32_t)(vs * kv_bytes) >> 4);
             for (int t = 0; ok && t < k.tiles; ++t, ++it) {
-                const int st = it & 1;
-                ok = wait(&bars.r_ready[st], (it >> 1) & 1);
+                const int st = it & (kStages - 1);
+                ok = wait(&bars.r_ready[st], (it >> kShift) & 1);
                 if (!ok) break;
                 tcgen05_fence_after();
                 const uint32_t r_lo = (uint32_t)dr + ((uint32_t)(st * panel_bytes) >> 4);
                 if (elect_one()) {
                     for (int x = 0; x < nk / 32; ++x)
-                        tcgen05_mma_i8(tmem + st * kStage + o_col, make_u64(r_lo + (x >> 2) * (kTile * 128 >> 4) + 2 * (x & 3), (uint32_t)(dr >> 32)),
+                        tcgen05_mma_i8(tmem + st * kCols + o_col, make_u64(r_lo + (x >> 2) * (kTile * 128 >> 4) + 2 * (x & 3), (uint32_t)(dr >> 32)),
                                        make_u64(v_lo + (x * 32 * D >> 4), (uint32_t)(dv >> 32)), kIdescPV, x != 0);
                     tcgen05_commit(smem_u32(&bars.o_full[st]));
                     if (t == k.tiles - 1) tcgen05_commit(smem_u32(&bars.v_free[vs]));
@@ -376,13 +382,15 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
             ++kc;
         }
     } else {
-        // ===================================================== row warps: threads t and t + 128 of a stage own row t, half of the
-        // keys and of the dims each
-        const int stage = warp >> 3, half = (warp >> 2) & 1, quarter = warp & 3, t = quarter * 32 + lane;
-        const uint32_t lanes = (uint32_t)(quarter * 32) << 16, s_at = tmem + lanes + stage * kStage, o_at = s_at + o_col + half * (D / 2);
-        const int width = nk >> 1, key0 = half * width;            // a multiple of 16
+        // ===================================================== row warps: thread t of a stage owns row t, or with t + 128 half of its
+        // keys and dims
+        const int stage = warp / (4 * kHalves), half = WIDE ? (warp >> 2) & 1 : 0, quarter = warp & 3, t = quarter * 32 + lane;
+        const uint32_t lanes = (uint32_t)(quarter * 32) << 16, s_at = tmem + lanes + stage * kCols, o_at = s_at + o_col + half * kDims;
+        const int width = nk / kHalves, key0 = half * width;       // a multiple of 16, or 32
         uint8_t *const panel = gen + (s_r - base) + stage * panel_bytes;
-        uint8_t *const staged = panel + (warp & 7) * (32 * kStageRow);      // (taken when the tile's products are through)
+        // where the warp stages its stores once the tile's products are through: WIDE, its share of the panel, which the others write again
+        // behind the next barrier of the stage alone; else the place of its own rows, which nobody else writes
+        uint8_t *const staged = panel + (WIDE ? (warp & 7) * (32 * kStageRow) : quarter * (32 * 128));
         constexpr bool kWide = OUT == HCCS_I32 || OUT == HCCS_F32;
         constexpr int kElem = kWide ? 4 : 2, kDimsAtATime = kStageRow / kElem;
         // a lane of the stores takes piece lane % 4 of rows lane / 4, + 8, ... of the warp's 32: where they lie in O (16-byte units)
@@ -392,7 +400,7 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
             const int row = quarter * 32 + i * 8 + (lane >> 2);
             store_at[i] = (row / a.group * a.Hq + row % a.group) * (D * kElem / 16) + (lane & 3);
         }
-        auto stage_barrier = [&]() { asm volatile("bar.sync %0, %1;" ::"r"(stage + 1), "n"(kStage) : "memory"); };
+        auto stage_barrier = [&]() { asm volatile("bar.sync %0, %1;" ::"r"(stage + 1), "n"(kStageThreads) : "memory"); };
         int it = 0, kc = 0;
         bool ok = true;          // a wait given up: the rest is walked through for the stage's barriers alone
         while (walk.next(a, plan, k)) {
@@ -400,7 +408,7 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
             auto store_rows = [&](int tile, int at_dim, bool zeros) {
                 const int left = min(rows_left - tile * plan.queries * a.group, plan.queries * a.group) - quarter * 32 - (lane >> 2);
                 uint4 *const out = reinterpret_cast<uint4 *>(static_cast<uint8_t *>(a.O) +
-                    ((((int64_t)k.seq.s0 + (int64_t)tile * plan.queries) * a.Hq + (int64_t)k.kvh * a.group) * D + half * (D / 2) + at_dim) * kElem);
+                    ((((int64_t)k.seq.s0 + (int64_t)tile * plan.queries) * a.Hq + (int64_t)k.kvh * a.group) * D + half * kDims + at_dim) * kElem);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int r = i * 8 + (lane >> 2);
@@ -410,8 +418,8 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
                 }
             };
             if (k.seq.n == 0) {                                    // nothing to see: zeros
-                for (int x = stage; x < k.tiles; x += 2)
-                    for (int dim = 0; dim < D / 2; dim += kDimsAtATime) store_rows(k.tile0 + x, dim, true);
+                for (int x = stage; x < k.tiles; x += kStages)
+                    for (int dim = 0; dim < kDims; dim += kDimsAtATime) store_rows(k.tile0 + x, dim, true);
                 continue;
             }
             const int h = k.kvh * a.group + t % a.group;
@@ -421,8 +429,8 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
             const float scale = a.scale[h];
             bool sums = false;                                     // sum V of the chunk has been waited for
             for (int x = 0; x < k.tiles; ++x, ++it) {
-                if ((it & 1) != stage) continue;
-                const uint32_t phase = (it >> 1) & 1;
+                if ((it & (kStages - 1)) != stage) continue;
+                const uint32_t phase = (it >> kShift) & 1;
                 // ---- the largest accumulator
                 if (ok) ok = wait(&bars.s_full[stage], phase);
                 tcgen05_fence_after();
@@ -440,7 +448,7 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
                     for (int j = 0; j < 32; j += 2) amax = __vimax3_s32(amax, (int)acc[j], (int)acc[j + 1]);
                 }
                 const int tail = key0 + (width & ~31);             // 16 more keys where the width is odd that way
-                if (ok && (width & 16) && tail < n) {
+                if (WIDE && ok && (width & 16) && tail < n) {
                     uint32_t acc[16];
                     tmem_ld16(s_at + tail, acc);
                     const uint32_t mask = low_bits(n - tail);
@@ -448,9 +456,13 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
                     for (int j = 0; j < 16; j += 2)
                         amax = __vimax3_s32(amax, (mask >> j) & 1 ? (int)acc[j] : kNone, (mask >> (j + 1)) & 1 ? (int)acc[j + 1] : kNone);
                 }
-                part_max[stage][half][t] = amax;
-                stage_barrier();
-                amax = max(amax, part_max[stage][half ^ 1][t]);
+                if constexpr (WIDE) {
+                    part_max[stage][half][t] = amax;
+                    stage_barrier();
+                    amax = max(amax, part_max[stage][half ^ 1][t]);
+                } else {
+                    __syncwarp();
+                }
                 // ---- r: with u = m - D, accumulators are clamped to [lo_u, hi], lo_u the smallest whose logit reaches max(u, -128); then
                 // clamp(acc - lo_u, 0, hi - lo_u)*(M << shl) + (((lo_u*M + R) << shl) - (u << 24)) has r as its top byte
                 const int u = ((int)((uint32_t)__viaddmin_s32_relu(amax, -rq.lo, rq.hi - rq.lo) * rq.mk + rq.ck) >> 24) - e.z;
@@ -490,7 +502,7 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
                     put16(key0 + i, w);
                     put16(key0 + i + 16, w + 4);
                 }
-                if (ok && (width & 16)) {
+                if (WIDE && ok && (width & 16)) {
                     uint32_t w[4] = {0u, 0u, 0u, 0u};
                     if (tail < n) {
                         uint32_t acc[16];
@@ -506,11 +518,13 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
                 }
                 tcgen05_fence_before();
                 if (apart) mbar_arrive(smem_u32(&bars.s_free[stage]));
-                part_sum[stage][half][t] = rsum;
+                if constexpr (WIDE) part_sum[stage][half][t] = rsum;
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 mbar_arrive(smem_u32(&bars.r_ready[stage]));
-                stage_barrier();
-                rsum += part_sum[stage][half ^ 1][t];
+                if constexpr (WIDE) {
+                    stage_barrier();
+                    rsum += part_sum[stage][half ^ 1][t];
+                }
                 const RowFactor f = row_factor(a, (int64_t)F * n + (int64_t)e.y * rsum, scale);
                 if (ok && !sums) {
                     ok = wait(&bars.sum_full[kc & 1], (kc >> 1) & 1);
@@ -523,12 +537,12 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
                 // In the integer modes rho goes into the factors (what it multiplies out to fits int32).
                 const int rho = OUT != HCCS_I32 && a.recip == HCCS_RECIP_REAL ? 1 : f.rho, by_r = e.y * rho, by_v = F * rho;
                 const bool tiny = OUT != HCCS_I32 && __any_sync(~0u, f.unit != 1.0f);
-                for (int y = 0; y < D / 2 * kElem / kStageRow; ++y) {
+                for (int y = 0; y < kDims * kElem / kStageRow; ++y) {
                     uint32_t o[kDimsAtATime];
                     tmem_ld(o_at + y * kDimsAtATime, o);
 #pragma unroll
                     for (int i = 0; i < kDimsAtATime; i += 4) {
-                        const int4 vs = *reinterpret_cast<const int4 *>(&vsum[kc & 1][half * (D / 2) + y * kDimsAtATime + i]);
+                        const int4 vs = *reinterpret_cast<const int4 *>(&vsum[kc & 1][half * kDims + y * kDimsAtATime + i]);
                         o[i] = (uint32_t)(by_r * (int)o[i] + by_v * vs.x);
                         o[i + 1] = (uint32_t)(by_r * (int)o[i + 1] + by_v * vs.y);
                         o[i + 2] = (uint32_t)(by_r * (int)o[i + 2] + by_v * vs.z);
@@ -555,7 +569,7 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
 #pragma unroll
                     for (int p = 0; p < 4; ++p)
                         *reinterpret_cast<uint4 *>(staged + lane * kStageRow + ((p ^ ((lane >> 1) & 3)) << 4)) = make_uint4(o[4 * p], o[4 * p + 1], o[4 * p + 2], o[4 * p + 3]);
-                    if (y == D / 2 * kElem / kStageRow - 1) {
+                    if (y == kDims * kElem / kStageRow - 1) {
                         tcgen05_fence_before();
                         if (!apart) mbar_arrive(smem_u32(&bars.s_free[stage]));
                     }
@@ -606,9 +620,10 @@ bool make_query_map(CUtensorMap *map, const CachedAttnArgs &a, int queries) {
 
 constexpr size_t kMaxSmem = 219 * 1024;    // dynamic; the kernel's own arrays take up to 6 KB more
 
-template <int D, int OUT>
+template <int D, int OUT, bool WIDE>
 cudaError_t launch_typed(const CachedAttnArgs &a, cudaStream_t stream) {
-    auto kernel = cross_short_kernel<D, OUT>;
+    auto kernel = cross_short_kernel<D, OUT, WIDE>;
+    constexpr int kStages = WIDE ? 2 : 4;
     static std::atomic<bool> raised[64];
     cudaError_t e = raise_limits((const void *)kernel, (int)kMaxSmem, raised);
     int dev = 0, sms = 0;
@@ -618,7 +633,7 @@ cudaError_t launch_typed(const CachedAttnArgs &a, cudaStream_t stream) {
     ShortPlan p;
     p.queries = kTile / a.group;
     p.keys = a.max_kv <= 32 ? 32 : (a.max_kv + 31) / 32 * 32;
-    const size_t fixed = 1024 + 2 * (size_t)kTile * D + 2 * (size_t)((p.keys + 127) / 128) * kTile * 128, kv = (size_t)p.keys * D;
+    const size_t fixed = 1024 + kStages * ((size_t)kTile * D + (size_t)((p.keys + 127) / 128) * kTile * 128), kv = (size_t)p.keys * D;
     p.v_slots = fixed + 4 * kv <= kMaxSmem ? 2 : 1;
     const size_t smem = fixed + (2 + p.v_slots) * kv;
     CUtensorMap mq, mk, mv;
@@ -629,14 +644,19 @@ cudaError_t launch_typed(const CachedAttnArgs &a, cudaStream_t stream) {
     return cudaGetLastError();
 }
 
+template <int D, bool WIDE>
+cudaError_t launch_keys(const CachedAttnArgs &a, cudaStream_t stream) {
+    switch (a.out_type) {
+        case HCCS_I32: return launch_typed<D, HCCS_I32, WIDE>(a, stream);
+        case HCCS_F32: return launch_typed<D, HCCS_F32, WIDE>(a, stream);
+        case HCCS_BF16: return launch_typed<D, HCCS_BF16, WIDE>(a, stream);
+        default: return launch_typed<D, HCCS_F16, WIDE>(a, stream);
+    }
+}
+
 template <int D>
 cudaError_t launch_head_dim(const CachedAttnArgs &a, cudaStream_t stream) {
-    switch (a.out_type) {
-        case HCCS_I32: return launch_typed<D, HCCS_I32>(a, stream);
-        case HCCS_F32: return launch_typed<D, HCCS_F32>(a, stream);
-        case HCCS_BF16: return launch_typed<D, HCCS_BF16>(a, stream);
-        default: return launch_typed<D, HCCS_F16>(a, stream);
-    }
+    return a.max_kv > 128 ? launch_keys<D, true>(a, stream) : launch_keys<D, false>(a, stream);
 }
 
 }  // namespace
