@@ -26,6 +26,7 @@ constexpr int kRowWarps = 16, kCopyWarp = 16, kQkWarp = 17, kPvWarp = 18, kSumWa
 constexpr int kThreads = 640;                    // 20 warps: 96 registers a thread
 constexpr int kTile = 128;
 constexpr int kMaxStages = 4;
+constexpr int kChunks = 4;                       // chunks that are known ahead
 constexpr int kMaxKeys = 256;
 constexpr uint32_t kTmemCols = 512;
 constexpr int kStageRow = 64;                    // bytes of a row that a warp stages at a time for its stores
@@ -39,13 +40,16 @@ struct ShortBarriers {
     uint64_t r_ready[kMaxStages], o_full[kMaxStages];
     uint64_t k_full[2], k_free[2], v_full[2], v_free[2];      // by chunk
     uint64_t sum_full[2], sum_free[2];           // sum V, by chunk
+    uint64_t chunk_full[kChunks], chunk_free[kChunks];
+    uint64_t met[kMaxStages];                    // the stage's row threads, twice per tile (WIDE)
     uint64_t drained[2];                         // a given-up CTA: the products of either issuer are through
 };
 
-// A chunk, the same for every role: tiles of one sequence and kv head.
+// A chunk: tiles of one sequence and kv head.  The copy warp finds them, the others read them from shared memory.
 struct Chunk {
-    int kvh, tile0, tiles;
-    SequenceAt seq;
+    int tiles;                                   // 0: no more chunks
+    int n, k0, kvh;                              // keys, the first one's place, kv head
+    int q0, rows;                                // first query, rows from there to the sequence's end
 };
 
 struct ShortPlan {
@@ -58,7 +62,7 @@ __device__ __forceinline__ int tiles_of(const CachedAttnArgs &a, const SequenceA
     return (min(seq.nq, a.max_q) + plan.queries - 1) / plan.queries;
 }
 
-// The chunks of a CTA, walked through by whole warps: tiles are in the order (sequence, kv head, tile).  A lane holds one of 32
+// The chunks of a CTA, walked through by a warp: tiles are in the order (sequence, kv head, tile).  A lane holds one of 32
 // neighbouring sequences, so that their lengths are read together and those without queries are skipped together.
 struct Walk {
     int q0, q1, k0, kv, first;                   // this lane's sequence, number first + lane
@@ -76,9 +80,9 @@ struct Walk {
             kv = __ldg(a.kv_len + mine);
         }
     }
-    // false: no more
-    __device__ __forceinline__ bool next(const CachedAttnArgs &a, const ShortPlan &plan, Chunk &k) {
-        if (left <= 0) return false;
+    __device__ __forceinline__ Chunk next(const CachedAttnArgs &a, const ShortPlan &plan) {
+        Chunk k = {0, 0, 0, 0, 0, 0};
+        if (left <= 0) return k;
         for (;;) {
             const SequenceAt mine = cross_sequence(a, q0, q1, k0, kv);
             const uint32_t some = __ballot_sync(~0u, mine.nq > 0) & ~low_bits(b - first);
@@ -89,19 +93,21 @@ struct Walk {
             }
             b = first + 32;
             kvh = tile = 0;
-            if (b >= a.B) return false;
+            if (b >= a.B) return k;
             window(a, b);
         }
         const int from = b - first;
-        k.seq = cross_sequence(a, __shfl_sync(~0u, q0, from), __shfl_sync(~0u, q1, from), __shfl_sync(~0u, k0, from), __shfl_sync(~0u, kv, from));
-        const int all = tiles_of(a, k.seq, plan);
+        const SequenceAt seq = cross_sequence(a, __shfl_sync(~0u, q0, from), __shfl_sync(~0u, q1, from), __shfl_sync(~0u, k0, from), __shfl_sync(~0u, kv, from));
+        k.n = seq.n;
+        k.k0 = seq.k0;
         k.kvh = kvh;
-        k.tile0 = tile;
-        k.tiles = (int)min((int64_t)(all - tile), left);
+        k.tiles = (int)min((int64_t)(tiles_of(a, seq, plan) - tile), left);
+        k.q0 = seq.s0 + tile * plan.queries;
+        k.rows = (min(seq.nq, a.max_q) - tile * plan.queries) * a.group;
         left -= k.tiles;
         tile = 0;
         if (++kvh == a.Hkv) { kvh = 0; ++b; }
-        return true;
+        return k;
     }
 };
 
@@ -172,7 +178,10 @@ __device__ __forceinline__ HeadRequant head_requant(int M, int sh) {
 __device__ __forceinline__ void tmem_ld(uint32_t at, uint32_t (&r)[16]) { tmem_ld16(at, r); }
 __device__ __forceinline__ void tmem_ld(uint32_t at, uint32_t (&r)[32]) { tmem_ld32(at, r); }
 
-// Values and their products with a factor, two at a time.
+// Two values plus a constant, and two products with a factor.
+__device__ __forceinline__ void add2(float &x, float &y, float by) {
+    asm("{\n\t.reg .b64 v, w;\n\tmov.b64 v, {%0, %1};\n\tmov.b64 w, {%2, %2};\n\tadd.rn.f32x2 v, v, w;\n\tmov.b64 {%0, %1}, v;\n\t}" : "+f"(x), "+f"(y) : "f"(by));
+}
 __device__ __forceinline__ void scale2(float &x, float &y, float by) {
     asm("{\n\t.reg .b64 v, w;\n\tmov.b64 v, {%0, %1};\n\tmov.b64 w, {%2, %2};\n\tmul.rn.f32x2 v, v, w;\n\tmov.b64 {%0, %1}, v;\n\t}" : "+f"(x), "+f"(y) : "f"(by));
 }
@@ -196,6 +205,8 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
     __shared__ __align__(16) int vsum[2][D];
     __shared__ int start[3];                                       // of the walk: sequence, kv head, tile
     __shared__ int64_t count;
+    __shared__ Chunk chunks[kChunks];
+    __shared__ int row_at[kTile];                                  // where a row of a tile lies in O, in 16-byte pieces
 
     const int tid = threadIdx.x, lane = tid & 31;
     const int warp = __shfl_sync(~0u, tid >> 5, 0);                // (uniform in the compiler's eyes too)
@@ -217,6 +228,11 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
             mbar_init(smem_u32(&bars.s_free[i]), kStageThreads);
             mbar_init(smem_u32(&bars.r_ready[i]), kStageThreads);
             mbar_init(smem_u32(&bars.o_full[i]), 1);
+            mbar_init(smem_u32(&bars.met[i]), kStageThreads);
+        }
+        for (int i = 0; i < kChunks; ++i) {
+            mbar_init(smem_u32(&bars.chunk_full[i]), 1);
+            mbar_init(smem_u32(&bars.chunk_free[i]), kRowWarps + 3);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&bars.k_full[i]), 1);
@@ -230,7 +246,10 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    if (warp == 0) find_start(a, plan, start, &count);
+    constexpr bool kWide = OUT == HCCS_I32 || OUT == HCCS_F32;
+    constexpr int kElem = kWide ? 4 : 2, kDimsAtATime = kStageRow / kElem;
+    if (tid < kTile) row_at[tid] = (tid / a.group * a.Hq + tid % a.group) * (D * kElem / 16);
+    if (warp == kCopyWarp) find_start(a, plan, start, &count);
     if (warp == kPvWarp) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(kTmemCols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -241,9 +260,16 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
     const uint32_t tmem = tmem_slot;
     auto wait = [&](uint64_t *bar, uint32_t parity) -> bool { return warp_wait(smem_u32(bar), parity, abortp, a.status, a.wait_cycles); };
 
-    Walk walk;
-    walk.b = start[0]; walk.kvh = start[1]; walk.tile = start[2]; walk.left = count;
-    walk.window(a, walk.b);
+    // chunk number c, for the roles but the copies: false when a wait was given up
+    auto chunk = [&](int c, Chunk &k) -> bool {
+        const bool ok = wait(&bars.chunk_full[c % kChunks], (c / kChunks) & 1);
+        if (ok) {
+            k = chunks[c % kChunks];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&bars.chunk_free[c % kChunks]));
+        }
+        return ok;
+    };
     Chunk k;
 
     if (warp == kCopyWarp) {
@@ -259,22 +285,34 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
             }
             __syncwarp();
         };
-        while (ok && walk.next(a, plan, k)) {
-            if (k.seq.n == 0) continue;
+        Walk walk;
+        walk.b = start[0]; walk.kvh = start[1]; walk.tile = start[2]; walk.left = count;
+        walk.window(a, walk.b);
+        for (int c = 0; ok; ++c) {
+            k = walk.next(a, plan);
+            if (c >= kChunks) ok = wait(&bars.chunk_free[c % kChunks], (c / kChunks - 1) & 1);
+            if (!ok) break;
+            if (lane == 0) {
+                chunks[c % kChunks] = k;
+                mbar_arrive(smem_u32(&bars.chunk_full[c % kChunks]));
+            }
+            __syncwarp();
+            if (k.tiles == 0) break;
+            if (k.n == 0) continue;
             const int ks = kc & 1, vs = plan.v_slots == 2 ? kc & 1 : 0, vround = plan.v_slots == 2 ? kc >> 1 : kc;
             if (kc >= 2) ok = wait(&bars.k_free[ks], ((kc >> 1) - 1) & 1);
             if (!ok) break;
-            copy(s_k + ks * kv_bytes, &map_k, k.kvh, k.seq.k0, &bars.k_full[ks], (uint32_t)kv_bytes);
+            copy(s_k + ks * kv_bytes, &map_k, k.kvh, k.k0, &bars.k_full[ks], (uint32_t)kv_bytes);
             ++kc;
             for (int t = 0; t < k.tiles; ++t, ++it) {
                 const int st = it & (kStages - 1);
                 if (it >= kStages) ok = wait(&bars.q_free[st], ((it >> kShift) - 1) & 1);
                 if (!ok) break;
-                copy(s_q + st * kTileBytes, &map_q, k.kvh * a.group, k.seq.s0 + (k.tile0 + t) * plan.queries, &bars.q_full[st], q_bytes);
+                copy(s_q + st * kTileBytes, &map_q, k.kvh * a.group, k.q0 + t * plan.queries, &bars.q_full[st], q_bytes);
                 if (t == 0) {
                     if (vround >= 1) ok = wait(&bars.v_free[vs], (vround - 1) & 1);
                     if (!ok) { ++it; break; }
-                    copy(s_v + vs * kv_bytes, &map_v, k.kvh, k.seq.k0, &bars.v_full[vs], (uint32_t)kv_bytes);
+                    copy(s_v + vs * kv_bytes, &map_v, k.kvh, k.k0, &bars.v_full[vs], (uint32_t)kv_bytes);
                     ++sent_v;
                 }
             }
@@ -290,8 +328,8 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
         const uint32_t idesc = kIdescQK | (uint32_t)(nk >> 3) << 17;
         int it = 0, kc = 0;
         bool ok = true;
-        while (ok && walk.next(a, plan, k)) {
-            if (k.seq.n == 0) continue;
+        for (int c = 0; ok && (ok = chunk(c, k)) && k.tiles > 0; ++c) {
+            if (k.n == 0) continue;
             const int ks = kc & 1;
             ok = wait(&bars.k_full[ks], (kc >> 1) & 1);
             const uint32_t k_lo = (uint32_t)dk + ((uint32_t)(ks * kv_bytes) >> 4);
@@ -319,8 +357,8 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
         const uint64_t dr = smem_desc(s_r, 16, 1024, kSwizzle128), dv = smem_desc(s_v, 8 * D, 8 * D, kSwizzle);
         int it = 0, kc = 0;
         bool ok = true;
-        while (ok && walk.next(a, plan, k)) {
-            if (k.seq.n == 0) continue;
+        for (int c = 0; ok && (ok = chunk(c, k)) && k.tiles > 0; ++c) {
+            if (k.n == 0) continue;
             const int vs = plan.v_slots == 2 ? kc & 1 : 0, vround = plan.v_slots == 2 ? kc >> 1 : kc;
             ok = wait(&bars.v_full[vs], vround & 1);
             const uint32_t v_lo = (uint32_t)dv + ((uint32_t)(vs * kv_bytes) >> 4);
@@ -347,8 +385,8 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
         const int piece = lane % kPieces, first = lane / kPieces;
         int kc = 0;
         bool ok = true;
-        while (ok && walk.next(a, plan, k)) {
-            if (k.seq.n == 0) continue;
+        for (int c = 0; ok && (ok = chunk(c, k)) && k.tiles > 0; ++c) {
+            if (k.n == 0) continue;
             const int vs = plan.v_slots == 2 ? kc & 1 : 0, vround = plan.v_slots == 2 ? kc >> 1 : kc;
             if (kc >= 2) ok = wait(&bars.sum_free[kc & 1], ((kc >> 1) - 1) & 1);
             if (ok) ok = wait(&bars.v_full[vs], vround & 1);
@@ -358,7 +396,7 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
 #pragma unroll
             for (int i = 0; i < 16; ++i) sum[i] = 0;
 #pragma unroll 2
-            for (int r = first; r < k.seq.n; r += kLanes) {
+            for (int r = first; r < k.n; r += kLanes) {
                 const uint4 w = *reinterpret_cast<const uint4 *>(v + r * D + ((piece ^ (D == 128 ? r & 7 : (r >> 1) & 3)) << 4));
                 const int x[4] = {(int)w.x, (int)w.y, (int)w.z, (int)w.w};
 #pragma unroll
@@ -391,74 +429,65 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
         // where the warp stages its stores once the tile's products are through: WIDE, its share of the panel, which the others write again
         // behind the next barrier of the stage alone; else the place of its own rows, which nobody else writes
         uint8_t *const staged = panel + (WIDE ? (warp & 7) * (32 * kStageRow) : quarter * (32 * 128));
-        constexpr bool kWide = OUT == HCCS_I32 || OUT == HCCS_F32;
-        constexpr int kElem = kWide ? 4 : 2, kDimsAtATime = kStageRow / kElem;
-        // a lane of the stores takes piece lane % 4 of rows lane / 4, + 8, ... of the warp's 32: where they lie in O (16-byte units)
-        int store_at[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int row = quarter * 32 + i * 8 + (lane >> 2);
-            store_at[i] = (row / a.group * a.Hq + row % a.group) * (D * kElem / 16) + (lane & 3);
-        }
-        auto stage_barrier = [&]() { asm volatile("bar.sync %0, %1;" ::"r"(stage + 1), "n"(kStageThreads) : "memory"); };
+        // a barrier of the stage's row threads, given up like every other wait: the first of a tile, then the second
+        auto meet = [&](uint32_t phase) -> bool {
+            mbar_arrive(smem_u32(&bars.met[stage]));
+            return wait(&bars.met[stage], phase);
+        };
         int it = 0, kc = 0;
-        bool ok = true;          // a wait given up: the rest is walked through for the stage's barriers alone
-        while (walk.next(a, plan, k)) {
-            const int rows_left = min(k.seq.nq, a.max_q) * a.group;
+        bool ok = true;
+        for (int c = 0; ok && (ok = chunk(c, k)) && k.tiles > 0; ++c) {
+            // a lane of the stores takes piece lane % 4 of rows lane / 4, + 8, ... of the warp's 32
             auto store_rows = [&](int tile, int at_dim, bool zeros) {
-                const int left = min(rows_left - tile * plan.queries * a.group, plan.queries * a.group) - quarter * 32 - (lane >> 2);
+                const int left = min(k.rows - tile * plan.queries * a.group, plan.queries * a.group) - quarter * 32 - (lane >> 2);
                 uint4 *const out = reinterpret_cast<uint4 *>(static_cast<uint8_t *>(a.O) +
-                    ((((int64_t)k.seq.s0 + (int64_t)tile * plan.queries) * a.Hq + (int64_t)k.kvh * a.group) * D + half * kDims + at_dim) * kElem);
+                    ((((int64_t)k.q0 + tile * plan.queries) * a.Hq + k.kvh * a.group) * D + half * kDims + at_dim) * kElem) + (lane & 3);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int r = i * 8 + (lane >> 2);
                     uint4 v = make_uint4(0, 0, 0, 0);
                     if (!zeros) v = *reinterpret_cast<const uint4 *>(staged + r * kStageRow + (((lane & 3) ^ ((r >> 1) & 3)) << 4));
-                    if (i * 8 < left) out[store_at[i]] = v;
+                    if (i * 8 < left) out[row_at[quarter * 32 + r]] = v;
                 }
             };
-            if (k.seq.n == 0) {                                    // nothing to see: zeros
+            if (k.n == 0) {                                        // nothing to see: zeros
                 for (int x = stage; x < k.tiles; x += kStages)
-                    for (int dim = 0; dim < kDims; dim += kDimsAtATime) store_rows(k.tile0 + x, dim, true);
+                    for (int dim = 0; dim < kDims; dim += kDimsAtATime) store_rows(x, dim, true);
                 continue;
             }
             const int h = k.kvh * a.group + t % a.group;
             const int4 e = *reinterpret_cast<const int4 *>(a.table + h);
             const HeadRequant rq = head_requant(a.mult[h], a.requant_shift);
-            const int F = e.x - e.y * e.z, n = k.seq.n;
+            const int F = e.x - e.y * e.z, n = k.n;
             const float scale = a.scale[h];
+            const int mine = min(max(n - key0, 0), width), whole = mine & ~31;      // keys of this thread's that there are
             bool sums = false;                                     // sum V of the chunk has been waited for
             for (int x = 0; x < k.tiles; ++x, ++it) {
                 if ((it & (kStages - 1)) != stage) continue;
                 const uint32_t phase = (it >> kShift) & 1;
                 // ---- the largest accumulator
-                if (ok) ok = wait(&bars.s_full[stage], phase);
+                ok = wait(&bars.s_full[stage], phase);
+                if (!ok) break;
                 tcgen05_fence_after();
                 int amax = kNone;
-                for (int i = 0; ok && i + 32 <= width; i += 32) {
-                    if (key0 + i >= n) break;
+#pragma unroll 1
+                for (int i = 0; i < whole; i += 32) {
                     uint32_t acc[32];
                     tmem_ld32(s_at + key0 + i, acc);
-                    if (key0 + i + 32 > n) {
-                        const uint32_t mask = low_bits(n - key0 - i);
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) acc[j] = (mask >> j) & 1 ? acc[j] : (uint32_t)kNone;
-                    }
 #pragma unroll
                     for (int j = 0; j < 32; j += 2) amax = __vimax3_s32(amax, (int)acc[j], (int)acc[j + 1]);
                 }
-                const int tail = key0 + (width & ~31);             // 16 more keys where the width is odd that way
-                if (WIDE && ok && (width & 16) && tail < n) {
+#pragma unroll 1
+                for (int i = whole; i < mine; i += 16) {
                     uint32_t acc[16];
-                    tmem_ld16(s_at + tail, acc);
-                    const uint32_t mask = low_bits(n - tail);
+                    tmem_ld16(s_at + key0 + i, acc);
 #pragma unroll
-                    for (int j = 0; j < 16; j += 2)
-                        amax = __vimax3_s32(amax, (mask >> j) & 1 ? (int)acc[j] : kNone, (mask >> (j + 1)) & 1 ? (int)acc[j + 1] : kNone);
+                    for (int j = 0; j < 16; ++j) amax = max(amax, i + j < mine ? (int)acc[j] : kNone);
                 }
                 if constexpr (WIDE) {
                     part_max[stage][half][t] = amax;
-                    stage_barrier();
+                    ok = meet(0);
+                    if (!ok) break;
                     amax = max(amax, part_max[stage][half ^ 1][t]);
                 } else {
                     __syncwarp();
@@ -480,41 +509,32 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
                 auto put16 = [&](int key, const uint32_t *w) {     // 16 keys of the row into the panel
                     *reinterpret_cast<uint4 *>(panel + (key >> 7) * (kTile * 128) + t * 128 + ((((key & 127) >> 4) ^ (t & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
                 };
-                auto masked = [&](uint32_t w, uint32_t mask) -> uint32_t { return w & ((((mask & 15u) * 0x00204081u) & 0x01010101u) * 255u); };
-                for (int i = 0; ok && i + 32 <= width; i += 32) {
-                    uint32_t w[8];
-                    if (key0 + i < n) {
-                        uint32_t acc[32];
-                        tmem_ld32(s_at + key0 + i, acc);
-                        const uint32_t mask = low_bits(n - key0 - i);
+#pragma unroll 1
+                for (int i = 0; i < whole; i += 32) {
+                    uint32_t acc[32], w[8];
+                    tmem_ld32(s_at + key0 + i, acc);
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) w[j] = bytes4(acc + 4 * j);
-                        if (mask != ~0u) {
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) w[j] = masked(w[j], mask >> (4 * j));
-                        }
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) rsum = (int)__dp4a(w[j], 0x01010101u, (uint32_t)rsum);
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) w[j] = 0u;
+                    for (int j = 0; j < 8; ++j) {
+                        w[j] = bytes4(acc + 4 * j);
+                        rsum = (int)__dp4a(w[j], 0x01010101u, (uint32_t)rsum);
                     }
                     put16(key0 + i, w);
                     put16(key0 + i + 16, w + 4);
                 }
-                if (WIDE && ok && (width & 16)) {
-                    uint32_t w[4] = {0u, 0u, 0u, 0u};
-                    if (tail < n) {
-                        uint32_t acc[16];
-                        tmem_ld16(s_at + tail, acc);
-                        const uint32_t mask = low_bits(n - tail);
+#pragma unroll 1
+                for (int i = whole; i < mine; i += 16) {
+                    uint32_t acc[16], w[4];
+                    tmem_ld16(s_at + key0 + i, acc);
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            w[j] = masked(bytes4(acc + 4 * j), mask >> (4 * j));
-                            rsum = (int)__dp4a(w[j], 0x01010101u, (uint32_t)rsum);
-                        }
+                    for (int j = 0; j < 4; ++j) {
+                        w[j] = bytes4(acc + 4 * j) & low_bits(8 * min(max(mine - i - 4 * j, 0), 4));
+                        rsum = (int)__dp4a(w[j], 0x01010101u, (uint32_t)rsum);
                     }
-                    put16(tail, w);
+                    put16(key0 + i, w);
+                }
+                for (int i = (mine + 15) & ~15; i < width; i += 16) {
+                    const uint32_t w[4] = {0u, 0u, 0u, 0u};
+                    put16(key0 + i, w);
                 }
                 tcgen05_fence_before();
                 if (apart) mbar_arrive(smem_u32(&bars.s_free[stage]));
@@ -522,48 +542,60 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 mbar_arrive(smem_u32(&bars.r_ready[stage]));
                 if constexpr (WIDE) {
-                    stage_barrier();
+                    ok = meet(1);
+                    if (!ok) break;
                     rsum += part_sum[stage][half ^ 1][t];
                 }
                 const RowFactor f = row_factor(a, (int64_t)F * n + (int64_t)e.y * rsum, scale);
-                if (ok && !sums) {
+                if (!sums) {
                     ok = wait(&bars.sum_full[kc & 1], (kc >> 1) & 1);
                     sums = true;
                 }
                 if (ok) ok = wait(&bars.o_full[stage], phase);
-                if (!ok) continue;
+                if (!ok) break;
                 tcgen05_fence_after();
                 // ---- the rows' outputs, 64 bytes of each at a time, through the warp's part of the panel: four lanes store a row's piece.
                 // In the integer modes rho goes into the factors (what it multiplies out to fits int32).
                 const int rho = OUT != HCCS_I32 && a.recip == HCCS_RECIP_REAL ? 1 : f.rho, by_r = e.y * rho, by_v = F * rho;
-                const bool tiny = OUT != HCCS_I32 && __any_sync(~0u, f.unit != 1.0f);
+                // Sums below 2^22 become floats by their place in the mantissa of 1.5 * 2^23, which the products' addend has in it already.
+                const bool small = OUT != HCCS_I32 && __all_sync(~0u, (int64_t)(F * n + e.y * rsum) * rho < 32768 && f.unit == 1.0f);
+                const uint32_t magic = small ? 0x4b400000u : 0u;
+                auto pack = [&](uint32_t (&o)[kDimsAtATime], int i, float v, float w) {
+                    if constexpr (OUT == HCCS_F32) {
+                        o[i] = __float_as_uint(v);
+                        o[i + 1] = __float_as_uint(w);
+                    } else if constexpr (OUT == HCCS_BF16) {
+                        const __nv_bfloat162 b2 = __floats2bfloat162_rn(v, w);
+                        o[i >> 1] = *reinterpret_cast<const uint32_t *>(&b2);
+                    } else {
+                        const __half2 h2 = __floats2half2_rn(v, w);
+                        o[i >> 1] = *reinterpret_cast<const uint32_t *>(&h2);
+                    }
+                };
+#pragma unroll 1
                 for (int y = 0; y < kDims * kElem / kStageRow; ++y) {
                     uint32_t o[kDimsAtATime];
                     tmem_ld(o_at + y * kDimsAtATime, o);
 #pragma unroll
                     for (int i = 0; i < kDimsAtATime; i += 4) {
                         const int4 vs = *reinterpret_cast<const int4 *>(&vsum[kc & 1][half * kDims + y * kDimsAtATime + i]);
-                        o[i] = (uint32_t)(by_r * (int)o[i] + by_v * vs.x);
-                        o[i + 1] = (uint32_t)(by_r * (int)o[i + 1] + by_v * vs.y);
-                        o[i + 2] = (uint32_t)(by_r * (int)o[i + 2] + by_v * vs.z);
-                        o[i + 3] = (uint32_t)(by_r * (int)o[i + 3] + by_v * vs.w);
+                        o[i] = (uint32_t)by_r * o[i] + ((uint32_t)by_v * (uint32_t)vs.x + magic);
+                        o[i + 1] = (uint32_t)by_r * o[i + 1] + ((uint32_t)by_v * (uint32_t)vs.y + magic);
+                        o[i + 2] = (uint32_t)by_r * o[i + 2] + ((uint32_t)by_v * (uint32_t)vs.z + magic);
+                        o[i + 3] = (uint32_t)by_r * o[i + 3] + ((uint32_t)by_v * (uint32_t)vs.w + magic);
                     }
                     if constexpr (OUT != HCCS_I32) {
+                        if (small) {
 #pragma unroll
-                        for (int i = 0; i < kDimsAtATime; i += 2) {
-                            float v = (float)(int)o[i], w = (float)(int)o[i + 1];
-                            scale2(v, w, f.scale);
-                            if (tiny) scale2(v, w, f.unit);
-                            if constexpr (OUT == HCCS_F32) {
-                                o[i] = __float_as_uint(v);
-                                o[i + 1] = __float_as_uint(w);
-                            } else if constexpr (OUT == HCCS_BF16) {
-                                const __nv_bfloat162 b2 = __floats2bfloat162_rn(v, w);
-                                o[i >> 1] = *reinterpret_cast<const uint32_t *>(&b2);
-                            } else {
-                                const __half2 h2 = __floats2half2_rn(v, w);
-                                o[i >> 1] = *reinterpret_cast<const uint32_t *>(&h2);
+                            for (int i = 0; i < kDimsAtATime; i += 2) {
+                                float v = __uint_as_float(o[i]), w = __uint_as_float(o[i + 1]);
+                                add2(v, w, -12582912.0f);
+                                scale2(v, w, f.scale);
+                                pack(o, i, v, w);
                             }
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < kDimsAtATime; i += 2) pack(o, i, (float)(int)o[i] * f.scale * f.unit, (float)(int)o[i + 1] * f.scale * f.unit);
                         }
                     }
 #pragma unroll
@@ -574,7 +606,7 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
                         if (!apart) mbar_arrive(smem_u32(&bars.s_free[stage]));
                     }
                     __syncwarp();
-                    store_rows(k.tile0 + x, y * kDimsAtATime, false);
+                    store_rows(x, y * kDimsAtATime, false);
                     __syncwarp();
                 }
             }
