@@ -669,6 +669,7 @@ static hccs_status_t write_tokens(hccs_ctx_t *ctx, const WriteCall &w, void *cud
     a.T = T; a.Hq = with_q ? w.Hq : 0; a.Hkv = with_kv ? w.Hkv : 0; a.d = d; a.page_shift = page_shift;
     a.dense_len = w.L;
     if (turns) a.rope = *rope;
+    a.axes = w.axes != nullptr;
     if (turns && w.axes) memcpy(a.axis, w.axes->axis, sizeof(a.axis));
     if (with_q) memcpy(a.step, w.q_step, sizeof(float) * w.Hq);
     if (with_kv) {

@@ -133,13 +133,14 @@ __device__ __noinline__ uint32_t code_pair(float a, float b, double position, do
     return (uint32_t)(m & 255) | (uint32_t)(n & 255) << 8;
 }
 
-// The position that turns a pair of token t: every pair goes by one axis.
+// The position that turns a pair of token t: with several axes every pair goes by its own.
+template <bool AXES>
 __device__ __forceinline__ double position_of(const CacheWriteArgs &a, int t, int pair) {
-    return (double)a.positions[a.axis[pair] * a.axis_stride + t * a.token_stride];
+    return (double)(AXES ? a.positions[a.axis[pair] * a.axis_stride + t * a.token_stride] : a.positions[t]);
 }
 
 // Items of heads whose rotated part is no multiple of 16 dims: a dim at a time, in fp32 where that is sure.
-template <typename T>
+template <bool AXES, typename T>
 __device__ __noinline__ int8_t code_of(const T *head, int dim, const CacheWriteArgs &a, const Turn *turn, int t, float step) {
     const int rot = a.rope.rot_dim;
     const bool inter = a.rope.interleaved != 0;
@@ -153,7 +154,7 @@ __device__ __noinline__ int8_t code_of(const T *head, int dim, const CacheWriteA
     const float z = __fmul_rn(fmaf(x, turn->c[skew(pair)], __fmul_rn(p, first ? -s : s)), inv);
     int n;
     if (fmaf(fabsf(x) + fabsf(p), fmaxf(fabsf((float)a.rope.scale) * inv * 0x1p-21f, 0x1p-125f), nearest(z, n)) < 0.5f) return (int8_t)max(min(n, 127), -128);
-    const double position = position_of(a, t, pair), freq = a.rope.freq[pair];
+    const double position = position_of<AXES>(a, t, pair), freq = a.rope.freq[pair];
     const uint32_t two = first ? code_pair(x, p, position, freq, a.rope.scale, step) : code_pair(p, x, position, freq, a.rope.scale, step) >> 8;
     return (int8_t)(two & 255);
 }
@@ -166,7 +167,7 @@ constexpr int kWriteThreads = 384;         // most threads per CTA: all items of
 constexpr int kTokens = 16;                // most tokens per CTA
 
 // DENSE: codes of all three kinds go to tensors [T/L, heads, L, d], L tokens of a head together (L = 1: [T, heads, d]).
-template <typename T, bool DENSE>
+template <typename T, bool DENSE, bool AXES>
 __global__ void __launch_bounds__(kWriteThreads, 2)
 cache_write_kernel(const __grid_constant__ CacheWriteArgs a, int items, int per_head_shift, int per_cta) {
     __shared__ Turn turn[kTokens];
@@ -206,10 +207,10 @@ cache_write_kernel(const __grid_constant__ CacheWriteArgs a, int items, int per_
         for (int pair = (int)threadIdx.x & (wide - 1); pair < half && tok0 < abreast; pair += wide) {
             const double freq = a.rope.freq[pair];
             const float scale = (float)a.rope.scale;
-            const int32_t *const positions = a.positions + a.axis[pair] * a.axis_stride;
+            const int32_t *const positions = AXES ? a.positions + a.axis[pair] * a.axis_stride : a.positions;
             for (int tok = tok0; tok < tokens; tok += abreast) {
                 // the angle as the definition rounds it, in turns, less the whole ones: exact but for 2^-53 of the turns
-                const double angle = __dmul_rn((double)positions[(t0 + tok) * a.token_stride], freq), turns = __dmul_rn(angle, 0.15915494309189533577);
+                const double angle = __dmul_rn((double)(AXES ? positions[(t0 + tok) * a.token_stride] : positions[t0 + tok]), freq), turns = __dmul_rn(angle, 0.15915494309189533577);
                 const double part = turns - rint(turns);
                 const float hi = (float)part, lo = (float)(part - (double)hi) * 6.2831853f;
                 float s, c;
@@ -350,17 +351,18 @@ cache_write_kernel(const __grid_constant__ CacheWriteArgs a, int items, int per_
     // What was next to a border, four pairs at a time (a dim at a time where items do not hold whole pairs).  Behind the loop: a
     // call in it, however rare, costs its registers.
     src -= (int64_t)tokens * stride;
+    if constexpr (!DENSE) q_dst -= (int64_t)tokens * a.Hq * a.d;
     while (redo) {
         const int bit = __ffs(redo) - 1, j = bit >> 1, g = bit & 1;
         redo &= redo - 1;
-        int8_t *const dst = dense ? row_at(t0 + j) : place(a.slots[t0 + j]);
+        int8_t *const dst = !dense ? place(a.slots[t0 + j]) : DENSE ? row_at(t0 + j) : q_dst + (int64_t)j * a.Hq * a.d;
         const T *const row = src + j * stride;
         const Turn &tn = turn[j];
         if (!aligned) {
 #pragma unroll 1
             for (int e = 0; e < 8; ++e) {
                 const int dim = (g ? dim_b : dim_a) + e;
-                dst[dim] = code_of(row, dim, a, &tn, t0 + j, step);
+                dst[dim] = code_of<AXES>(row, dim, a, &tn, t0 + j, step);
             }
             continue;
         }
@@ -384,7 +386,7 @@ cache_write_kernel(const __grid_constant__ CacheWriteArgs a, int items, int per_
         for (int i = 0; i < 4; ++i) {
             if (!((unsure >> i) & 1)) continue;
             const float x = i == 0 ? u[0] : i == 1 ? u[1] : i == 2 ? u[2] : u[3], y = i == 0 ? v[0] : i == 1 ? v[1] : i == 2 ? v[2] : v[3];
-            const uint32_t n2 = code_pair(x, y, position_of(a, t0 + j, first + i), a.rope.freq[first + i], a.rope.scale, step);
+            const uint32_t n2 = code_pair(x, y, position_of<AXES>(a, t0 + j, first + i), a.rope.freq[first + i], a.rope.scale, step);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 nu[k] = k == i ? (int8_t)(n2 & 255) : nu[k];
@@ -505,8 +507,9 @@ cudaError_t write_typed(const CacheWriteArgs &a, cudaStream_t stream) {
     int per_cta = (int)((all + slots * waves - 1) / (slots * waves));
     per_cta = per_cta < 1 ? 1 : per_cta > kTokens ? kTokens : per_cta;
     const dim3 grid((unsigned)((a.T + per_cta - 1) / per_cta), (unsigned)groups);
-    if (a.dense_len) cache_write_kernel<T, true><<<grid, threads, 0, stream>>>(a, items, shift, per_cta);
-    else cache_write_kernel<T, false><<<grid, threads, 0, stream>>>(a, items, shift, per_cta);
+    if (a.dense_len) cache_write_kernel<T, true, true><<<grid, threads, 0, stream>>>(a, items, shift, per_cta);
+    else if (a.axes) cache_write_kernel<T, false, true><<<grid, threads, 0, stream>>>(a, items, shift, per_cta);
+    else cache_write_kernel<T, false, false><<<grid, threads, 0, stream>>>(a, items, shift, per_cta);
     return cudaGetLastError();
 }
 

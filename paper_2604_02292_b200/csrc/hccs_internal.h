@@ -68,7 +68,7 @@ struct FusedArgs {
 struct CacheWriteArgs {
     const void *q, *k, *v;
     int64_t q_stride, k_stride, v_stride;       // elements between tokens
-    const int32_t *positions;                   // of token t on axis x: positions[x * axis_stride + t * token_stride]
+    const int32_t *positions;                   // of token t, or on axis x: positions[x * axis_stride + t * token_stride]
     int64_t axis_stride, token_stride;
     const int64_t *slots;
     int8_t *q8, *k_pages, *v_pages;             // (dense: k_pages and v_pages are tensors like q8)
@@ -77,6 +77,7 @@ struct CacheWriteArgs {
     int32_t T, Hq, Hkv, d, page_shift;
     int32_t dense_len;                          // 0: pages; L: tensors [T/L, heads, L, d]
     hccs_rope_t rope;                           // rot_dim 0: none
+    int32_t axes;                               // several axes
     uint8_t axis[HCCS_MAX_ROT_DIM / 2];         // of pair i
     float step[3 * HCCS_MAX_CACHE_HEADS];       // q, k and v, HCCS_MAX_CACHE_HEADS apart
 };
