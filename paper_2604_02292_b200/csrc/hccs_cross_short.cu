@@ -29,7 +29,6 @@ constexpr int kMaxStages = 4;
 constexpr int kChunks = 4;                       // chunks that are known ahead
 constexpr int kMaxKeys = 256;
 constexpr uint32_t kTmemCols = 512;
-constexpr int kStageRow = 64;                    // bytes of a row that a warp stages at a time for its stores
 
 constexpr uint32_t kIdescQK = instr_desc(1, 1, 0, 128, 0);                      // (the keys join at run time)
 template <int D> constexpr uint32_t kIdescPVOf = instr_desc(0, 1, 1, 128, D);   // r.V: uint8 x int8, V MN-major
@@ -62,12 +61,16 @@ __device__ __forceinline__ int tiles_of(const CachedAttnArgs &a, const SequenceA
     return (min(seq.nq, a.max_q) + plan.queries - 1) / plan.queries;
 }
 
+// What a tile of a sequence costs, in parts: its rows' outputs and waits, and 16 keys a part (tiles of 256 and of 100 keys measure nearly
+// alike, 3900 cycles for heads of 128).
+__device__ __forceinline__ int tile_cost(const SequenceAt &seq) { return seq.n == 0 ? 4 : 24 + ((seq.n + 15) >> 4); }
+
 // The chunks of a CTA, walked through by a warp: tiles are in the order (sequence, kv head, tile).  A lane holds one of 32
 // neighbouring sequences, so that their lengths are read together and those without queries are skipped together.
 struct Walk {
     int q0, q1, k0, kv, first;                   // this lane's sequence, number first + lane
     int b, kvh, tile;
-    int64_t left;                                // tiles still to come
+    int64_t left;                                // cost of the tiles still to come (the last may go beyond)
 
     __device__ __forceinline__ void window(const CachedAttnArgs &a, int from) {
         const int mine = from + (int)(threadIdx.x & 31);
@@ -101,25 +104,28 @@ struct Walk {
         k.n = seq.n;
         k.k0 = seq.k0;
         k.kvh = kvh;
-        k.tiles = (int)min((int64_t)(tiles_of(a, seq, plan) - tile), left);
+        const int cost = tile_cost(seq);
+        k.tiles = (int)min((int64_t)(tiles_of(a, seq, plan) - tile), (left + cost - 1) / cost);
         k.q0 = seq.s0 + tile * plan.queries;
         k.rows = (min(seq.nq, a.max_q) - tile * plan.queries) * a.group;
-        left -= k.tiles;
+        left -= (int64_t)k.tiles * cost;
         tile = 0;
         if (++kvh == a.Hkv) { kvh = 0; ++b; }
         return k;
     }
 };
 
-// Where a CTA's walk starts, found by one warp: a lane counts the tiles of its share of the sequences.
-__device__ __forceinline__ void find_start(const CachedAttnArgs &a, const ShortPlan &plan, int *start, int64_t *count) {
+// Where a CTA's walk starts and how much it takes, found by one warp: CTAs share the cost evenly, and a tile goes to the one in whose
+// part it begins.  A lane adds up its share of the sequences.
+__device__ __forceinline__ void find_start(const CachedAttnArgs &a, const ShortPlan &plan, int *start, int64_t *left) {
     const int lane = threadIdx.x & 31, share = (a.B + 31) / 32, b0 = min(lane * share, a.B), b1 = min(b0 + share, a.B);
+    auto cost_of = [&](const SequenceAt &seq) -> int64_t { return (int64_t)tiles_of(a, seq, plan) * tile_cost(seq) * a.Hkv; };
     int64_t mine = 0;
     bool cut = false;
 #pragma unroll 4
     for (int b = b0; b < b1; ++b) {
         const SequenceAt seq = sequence_at<true>(a, b);
-        mine += tiles_of(a, seq, plan);
+        mine += cost_of(seq);
         cut |= seq.cut;
     }
     if (cut && blockIdx.x == 0) atomicOr(a.status, STATUS_BAD_LENGTH);
@@ -129,23 +135,31 @@ __device__ __forceinline__ void find_start(const CachedAttnArgs &a, const ShortP
         const int64_t v = __shfl_up_sync(~0u, upto, o);
         if (lane >= o) upto += v;
     }
-    const int64_t all = __shfl_sync(~0u, upto, 31) * a.Hkv, per = all / gridDim.x, more = all % gridDim.x;
-    const int64_t from = blockIdx.x * per + min((int64_t)blockIdx.x, more);
-    if (lane == 0) { start[0] = start[1] = start[2] = 0; *count = per + ((int64_t)blockIdx.x < more ? 1 : 0); }
-    __syncwarp();
-    int64_t before = (upto - mine) * a.Hkv;
-    if (from >= before && from < upto * a.Hkv) {
-        for (int b = b0; b < b1; ++b) {
-            const int n = tiles_of(a, sequence_at<true>(a, b), plan);
-            if (from < before + (int64_t)n * a.Hkv) {
-                const int64_t off = from - before;
-                start[0] = b;
-                start[1] = (int)(off / n);
-                start[2] = (int)(off % n);
-                break;
+    const int64_t all = __shfl_sync(~0u, upto, 31), per = (all + gridDim.x - 1) / gridDim.x;
+    const int64_t from = min(per * blockIdx.x, all), to = min(from + per, all);
+    // the first tile that begins at `from` or behind it: a lane looks in its own share, the first one to have it counts
+    int64_t before = upto - mine, begin = to;
+    int first_b = 0, pair = 0, tile = 0;
+    if (upto > from) {
+        for (int b = b0; b < b1 && begin == to; ++b) {
+            const SequenceAt seq = sequence_at<true>(a, b);
+            const int tiles = tiles_of(a, seq, plan), cost = tile_cost(seq);
+            const int64_t skip = (max(from - before, (int64_t)0) + cost - 1) / cost;      // tiles of this sequence
+            if (skip < (int64_t)tiles * a.Hkv && before + skip * cost < to) {
+                begin = before + skip * cost;
+                first_b = b;
+                pair = (int)(skip / tiles);
+                tile = (int)(skip % tiles);
             }
-            before += (int64_t)n * a.Hkv;
+            before += (int64_t)tiles * a.Hkv * cost;
         }
+    }
+    const uint32_t some = __ballot_sync(~0u, begin < to);
+    if (lane == (some ? __ffs(some) - 1 : 0)) {
+        start[0] = first_b;
+        start[1] = pair;
+        start[2] = tile;
+        *left = to - begin;
     }
 }
 
@@ -177,6 +191,14 @@ __device__ __forceinline__ HeadRequant head_requant(int M, int sh) {
 // N columns of tensor memory (load and wait in one statement)
 __device__ __forceinline__ void tmem_ld(uint32_t at, uint32_t (&r)[16]) { tmem_ld16(at, r); }
 __device__ __forceinline__ void tmem_ld(uint32_t at, uint32_t (&r)[32]) { tmem_ld32(at, r); }
+
+// Two 16 x 16 blocks of bytes, their rows at the addresses of lanes 0..15 and 16..31, transposed: word 2m + i of lane l has
+// rows 4 * (l % 4) .. + 3 of column l / 4 + 8i of block m.
+__device__ __forceinline__ void ldmatrix_b8_trans(uint32_t row, uint32_t (&w)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m16n16.x2.trans.shared.b8 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(row) : "memory");
+}
+__device__ __forceinline__ int dp4a_s8(uint32_t a, uint32_t b, int c) { return __dp4a((int)a, (int)b, c); }
 
 // Two values plus a constant, and two products with a factor.
 __device__ __forceinline__ void add2(float &x, float &y, float by) {
@@ -247,7 +269,10 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     constexpr bool kWide = OUT == HCCS_I32 || OUT == HCCS_F32;
-    constexpr int kElem = kWide ? 4 : 2, kDimsAtATime = kStageRow / kElem;
+    constexpr int kElem = kWide ? 4 : 2, kDimsAtATime = 64 / kElem;              // outputs of a thread in registers: 64 bytes
+    // bytes of a row that a warp stages for its stores: a line of memory where the warp has one (with 64 everywhere, 24 ragged texts on
+    // 256 patches took 56.3 us instead of 54.1)
+    constexpr int kStageRow = kDims * kElem < 128 ? kDims * kElem : 128, kRowLanes = kStageRow / 16, kRowsAtATime = 32 / kRowLanes;
     if (tid < kTile) row_at[tid] = (tid / a.group * a.Hq + tid % a.group) * (D * kElem / 16);
     if (warp == kCopyWarp) find_start(a, plan, start, &count);
     if (warp == kPvWarp) {
@@ -285,11 +310,25 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
             }
             __syncwarp();
         };
+        auto keys = [&](const Chunk &k) -> bool {
+            if (kc >= 2 && !wait(&bars.k_free[kc & 1], ((kc >> 1) - 1) & 1)) return false;
+            copy(s_k + (kc & 1) * kv_bytes, &map_k, k.kvh, k.k0, &bars.k_full[kc & 1], (uint32_t)kv_bytes);
+            ++kc;
+            return true;
+        };
+        auto values = [&](const Chunk &k) -> bool {
+            const int vs = sent_v % plan.v_slots, round = sent_v / plan.v_slots;
+            if (round >= 1 && !wait(&bars.v_free[vs], (round - 1) & 1)) return false;
+            copy(s_v + vs * kv_bytes, &map_v, k.kvh, k.k0, &bars.v_full[vs], (uint32_t)kv_bytes);
+            ++sent_v;
+            return true;
+        };
         Walk walk;
         walk.b = start[0]; walk.kvh = start[1]; walk.tile = start[2]; walk.left = count;
         walk.window(a, walk.b);
+        k = walk.next(a, plan);
+        bool early = false;                                        // K (and V, where it has two slots) of the chunk are on their way
         for (int c = 0; ok; ++c) {
-            k = walk.next(a, plan);
             if (c >= kChunks) ok = wait(&bars.chunk_free[c % kChunks], (c / kChunks - 1) & 1);
             if (!ok) break;
             if (lane == 0) {
@@ -298,24 +337,25 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
             }
             __syncwarp();
             if (k.tiles == 0) break;
-            if (k.n == 0) continue;
-            const int ks = kc & 1, vs = plan.v_slots == 2 ? kc & 1 : 0, vround = plan.v_slots == 2 ? kc >> 1 : kc;
-            if (kc >= 2) ok = wait(&bars.k_free[ks], ((kc >> 1) - 1) & 1);
-            if (!ok) break;
-            copy(s_k + ks * kv_bytes, &map_k, k.kvh, k.k0, &bars.k_full[ks], (uint32_t)kv_bytes);
-            ++kc;
-            for (int t = 0; t < k.tiles; ++t, ++it) {
-                const int st = it & (kStages - 1);
-                if (it >= kStages) ok = wait(&bars.q_free[st], ((it >> kShift) - 1) & 1);
-                if (!ok) break;
-                copy(s_q + st * kTileBytes, &map_q, k.kvh * a.group, k.q0 + t * plan.queries, &bars.q_full[st], q_bytes);
-                if (t == 0) {
-                    if (vround >= 1) ok = wait(&bars.v_free[vs], (vround - 1) & 1);
-                    if (!ok) { ++it; break; }
-                    copy(s_v + vs * kv_bytes, &map_v, k.kvh, k.k0, &bars.v_full[vs], (uint32_t)kv_bytes);
-                    ++sent_v;
+            const Chunk next = walk.next(a, plan);
+            if (k.n > 0) {
+                if (!early) ok = keys(k);
+                const bool there = early && plan.v_slots == 2;
+                early = false;
+                for (int t = 0; ok && t < k.tiles; ++t, ++it) {
+                    const int st = it & (kStages - 1);
+                    if (it >= kStages) ok = wait(&bars.q_free[st], ((it >> kShift) - 1) & 1);
+                    if (!ok) break;
+                    copy(s_q + st * kTileBytes, &map_q, k.kvh * a.group, k.q0 + t * plan.queries, &bars.q_full[st], q_bytes);
+                    if (t == 0 && !there) ok = values(k);
+                    // the next chunk's follow a few tiles later: their places are those of the chunk before this one
+                    if (ok && t == min(kStages - 1, k.tiles - 1) && next.tiles > 0 && next.n > 0) {
+                        ok = keys(next) && (plan.v_slots == 1 || values(next));
+                        early = true;
+                    }
                 }
             }
+            k = next;
         }
         // (the last copy into each place has landed before the CTA may leave, whatever became of its readers; again with a limit)
         for (int x = max(it - kStages, 0); x < it; ++x) mbar_wait_bounded(smem_u32(&bars.q_full[x & (kStages - 1)]), (x >> kShift) & 1, a.wait_cycles);
@@ -380,9 +420,10 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
             ++kc;
         }
     } else if (warp == kSumWarp) {
-        // ===================================================== sum V: a lane adds 16 dims of every kLanes-th key
-        constexpr int kPieces = D / 16, kLanes = 32 / kPieces;
-        const int piece = lane % kPieces, first = lane / kPieces;
+        // ===================================================== sum V.  32 keys of 16 dims at a time are loaded transposed: a word of lane l
+        // holds four keys (those from 4 * (l % 4) on) of dim l / 4, the second one of dim l / 4 + 8, and so on for 16 keys more
+        constexpr int kPieces = D / 16;
+        const int col = lane >> 2;
         int kc = 0;
         bool ok = true;
         for (int c = 0; ok && (ok = chunk(c, k)) && k.tiles > 0; ++c) {
@@ -391,26 +432,29 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
             if (kc >= 2) ok = wait(&bars.sum_free[kc & 1], ((kc >> 1) - 1) & 1);
             if (ok) ok = wait(&bars.v_full[vs], vround & 1);
             if (!ok) break;
-            const uint8_t *v = gen + (s_v - base) + vs * kv_bytes;
-            int sum[16];
+            const uint32_t v = s_v + vs * kv_bytes;
+            int sum[kPieces][2];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sum[i] = 0;
-#pragma unroll 2
-            for (int r = first; r < k.n; r += kLanes) {
-                const uint4 w = *reinterpret_cast<const uint4 *>(v + r * D + ((piece ^ (D == 128 ? r & 7 : (r >> 1) & 3)) << 4));
-                const int x[4] = {(int)w.x, (int)w.y, (int)w.z, (int)w.w};
+            for (int p = 0; p < kPieces; ++p) sum[p][0] = sum[p][1] = 0;
+            for (int r0 = 0; r0 < k.n; r0 += 32) {
+                const int r = r0 + lane, first = r0 + (lane & 3) * 4;
+                const uint32_t m0 = low_bits(8 * min(max(k.n - first, 0), 4)), m1 = low_bits(8 * min(max(k.n - first - 16, 0), 4));
 #pragma unroll
-                for (int i = 0; i < 16; ++i) sum[i] = __dp4a(x[i >> 2], 1 << (8 * (i & 3)), sum[i]);
+                for (int p = 0; p < kPieces; ++p) {
+                    uint32_t w[4];
+                    ldmatrix_b8_trans(v + r * D + ((p ^ (D == 128 ? r & 7 : (r >> 1) & 3)) << 4), w);
+                    sum[p][0] = dp4a_s8(w[0] & m0, 0x01010101u, dp4a_s8(w[2] & m1, 0x01010101u, sum[p][0]));
+                    sum[p][1] = dp4a_s8(w[1] & m0, 0x01010101u, dp4a_s8(w[3] & m1, 0x01010101u, sum[p][1]));
+                }
             }
 #pragma unroll
-            for (int o = kPieces; o < 32; o <<= 1)
+            for (int p = 0; p < kPieces; ++p)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) sum[i] += __shfl_xor_sync(~0u, sum[i], o);
-            if (first == 0) {
-#pragma unroll
-                for (int i = 0; i < 16; i += 4)
-                    *reinterpret_cast<int4 *>(&vsum[kc & 1][piece * 16 + i]) = make_int4(sum[i], sum[i + 1], sum[i + 2], sum[i + 3]);
-            }
+                for (int i = 0; i < 2; ++i) {
+                    sum[p][i] += __shfl_xor_sync(~0u, sum[p][i], 1);
+                    sum[p][i] += __shfl_xor_sync(~0u, sum[p][i], 2);
+                    if ((lane & 3) == 0) vsum[kc & 1][p * 16 + col + 8 * i] = sum[p][i];
+                }
             __syncwarp();
             if (lane == 0) {
                 mbar_arrive(smem_u32(&bars.sum_full[kc & 1]));
@@ -429,6 +473,8 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
         // where the warp stages its stores once the tile's products are through: WIDE, its share of the panel, which the others write again
         // behind the next barrier of the stage alone; else the place of its own rows, which nobody else writes
         uint8_t *const staged = panel + (WIDE ? (warp & 7) * (32 * kStageRow) : quarter * (32 * 128));
+        // piece `piece` of the warp's row r: eight neighbouring rows' pieces lie on different banks
+        auto staged_at = [&](int r, int piece) -> int { return r * kStageRow + ((piece ^ (kRowLanes == 8 ? r & 7 : (r >> 1) & 3)) << 4); };
         // a barrier of the stage's row threads, given up like every other wait: the first of a tile, then the second
         auto meet = [&](uint32_t phase) -> bool {
             mbar_arrive(smem_u32(&bars.met[stage]));
@@ -437,22 +483,23 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
         int it = 0, kc = 0;
         bool ok = true;
         for (int c = 0; ok && (ok = chunk(c, k)) && k.tiles > 0; ++c) {
-            // a lane of the stores takes piece lane % 4 of rows lane / 4, + 8, ... of the warp's 32
+            // a lane of the stores takes piece lane % kRowLanes of rows lane / kRowLanes, + kRowsAtATime, ... of the warp's 32
             auto store_rows = [&](int tile, int at_dim, bool zeros) {
-                const int left = min(k.rows - tile * plan.queries * a.group, plan.queries * a.group) - quarter * 32 - (lane >> 2);
+                const int r0 = lane / kRowLanes, piece = lane % kRowLanes;
+                const int left = min(k.rows - tile * plan.queries * a.group, plan.queries * a.group) - quarter * 32 - r0;
                 uint4 *const out = reinterpret_cast<uint4 *>(static_cast<uint8_t *>(a.O) +
-                    ((((int64_t)k.q0 + tile * plan.queries) * a.Hq + k.kvh * a.group) * D + half * kDims + at_dim) * kElem) + (lane & 3);
+                    ((((int64_t)k.q0 + tile * plan.queries) * a.Hq + k.kvh * a.group) * D + half * kDims + at_dim) * kElem) + piece;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int r = i * 8 + (lane >> 2);
+                for (int i = 0; i < kRowLanes; ++i) {
+                    const int r = i * kRowsAtATime + r0;
                     uint4 v = make_uint4(0, 0, 0, 0);
-                    if (!zeros) v = *reinterpret_cast<const uint4 *>(staged + r * kStageRow + (((lane & 3) ^ ((r >> 1) & 3)) << 4));
-                    if (i * 8 < left) out[row_at[quarter * 32 + r]] = v;
+                    if (!zeros) v = *reinterpret_cast<const uint4 *>(staged + staged_at(r, piece));
+                    if (i * kRowsAtATime < left) out[row_at[quarter * 32 + r]] = v;
                 }
             };
             if (k.n == 0) {                                        // nothing to see: zeros
                 for (int x = stage; x < k.tiles; x += kStages)
-                    for (int dim = 0; dim < kDims; dim += kDimsAtATime) store_rows(x, dim, true);
+                    for (int dim = 0; dim < kDims; dim += kStageRow / kElem) store_rows(x, dim, true);
                 continue;
             }
             const int h = k.kvh * a.group + t % a.group;
@@ -554,11 +601,14 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
                 if (ok) ok = wait(&bars.o_full[stage], phase);
                 if (!ok) break;
                 tcgen05_fence_after();
-                // ---- the rows' outputs, 64 bytes of each at a time, through the warp's part of the panel: four lanes store a row's piece.
-                // In the integer modes rho goes into the factors (what it multiplies out to fits int32).
-                const int rho = OUT != HCCS_I32 && a.recip == HCCS_RECIP_REAL ? 1 : f.rho, by_r = e.y * rho, by_v = F * rho;
-                // Sums below 2^22 become floats by their place in the mantissa of 1.5 * 2^23, which the products' addend has in it already.
-                const bool small = OUT != HCCS_I32 && __all_sync(~0u, (int64_t)(F * n + e.y * rsum) * rho < 32768 && f.unit == 1.0f);
+                // ---- the rows' outputs, 64 bytes of each at a time, through the warp's part of the panel, from which neighbouring lanes store a row.
+                // Sums below 2^22 (ordinary tables) become floats by their place in the mantissa of 1.5 * 2^23, which the products' addend has in
+                // it already; their product with rho is a whole number below 2^24, so exact.  (A converter has a quarter of the other
+                // pipes' rate: with it 24 ragged texts on 256 patches, leading-bit reciprocal, took 57 us.)
+                const bool small = OUT != HCCS_I32 && __all_sync(~0u, F * n + e.y * rsum < 32768 && f.unit == 1.0f);
+                const int whole_rho = a.recip == HCCS_RECIP_REAL ? 1 : f.rho;
+                const float rho = (float)whole_rho;
+                const int by_r = e.y * (small ? 1 : whole_rho), by_v = F * (small ? 1 : whole_rho);
                 const uint32_t magic = small ? 0x4b400000u : 0u;
                 auto pack = [&](uint32_t (&o)[kDimsAtATime], int i, float v, float w) {
                     if constexpr (OUT == HCCS_F32) {
@@ -573,7 +623,7 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
                     }
                 };
 #pragma unroll 1
-                for (int y = 0; y < kDims * kElem / kStageRow; ++y) {
+                for (int y = 0; y < kDims / kDimsAtATime; ++y) {
                     uint32_t o[kDimsAtATime];
                     tmem_ld(o_at + y * kDimsAtATime, o);
 #pragma unroll
@@ -590,6 +640,7 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
                             for (int i = 0; i < kDimsAtATime; i += 2) {
                                 float v = __uint_as_float(o[i]), w = __uint_as_float(o[i + 1]);
                                 add2(v, w, -12582912.0f);
+                                scale2(v, w, rho);
                                 scale2(v, w, f.scale);
                                 pack(o, i, v, w);
                             }
@@ -600,14 +651,16 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
                     }
 #pragma unroll
                     for (int p = 0; p < 4; ++p)
-                        *reinterpret_cast<uint4 *>(staged + lane * kStageRow + ((p ^ ((lane >> 1) & 3)) << 4)) = make_uint4(o[4 * p], o[4 * p + 1], o[4 * p + 2], o[4 * p + 3]);
-                    if (y == kDims * kElem / kStageRow - 1) {
+                        *reinterpret_cast<uint4 *>(staged + staged_at(lane, (y * 4 + p) % kRowLanes)) = make_uint4(o[4 * p], o[4 * p + 1], o[4 * p + 2], o[4 * p + 3]);
+                    if (y == kDims / kDimsAtATime - 1) {
                         tcgen05_fence_before();
                         if (!apart) mbar_arrive(smem_u32(&bars.s_free[stage]));
                     }
-                    __syncwarp();
-                    store_rows(x, y * kDimsAtATime, false);
-                    __syncwarp();
+                    if ((y * 4 + 4) % kRowLanes == 0) {
+                        __syncwarp();
+                        store_rows(x, (y + 1) * kDimsAtATime - kStageRow / kElem, false);
+                        __syncwarp();
+                    }
                 }
             }
             // (a warp without a tile in this chunk waits as well: nobody is a chunk ahead of the sums)
