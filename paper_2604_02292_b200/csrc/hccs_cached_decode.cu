@@ -79,11 +79,12 @@ struct Sizes {
 // D: head dim.  HI: more than 8 rows (the fragments' rows 8..15 are rows too; otherwise row 8 is all ones and
 // collects sum V for nothing).  tiles_per_warp bounds what shared memory holds.
 // CROSS: queries on an encoder's states.  The rows of a kv head are its (query, head) pairs, all of which see the same keys:
-// those of the sequence, or where max_q is 1 those of the query's key range.
+// those of the sequence, or where max_q is 1 those of the query's key range.  Up to `merge` neighbouring sequences of one query that read the
+// same states (hypotheses about one input) are rows of one CTA too, that of the first of them.
 template <int D, bool HI, int W, bool CROSS>
 __global__ void __launch_bounds__(32 * W, 16 / W)
 cached_decode_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_constant__ CUtensorMap map_k,
-                     const __grid_constant__ CUtensorMap map_v, int row_tiles, int tiles_per_warp) {
+                     const __grid_constant__ CUtensorMap map_v, int row_tiles, int tiles_per_warp, int merge) {
     using S = Sizes<D, HI, W>;
     constexpr int kWarps = W, kThreads = 32 * W;
     constexpr int kChunks = D / 64;            // 16-byte chunks of a K row per lane
@@ -105,7 +106,7 @@ cached_decode_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_cons
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, c = lane & 3, nn = lane >> 2;
     uint8_t *const smem = smem_raw + (((smem_u32(smem_raw) + 1023u) & ~1023u) - smem_u32(smem_raw));      // (the swizzles count from there)
     if (tid == 0) abort_flag = 0;
-    if (split > 1) cluster_arrive();           // the other CTAs run: waited for before the first push
+    if (!CROSS && split > 1) cluster_arrive(); // the other CTAs run: waited for before the first push
     const int32_t *table = CROSS ? nullptr : a.page_table + (int64_t)b * a.max_pages;
     // tiles in turn to the warps of the cluster: the first does not depend on the length
     const int first = rank * kWarps + warp, stride = kWarps * split;
@@ -115,9 +116,29 @@ cached_decode_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_cons
     };
     int page[2] = {page_at(first * kTileKeys), page_at(first * kTileKeys + 16)};
     const SequenceAt seq = sequence_at<CROSS>(a, b);
-    const int rows = CROSS ? min(kRows, min(seq.nq, a.max_q) * a.group - row0) : min(kRows, a.group - row0);
+    int together = 1;                          // sequences
+    if (CROSS && merge > 1) {
+        // blocks of `merge` sequences: in a block, those with the states of the one before them leave
+        const int from = b - b % merge, other = min(from + min(lane, merge - 1), a.B - 1);
+        const int ks = a.k_start[other], kl = a.kv_len[other];
+        const int mine = __shfl_sync(~0u, ks, b - from), keys = __shfl_sync(~0u, kl, b - from);
+        const uint32_t same = __ballot_sync(~0u, lane < merge && from + lane < a.B && ks == mine && kl == keys) >> (b - from);
+        const bool follows = __shfl_sync(~0u, (int)(ks == mine && kl == keys), max(b - from - 1, 0)) && b > from;
+        if (follows) {
+            if (seq.cut && tid == 0 && blockIdx.x + blockIdx.y == 0) atomicOr(a.status, STATUS_BAD_LENGTH);
+            return;                            // (the whole cluster)
+        }
+        together = same == ~0u ? 32 : __ffs(~same) - 1;
+    }
+    if (CROSS && split > 1) cluster_arrive();
+    const int rows = !CROSS ? min(kRows, a.group - row0) : merge > 1 ? together * a.group : min(kRows, min(seq.nq, a.max_q) * a.group - row0);
     const int head0 = kvh * a.group + row0;
-    auto query_of = [&](int row) -> int { return CROSS ? (row0 + row) / a.group : 0; };
+    // the row's token, or -1: its sequence has none
+    auto token_of = [&](int row) -> int {
+        if (!CROSS || merge <= 1) return seq.nq <= 0 ? -1 : seq.s0 + (CROSS ? (row0 + row) / a.group : 0);
+        const int at = b + row / a.group, s0 = min(max(a.q_start[at], 0), a.T);
+        return min(a.q_start[at + 1], a.T) > s0 ? s0 : -1;
+    };
     auto head_of = [&](int row) -> int { return CROSS ? kvh * a.group + (row0 + row) % a.group : head0 + row; };
     if (seq.cut && tid == 0 && blockIdx.x + blockIdx.y == 0) atomicOr(a.status, STATUS_BAD_LENGTH);
     // the new token sees the keys before it and, unless a tree mask hides it, itself
@@ -130,12 +151,12 @@ cached_decode_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_cons
         n = max(min(r.y, n) - x, 0);
         k0 += n > 0 ? x : 0;
     }
-    const int tiles = seq.nq > 0 && rows > 0 ? (n + kTileKeys - 1) / kTileKeys : 0;
+    const int tiles = (seq.nq > 0 || (CROSS && merge > 1)) && rows > 0 ? (n + kTileKeys - 1) / kTileKeys : 0;
     const int mine = min(first < tiles ? (tiles - first + stride - 1) / stride : 0, tiles_per_warp);
 
     const uint32_t ring = smem_u32(smem) + (uint32_t)(warp * kDepth * S::kTileBytes);
     // logits of a tile: [half of its keys][row, four words of four keys each]; a lane whose row is none has no place
-    const int max_rows = min(kRows, CROSS ? a.max_q * a.group : a.group), x_half = 4 * max_rows, x_tile = 2 * x_half;
+    const int max_rows = min(kRows, CROSS ? a.max_q * a.group * merge : a.group), x_half = 4 * max_rows, x_tile = 2 * x_half;
     uint32_t *const xs = reinterpret_cast<uint32_t *>(smem + S::kRing) + warp * x_tile + lane;               // + tile * kWarps * x_tile
     uint32_t *const seen_s = reinterpret_cast<uint32_t *>(smem + S::kRing) + (size_t)tiles_per_warp * kWarps * x_tile + warp;   // + tile * kWarps
     const bool has0 = nn < max_rows, has1 = HI && nn + 8 < max_rows;
@@ -217,12 +238,16 @@ cached_decode_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_cons
     // Q as A fragments: lane (nn, c) holds chunk c (and c + 4) of rows nn and nn + 8
     uint32_t qf[2 * kChunks][4];
     {
-        auto q = [&](int row) -> const int8_t * { return a.Q + (((int64_t)seq.s0 + query_of(row)) * a.Hq + head_of(row)) * D; };
+        auto q = [&](int row) -> const int8_t * {          // NULL: no such row, or nothing to see
+            const int token = row < rows && mine > 0 ? token_of(row) : -1;
+            return token < 0 ? nullptr : a.Q + ((int64_t)token * a.Hq + head_of(row)) * D;
+        };
+        const int8_t *const q0 = q(nn), *const q1 = HI ? q(nn + 8) : nullptr;
 #pragma unroll
         for (int ch = 0; ch < kChunks; ++ch) {
             uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
-            if (nn < rows && mine > 0) lo = *reinterpret_cast<const uint4 *>(q(nn) + ch * 64 + c * 16);
-            if (HI && nn + 8 < rows && mine > 0) hi = *reinterpret_cast<const uint4 *>(q(nn + 8) + ch * 64 + c * 16);
+            if (q0) lo = *reinterpret_cast<const uint4 *>(q0 + ch * 64 + c * 16);
+            if (q1) hi = *reinterpret_cast<const uint4 *>(q1 + ch * 64 + c * 16);
             qf[2 * ch][0] = lo.x; qf[2 * ch][1] = hi.x; qf[2 * ch][2] = lo.y; qf[2 * ch][3] = hi.y;
             qf[2 * ch + 1][0] = lo.z; qf[2 * ch + 1][1] = hi.z; qf[2 * ch + 1][2] = lo.w; qf[2 * ch + 1][3] = hi.w;
         }
@@ -436,10 +461,12 @@ cached_decode_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_cons
     }
 
     // ---- join: a thread finishes four dims of a row
-    if (seq.nq > 0)
+    if (seq.nq > 0 || (CROSS && merge > 1))
         for (int i = tid; i < rows * own; i += kThreads) {
             const int row = i / own, q = i % own;
             if (q * split + rank >= kQuads) continue;
+            const int token = token_of(row);
+            if (token < 0) continue;
             int rv[4] = {0, 0, 0, 0}, vs[4] = {0, 0, 0, 0}, rs = 0, keys = 0;
             for (int r = 0; r < split; ++r) {
                 const int4 p = all_quads[(r * own + q) * (kRows + 1) + row], s = all_quads[(r * own + q) * (kRows + 1) + kRows];
@@ -454,7 +481,7 @@ cached_decode_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_cons
             int64_t num[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) num[e] = F * vs[e] + (int64_t)th.S * rv[e];
-            store_output4(a, (((int64_t)seq.s0 + query_of(row)) * a.Hq + h) * D + 4 * (q * split + rank), num, row_factor(a, F * keys + (int64_t)th.S * rs, a.scale[h]));
+            store_output4(a, ((int64_t)token * a.Hq + h) * D + 4 * (q * split + rank), num, row_factor(a, F * keys + (int64_t)th.S * rs, a.scale[h]));
         }
 }
 
@@ -500,7 +527,7 @@ cudaError_t plan_for(const CachedAttnArgs &a, int64_t groups, int rows, Plan &be
 }
 
 template <int D, bool HI, int W, bool CROSS>
-cudaError_t launch_plan(const CachedAttnArgs &a, const Plan &p, int rows, int row_tiles, cudaStream_t stream) {
+cudaError_t launch_plan(const CachedAttnArgs &a, const Plan &p, int rows, int row_tiles, int merge, cudaStream_t stream) {
     CUtensorMap mk, mv;
     if (CROSS ? !make_states_map(&mk, a.k_pages, a.k_stride, a, kTileKeys) || !make_states_map(&mv, a.v_pages, a.v_stride, a, kTileKeys)
               : !make_page_map(&mk, a.k_pages, a, kTileKeys) || !make_page_map(&mv, a.v_pages, a, kTileKeys))
@@ -517,13 +544,19 @@ cudaError_t launch_plan(const CachedAttnArgs &a, const Plan &p, int rows, int ro
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, cached_decode_kernel<D, HI, W, CROSS>, a, mk, mv, row_tiles, p.per_warp);
+    return cudaLaunchKernelEx(&cfg, cached_decode_kernel<D, HI, W, CROSS>, a, mk, mv, row_tiles, p.per_warp, merge);
 }
 
 template <int D, bool HI, bool CROSS>
 cudaError_t launch_typed(const CachedAttnArgs &a, cudaStream_t stream) {
     constexpr int kRows = Sizes<D, HI, 8>::kRows;
-    const int rows = CROSS ? a.max_q * a.group : a.group;           // of a kv head
+    int rows = CROSS ? a.max_q * a.group : a.group;                 // of a kv head
+    // Room for the rows of sequences that share their states, where there may be any and the logits of all rows leave room for two
+    // CTAs on an SM
+    int merge = 1;
+    if (CROSS && a.max_q == 1 && !a.key_range && a.B > 1 && Sizes<D, HI, 8>::smem((a.max_kv + kTileKeys - 1) / kTileKeys + 8, kRows) <= kHalfSmem)
+        merge = kRows / a.group > 1 ? kRows / a.group : 1;
+    rows *= merge;
     const int row_tiles = (rows + kRows - 1) / kRows;
     const int64_t groups = (int64_t)a.B * a.Hkv * row_tiles;
     Plan p8, p16;
@@ -533,8 +566,8 @@ cudaError_t launch_typed(const CachedAttnArgs &a, cudaStream_t stream) {
     // (sixteen warps' rings leave no room for the logits of many rows of long caches: d = 128, 16 rows, more than 81920 keys;
     // eight warps in clusters of sixteen hold all that is allowed)
     if (p8.cost == HUGE_VAL && p16.cost == HUGE_VAL) return cudaErrorInvalidConfiguration;
-    return p16.cost < p8.cost ? launch_plan<D, HI, 16, CROSS>(a, p16, rows, row_tiles, stream)
-                              : launch_plan<D, HI, 8, CROSS>(a, p8, rows, row_tiles, stream);
+    return p16.cost < p8.cost ? launch_plan<D, HI, 16, CROSS>(a, p16, rows, row_tiles, merge, stream)
+                              : launch_plan<D, HI, 8, CROSS>(a, p8, rows, row_tiles, merge, stream);
 }
 
 template <bool CROSS>

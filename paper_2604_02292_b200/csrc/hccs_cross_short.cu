@@ -310,13 +310,13 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
             }
             __syncwarp();
         };
-        auto keys = [&](const Chunk &k) -> bool {
+        auto keys = [&]() -> bool {
             if (kc >= 2 && !wait(&bars.k_free[kc & 1], ((kc >> 1) - 1) & 1)) return false;
             copy(s_k + (kc & 1) * kv_bytes, &map_k, k.kvh, k.k0, &bars.k_full[kc & 1], (uint32_t)kv_bytes);
             ++kc;
             return true;
         };
-        auto values = [&](const Chunk &k) -> bool {
+        auto values = [&]() -> bool {
             const int vs = sent_v % plan.v_slots, round = sent_v / plan.v_slots;
             if (round >= 1 && !wait(&bars.v_free[vs], (round - 1) & 1)) return false;
             copy(s_v + vs * kv_bytes, &map_v, k.kvh, k.k0, &bars.v_full[vs], (uint32_t)kv_bytes);
@@ -326,9 +326,8 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
         Walk walk;
         walk.b = start[0]; walk.kvh = start[1]; walk.tile = start[2]; walk.left = count;
         walk.window(a, walk.b);
-        k = walk.next(a, plan);
-        bool early = false;                                        // K (and V, where it has two slots) of the chunk are on their way
         for (int c = 0; ok; ++c) {
+            k = walk.next(a, plan);
             if (c >= kChunks) ok = wait(&bars.chunk_free[c % kChunks], (c / kChunks - 1) & 1);
             if (!ok) break;
             if (lane == 0) {
@@ -337,25 +336,15 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
             }
             __syncwarp();
             if (k.tiles == 0) break;
-            const Chunk next = walk.next(a, plan);
-            if (k.n > 0) {
-                if (!early) ok = keys(k);
-                const bool there = early && plan.v_slots == 2;
-                early = false;
-                for (int t = 0; ok && t < k.tiles; ++t, ++it) {
-                    const int st = it & (kStages - 1);
-                    if (it >= kStages) ok = wait(&bars.q_free[st], ((it >> kShift) - 1) & 1);
-                    if (!ok) break;
-                    copy(s_q + st * kTileBytes, &map_q, k.kvh * a.group, k.q0 + t * plan.queries, &bars.q_full[st], q_bytes);
-                    if (t == 0 && !there) ok = values(k);
-                    // the next chunk's follow a few tiles later: their places are those of the chunk before this one
-                    if (ok && t == min(kStages - 1, k.tiles - 1) && next.tiles > 0 && next.n > 0) {
-                        ok = keys(next) && (plan.v_slots == 1 || values(next));
-                        early = true;
-                    }
-                }
+            if (k.n == 0) continue;
+            ok = keys();
+            for (int t = 0; ok && t < k.tiles; ++t, ++it) {
+                const int st = it & (kStages - 1);
+                if (it >= kStages) ok = wait(&bars.q_free[st], ((it >> kShift) - 1) & 1);
+                if (!ok) break;
+                copy(s_q + st * kTileBytes, &map_q, k.kvh * a.group, k.q0 + t * plan.queries, &bars.q_full[st], q_bytes);
+                if (t == 0) ok = values();
             }
-            k = next;
         }
         // (the last copy into each place has landed before the CTA may leave, whatever became of its readers; again with a limit)
         for (int x = max(it - kStages, 0); x < it; ++x) mbar_wait_bounded(smem_u32(&bars.q_full[x & (kStages - 1)]), (x >> kShift) & 1, a.wait_cycles);

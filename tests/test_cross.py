@@ -395,6 +395,20 @@ def test_shared_states(hccs, ctx, d, hq, hkv, length, dtype):
         cross(hccs, ctx, rng, [queries, queries, 2, queries], [length, length, 9, length], hq, hkv, d, "div", dtype, share=[0, 0, 2, 0])
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,hq,hkv", [(64, 3, 3), (128, 2, 1), (64, 12, 2), (128, 9, 1), (64, 20, 1)])
+@pytest.mark.parametrize("norm,dtype", [("div", "i32"), ("real", "f32")])
+def test_single_queries_of_sequences_with_the_same_states(hccs, ctx, d, hq, hkv, norm, dtype):
+    """Runs of hypotheses of one input: longer than a CTA takes together, across its blocks, broken by others, some without a query."""
+    rng = np.random.default_rng(d + hq)
+    share = [0] * 11 + [11, 12, 12, 12, 15, 12, 17, 17, 11, 11]
+    lens = [201] * 11 + [64, 33, 33, 33, 0, 33, 1500, 1500, 64, 64]
+    q_lens = [1] * len(lens)
+    q_lens[0] = q_lens[4] = q_lens[13] = 0
+    cross(hccs, ctx, rng, q_lens, lens, hq, hkv, d, norm, dtype, share=share, theta=_theta(rng, hq, 1500, False))
+    cross(hccs, ctx, rng, [0, 0, 1, 0], [70] * 4, hq, hkv, d, norm, dtype, share=[0, 0, 0, 0])
+
+
 def _some_ranges(rng, q_lens, k_lens):
     out = []
     for nq, n in zip(q_lens, k_lens):
