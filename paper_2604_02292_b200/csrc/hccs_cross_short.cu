@@ -55,6 +55,7 @@ struct ShortPlan {
     int keys;                                    // of the K and V tiles: a multiple of 32
     int v_slots;
     int queries;                                 // per tile
+    int warp_queries;                            // whole ones among the 32 rows of a warp, or 0: its rows are cut by heads
 };
 
 __device__ __forceinline__ int tiles_of(const CachedAttnArgs &a, const SequenceAt &seq, const ShortPlan &plan) {
@@ -212,7 +213,7 @@ __device__ __forceinline__ void scale2(float &x, float &y, float by) {
 template <int D, int OUT, bool WIDE>
 __global__ void __launch_bounds__(kThreads, 1)
 cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
-                   const __grid_constant__ CUtensorMap map_v, const ShortPlan plan) {
+                   const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_o, const ShortPlan plan) {
     constexpr int kTileBytes = kTile * D;
     constexpr int kStages = WIDE ? 2 : 4, kHalves = WIDE ? 2 : 1, kShift = WIDE ? 1 : 2;
     constexpr int kCols = (int)kTmemCols / kStages;                // tensor-memory columns of a stage
@@ -241,6 +242,10 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
     const uint32_t o_col = nk + D <= kCols ? kCols - D : 0;        // O's columns in its stage's part
     const bool apart = o_col != 0;
 
+    if (warp == kCopyWarp && lane < 4) {
+        const CUtensorMap *const map = lane == 0 ? &map_q : lane == 1 ? &map_k : lane == 2 ? &map_v : &map_o;
+        asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+    }
     if (tid == 0) {
         abort_flag = 0;
         for (int i = 0; i < kStages; ++i) {
@@ -464,6 +469,11 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
         uint8_t *const staged = panel + (WIDE ? (warp & 7) * (32 * kStageRow) : quarter * (32 * 128));
         // piece `piece` of the warp's row r: eight neighbouring rows' pieces lie on different banks
         auto staged_at = [&](int r, int piece) -> int { return r * kStageRow + ((piece ^ (kRowLanes == 8 ? r & 7 : (r >> 1) & 3)) << 4); };
+        // the warp's copies have read what they store: its place may be written again
+        auto stored = [&]() {
+            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+            __syncwarp();
+        };
         // a barrier of the stage's row threads, given up like every other wait: the first of a tile, then the second
         auto meet = [&](uint32_t phase) -> bool {
             mbar_arrive(smem_u32(&bars.met[stage]));
@@ -474,8 +484,17 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
         for (int c = 0; ok && (ok = chunk(c, k)) && k.tiles > 0; ++c) {
             // a lane of the stores takes piece lane % kRowLanes of rows lane / kRowLanes, + kRowsAtATime, ... of the warp's 32
             auto store_rows = [&](int tile, int at_dim, bool zeros) {
+                const int there = min(k.rows - tile * plan.queries * a.group, plan.queries * a.group) - quarter * 32;
+                if (!zeros && plan.warp_queries != 0 && there >= 32) {
+                    // all 32 rows: one copy, which runs beside the next tile's first pass
+                    if (lane == 0) {
+                        tma_store_3d(&map_o, (half * kDims + at_dim) * kElem, k.kvh * a.group, k.q0 + tile * plan.queries + quarter * plan.warp_queries, smem_u32(staged));
+                        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                    }
+                    return;
+                }
                 const int r0 = lane / kRowLanes, piece = lane % kRowLanes;
-                const int left = min(k.rows - tile * plan.queries * a.group, plan.queries * a.group) - quarter * 32 - r0;
+                const int left = there - r0;
                 uint4 *const out = reinterpret_cast<uint4 *>(static_cast<uint8_t *>(a.O) +
                     ((((int64_t)k.q0 + tile * plan.queries) * a.Hq + k.kvh * a.group) * D + half * kDims + at_dim) * kElem) + piece;
 #pragma unroll
@@ -520,13 +539,12 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
 #pragma unroll
                     for (int j = 0; j < 16; ++j) amax = max(amax, i + j < mine ? (int)acc[j] : kNone);
                 }
+                stored();
                 if constexpr (WIDE) {
                     part_max[stage][half][t] = amax;
                     ok = meet(0);
                     if (!ok) break;
                     amax = max(amax, part_max[stage][half ^ 1][t]);
-                } else {
-                    __syncwarp();
                 }
                 // ---- r: with u = m - D, accumulators are clamped to [lo_u, hi], lo_u the smallest whose logit reaches max(u, -128); then
                 // clamp(acc - lo_u, 0, hi - lo_u)*(M << shl) + (((lo_u*M + R) << shl) - (u << 24)) has r as its top byte
@@ -613,6 +631,7 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
                 };
 #pragma unroll 1
                 for (int y = 0; y < kDims / kDimsAtATime; ++y) {
+                    if (y > 0 && (y * 4) % kRowLanes == 0) stored();
                     uint32_t o[kDimsAtATime];
                     tmem_ld(o_at + y * kDimsAtATime, o);
 #pragma unroll
@@ -640,12 +659,13 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
                     }
 #pragma unroll
                     for (int p = 0; p < 4; ++p)
-                        *reinterpret_cast<uint4 *>(staged + staged_at(lane, (y * 4 + p) % kRowLanes)) = make_uint4(o[4 * p], o[4 * p + 1], o[4 * p + 2], o[4 * p + 3]);
+                        *reinterpret_cast<uint4 *>(staged + (staged_at(lane, 0) ^ (((y * 4 + p) % kRowLanes) << 4))) = make_uint4(o[4 * p], o[4 * p + 1], o[4 * p + 2], o[4 * p + 3]);
                     if (y == kDims / kDimsAtATime - 1) {
                         tcgen05_fence_before();
                         if (!apart) mbar_arrive(smem_u32(&bars.s_free[stage]));
                     }
                     if ((y * 4 + 4) % kRowLanes == 0) {
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                         __syncwarp();
                         store_rows(x, (y + 1) * kDimsAtATime - kStageRow / kElem, false);
                         __syncwarp();
@@ -658,6 +678,7 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
             if (lane == 0) mbar_arrive(smem_u32(&bars.sum_free[kc & 1]));
             ++kc;
         }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     __syncwarp();
     tcgen05_fence_before();
@@ -679,16 +700,16 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
     }
 }
 
-// Queries as [T][Hq][D] bytes, boxes of a kv head's heads and a tile's queries.
-bool make_query_map(CUtensorMap *map, const CachedAttnArgs &a, int queries) {
+// Queries, or outputs, as [T][Hq][row bytes], boxes of `inner` bytes of a kv head's heads and some queries.
+bool make_rows_map(CUtensorMap *map, const void *rows, int row_bytes, int inner, const CachedAttnArgs &a, int queries) {
     EncodeTiledFn fn = encode_tiled_fn();
     if (!fn) return false;
-    const cuuint64_t dims[3] = {(cuuint64_t)a.d, (cuuint64_t)a.Hq, (cuuint64_t)a.T};
-    const cuuint64_t strides[2] = {(cuuint64_t)a.d, (cuuint64_t)a.Hq * a.d};
-    const cuuint32_t box[3] = {(cuuint32_t)a.d, (cuuint32_t)a.group, (cuuint32_t)queries};
+    const cuuint64_t dims[3] = {(cuuint64_t)row_bytes, (cuuint64_t)a.Hq, (cuuint64_t)a.T};
+    const cuuint64_t strides[2] = {(cuuint64_t)row_bytes, (cuuint64_t)a.Hq * row_bytes};
+    const cuuint32_t box[3] = {(cuuint32_t)inner, (cuuint32_t)a.group, (cuuint32_t)queries};
     const cuuint32_t estr[3] = {1, 1, 1};
-    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<int8_t *>(a.Q), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-              a.d == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void *>(rows), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              inner == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -710,11 +731,14 @@ cudaError_t launch_typed(const CachedAttnArgs &a, cudaStream_t stream) {
     const size_t fixed = 1024 + kStages * ((size_t)kTile * D + (size_t)((p.keys + 127) / 128) * kTile * 128), kv = (size_t)p.keys * D;
     p.v_slots = fixed + 4 * kv <= kMaxSmem ? 2 : 1;
     const size_t smem = fixed + (2 + p.v_slots) * kv;
-    CUtensorMap mq, mk, mv;
-    if (!make_query_map(&mq, a, p.queries) || !make_states_map(&mk, a.k_pages, a.k_stride, a, p.keys) || !make_states_map(&mv, a.v_pages, a.v_stride, a, p.keys))
+    // (a warp's rows are whole queries where the heads of a kv head divide 32; the map of the outputs is not used otherwise)
+    p.warp_queries = 32 % a.group == 0 ? 32 / a.group : 0;
+    constexpr int kElem = OUT == HCCS_I32 || OUT == HCCS_F32 ? 4 : 2, kRow = (WIDE ? D / 2 : D) * kElem;
+    CUtensorMap mq, mk, mv, mo;
+    if (!make_rows_map(&mq, a.Q, D, D, a, p.queries) || !make_rows_map(&mo, a.O, D * kElem, kRow < 128 ? kRow : 128, a, p.warp_queries ? p.warp_queries : 1) || !make_states_map(&mk, a.k_pages, a.k_stride, a, p.keys) || !make_states_map(&mv, a.v_pages, a.v_stride, a, p.keys))
         return cudaErrorInvalidValue;
     const int64_t most = (int64_t)a.B * a.Hkv * (((int64_t)a.max_q + p.queries - 1) / p.queries);      // tiles
-    kernel<<<(unsigned)(most < sms ? most : sms), kThreads, smem, stream>>>(a, mq, mk, mv, p);
+    kernel<<<(unsigned)(most < sms ? most : sms), kThreads, smem, stream>>>(a, mq, mk, mv, mo, p);
     return cudaGetLastError();
 }
 
