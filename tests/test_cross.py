@@ -446,3 +446,257 @@ def test_key_ranges_of_images(hccs, ctx, d):
     none = [(0, 0)] * 700
     out, _ = cross(hccs, ctx, rng, q_lens, k_lens, 4, 2, d, "real", "f32", ranges=none, wide=True)
     assert (out[:700] == 0).all()
+
+
+# ------------------------------------------------------------------------------------------- as programs use them
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,hq,hkv", [(64, 4, 4), (128, 8, 2)])
+def test_vision_language_step(hccs, d, hq, hkv):
+    """Patches of images with rows and columns through the encoder's attention; its keys and values as states; a prompt and a
+    token of the decoder look at them, and write their own keys with three axes into the cache that they attend to."""
+    import torch
+    from oracle import hccs_oracle as rows
+    rng = np.random.default_rng(d)
+    B, L, page = 2, 60, 16
+    ctx = hccs.Context(0)
+    theta = np.array([(100, 1, 60)] * hq, np.int32)
+    ctx.hccs_params_upload(theta, 128)
+    mult, scale = np.full(hq, 900, np.int32), np.full(hq, 0.03, np.float32)
+    steps = [np.full(n, 0.03, np.float32) for n in (hq, hkv, hkv)]
+    image = hccs.hccs_rope_axes(d, (d // 4, d // 4), restart=True)
+    half = d // 2
+    # the encoder: heads first, one kv head per query head
+    q, k, v = _tokens(rng, B * L, hq, hq, d, "bf16")
+    pos = np.stack([np.tile(np.arange(L) // 10, B), np.tile(np.arange(L) % 10, B)]).astype(np.int32)
+    P = torch.from_numpy(pos).cuda()
+    q8, k8, v8 = (torch.empty((B, hq, L, d), dtype=torch.int8, device="cuda") for _ in range(3))
+    out = torch.empty((B, hq, L, d), dtype=torch.int32, device="cuda")
+    ctx.hccs_states_write(q, k, v, q8, k8, v8, P, steps[0], steps[0], steps[0], rope=image)
+    ctx.hccs_attention_fused(q8, k8, v8, out, mult, 20)
+    freq, axis = list(image.rope.freq)[:half], list(image.axis)[:half]
+    turned = [orc.quantise(orc.rotate_axes(t.float().cpu().numpy(), pos, freq, axis, False, 1.0), steps[0]).reshape(B, L, hq, d).transpose(0, 2, 1, 3)
+              for t in (q, k)] + [orc.quantise(v.float().cpu().numpy(), steps[0]).reshape(B, L, hq, d).transpose(0, 2, 1, 3)]
+    for got, want in zip((q8, k8, v8), turned):
+        assert (got.cpu().numpy() == want).all()
+    want = rows.attention(*turned, mult, 20, theta)
+    assert (out.cpu().numpy() == want).all()
+    # the states that the decoder looks at
+    _, k, v = _tokens(rng, B * L, hq, hkv, d, "f16")
+    k8, v8 = (torch.empty((B * L, hkv, d), dtype=torch.int8, device="cuda") for _ in range(2))
+    ctx.hccs_states_write(None, k, v, None, k8, v8, None, None, steps[1], steps[2])
+    kk, vv = (orc.quantise(t.float().cpu().numpy(), steps[1]) for t in (k, v))
+    k_start, k_len = torch.tensor([0, L], dtype=torch.int32).cuda(), torch.tensor([L, L - 7], dtype=torch.int32).cuda()
+    pool_k, pool_v = (torch.zeros((12, hkv, page, d), dtype=torch.int8, device="cuda") for _ in range(2))
+    table = torch.tensor([[3, 1, 4], [0, 5, 9]], dtype=torch.int32).cuda()
+    text = hccs.hccs_rope_axes(d, (half - 2 * (half // 3), half // 3, half // 3), order=hccs.HCCS_AXES_TURNS)
+    done = 0
+    for n in (20, 1):                                      # a prompt of two texts, then a token of each
+        T = 2 * n
+        q, k, v = _tokens(rng, T, hq, hkv, d, "bf16")
+        at = np.concatenate([done + np.arange(n)] * 2)
+        pos = np.stack([at, at, at]).astype(np.int32)
+        slots = torch.tensor([int(table[b, j // page]) * page + j % page for b in range(2) for j in range(done, done + n)]).cuda()
+        q8 = torch.empty((T, hq, d), dtype=torch.int8, device="cuda")
+        start = torch.tensor([0, n, T], dtype=torch.int32).cuda()
+        ctx.hccs_cache_write_axes(q, k, v, q8, pool_k, pool_v, torch.from_numpy(pos).cuda(), slots, *steps, rope=text)
+        done += n
+        kv_len = torch.full((2,), done, dtype=torch.int32).cuda()
+        own, seen = (torch.empty((T, hq, d), dtype=torch.float32, device="cuda") for _ in range(2))
+        ctx.hccs_attention_cached(q8, pool_k, pool_v, table, start, kv_len, own, mult, 20, max_q=n, max_kv=done, out_scale=scale, flags=hccs.HCCS_RECIP_REAL)
+        ctx.hccs_attention_cross(q8, k8, v8, start, k_start, k_len, seen, mult, 20, max_q=n, max_kv=L, out_scale=scale, flags=hccs.HCCS_RECIP_REAL)
+        codes = orc.quantise(orc.rotate_axes(q.float().cpu().numpy(), pos, list(text.rope.freq)[:half], list(text.axis)[:half], False, 1.0), steps[0])
+        assert (q8.cpu().numpy() == codes).all()
+        compare(own, *orc.attend(codes, pool_k.cpu().numpy(), pool_v.cpu().numpy(), table.cpu().numpy(), [0, n, T], [done, done], theta, mult, 20),
+                "real", "f32", scale)
+        compare(seen, *orc.cross(codes, kk, vv, [0, n, T], [0, L], [L, L - 7], theta, mult, 20), "real", "f32", scale)
+    assert ctx.hccs_device_status() == 0
+    ctx.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("queries,length", [(1, 300), (3, 500), (40, 100), (150, 200), (60, 900)])
+def test_cross_captured_replayed_and_on_streams(hccs, ctx, queries, length):
+    """Every kernel: the same in a graph replayed on other inputs, and on two streams at once."""
+    import torch
+    rng = np.random.default_rng(queries)
+    hq, hkv, d = 4, 2, 64
+    theta = _theta(rng, hq, length, False)
+    kv = [rng.integers(-128, 128, (length + 6, 2 * hkv, d), dtype=np.int8) for _ in range(2)]
+    outs = [cross(hccs, ctx, rng, [queries], [length], hq, hkv, d, "div", "i32", theta=theta, mult=np.full(hq, 500, np.int32), kv=x)
+            for x in kv]
+    args = [list(o[1][0]) for o in outs]
+    kw = outs[0][1][1]
+    want = [o[0].clone() for o in outs]
+    for o in outs:
+        o[0].fill_(5)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for _ in range(5):
+        for s, a in zip(streams, args):
+            ctx.hccs_attention_cross(*a, **kw, stream=s)
+    torch.cuda.synchronize()
+    for o, w in zip(outs, want):
+        assert (o[0][:queries] == w[:queries]).all()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ctx.hccs_attention_cross(*args[0], **kw)
+    for i in range(4):                                     # its inputs take the other call's values and back
+        j = i % 2
+        for k in range(3):
+            args[0][k].copy_(args[1][k] if j else torch.from_numpy(kv[0][:, :hkv] if k == 1 else kv[0][:, hkv:]).cuda() if k else args[0][0])
+        if i == 0:
+            first = args[0][0].clone()
+        args[0][0].copy_(args[1][0] if j else first)
+        outs[0][0].fill_(9)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert (outs[0][0][:queries] == want[j][:queries]).all()
+    assert ctx.hccs_device_status() == 0
+
+
+@pytest.mark.gpu
+def test_writes_captured_and_replayed(hccs):
+    import torch
+    rng = np.random.default_rng(1)
+    T, hq, hkv, d = 33, 4, 2, 64
+    ctx = hccs.Context(0)
+    q, k, v = _tokens(rng, T, hq, hkv, d, "bf16")
+    steps = [np.full(n, 0.03, np.float32) for n in (hq, hkv, hkv)]
+    rope = hccs.hccs_rope_axes(d, (8, 12, 12))
+    pos = torch.from_numpy(rng.integers(0, 99, (3, T)).astype(np.int32)).cuda()
+    out = [torch.zeros((T, n, d), dtype=torch.int8, device="cuda") for n in (hq, hkv, hkv)]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ctx.hccs_states_write(q, k, v, *out, pos, *steps, rope=rope)
+    for seed in range(3):
+        for t in (q, k, v):
+            t.copy_(torch.from_numpy(rng.standard_normal(t.shape).astype(np.float32)).cuda())
+        pos.copy_(torch.from_numpy(rng.integers(0, 99, (3, T)).astype(np.int32)).cuda())
+        graph.replay()
+        torch.cuda.synchronize()
+        for t, got, step, turn in zip((q, k, v), out, steps, (True, True, False)):
+            x = t.float().cpu().numpy()
+            y = orc.rotate_axes(x, pos.cpu().numpy(), list(rope.rope.freq)[:32], list(rope.axis)[:32], False, 1.0) if turn else x
+            assert (got.cpu().numpy() == orc.quantise(y, step)).all()
+    ctx.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("queries", [1, 3, 40, 200])
+def test_lengths_outside_their_bounds(hccs, ctx, queries):
+    """Starts and lengths that leave the states, queries beyond max_q, keys beyond max_kv, starts that leave the tokens: nothing
+    outside is read or written, the rest is right, and the status word tells."""
+    import torch
+    rng = np.random.default_rng(queries)
+    hq, hkv, d, S, dev = 4, 2, 64, 90, "cuda"
+    theta, mult = _theta(rng, hq, 300, False), np.full(hq, 500, np.int32)
+    ctx.hccs_params_upload(theta, 300)
+    kv = rng.integers(-128, 128, (S, 2 * hkv, d), dtype=np.int8)
+    K, V = (torch.from_numpy(np.ascontiguousarray(x)).to(dev) for x in (kv[:, :hkv], kv[:, hkv:]))
+    T = 3 * queries
+    q = rng.integers(-128, 128, (T, hq, d), dtype=np.int8)
+    for k_start, k_len, starts, max_q, max_kv, real in (
+            ([0, 80, 0], [50, 30, 90], [0, queries, 2 * queries, T], queries, 90, ([0, 80, 0], [50, 10, 90])),       # beyond the states
+            ([-4, 91, 90], [50, 3, 7], [0, queries, 2 * queries, T], queries, 90, ([0, 0, 0], [0, 0, 0])),
+            ([0, 5, 2**31 - 1], [-3, 2**31 - 1, 2**31 - 1], [0, queries, 2 * queries, T], queries, 90, ([0, 5, 0], [0, 85, 0])),
+            ([0, 10, 20], [70, 70, 30], [0, queries, 2 * queries, T], queries, 40, ([0, 10, 20], [40, 40, 30])),      # max_kv
+            ([0, 10, 20], [70, 60, 30], [0, queries, 2 * queries, T + 50], queries, 90, ([0, 10, 20], [70, 60, 30]))):   # q_start
+        out = torch.full((T, hq, d), 77, dtype=torch.int32, device=dev)
+        ctx.hccs_attention_cross(torch.from_numpy(q).to(dev), K, V, torch.tensor(starts, dtype=torch.int32, device=dev),
+                                 torch.tensor(k_start, dtype=torch.int32, device=dev), torch.tensor(k_len, dtype=torch.int32, device=dev),
+                                 out, mult, 20, max_q=max_q, max_kv=max_kv)
+        word = ctx.hccs_device_status()
+        assert word == (16 if starts[-1] <= T else 0), (word, k_start)
+        num, zs, cnt = orc.cross(q, kv[:, :hkv], kv[:, hkv:], [min(s, T) for s in starts], *real, theta, mult, 20)
+        compare(out, num, zs, cnt, "div", "i32", None)
+    if queries > 1:                                        # queries beyond max_q keep what was there
+        out = torch.full((T, hq, d), 77, dtype=torch.int32, device=dev)
+        starts = [0, queries, queries + 1, T]
+        ctx.hccs_attention_cross(torch.from_numpy(q).to(dev), K, V, torch.tensor(starts, dtype=torch.int32, device=dev),
+                                 torch.zeros(3, dtype=torch.int32, device=dev), torch.full((3,), 60, dtype=torch.int32, device=dev), out, mult, 20,
+                                 max_q=queries, max_kv=60)
+        assert ctx.hccs_device_status() == 16
+        num, zs, cnt = orc.cross(q, kv[:, :hkv], kv[:, hkv:], starts, [0] * 3, [60] * 3, theta, mult, 20)
+        seen = np.zeros(T, bool)
+        for a, b in zip(starts, starts[1:]):
+            seen[a:min(b, a + queries)] = True
+        got = out.cpu().numpy()
+        assert (got[seen] == orc.integer_output(num, zs, cnt, False)[seen]).all() and (got[~seen] == 77).all()
+
+
+@pytest.mark.gpu
+def test_cross_refusals(hccs):
+    import torch
+    ctx = hccs.Context(0)
+    dev = "cuda"
+    Q = torch.zeros((6, 4, 64), dtype=torch.int8, device=dev)
+    K = torch.zeros((50, 2, 64), dtype=torch.int8, device=dev)
+    st, k0, kl = (torch.tensor(x, dtype=torch.int32, device=dev) for x in ([0, 3, 6], [0, 20], [20, 30]))
+    O = torch.zeros((6, 4, 64), dtype=torch.float32, device=dev)
+    mult, scale = np.full(4, 100, np.int32), np.ones(4, np.float32)
+
+    def call(**kw):
+        a = dict(Q=Q, K=K, V=K, st=st, k0=k0, kl=kl, O=O, mult=mult, mq=3, mkv=30, kr=None, scale=scale, flags=0)
+        a.update(kw)
+        ctx.hccs_attention_cross(a["Q"], a["K"], a["V"], a["st"], a["k0"], a["kl"], a["O"], a["mult"], 20, max_q=a["mq"], max_kv=a["mkv"],
+                                 key_range=a["kr"], out_scale=a["scale"], flags=a["flags"])
+    with pytest.raises(hccs.HccsError) as ei:
+        call()
+    assert ei.value.status == hccs.HCCS_ERR_NOT_UPLOADED
+    ctx.hccs_params_upload_wide(np.array([(500, 2, 100)] * 4, np.int32), 40)
+    for kw, status in ((dict(), hccs.HCCS_ERR_CONSTRAINT), (dict(flags=8, mkv=41), hccs.HCCS_ERR_CONSTRAINT)):
+        with pytest.raises(hccs.HccsError) as ei:
+            call(**kw)
+        assert ei.value.status == status
+    call(flags=8)
+    ctx.hccs_params_upload(np.array([(300, 1, 10)] * 4, np.int32), 64)
+    call()
+    wide = torch.zeros((50, 2, 80), dtype=torch.int8, device=dev)
+    for kw in (dict(K=K[:, :, :32]), dict(V=K[:40]), dict(K=K.float(), V=K.float()), dict(K=K.cpu()), dict(K=K.transpose(0, 1)[:, :2]),
+               dict(K=wide[:, :, :64], V=wide[:, :, :64]), dict(st=st[:2]), dict(st=st.long()), dict(k0=k0[:1]), dict(kl=kl.float()), dict(O=O[:5]),
+               dict(Q=Q.cpu()), dict(kr=torch.zeros((6, 2), dtype=torch.int64, device=dev)), dict(kr=torch.zeros((5, 2), dtype=torch.int32, device=dev)),
+               dict(mult=mult[:3]), dict(scale=scale[:3])):
+        with pytest.raises(ValueError):
+            call(**kw)
+    for kw in (dict(scale=None), dict(O=O.int()), dict(flags=1), dict(mq=-1)):
+        with pytest.raises(hccs.HccsError):
+            call(**kw)
+    # nothing to do, and states that are none
+    call(Q=Q[:0], O=O[:0], st=torch.zeros(3, dtype=torch.int32, device=dev))
+    call(mq=0)
+    O.fill_(3)
+    for queries in (3, 1):
+        call(K=K[:0], V=K[:0], kl=torch.zeros(2, dtype=torch.int32, device=dev), k0=torch.zeros(2, dtype=torch.int32, device=dev), mq=queries, mkv=0)
+        torch.cuda.synchronize()
+    assert (O == 0).all() and ctx.hccs_device_status() == 16         # (the second call was short of queries)
+    ctx.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("queries,length,hq,hkv,d,ranges", [(1, 70000, 8, 2, 128, False), (5, 4000, 3, 1, 64, False), (300, 250, 16, 2, 128, False), (90, 3001, 12, 3, 64, True)])
+def test_large_sums(hccs, ctx, queries, length, hq, hkv, d, ranges):
+    """Codes of the largest magnitude, tables of the largest scores: every sum at its limit."""
+    rng = np.random.default_rng(length)
+    kv = np.where(rng.random((length + 6, 2 * hkv, d)) < 0.5, -128, 127).astype(np.int8)
+    kv[:, hkv:] = -128
+    q = np.where(rng.random((queries, hq, d)) < 0.5, -128, 127).astype(np.int8)
+    theta = np.array([(32767, [1, 127, 0][i % 3], 127) for i in range(hq)], np.int32)
+    r = [(int(a), int(a) + 1500) for a in rng.integers(0, length - 1500, queries)] if ranges else None
+    cross(hccs, ctx, rng, [queries], [length], hq, hkv, d, "real", "f32", wide=True, theta=theta, q=q, kv=kv, ranges=r,
+          mult=np.array([[8191, 40, 0][i % 3] for i in range(hq)], np.int32))
+    for shift, m in ((1, 0), (2, 1), (24, 8191), (14, 8190), (14, 1)):
+        cross(hccs, ctx, rng, [queries], [length], hq, hkv, d, "real", "f32", wide=True, theta=theta, ranges=r, shift=shift, mult=np.full(hq, m, np.int32))
+
+
+@pytest.mark.gpu
+def test_many_sequences_share_the_device_evenly(hccs, ctx):
+    """More sequences than lanes, most of them without queries or keys, tiles of all costs: every row once."""
+    rng = np.random.default_rng(8)
+    B = 150
+    q_lens = [int(n) if rng.random() < 0.5 else 0 for n in rng.integers(1, 60, B)]
+    q_lens[7] = 400
+    k_lens = [int(n) if rng.random() < 0.9 else 0 for n in rng.integers(1, 257, B)]
+    cross(hccs, ctx, rng, q_lens, k_lens, 3, 3, 64, "div", "i32", theta=_theta(rng, 3, 256, False))
+    cross(hccs, ctx, rng, [n % 20 for n in q_lens], [min(n, 128) for n in k_lens], 8, 2, 128, "clb", "f16", theta=_theta(rng, 8, 128, False), max_q=20)
+    cross(hccs, ctx, rng, [0] * 40 + [1] + [0] * 40, [30] * 81, 20, 1, 64, "div", "i32")
