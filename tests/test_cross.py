@@ -700,3 +700,22 @@ def test_many_sequences_share_the_device_evenly(hccs, ctx):
     cross(hccs, ctx, rng, q_lens, k_lens, 3, 3, 64, "div", "i32", theta=_theta(rng, 3, 256, False))
     cross(hccs, ctx, rng, [n % 20 for n in q_lens], [min(n, 128) for n in k_lens], 8, 2, 128, "clb", "f16", theta=_theta(rng, 8, 128, False), max_q=20)
     cross(hccs, ctx, rng, [0] * 40 + [1] + [0] * 40, [30] * 81, 20, 1, 64, "div", "i32")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("queries,length", [(1, 200), (40, 60), (40, 200), (60, 500)])
+@pytest.mark.parametrize("scale", [1e-30, 3e-38, 1e30])
+def test_scales_of_any_size(hccs, ctx, queries, length, scale):
+    """Quotients below the normal range of fp32 keep their bits."""
+    import torch
+    rng = np.random.default_rng(length)
+    hq, hkv, d = 4, 2, 64
+    out, (args, kw, theta) = cross(hccs, ctx, rng, [queries], [length], hq, hkv, d, "real", "f32", wide=True)
+    kw["out_scale"] = np.full(hq, scale, np.float32)
+    ctx.hccs_attention_cross(*args, **kw)
+    kv = [t.cpu().numpy() for t in args[1:3]]
+    num, zs, cnt = orc.cross(args[0].cpu().numpy()[:queries], *kv, [0, queries], [3], [length], theta, args[7], 20)
+    want = num / zs[..., None] * np.float64(np.float32(scale))
+    got = _values(out[:queries])
+    # the product itself may lie below the normal range: half of its last place there is 2^-150
+    assert (np.abs(got - want) <= np.abs(want) * 4 * 2.0 ** -24 + 2.0 ** -150).all()
