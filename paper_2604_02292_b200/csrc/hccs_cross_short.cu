@@ -13,8 +13,11 @@
 // stores its rows, the others have the integer pipe.  O takes columns of its own in the stage's part where the keys leave room,
 // else those of S (all of whose logits have been read twice by then).
 //
-// Roles: sixteen row warps, a warp each for the copies, Q.K^T, r.V, and
-// the sums of V.
+// Roles: sixteen row warps, a warp each for the copies, Q.K^T, r.V, and the sums of V.
+//
+// Bound: the chain of a tile (product, tensor memory, arithmetic, product, outputs), with five warps per scheduler to cover it: issue slots
+// 53 to 62 % busy, tensor pipe 10 to 21 %.  8 x 4096 queries on 77 keys (16 heads of 64, fp16 out): 34 us, 3.0 TB/s of Q and O; 24 ragged texts
+// of up to 700 on up to 256 keys (32 heads on 8 of 128, bf16 out): 47 us.  The kernel for longer states takes 226 and 176.
 #include "hccs_cached.cuh"
 #include "hccs_tcgen05.cuh"
 
@@ -37,8 +40,8 @@ struct ShortBarriers {
     uint64_t q_full[kMaxStages], q_free[kMaxStages];               // a stage's Q tile
     uint64_t s_full[kMaxStages], s_free[kMaxStages];               // its logits
     uint64_t r_ready[kMaxStages], o_full[kMaxStages];
-    uint64_t k_full[2], k_free[2], v_full[2], v_free[2];      // by chunk
-    uint64_t sum_full[2], sum_free[2];           // sum V, by chunk
+    uint64_t k_full[kChunks], k_free[kChunks], v_full[kChunks], v_free[kChunks];      // by chunk
+    uint64_t sum_full[kChunks], sum_free[kChunks];     // sum V, by chunk
     uint64_t chunk_full[kChunks], chunk_free[kChunks];
     uint64_t met[kMaxStages];                    // the stage's row threads, twice per tile (WIDE)
     uint64_t drained[2];                         // a given-up CTA: the products of either issuer are through
@@ -53,7 +56,7 @@ struct Chunk {
 
 struct ShortPlan {
     int keys;                                    // of the K and V tiles: a multiple of 32
-    int v_slots;
+    int k_shift, v_shift;                        // places for K and for V: 1 << shift, kChunks at most
     int queries;                                 // per tile
     int warp_queries;                            // whole ones among the 32 rows of a warp, or 0: its rows are cut by heads
 };
@@ -106,7 +109,8 @@ struct Walk {
         k.k0 = seq.k0;
         k.kvh = kvh;
         const int cost = tile_cost(seq);
-        k.tiles = (int)min((int64_t)(tiles_of(a, seq, plan) - tile), (left + cost - 1) / cost);
+        k.tiles = tiles_of(a, seq, plan) - tile;
+        if ((int64_t)k.tiles * cost > left) k.tiles = (int)((left + cost - 1) / cost);       // (a division in the last chunk alone)
         k.q0 = seq.s0 + tile * plan.queries;
         k.rows = (min(seq.nq, a.max_q) - tile * plan.queries) * a.group;
         left -= (int64_t)k.tiles * cost;
@@ -225,7 +229,7 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
     __shared__ int part_max[kStages][kHalves][WIDE ? kTile : 1], part_sum[kStages][kHalves][WIDE ? kTile : 1];   // [stage][half][row]
-    __shared__ __align__(16) int vsum[2][D];
+    __shared__ __align__(16) int vsum[kChunks][D];
     __shared__ int start[3];                                       // of the walk: sequence, kv head, tile
     __shared__ int64_t count;
     __shared__ Chunk chunks[kChunks];
@@ -238,9 +242,10 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t *gen = smem_raw + (base - smem_u32(smem_raw));
     const int panel_bytes = ((nk + 127) >> 7) * kTile * 128;       // r of a stage: 128 rows x 128 keys, 128-byte swizzle, once or twice
-    const uint32_t s_q = base, s_k = s_q + kStages * kTileBytes, s_v = s_k + 2 * kv_bytes, s_r = s_v + plan.v_slots * kv_bytes;
+    const uint32_t s_q = base, s_k = s_q + kStages * kTileBytes, s_v = s_k + (kv_bytes << plan.k_shift), s_r = s_v + (kv_bytes << plan.v_shift);
     const uint32_t o_col = nk + D <= kCols ? kCols - D : 0;        // O's columns in its stage's part
     const bool apart = o_col != 0;
+    const int k_mask = (1 << plan.k_shift) - 1, v_mask = (1 << plan.v_shift) - 1;
 
     if (warp == kCopyWarp && lane < 4) {
         const CUtensorMap *const map = lane == 0 ? &map_q : lane == 1 ? &map_k : lane == 2 ? &map_v : &map_o;
@@ -258,18 +263,18 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
             mbar_init(smem_u32(&bars.met[i]), kStageThreads);
         }
         for (int i = 0; i < kChunks; ++i) {
+            mbar_init(smem_u32(&bars.sum_full[i]), 1);
+            mbar_init(smem_u32(&bars.sum_free[i]), kRowWarps);
             mbar_init(smem_u32(&bars.chunk_full[i]), 1);
             mbar_init(smem_u32(&bars.chunk_free[i]), kRowWarps + 3);
         }
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < kChunks; ++i) {
             mbar_init(smem_u32(&bars.k_full[i]), 1);
             mbar_init(smem_u32(&bars.k_free[i]), 1);
             mbar_init(smem_u32(&bars.v_full[i]), 1);
             mbar_init(smem_u32(&bars.v_free[i]), 2);               // the products and the sums
-            mbar_init(smem_u32(&bars.sum_full[i]), 1);
-            mbar_init(smem_u32(&bars.sum_free[i]), kRowWarps);
-            mbar_init(smem_u32(&bars.drained[i]), 1);
         }
+        for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&bars.drained[i]), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -290,21 +295,21 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
     const uint32_t tmem = tmem_slot;
     auto wait = [&](uint64_t *bar, uint32_t parity) -> bool { return warp_wait(smem_u32(bar), parity, abortp, a.status, a.wait_cycles); };
 
-    // chunk number c, for the roles but the copies: false when a wait was given up
+    // chunk number c, for the roles but the copies (false when a wait was given up), and that this warp is through with it
     auto chunk = [&](int c, Chunk &k) -> bool {
         const bool ok = wait(&bars.chunk_full[c % kChunks], (c / kChunks) & 1);
-        if (ok) {
-            k = chunks[c % kChunks];
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&bars.chunk_free[c % kChunks]));
-        }
+        if (ok) k = chunks[c % kChunks];
         return ok;
+    };
+    auto through = [&](int c) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&bars.chunk_free[c % kChunks]));
     };
     Chunk k;
 
     if (warp == kCopyWarp) {
         // ===================================================== copies: K and V of a chunk and the Q of its tiles, in the order in which they
-        // are needed; tile number `it` of the CTA goes into stage it % kStages, chunk number kc into slot kc & 1 (or, V, the only one)
+        // are needed; tile number `it` of the CTA goes into stage it % kStages, chunk number kc into the places of K and V in turn
         int it = 0, kc = 0, sent_v = 0;
         bool ok = true;
         const uint32_t q_bytes = (uint32_t)(plan.queries * a.group * D);
@@ -316,13 +321,14 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
             __syncwarp();
         };
         auto keys = [&]() -> bool {
-            if (kc >= 2 && !wait(&bars.k_free[kc & 1], ((kc >> 1) - 1) & 1)) return false;
-            copy(s_k + (kc & 1) * kv_bytes, &map_k, k.kvh, k.k0, &bars.k_full[kc & 1], (uint32_t)kv_bytes);
+            const int ks = kc & k_mask, round = kc >> plan.k_shift;
+            if (round >= 1 && !wait(&bars.k_free[ks], (round - 1) & 1)) return false;
+            copy(s_k + ks * kv_bytes, &map_k, k.kvh, k.k0, &bars.k_full[ks], (uint32_t)kv_bytes);
             ++kc;
             return true;
         };
         auto values = [&]() -> bool {
-            const int vs = sent_v % plan.v_slots, round = sent_v / plan.v_slots;
+            const int vs = sent_v & v_mask, round = sent_v >> plan.v_shift;
             if (round >= 1 && !wait(&bars.v_free[vs], (round - 1) & 1)) return false;
             copy(s_v + vs * kv_bytes, &map_v, k.kvh, k.k0, &bars.v_full[vs], (uint32_t)kv_bytes);
             ++sent_v;
@@ -353,9 +359,9 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
         }
         // (the last copy into each place has landed before the CTA may leave, whatever became of its readers; again with a limit)
         for (int x = max(it - kStages, 0); x < it; ++x) mbar_wait_bounded(smem_u32(&bars.q_full[x & (kStages - 1)]), (x >> kShift) & 1, a.wait_cycles);
-        for (int x = max(kc - 2, 0); x < kc; ++x) mbar_wait_bounded(smem_u32(&bars.k_full[x & 1]), (x >> 1) & 1, a.wait_cycles);
-        for (int x = max(sent_v - plan.v_slots, 0); x < sent_v; ++x)
-            mbar_wait_bounded(smem_u32(&bars.v_full[x % plan.v_slots]), (x / plan.v_slots) & 1, a.wait_cycles);
+        for (int x = max(kc - 1 - k_mask, 0); x < kc; ++x) mbar_wait_bounded(smem_u32(&bars.k_full[x & k_mask]), (x >> plan.k_shift) & 1, a.wait_cycles);
+        for (int x = max(sent_v - 1 - v_mask, 0); x < sent_v; ++x)
+            mbar_wait_bounded(smem_u32(&bars.v_full[x & v_mask]), (x >> plan.v_shift) & 1, a.wait_cycles);
     } else if (warp == kQkWarp) {
         // ===================================================== S = Q.K^T (the whole warp walks, an elected thread issues)
         const uint64_t dq = smem_desc(s_q, 16, 8 * D, kSwizzle), dk = smem_desc(s_k, 16, 8 * D, kSwizzle);
@@ -363,9 +369,10 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
         int it = 0, kc = 0;
         bool ok = true;
         for (int c = 0; ok && (ok = chunk(c, k)) && k.tiles > 0; ++c) {
+            through(c);
             if (k.n == 0) continue;
-            const int ks = kc & 1;
-            ok = wait(&bars.k_full[ks], (kc >> 1) & 1);
+            const int ks = kc & k_mask;
+            ok = wait(&bars.k_full[ks], (kc >> plan.k_shift) & 1);
             const uint32_t k_lo = (uint32_t)dk + ((uint32_t)(ks * kv_bytes) >> 4);
             for (int t = 0; ok && t < k.tiles; ++t, ++it) {
                 const int st = it & (kStages - 1);
@@ -392,8 +399,9 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
         int it = 0, kc = 0;
         bool ok = true;
         for (int c = 0; ok && (ok = chunk(c, k)) && k.tiles > 0; ++c) {
+            through(c);
             if (k.n == 0) continue;
-            const int vs = plan.v_slots == 2 ? kc & 1 : 0, vround = plan.v_slots == 2 ? kc >> 1 : kc;
+            const int vs = kc & v_mask, vround = kc >> plan.v_shift;
             ok = wait(&bars.v_full[vs], vround & 1);
             const uint32_t v_lo = (uint32_t)dv + ((uint32_t)(vs * kv_bytes) >> 4);
             for (int t = 0; ok && t < k.tiles; ++t, ++it) {
@@ -421,9 +429,10 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
         int kc = 0;
         bool ok = true;
         for (int c = 0; ok && (ok = chunk(c, k)) && k.tiles > 0; ++c) {
+            through(c);
             if (k.n == 0) continue;
-            const int vs = plan.v_slots == 2 ? kc & 1 : 0, vround = plan.v_slots == 2 ? kc >> 1 : kc;
-            if (kc >= 2) ok = wait(&bars.sum_free[kc & 1], ((kc >> 1) - 1) & 1);
+            const int vs = kc & v_mask, vround = kc >> plan.v_shift;
+            if (kc >= kChunks) ok = wait(&bars.sum_free[kc % kChunks], (kc / kChunks - 1) & 1);
             if (ok) ok = wait(&bars.v_full[vs], vround & 1);
             if (!ok) break;
             const uint32_t v = s_v + vs * kv_bytes;
@@ -447,11 +456,11 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
                 for (int i = 0; i < 2; ++i) {
                     sum[p][i] += __shfl_xor_sync(~0u, sum[p][i], 1);
                     sum[p][i] += __shfl_xor_sync(~0u, sum[p][i], 2);
-                    if ((lane & 3) == 0) vsum[kc & 1][p * 16 + col + 8 * i] = sum[p][i];
+                    if ((lane & 3) == 0) vsum[kc % kChunks][p * 16 + col + 8 * i] = sum[p][i];
                 }
             __syncwarp();
             if (lane == 0) {
-                mbar_arrive(smem_u32(&bars.sum_full[kc & 1]));
+                mbar_arrive(smem_u32(&bars.sum_full[kc % kChunks]));
                 mbar_arrive(smem_u32(&bars.v_free[vs]));
             }
             __syncwarp();
@@ -508,6 +517,21 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
             if (k.n == 0) {                                        // nothing to see: zeros
                 for (int x = stage; x < k.tiles; x += kStages)
                     for (int dim = 0; dim < kDims; dim += kStageRow / kElem) store_rows(x, dim, true);
+                through(c);
+                continue;
+            }
+            // A stage without a tile in this chunk only says so.  (A row warp is through with a chunk when it has said so, and nobody is kChunks
+            // chunks ahead of it: no warp speaks for a later use of a place before all have for this one.  With heads looked up and sums waited
+            // for by all stages in all chunks, 24 ragged texts on 256 patches took 49.5 us instead of 47.4.)
+            auto sums_read = [&]() {
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&bars.sum_free[kc % kChunks]));
+                ++kc;
+                through(c);
+            };
+            if (((stage - it) & (kStages - 1)) >= k.tiles) {
+                it += k.tiles;
+                sums_read();
                 continue;
             }
             const int h = k.kvh * a.group + t % a.group;
@@ -602,7 +626,7 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
                 }
                 const RowFactor f = row_factor(a, (int64_t)F * n + (int64_t)e.y * rsum, scale);
                 if (!sums) {
-                    ok = wait(&bars.sum_full[kc & 1], (kc >> 1) & 1);
+                    ok = wait(&bars.sum_full[kc % kChunks], (kc / kChunks) & 1);
                     sums = true;
                 }
                 if (ok) ok = wait(&bars.o_full[stage], phase);
@@ -636,7 +660,7 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
                     tmem_ld(o_at + y * kDimsAtATime, o);
 #pragma unroll
                     for (int i = 0; i < kDimsAtATime; i += 4) {
-                        const int4 vs = *reinterpret_cast<const int4 *>(&vsum[kc & 1][half * kDims + y * kDimsAtATime + i]);
+                        const int4 vs = *reinterpret_cast<const int4 *>(&vsum[kc % kChunks][half * kDims + y * kDimsAtATime + i]);
                         o[i] = (uint32_t)by_r * o[i] + ((uint32_t)by_v * (uint32_t)vs.x + magic);
                         o[i + 1] = (uint32_t)by_r * o[i + 1] + ((uint32_t)by_v * (uint32_t)vs.y + magic);
                         o[i + 2] = (uint32_t)by_r * o[i + 2] + ((uint32_t)by_v * (uint32_t)vs.z + magic);
@@ -672,11 +696,7 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
                     }
                 }
             }
-            // (a warp without a tile in this chunk waits as well: nobody is a chunk ahead of the sums)
-            if (ok && !sums) ok = wait(&bars.sum_full[kc & 1], (kc >> 1) & 1);
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&bars.sum_free[kc & 1]));
-            ++kc;
+            sums_read();
         }
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
@@ -713,7 +733,7 @@ bool make_rows_map(CUtensorMap *map, const void *rows, int row_bytes, int inner,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-constexpr size_t kMaxSmem = 219 * 1024;    // dynamic; the kernel's own arrays take up to 6 KB more
+constexpr size_t kMaxSmem = 219 * 1024;    // dynamic; the kernel's own arrays take up to 7 KB more
 
 template <int D, int OUT, bool WIDE>
 cudaError_t launch_typed(const CachedAttnArgs &a, cudaStream_t stream) {
@@ -729,8 +749,11 @@ cudaError_t launch_typed(const CachedAttnArgs &a, cudaStream_t stream) {
     p.queries = kTile / a.group;
     p.keys = a.max_kv <= 32 ? 32 : (a.max_kv + 31) / 32 * 32;
     const size_t fixed = 1024 + kStages * ((size_t)kTile * D + (size_t)((p.keys + 127) / 128) * kTile * 128), kv = (size_t)p.keys * D;
-    p.v_slots = fixed + 4 * kv <= kMaxSmem ? 2 : 1;
-    const size_t smem = fixed + (2 + p.v_slots) * kv;
+    // Four chunks on their way where there is room: sequences of few queries are chunks of one tile, and V's place is taken until the tile's
+    // last product
+    p.k_shift = fixed + 8 * kv <= kMaxSmem ? 2 : 1;
+    p.v_shift = p.k_shift == 2 ? 2 : fixed + 4 * kv <= kMaxSmem ? 1 : 0;
+    const size_t smem = fixed + (kv << p.k_shift) + (kv << p.v_shift);
     // (a warp's rows are whole queries where the heads of a kv head divide 32; the map of the outputs is not used otherwise)
     p.warp_queries = 32 % a.group == 0 ? 32 / a.group : 0;
     constexpr int kElem = OUT == HCCS_I32 || OUT == HCCS_F32 ? 4 : 2, kRow = (WIDE ? D / 2 : D) * kElem;
