@@ -462,13 +462,14 @@ class Context:
         """(address, stride of the axes, stride of the tokens) of positions [axes,T]."""
         if positions is None:
             return None, 0, 0
-        if positions.get_device() != self.device or positions.dtype not in _I32 or positions.ndim != 2 or positions.shape[1] != T:
+        shape = positions.shape
+        if positions.get_device() != self.device or positions.dtype not in _I32 or len(shape) != 2 or shape[1] != T:
             if positions.get_device() == self.device:
-                self._explain(positions.contiguous(), "positions", 4, (positions.shape[0], T))
+                self._explain(positions.contiguous(), "positions", 4, (shape[0] if len(shape) else 0, T))
             self._explain(positions, "positions", 4)
-        if rope is not None and positions.shape[0] < rope.num_axes:
-            raise ValueError(f"positions have {positions.shape[0]} axes, the rotation {rope.num_axes}")
-        return positions.data_ptr(), positions.stride(0), positions.stride(1)
+        if rope is not None and shape[0] < rope.num_axes:
+            raise ValueError(f"positions have {shape[0]} axes, the rotation {rope.num_axes}")
+        return positions.data_ptr(), *positions.stride()
 
     # -- hccs_states_write
     def hccs_states_write(self, q, k, v, q8, k8, v8, positions, q_step, k_step, v_step, rope: RopeAxes | None = None, stream=None) -> None:
@@ -644,8 +645,10 @@ class Context:
         if t.get_device() != self.device:
             raise ValueError(f"{name} must live on cuda:{self.device}, not {t.device}")
         T, heads, d = t.shape
-        if t is not some and (t.dtype != some.dtype or T != some.shape[0] or d != some.shape[2]):
-            raise ValueError(f"{name} must be [{some.shape[0]}, heads, {some.shape[2]}] of {some.dtype}, got {tuple(t.shape)} of {t.dtype}")
+        if t is not some:
+            n, _, dim = some.shape
+            if t.dtype != some.dtype or T != n or d != dim:
+                raise ValueError(f"{name} must be [{n}, heads, {dim}] of {some.dtype}, got {tuple(t.shape)} of {t.dtype}")
         a, b, c = t.stride()
         if T and heads and (c != 1 or (heads > 1 and b != d)):
             raise ValueError(f"{name} must be contiguous inside a token")
@@ -653,9 +656,10 @@ class Context:
 
     def _states(self, t, name, like) -> int:
         """Bytes between the keys of int8 states [S, heads, d] that are contiguous inside a key."""
-        if t.get_device() != self.device or t.dtype not in _I8 or t.shape != like.shape:
+        shape = t.shape
+        if t.get_device() != self.device or t.dtype not in _I8 or (t is not like and shape != like.shape):
             self._explain(t if t.get_device() != self.device or t.is_contiguous() else t.contiguous(), name, 1, like.shape)
-        S, heads, d = t.shape
+        S, heads, d = shape
         a, b, c = t.stride()
         if S and heads and (c != 1 or (heads > 1 and b != d)):
             raise ValueError(f"{name} must be contiguous inside a key")
@@ -727,19 +731,22 @@ def _type_of(t) -> int:
 
 
 # Host arrays go to the library as the bytes of their values (it copies them before it returns).
+_NP_F32, _NP_I32 = np.dtype(np.float32), np.dtype(np.int32)
+
+
 def _bytes(v, name, n, dtype) -> bytes:
-    arr = v if type(v) is np.ndarray and v.dtype == dtype else np.asarray(v, dtype=dtype)
+    arr = v if type(v) is np.ndarray and v.dtype is dtype else np.asarray(v, dtype=dtype)
     if arr.size != n:
         raise ValueError(f"{name} must have {n} entries, got {arr.size}")
     return arr.tobytes()
 
 
 def _floats(v, name, n) -> bytes:
-    return _bytes(v, name, n, np.float32)
+    return _bytes(v, name, n, _NP_F32)
 
 
 def _ints(v, name, n) -> bytes:
-    return _bytes(v, name, n, np.int32)
+    return _bytes(v, name, n, _NP_I32)
 
 
 def _check_tensor(t, name, itemsize, shape=None, device="cuda"):
