@@ -172,6 +172,7 @@ template <typename T, bool DENSE, bool AXES>
 __global__ void __launch_bounds__(kWriteThreads, 2)
 cache_write_kernel(const __grid_constant__ CacheWriteArgs a, int items, int per_head_shift, int per_cta) {
     __shared__ Turn turn[kTokens];
+    previous_kernel_done();
     const int t0 = blockIdx.x * per_cta;
     const int tokens = min(per_cta, a.T - t0);
     const int rot = a.rope.rot_dim, half = rot >> 1;
@@ -508,10 +509,17 @@ cudaError_t write_typed(const CacheWriteArgs &a, cudaStream_t stream) {
     int per_cta = (int)((all + slots * waves - 1) / (slots * waves));
     per_cta = per_cta < 1 ? 1 : per_cta > kTokens ? kTokens : per_cta;
     const dim3 grid((unsigned)((a.T + per_cta - 1) / per_cta), (unsigned)groups);
-    if (a.dense_len) cache_write_kernel<T, true, true><<<grid, threads, 0, stream>>>(a, items, shift, per_cta);
-    else if (a.axes) cache_write_kernel<T, false, true><<<grid, threads, 0, stream>>>(a, items, shift, per_cta);
-    else cache_write_kernel<T, false, false><<<grid, threads, 0, stream>>>(a, items, shift, per_cta);
-    return cudaGetLastError();
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, a.dense_len ? cache_write_kernel<T, true, true> : a.axes ? cache_write_kernel<T, false, true> : cache_write_kernel<T, false, false>,
+                              a, items, shift, per_cta);
 }
 
 template <typename T>

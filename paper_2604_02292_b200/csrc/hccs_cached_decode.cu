@@ -108,6 +108,7 @@ cached_decode_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_cons
     uint8_t *const smem = smem_raw + (((smem_u32(smem_raw) + 1023u) & ~1023u) - smem_u32(smem_raw));      // (the swizzles count from there)
     if (tid == 0) abort_flag = 0;
     if (!CROSS && split > 1) cluster_arrive(); // the other CTAs run: waited for before the first push
+    if constexpr (CROSS) previous_kernel_done();
     const int32_t *table = CROSS ? nullptr : a.page_table + (int64_t)b * a.max_pages;
     // tiles in turn to the warps of the cluster: the first does not depend on the length
     const int first = rank * kWarps + warp, stride = kWarps * split;
@@ -538,13 +539,15 @@ cudaError_t launch_plan(const CachedAttnArgs &a, const Plan &p, int rows, int ro
     cfg.blockDim = dim3(32 * W);
     cfg.dynamicSmemBytes = Sizes<D, HI, W>::smem(p.per_warp * W, rows);
     cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = (unsigned)p.split;
     attr[0].val.clusterDim.y = 1;
     attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = CROSS ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, cached_decode_kernel<D, HI, W, CROSS>, a, mk, mv, row_tiles, p.per_warp, merge);
 }
 

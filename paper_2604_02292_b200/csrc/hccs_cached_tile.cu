@@ -106,6 +106,7 @@ cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
 
     const int tid = threadIdx.x, lane = tid & 31;
     const int warp = __shfl_sync(~0u, tid >> 5, 0);                        // (uniform in the compiler's eyes too)
+    if constexpr (CROSS) previous_kernel_done();
     const int b = blockIdx.z, kvh = blockIdx.y;
     const int rank = (int)blockIdx.x % split;
     const int rt = (int)(gridDim.x / split - 1 - blockIdx.x / split);      // the tiles with the most keys first
@@ -680,13 +681,15 @@ cudaError_t launch_typed(const CachedAttnArgs &a, cudaStream_t stream) {
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = (unsigned)split;
     attr[0].val.clusterDim.y = 1;
     attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = CROSS ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kernel, a, mk, mv, split, tile_rows);
 }
 

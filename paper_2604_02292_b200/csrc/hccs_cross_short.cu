@@ -284,6 +284,7 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
     // 256 patches took 56.3 us instead of 54.1)
     constexpr int kStageRow = kDims * kElem < 128 ? kDims * kElem : 128, kRowLanes = kStageRow / 16, kRowsAtATime = 32 / kRowLanes;
     if (tid < kTile) row_at[tid] = (tid / a.group * a.Hq + tid % a.group) * (D * kElem / 16);
+    previous_kernel_done();
     if (warp == kCopyWarp) find_start(a, plan, start, &count);
     if (warp == kPvWarp) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(kTmemCols) : "memory");
@@ -761,8 +762,17 @@ cudaError_t launch_typed(const CachedAttnArgs &a, cudaStream_t stream) {
     if (!make_rows_map(&mq, a.Q, D, D, a, p.queries) || !make_rows_map(&mo, a.O, D * kElem, kRow < 128 ? kRow : 128, a, p.warp_queries ? p.warp_queries : 1) || !make_states_map(&mk, a.k_pages, a.k_stride, a, p.keys) || !make_states_map(&mv, a.v_pages, a.v_stride, a, p.keys))
         return cudaErrorInvalidValue;
     const int64_t most = (int64_t)a.B * a.Hkv * (((int64_t)a.max_q + p.queries - 1) / p.queries);      // tiles
-    kernel<<<(unsigned)(most < sms ? most : sms), kThreads, smem, stream>>>(a, mq, mk, mv, mo, p);
-    return cudaGetLastError();
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(most < sms ? most : sms));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, a, mq, mk, mv, mo, p);
 }
 
 template <int D, bool WIDE>

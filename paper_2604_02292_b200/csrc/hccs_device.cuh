@@ -60,6 +60,9 @@ __device__ __forceinline__ int valid_keys(uint32_t b, uint32_t i, const RowArgs 
     return nv;
 }
 
+// A kernel launched behind another one with programmatic dependence: nothing before this touches what the other may still write.
+__device__ __forceinline__ void previous_kernel_done() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 // ---- mbarrier waits with a limit (shared by the TMA-staged row kernel, the fused kernel and the
 // wait-limit probe): no wait in this library spins without one.
 __device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
