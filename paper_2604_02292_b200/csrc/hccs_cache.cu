@@ -4,8 +4,8 @@
 // Every element is read once and written once (2 or 4 bytes in and one out, or the reverse).  Reading back is bound by
 // HBM: 8 sequences of 8192 tokens (8 heads of 128, to bf16) in 65 us, 6.2 TB/s.  Writing is bound by instructions, about
 // twenty per element with the margins below (issue slots 70 % busy, DRAM 45 %): 16384 tokens (32 + 8 + 8 heads of 128,
-// bf16, all of a head rotated) in 74 us, 4.1 TB/s; without rotation 60 us, 5.0 TB/s.  With positions of three axes 80 us; to dense tensors, 16 x
-// 1024 tokens of 3 x 12 heads of 64, fp16, two axes, 35 us; keys and values of 11992 tokens, 16 heads of 64, fp32, not rotated, 24.6 us, 5.0 TB/s.
+// bf16, all of a head rotated) in 74 us, 4.1 TB/s; without rotation 60 us, 5.0 TB/s.  With positions of three axes 77 us; to dense tensors, 16 x
+// 1024 tokens of 3 x 12 heads of 64, fp16, two axes, 32.7 us; keys and values of 11992 tokens, 16 heads of 64, fp32, not rotated, 22.1 us, 5.6 TB/s.
 //
 // Exactness of the codes.  A code is the exact quotient y / step rounded to nearest; a border decides a whole
 // step, so the value next to it needs more than fp32.  Computed in fp32,

@@ -81,7 +81,8 @@ struct Sizes {
 // CROSS: queries on an encoder's states.  The rows of a kv head are its (query, head) pairs, all of which see the same keys:
 // those of the sequence, or where max_q is 1 those of the query's key range.  Up to `merge` neighbouring sequences of one query that read the
 // same states (hypotheses about one input) are rows of one CTA too, that of the first of them: 32 queries, two by two on the same states of up to
-// 1499 keys (16 heads of 64), in 14.4 us instead of 20.5.  8 queries on 32768 keys (32 heads on 8 of 128): 89 us, 6.0 TB/s.
+// 1499 keys (16 heads of 64), in 14.4 us instead of 20.5 (12.0 since kernels overlap).  8 queries on 32768 keys (32 heads on 8 of 128): 86.6 us,
+// 6.2 TB/s.
 template <int D, bool HI, int W, bool CROSS>
 __global__ void __launch_bounds__(32 * W, 16 / W)
 cached_decode_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_constant__ CUtensorMap map_k,

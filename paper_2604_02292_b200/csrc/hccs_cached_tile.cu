@@ -80,8 +80,8 @@ template <int D> constexpr uint32_t kIdescPVOf = instr_desc(0, 1, 1, 128, D);   
 
 // CROSS: queries on an encoder's states.  A row sees keys [first, end) of its sequence, all of them where there are no key
 // ranges; the blocks that every row of the tile sees whole come first, then the others (the order of blocks is free:
-// the sums are exact).  2048 queries on each of two states of 6404 keys (32 heads on 8 of 128): 315 us, 0.42 of the int8 rate counting two
-// products; 1001 queries on 2404 keys, twice, that see 601 of them or none (16 heads on 4): 33 us.
+// the sums are exact).  2048 queries on each of two states of 6404 keys (32 heads on 8 of 128): 314 us, 0.42 of the int8 rate counting two
+// products; 1001 queries on 2404 keys, twice, that see 601 of them or none (16 heads on 4): 31 us.
 template <int D, bool CROSS>
 __global__ void __launch_bounds__(kThreads, 1)
 cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_constant__ CUtensorMap map_k,

@@ -16,8 +16,8 @@
 // Roles: sixteen row warps, a warp each for the copies, Q.K^T, r.V, and the sums of V.
 //
 // Bound: the chain of a tile (product, tensor memory, arithmetic, product, outputs), with five warps per scheduler to cover it: issue slots
-// 53 to 62 % busy, tensor pipe 10 to 21 %.  8 x 4096 queries on 77 keys (16 heads of 64, fp16 out): 34 us, 3.0 TB/s of Q and O; 24 ragged texts
-// of up to 700 on up to 256 keys (32 heads on 8 of 128, bf16 out): 47 us.  The kernel for longer states takes 226 and 176.
+// 53 to 62 % busy, tensor pipe 10 to 21 %.  8 x 4096 queries on 77 keys (16 heads of 64, fp16 out): 32 us, 3.2 TB/s of Q and O; 24 ragged texts
+// of up to 700 on up to 256 keys (32 heads on 8 of 128, bf16 out): 45.5 us.  The kernel for longer states takes 226 and 176.
 #include "hccs_cached.cuh"
 #include "hccs_tcgen05.cuh"
 

@@ -60,7 +60,9 @@ __device__ __forceinline__ int valid_keys(uint32_t b, uint32_t i, const RowArgs 
     return nv;
 }
 
-// A kernel launched behind another one with programmatic dependence: nothing before this touches what the other may still write.
+// A kernel launched behind another one with programmatic dependence (it starts while the other leaves, which saves 2 to 2.7 us): nothing
+// before this touches what the other may still write.  (Kernels that let the next one in from their first instruction on are no faster, small
+// ones 0.6 us slower.)
 __device__ __forceinline__ void previous_kernel_done() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 // ---- mbarrier waits with a limit (shared by the TMA-staged row kernel, the fused kernel and the
