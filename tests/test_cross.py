@@ -719,3 +719,63 @@ def test_scales_of_any_size(hccs, ctx, queries, length, scale):
     got = _values(out[:queries])
     # the product itself may lie below the normal range: half of its last place there is 2^-150
     assert (np.abs(got - want) <= np.abs(want) * 4 * 2.0 ** -24 + 2.0 ** -150).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("queries,length", [(1, 900), (3, 300), (50, 120), (90, 220), (70, 700)])
+def test_chain_of_calls_without_a_pause(hccs, ctx, queries, length):
+    """Every call reads what the one before it writes, or writes what that one reads, and starts while it leaves."""
+    import torch
+    rng = np.random.default_rng(length)
+    hq, hkv, d, n = 4, 2, 64, 6
+    theta, mult = _theta(rng, hq, length, False), np.full(hq, 500, np.int32)
+    ctx.hccs_params_upload(theta, length)
+    steps = [np.full(m, 0.03, np.float32) for m in (hq, hkv, hkv)]
+    rope = hccs.hccs_rope_axes(d, (16, 16))
+    pos = [torch.from_numpy(rng.integers(0, 50, (2, t)).astype(np.int32)).cuda() for t in (queries, length)]
+    q = [torch.from_numpy(rng.standard_normal((queries, hq, d)).astype(np.float32)).cuda() for _ in range(n)]
+    kv = [torch.from_numpy(rng.standard_normal((2, length, hkv, d)).astype(np.float32)).cuda() for _ in range(n)]
+    q8 = torch.empty((queries, hq, d), dtype=torch.int8, device="cuda")
+    k8, v8 = (torch.empty((length, hkv, d), dtype=torch.int8, device="cuda") for _ in range(2))
+    start, k0, kl = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([0, queries], [0], [length]))
+    outs = [torch.empty((queries, hq, d), dtype=torch.int32, device="cuda") for _ in range(40)]
+
+    def call(i, out):
+        ctx.hccs_states_write(None, kv[i][0], kv[i][1], None, k8, v8, pos[1], None, steps[1], steps[2], rope=rope)
+        ctx.hccs_states_write(q[i], None, None, q8, None, None, pos[0], steps[0], None, None, rope=rope)
+        ctx.hccs_attention_cross(q8, k8, v8, start, k0, kl, out, mult, 20, max_q=queries, max_kv=length)
+    want = []
+    for i in range(n):
+        out = torch.empty_like(outs[0])
+        call(i, out)
+        torch.cuda.synchronize()
+        want.append(out)
+        num, zs, cnt = orc.cross(*(t.cpu().numpy() for t in (q8, k8, v8)), [0, queries], [0], [length], theta, mult, 20)
+        compare(out, num, zs, cnt, "div", "i32", None)
+    for j, out in enumerate(outs):
+        call(j % n, out)
+    torch.cuda.synchronize()
+    for j, out in enumerate(outs):
+        assert torch.equal(out, want[j % n]), j
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("queries", [1, 40, 200])
+def test_states_beyond_four_gigabytes(hccs, ctx, queries):
+    """Keys whose offsets do not fit 32 bits."""
+    import torch
+    rng = np.random.default_rng(queries)
+    hq, hkv, d, S = 128, 128, 128, 150000
+    n = 400 if queries == 200 else 200
+    states = torch.zeros((S, 2 * hkv, d), dtype=torch.int8, device="cuda")
+    tail = rng.integers(-128, 128, (n, 2 * hkv, d), dtype=np.int8)
+    states[S - n:] = torch.from_numpy(tail).cuda()
+    theta, mult = _theta(rng, hq, n, False), np.full(hq, 400, np.int32)
+    ctx.hccs_params_upload(theta, n)
+    q = rng.integers(-128, 128, (queries, hq, d), dtype=np.int8)
+    out = torch.empty((queries, hq, d), dtype=torch.int32, device="cuda")
+    ctx.hccs_attention_cross(torch.from_numpy(q).cuda(), states[:, :hkv], states[:, hkv:], *(torch.tensor(x, dtype=torch.int32, device="cuda") for x in
+                             ([0, queries], [S - n], [n])), out, mult, 20, max_q=queries, max_kv=n)
+    num, zs, cnt = orc.cross(q, tail[:, :hkv], tail[:, hkv:], [0, queries], [0], [n], theta, mult, 20)
+    compare(out, num, zs, cnt, "div", "i32", None)
+    assert ctx.hccs_device_status() == 0
