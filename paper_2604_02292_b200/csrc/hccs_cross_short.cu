@@ -306,7 +306,7 @@ cross_short_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_consta
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&bars.chunk_free[c % kChunks]));
     };
-    Chunk k;
+    Chunk k = {};
 
     if (warp == kCopyWarp) {
         // ===================================================== copies: K and V of a chunk and the Q of its tiles, in the order in which they
