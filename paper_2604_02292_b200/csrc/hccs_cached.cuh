@@ -46,6 +46,14 @@ __device__ __forceinline__ SequenceAt cross_sequence(const CachedAttnArgs &a, in
     q.cut = q.n != kv || k0 < 0 || k0 > a.states || q.nq > a.max_q;
     return q;
 }
+// Keys [x, y) that query q of a sequence sees of an encoder's states: x = y = 0 where none.  Bounds are any int32, so they are cut
+// and compared before one is taken from the other.
+__device__ __forceinline__ int2 range_of(const CachedAttnArgs &a, const SequenceAt &seq, int q) {
+    if (!a.key_range) return make_int2(0, seq.n);
+    const int2 r = reinterpret_cast<const int2 *>(a.key_range)[(int64_t)seq.s0 + q];
+    const int x = max(r.x, 0), y = min(r.y, seq.n);
+    return x < y ? make_int2(x, y) : make_int2(0, 0);
+}
 template <bool CROSS = false>
 __device__ __forceinline__ SequenceAt sequence_at(const CachedAttnArgs &a, int b) {
     if constexpr (CROSS) return cross_sequence(a, a.q_start[b], a.q_start[b + 1], a.k_start[b], a.kv_len[b]);

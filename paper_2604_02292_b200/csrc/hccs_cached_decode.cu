@@ -149,10 +149,9 @@ cached_decode_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_cons
     if (a.tree_mask && seq.nq > 0) self = a.tree_mask[(int64_t)seq.s0 * a.tree_words] & 1;
     int n = CROSS ? seq.n : min(max(seq.prefix + self, 0), seq.n), k0 = seq.k0;
     if (CROSS && a.key_range && seq.nq > 0) {
-        const int2 r = reinterpret_cast<const int2 *>(a.key_range)[seq.s0];
-        const int x = max(r.x, 0);
-        n = max(min(r.y, n) - x, 0);
-        k0 += n > 0 ? x : 0;
+        const int2 r = range_of(a, seq, 0);
+        n = r.y - r.x;
+        k0 += r.x;
     }
     const int tiles = (seq.nq > 0 || (CROSS && merge > 1)) && rows > 0 ? (n + kTileKeys - 1) / kTileKeys : 0;
     const int mine = min(first < tiles ? (tiles - first + stride - 1) / stride : 0, tiles_per_warp);

@@ -67,13 +67,6 @@ struct TileBarriers {
 
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
-// Keys [x, y) that query q of a sequence sees of an encoder's states: x = y = 0 where none.
-__device__ __forceinline__ int2 range_of(const CachedAttnArgs &a, const SequenceAt &seq, int q) {
-    if (!a.key_range) return make_int2(0, seq.n);
-    const int2 r = reinterpret_cast<const int2 *>(a.key_range)[(int64_t)seq.s0 + q];
-    const int x = max(r.x, 0), y = min(r.y, seq.n);
-    return x < y ? make_int2(x, y) : make_int2(0, 0);
-}
 
 template <int D> constexpr int kSlotsOf = D == 128 ? 8 : kMaxSlots;
 template <int D> constexpr uint32_t kIdescPVOf = instr_desc(0, 1, 1, 128, D);   // r.V and mask.V: uint8 x int8, V MN-major

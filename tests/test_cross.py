@@ -779,3 +779,19 @@ def test_states_beyond_four_gigabytes(hccs, ctx, queries):
     num, zs, cnt = orc.cross(q, tail[:, :hkv], tail[:, hkv:], [0, queries], [0], [n], theta, mult, 20)
     compare(out, num, zs, cnt, "div", "i32", None)
     assert ctx.hccs_device_status() == 0
+
+
+I32_MIN, I32_MAX = -2**31, 2**31 - 1
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("queries", [1, 3, 40])
+@pytest.mark.parametrize("bounds", [(40, I32_MIN), (1, I32_MIN), (I32_MAX, I32_MIN), (I32_MAX, -2), (I32_MIN, I32_MAX), (I32_MAX, I32_MAX),
+                                    (I32_MIN, I32_MIN), (5, I32_MAX), (I32_MIN, 3), (I32_MIN, 0)])
+def test_key_ranges_with_bounds_of_any_size(hccs, ctx, queries, bounds):
+    """Bounds up to the ends of int32: cut to the sequence's keys, whatever lies behind them.  Every sequence has others' states around it."""
+    rng = np.random.default_rng(queries)
+    k_lens = [100, 0, 90, 1, 300, 64]
+    out, _ = cross(hccs, ctx, rng, [queries] * len(k_lens), k_lens, 4, 2, 64, "div", "i32", ranges=[bounds] * (queries * len(k_lens)), gap=0)
+    if max(bounds[0], 0) >= bounds[1]:
+        assert (out[:queries * len(k_lens)] == 0).all()
