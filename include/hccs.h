@@ -460,7 +460,8 @@ hccs_status_t hccs_attention_cached(hccs_ctx_t *ctx, const int8_t *Q, const int8
  *   max_q, max_kv (host)  bounds of the lengths of this call, which choose kernel and grid: queries beyond max_q are not
  *                computed and keys beyond max_kv are not seen, both reported.  max_kv beyond n_design is
  *                HCCS_ERR_CONSTRAINT, beyond HCCS_MAX_CACHE_KEYS HCCS_ERR_UNSUPPORTED
- * Keys outside 0..S-1 are not seen and reported (bit 4 of the status word); q_start is cut to 0..T.  Rows no sequence has are left as they are.
+ * Keys from S on are not seen and reported (bit 4 of the status word); where k_start is not in 0..S none of the sequence's keys is seen, which is
+ * reported unless k_len is 0.  q_start is cut to 0..T.  Rows no sequence has are left as they are.
  */
 hccs_status_t hccs_attention_cross(hccs_ctx_t *ctx, const int8_t *Q, const int8_t *K, const int8_t *V,
                                    int64_t k_stride, int64_t v_stride, const int32_t *q_start,

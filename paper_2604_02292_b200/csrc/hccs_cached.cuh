@@ -43,7 +43,7 @@ __device__ __forceinline__ SequenceAt cross_sequence(const CachedAttnArgs &a, in
     q.k0 = k0;
     q.n = k0 < 0 || k0 > a.states ? 0 : max(min(min(kv, a.states - k0), a.max_kv), 0);
     q.prefix = q.n;
-    q.cut = q.n != kv || k0 < 0 || k0 > a.states || q.nq > a.max_q;
+    q.cut = q.n != kv || q.nq > a.max_q;       // (without keys no start is a wrong one)
     return q;
 }
 // Keys [x, y) that query q of a sequence sees of an encoder's states: x = y = 0 where none.  Bounds are any int32, so they are cut

@@ -795,3 +795,29 @@ def test_key_ranges_with_bounds_of_any_size(hccs, ctx, queries, bounds):
     out, _ = cross(hccs, ctx, rng, [queries] * len(k_lens), k_lens, 4, 2, 64, "div", "i32", ranges=[bounds] * (queries * len(k_lens)), gap=0)
     if max(bounds[0], 0) >= bounds[1]:
         assert (out[:queries * len(k_lens)] == 0).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("queries,length,ranges", [(1, 60, False), (1, 60, True), (3, 60, False), (40, 60, False), (40, 200, False), (40, 300, False), (40, 60, True)])
+def test_starts_of_sequences_without_keys(hccs, ctx, queries, length, ranges):
+    """A sequence without keys has none outside the states, wherever it is said to start (padding of a batch, say): nothing is
+    reported, and its rows are zeros.  With keys such a start is reported, and none of them is seen."""
+    import torch
+    rng = np.random.default_rng(queries + length)
+    hq, hkv, d, S, dev = 4, 2, 64, length + 20, "cuda"
+    theta, mult = _theta(rng, hq, length, False), np.full(hq, 500, np.int32)
+    ctx.hccs_params_upload(theta, length)
+    K, V = (rng.integers(-128, 128, (S, hkv, d), dtype=np.int8) for _ in range(2))
+    k_start, k_len = [-1, 3, S + 1, I32_MIN, I32_MAX, S], [0, length, 0, 0, 0, 0]
+    B = len(k_start)
+    T = B * queries
+    q = rng.integers(-128, 128, (T, hq, d), dtype=np.int8)
+    starts = [i * queries for i in range(B + 1)]
+    R = torch.tensor([[0, length]] * T, dtype=torch.int32, device=dev) if ranges else None
+    for last, word in ((k_len[0], 0), (1, 16)):
+        k_len[0] = last
+        out = torch.full((T, hq, d), 77, dtype=torch.int32, device=dev)
+        ctx.hccs_attention_cross(*(torch.from_numpy(x).to(dev) for x in (q, K, V)), *(torch.tensor(x, dtype=torch.int32, device=dev) for x in
+                                 (starts, k_start, k_len)), out, mult, 20, max_q=queries, max_kv=length, key_range=R)
+        assert ctx.hccs_device_status() == word
+        compare(out, *orc.cross(q, K, V, starts, k_start, [0] + k_len[1:], theta, mult, 20), "div", "i32", None)
