@@ -436,12 +436,16 @@ class Context:
         q_stride = k_stride = v_stride = 0
         dev, dtype = self.device, some.dtype
         if q is not None:
+            if q8 is None:
+                raise ValueError("q8 must be given with q")
             Hq = q.shape[1]
             if q8.get_device() != dev or q8.shape != q.shape or q8.dtype not in _I8 or not q8.is_contiguous():
                 self._explain(q8, "q8", 1, q.shape)
             qp, q8p, qs = q.data_ptr(), q8.data_ptr(), _floats(q_step, "q_step", Hq)
             q_stride = self._tokens(q, "q", some)
         if k is not None:
+            if k_pages is None or v_pages is None or slots is None:
+                raise ValueError("k_pages, v_pages and slots must be given with k and v")
             shape = k.shape
             Hkv = shape[1]
             pages, _, size, _ = pool = k_pages.shape
@@ -481,6 +485,10 @@ class Context:
             raise ValueError("q or k and v must be given")
         if (k is None) != (v is None):
             raise ValueError("k and v go together")
+        if q is not None and q8 is None:
+            raise ValueError("q8 must be given with q")
+        if k is not None and (k8 is None or v8 is None):
+            raise ValueError("k8 and v8 must be given with k and v")
         T, _, d = some.shape
         heads_first = out.ndim == 4
         L = out.shape[2] if heads_first else 1

@@ -821,3 +821,37 @@ def test_starts_of_sequences_without_keys(hccs, ctx, queries, length, ranges):
                                  (starts, k_start, k_len)), out, mult, 20, max_q=queries, max_kv=length, key_range=R)
         assert ctx.hccs_device_status() == word
         compare(out, *orc.cross(q, K, V, starts, k_start, [0] + k_len[1:], theta, mult, 20), "div", "i32", None)
+
+
+@pytest.mark.gpu
+def test_outputs_that_are_missing(hccs):
+    """What goes with a given input and is None is named, in the writes to dense tensors and to the cache."""
+    import torch
+    ctx = hccs.Context(0)
+    dev = "cuda"
+    x = torch.zeros((6, 2, 64), device=dev)
+    new = {n: torch.zeros((6, 2, 64), dtype=torch.int8, device=dev) for n in ("q8", "k8", "v8")}
+    pools = {n: torch.zeros((1, 2, 16, 64), dtype=torch.int8, device=dev) for n in ("k_pages", "v_pages")}
+    slots = torch.arange(6, device=dev)
+    steps = [np.full(2, 0.1, np.float32)] * 3
+    for gone in ("q8", "k8", "v8"):
+        for q, k in ((x, x), (x, None), (None, x)):
+            a = dict(new)
+            a[gone] = None
+            if (q if gone == "q8" else k) is None:             # goes with nothing that is given
+                ctx.hccs_states_write(q, k, k, a["q8"], a["k8"], a["v8"], None, *steps)
+                continue
+            with pytest.raises(ValueError, match=gone):
+                ctx.hccs_states_write(q, k, k, a["q8"], a["k8"], a["v8"], None, *steps)
+    for gone in ("q8", "k_pages", "v_pages", "slots"):
+        for q, k in ((x, x), (x, None), (None, x)):
+            for call in (ctx.hccs_cache_write, ctx.hccs_cache_write_axes):
+                a = dict(new, **pools, slots=slots)
+                a[gone] = None
+                if (q if gone == "q8" else k) is None:
+                    call(q, k, k, a["q8"], a["k_pages"], a["v_pages"], None, a["slots"], *steps)
+                    continue
+                with pytest.raises(ValueError, match=gone):
+                    call(q, k, k, a["q8"], a["k_pages"], a["v_pages"], None, a["slots"], *steps)
+    assert ctx.hccs_device_status() == 0
+    ctx.close()
