@@ -110,10 +110,6 @@ class Rope(ctypes.Structure):
         for i, f in enumerate(freq):
             self.freq[i] = f
 
-    @property
-    def _ref(self):
-        return ctypes.byref(self)
-
 
 class RopeAxes(ctypes.Structure):
     """``hccs_rope_axes_t``: frequencies and, per pair of rotated dims, the axis whose positions turn it."""
@@ -129,10 +125,6 @@ class RopeAxes(ctypes.Structure):
         super().__init__(Rope(freq, interleaved, scale), count)
         for i, x in enumerate(axis):
             self.axis[i] = x
-
-    @property
-    def _ref(self):
-        return ctypes.byref(self)
 
 
 class _RopeScaling(ctypes.Structure):
@@ -399,14 +391,14 @@ class Context:
         are any multiple of 16 bytes apart."""
         (some, T, d, Hq, Hkv, pages, size, qp, kp, vp, q8p, kpp, vpp, slotp, qs, ks, vs, q_stride, k_stride,
          v_stride) = self._paged_tokens(q, k, v, q8, k_pages, v_pages, slots, q_step, k_step, v_step)
-        dev, posp = self.device, None
+        dev, posp, ropep = self.device, None, _rotation(rope, Rope)
         if positions is not None:
             if positions.get_device() != dev or positions.dtype not in _I32 or positions.shape != (T,) or not positions.is_contiguous():
                 self._explain(positions, "positions", 4, (T,))
             posp = positions.data_ptr()
         st = _lib.hccs_cache_write(self._h, qp, kp, vp, _type_of(some), q_stride, k_stride, v_stride, posp, slotp,
-                                   rope._ref if rope is not None else None, qs, ks, vs, q8p, kpp, vpp,
-                                   T, Hq, Hkv, d, pages, size, _raw_stream(dev) if stream is None else _stream_ptr(stream))
+                                   ropep, qs, ks, vs, q8p, kpp, vpp, T, Hq, Hkv, d, pages, size,
+                                   _raw_stream(dev) if stream is None else _stream_ptr(stream))
         if st != HCCS_OK:
             raise HccsError(st, "hccs_cache_write")
 
@@ -416,9 +408,10 @@ class Context:
         """:meth:`hccs_cache_write` with positions [axes,T] (int32, any strides: the transpose of [T,axes] as well)."""
         (some, T, d, Hq, Hkv, pages, size, qp, kp, vp, q8p, kpp, vpp, slotp, qs, ks, vs, q_stride, k_stride,
          v_stride) = self._paged_tokens(q, k, v, q8, k_pages, v_pages, slots, q_step, k_step, v_step)
+        ropep = _rotation(rope, RopeAxes)
         posp, axis_stride, token_stride = self._axes(positions, rope, T)
         st = _lib.hccs_cache_write_axes(self._h, qp, kp, vp, _type_of(some), q_stride, k_stride, v_stride, posp, axis_stride, token_stride,
-                                        slotp, rope._ref if rope is not None else None, qs, ks, vs, q8p, kpp, vpp, T, Hq, Hkv, d, pages,
+                                        slotp, ropep, qs, ks, vs, q8p, kpp, vpp, T, Hq, Hkv, d, pages,
                                         size, _raw_stream(self.device) if stream is None else _stream_ptr(stream))
         if st != HCCS_OK:
             raise HccsError(st, "hccs_cache_write_axes")
@@ -514,9 +507,10 @@ class Context:
             k_stride, v_stride = self._tokens(k, "k", some), self._tokens(v, "v", some)
             kp, vp, k8p, v8p = k.data_ptr(), v.data_ptr(), dense(k8, "k8", Hkv), dense(v8, "v8", Hkv)
             ks, vs = _floats(k_step, "k_step", Hkv), _floats(v_step, "v_step", Hkv)
+        ropep = _rotation(rope, RopeAxes)
         posp, axis_stride, token_stride = self._axes(positions, rope, T)
         st = _lib.hccs_states_write(self._h, qp, kp, vp, _type_of(some), q_stride, k_stride, v_stride, posp, axis_stride, token_stride,
-                                    rope._ref if rope is not None else None, qs, ks, vs, q8p, k8p, v8p, T, max(L, 1), Hq, Hkv, d,
+                                    ropep, qs, ks, vs, q8p, k8p, v8p, T, max(L, 1), Hq, Hkv, d,
                                     _raw_stream(self.device) if stream is None else _stream_ptr(stream))
         if st != HCCS_OK:
             raise HccsError(st, "hccs_states_write")
@@ -736,6 +730,15 @@ def _type_of(t) -> int:
             raise ValueError(f"int32, float32, bfloat16 or float16 is wanted, got {t.dtype}")
         kind = _TYPES[t.dtype]
     return kind
+
+
+# The library reads a rotation by the layout of the call's own kind.
+def _rotation(rope, kind):
+    if rope is None:
+        return None
+    if not isinstance(rope, kind):
+        raise ValueError(f"rope must be a {kind.__name__}, not a {type(rope).__name__}")
+    return ctypes.byref(rope)
 
 
 # Host arrays go to the library as the bytes of their values (it copies them before it returns).

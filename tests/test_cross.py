@@ -855,3 +855,34 @@ def test_outputs_that_are_missing(hccs):
                     call(q, k, k, a["q8"], a["k_pages"], a["v_pages"], None, a["slots"], *steps)
     assert ctx.hccs_device_status() == 0
     ctx.close()
+
+
+@pytest.mark.gpu
+def test_rotations_of_the_other_kind(hccs):
+    """Rope and RopeAxes have different layouts: each write takes its own alone."""
+    import torch
+    ctx = hccs.Context(0)
+    dev = "cuda"
+    x = torch.zeros((6, 2, 64), device=dev)
+    q8, k8, v8 = (torch.zeros((6, 2, 64), dtype=torch.int8, device=dev) for _ in range(3))
+    kp, vp = (torch.zeros((1, 2, 16, 64), dtype=torch.int8, device=dev) for _ in range(2))
+    slots, steps = torch.arange(6, device=dev), [np.full(2, 0.1, np.float32)] * 3
+    one, several = hccs.hccs_rope_frequencies(64), hccs.hccs_rope_axes(64, (16, 16))
+    pos1, pos2 = torch.zeros(6, dtype=torch.int32, device=dev), torch.zeros((2, 6), dtype=torch.int32, device=dev)
+
+    def dense(rope, positions):
+        ctx.hccs_states_write(x, x, x, q8, k8, v8, positions, *steps, rope=rope)
+
+    def paged(rope, positions):
+        ctx.hccs_cache_write_axes(x, x, x, q8, kp, vp, positions, slots, *steps, rope=rope)
+
+    def plain(rope, positions):
+        ctx.hccs_cache_write(x, x, x, q8, kp, vp, positions, slots, *steps, rope=rope)
+    for call, right, wrong, positions in ((plain, one, several, pos1), (paged, several, one, pos2), (dense, several, one, pos2)):
+        call(right, positions)
+        call(None, None)
+        for bad in (wrong, 64):
+            for p in (positions, None):
+                with pytest.raises(ValueError, match="rope"):
+                    call(bad, p)
+    ctx.close()
