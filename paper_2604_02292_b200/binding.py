@@ -461,9 +461,9 @@ class Context:
             return None, 0, 0
         shape = positions.shape
         if positions.get_device() != self.device or positions.dtype not in _I32 or len(shape) != 2 or shape[1] != T:
-            if positions.get_device() == self.device:
-                self._explain(positions.contiguous(), "positions", 4, (shape[0] if len(shape) else 0, T))
-            self._explain(positions, "positions", 4)
+            # (a copy, since any strides will do; and a first call's types are known from here on)
+            self._explain(positions if positions.get_device() != self.device else positions.contiguous(), "positions", 4,
+                          (shape[0] if len(shape) else 0, T))
         if rope is not None and shape[0] < rope.num_axes:
             raise ValueError(f"positions have {shape[0]} axes, the rotation {rope.num_axes}")
         return positions.data_ptr(), *positions.stride()

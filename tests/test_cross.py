@@ -886,3 +886,23 @@ def test_rotations_of_the_other_kind(hccs):
                 with pytest.raises(ValueError, match="rope"):
                     call(bad, p)
     ctx.close()
+
+
+@pytest.mark.gpu
+def test_positions_of_any_strides_in_a_first_call(hccs):
+    """The integer types are looked up in the first call that meets one; it takes a transpose as later ones do."""
+    import torch
+    from paper_2604_02292_b200 import binding
+    ctx = hccs.Context(0)
+    x = torch.zeros((6, 2, 64), device="cuda")
+    q8 = torch.empty((6, 2, 64), dtype=torch.int8, device="cuda")
+    rope, step = hccs.hccs_rope_axes(64, (16, 16)), np.full(2, 0.1, np.float32)
+    for positions in (torch.zeros((6, 2), dtype=torch.int32, device="cuda").t(), torch.zeros((2, 12), dtype=torch.int32, device="cuda")[:, ::2]):
+        binding._I32.clear()
+        ctx.hccs_states_write(x, None, None, q8, None, None, positions, step, None, None, rope=rope)
+        assert (q8 == 0).all()
+    for bad in (torch.zeros((6, 2), device="cuda").t(), torch.zeros((2, 6), dtype=torch.int64, device="cuda")):
+        binding._I32.clear()
+        with pytest.raises(ValueError):
+            ctx.hccs_states_write(x, None, None, q8, None, None, bad, step, None, None, rope=rope)
+    ctx.close()
