@@ -906,3 +906,78 @@ def test_positions_of_any_strides_in_a_first_call(hccs):
         with pytest.raises(ValueError):
             ctx.hccs_states_write(x, None, None, q8, None, None, bad, step, None, None, rope=rope)
     ctx.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("queries,length", [(1, 300), (3, 500), (40, 100), (150, 200), (60, 900)])
+def test_captured_between_copies_and_other_streams(hccs, ctx, queries, length):
+    """Calls captured behind copies and fills, and behind work of another stream that is joined: every input has arrived by then."""
+    import torch
+    rng = np.random.default_rng(length)
+    hq, hkv, d, dev = 4, 2, 64, "cuda"
+    theta, mult = _theta(rng, hq, length, False), np.full(hq, 500, np.int32)
+    ctx.hccs_params_upload(theta, length)
+    steps = [np.full(m, 0.03, np.float32) for m in (hq, hkv, hkv)]
+    fresh = [torch.from_numpy(rng.standard_normal(s).astype(np.float32)).to(dev) for s in ((queries, hq, d), (length, hkv, d), (length, hkv, d))]
+    q, k, v = (torch.zeros_like(t) for t in fresh)
+    q8, k8, v8 = (torch.zeros(t.shape, dtype=torch.int8, device=dev) for t in fresh)
+    start, k0, kl = (torch.tensor(x, dtype=torch.int32, device=dev) for x in ([0, queries], [0], [length]))
+    out = torch.empty((queries, hq, d), dtype=torch.int32, device=dev)
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph):
+        main = torch.cuda.current_stream()
+        side.wait_stream(main)
+        with torch.cuda.stream(side):
+            k.copy_(fresh[1])
+            v.copy_(fresh[2])
+            ctx.hccs_states_write(None, k, v, None, k8, v8, None, None, steps[1], steps[2])
+        q.copy_(fresh[0])
+        ctx.hccs_states_write(q, None, None, q8, None, None, None, steps[0], None, None)
+        main.wait_stream(side)
+        ctx.hccs_attention_cross(q8, k8, v8, start, k0, kl, out, mult, 20, max_q=queries, max_kv=length)
+        q8.zero_()
+        k8.zero_()
+    for _ in range(3):
+        for t in fresh:
+            t.copy_(torch.from_numpy(rng.standard_normal(t.shape).astype(np.float32)))
+        out.fill_(9)
+        graph.replay()
+        torch.cuda.synchronize()
+        codes = [orc.quantise(t.cpu().numpy(), s) for t, s in zip(fresh, steps)]
+        compare(out, *orc.cross(*codes, [0, queries], [0], [length], theta, mult, 20), "div", "i32", None)
+    assert ctx.hccs_device_status() == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("queries,hq,ranges", [(1, 16, False), (1, 16, True), (2, 8, False), (4, 2, False), (1, 5, False), (20, 2, False)])
+def test_longest_states(hccs, ctx, d, queries, hq, ranges):
+    """As many keys as a call may have, in the most rows that the kernel for few rows takes, and in the kernel for many."""
+    rng = np.random.default_rng(d + queries)
+    n = hccs.HCCS_MAX_CACHE_KEYS
+    r = [(n - 5000 * (i + 1), I32_MAX) for i in range(queries)] if ranges else None
+    cross(hccs, ctx, rng, [queries], [n], hq, 1, d, "real", "f32", wide=True, ranges=r)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("queries,length", [(1, 100), (4, 100), (40, 100), (40, 200), (40, 400)])
+def test_keys_and_values_with_strides_of_their_own(hccs, ctx, queries, length):
+    import torch
+    rng = np.random.default_rng(length)
+    out, (args, kw, _) = cross(hccs, ctx, rng, [queries], [length], 4, 2, 64, "div", "i32", fused=True)
+    want = out.clone()
+    for K, V in ((args[1].contiguous(), args[2]), (args[1], args[2].contiguous())):
+        out.fill_(5)
+        ctx.hccs_attention_cross(args[0], K, V, *args[3:], **kw)
+        torch.cuda.synchronize()
+        assert torch.equal(out[:queries], want[:queries])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hq,hkv,d", [(100, 1, 64), (128, 1, 128), (129, 1, 64), (256, 1, 128), (256, 256, 64), (96, 3, 64)])
+@pytest.mark.parametrize("queries,length,ranges", [(1, 700, False), (1, 90, True), (9, 90, False), (9, 250, False), (5, 700, True)])
+def test_groups_of_any_size(hccs, ctx, hq, hkv, d, queries, length, ranges):
+    """Up to all query heads on one kv head: more than a tile of 128 rows holds, and as many kv heads as there may be."""
+    rng = np.random.default_rng(hq)
+    q_lens, k_lens = [queries, 1, 0, queries], [length, 3, 5, length // 2]
+    cross(hccs, ctx, rng, q_lens, k_lens, hq, hkv, d, "real", "bf16", ranges=_some_ranges(rng, q_lens, k_lens) if ranges else None, wide=True)
