@@ -73,7 +73,7 @@ __device__ __forceinline__ SequenceAt sequence_at(const CachedAttnArgs &a, int b
 // Requantisation of one head, x = clamp((acc*M + R) >> sh, -128, 127) with R = 2^(sh-1), as one clamp and one
 // multiply-add: with lo and hi the accumulators between which x moves from -128 to 127 (steps below one, so
 // both ends are reached) and k = 24 - sh, clamp(acc - lo, 0, hi - lo) * (M << k) + ((lo*M + R) << k) has x as
-// its (signed) top byte; every value fits 32 bits.  M = 0 gives x = 0.
+// its (signed) top byte; every value fits 32 bits.  M = 0 gives x = 0.  (The kernel for few keys has the same rule without fp64, head_requant.)
 struct Requant {
     uint32_t mk, ck;
     int neg_lo, span;

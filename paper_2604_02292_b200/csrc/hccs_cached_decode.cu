@@ -80,9 +80,9 @@ struct Sizes {
 // collects sum V for nothing).  tiles_per_warp bounds what shared memory holds.
 // CROSS: queries on an encoder's states.  The rows of a kv head are its (query, head) pairs, all of which see the same keys:
 // those of the sequence, or where max_q is 1 those of the query's key range.  Up to `merge` neighbouring sequences of one query that read the
-// same states (hypotheses about one input) are rows of one CTA too, that of the first of them: 32 queries, two by two on the same states of up to
-// 1499 keys (16 heads of 64), in 14.4 us instead of 20.5 (12.0 since kernels overlap).  8 queries on 32768 keys (32 heads on 8 of 128): 86.6 us,
-// 6.2 TB/s.
+// same states (hypotheses about one input) are rows of one CTA too, that of the first of them, where launch_typed leaves room for them: 32
+// queries, two by two on the same states of up to 1499 keys (16 heads of 64), in 14.4 us instead of 20.5 (12.0 to 12.4 since kernels overlap).
+// 8 queries on 32768 keys (32 heads on 8 of 128): 84 to 90 us, 6.0 to 6.4 TB/s.
 template <int D, bool HI, int W, bool CROSS>
 __global__ void __launch_bounds__(32 * W, 16 / W)
 cached_decode_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_constant__ CUtensorMap map_k,
@@ -555,8 +555,12 @@ template <int D, bool HI, bool CROSS>
 cudaError_t launch_typed(const CachedAttnArgs &a, cudaStream_t stream) {
     constexpr int kRows = Sizes<D, HI, 8>::kRows;
     int rows = CROSS ? a.max_q * a.group : a.group;                 // of a kv head
-    // Room for the rows of sequences that share their states, where there may be any and the logits of all rows leave room for two
-    // CTAs on an SM
+    // Room for the rows of sequences that share their states, eight rows in all (so none with more than four heads per kv head), where
+    // there may be any and the logits of eight rows leave room for two CTAs on an SM: up to 3872 keys of 128 dims, 7936 of 64.
+    // Whether any share is known on the device alone.  32 queries, four by four on the same states (16 heads of 128): on 577, 1499, 3872
+    // keys 10.7, 16.4, 32.9 us, apart 18.4, 29.6, 60.6; with two by two of four heads per kv head no change (16.2, apart 15.9).  Beyond
+    // that they stay apart: on 3904, 8192, 16384 keys 61, 115, 220 us, together 33, 46, 90; but room that nobody takes costs 4 to 9 % there
+    // (32 queries that share nothing, 16384 keys: 325 us, with room 339; 8 on 32768 keys, 32 heads on 8: 84, 91).
     int merge = 1;
     if (CROSS && a.max_q == 1 && !a.key_range && a.B > 1 && Sizes<D, HI, 8>::smem((a.max_kv + kTileKeys - 1) / kTileKeys + 8, kRows) <= kHalfSmem)
         merge = kRows / a.group > 1 ? kRows / a.group : 1;

@@ -73,8 +73,8 @@ template <int D> constexpr uint32_t kIdescPVOf = instr_desc(0, 1, 1, 128, D);   
 
 // CROSS: queries on an encoder's states.  A row sees keys [first, end) of its sequence, all of them where there are no key
 // ranges; the blocks that every row of the tile sees whole come first, then the others (the order of blocks is free:
-// the sums are exact).  2048 queries on each of two states of 6404 keys (32 heads on 8 of 128): 314 us, 0.42 of the int8 rate counting two
-// products; 1001 queries on 2404 keys, twice, that see 601 of them or none (16 heads on 4): 31 us.
+// the sums are exact).  2048 queries on each of two states of 6404 keys (32 heads on 8 of 128): 310 us, in runs among other work up to 346, 0.42
+// to 0.38 of the int8 rate counting two products; 1001 queries on 2404 keys, twice, that see 601 of them or none (16 heads on 4): 31 us.
 template <int D, bool CROSS>
 __global__ void __launch_bounds__(kThreads, 1)
 cached_tile_kernel(const __grid_constant__ CachedAttnArgs a, const __grid_constant__ CUtensorMap map_k,
@@ -637,7 +637,9 @@ template <int D, bool CROSS>
 cudaError_t launch_typed(const CachedAttnArgs &a, cudaStream_t stream) {
     const int64_t rows = (int64_t)a.max_q * a.group;
     // Tiles of 127 rows leave room for the row of ones; full ones are taken where a row less would mean a tile more,
-    // unless there are many anyway (a second product per block costs a tile about 15 %)
+    // unless there are many anyway (a second product per block costs a tile about 15 %).  CROSS, full ones instead: 2 x 2048 queries on
+    // 6404 keys (32 heads on 8 of 128) 342 us instead of 310, 8 x 1024 on 1499 (8 heads of 128) 73.4 instead of 66.6; but 8 x 1024 of 16 heads of 64
+    // on 577 keys 72 instead of 81, on 2404 141.5 instead of 145.5: the rule goes by the former.
     const int64_t tiles127 = (rows + kTile - 2) / (kTile - 1), tiles128 = (rows + kTile - 1) / kTile;
     const int tile_rows = tiles127 == tiles128 || tiles128 >= 8 ? kTile - 1 : kTile;
     const int row_tiles = (int)(tile_rows == kTile ? tiles128 : tiles127);
@@ -696,7 +698,12 @@ cudaError_t launch_cached_attention(const CachedAttnArgs &a, cudaStream_t stream
 }
 
 cudaError_t launch_cross_attention(const CachedAttnArgs &a, cudaStream_t stream, uint64_t *launches) {
-    // up to sixteen rows of a kv head, all of which see the same keys, go through the kernel that is bound by HBM
+    // Up to sixteen rows of a kv head, all of which see the same keys, go through the kernel that is bound by HBM; sixteen is what its
+    // products hold.  32 sequences of 16 queries (16 heads of 64), on 577, 1499, 4096 keys: 17.5, 29.0, 57.3 us, through the kernel for many 38.8,
+    // 55.0, 95.1; on 77, 250: 12.2, 13.5, through the one for few keys 16.0, 16.1.  One sequence: 6.3 to 10.6, the others 7.1 to 13.1.
+    // Then the kernel for few keys wherever it holds them (256: two stages of tensor memory): 8 x 4096 queries on 256 keys (16 heads of 64)
+    // 53 us, through the one for many 246 (on 257: 262); 2 x 1000 (32 heads on 8 of 128) 16.3, 40.6 (44.4); 32 x 20 (8 heads of 64) 10.3,
+    // 16.4 (17.9).
     const bool few = a.max_q == 1 || (!a.key_range && (int64_t)a.max_q * a.group <= 16);
     const cudaError_t e = few ? launch_cross_decode(a, stream) : cross_short_fits(a) ? launch_cross_short(a, stream)
                           : a.d == 128 ? launch_typed<128, true>(a, stream) : launch_typed<64, true>(a, stream);

@@ -16,8 +16,13 @@
 // Roles: sixteen row warps, a warp each for the copies, Q.K^T, r.V, and the sums of V.
 //
 // Bound: the chain of a tile (product, tensor memory, arithmetic, product, outputs), with five warps per scheduler to cover it: issue slots
-// 53 to 62 % busy, tensor pipe 10 to 21 %.  8 x 4096 queries on 77 keys (16 heads of 64, fp16 out): 32 us, 3.2 TB/s of Q and O; 24 ragged texts
-// of up to 700 on up to 256 keys (32 heads on 8 of 128, bf16 out): 45.5 us.  The kernel for longer states takes 226 and 176.
+// 52 to 61 % busy, tensor pipe 10 to 21 %.  8 x 4096 queries on 77 keys (16 heads of 64, fp16 out): 31 to 32 us, 3.2 TB/s of Q and O; 24 ragged
+// texts of up to 700 on up to 256 keys (32 heads on 8 of 128, bf16 out): 45 us.  The kernel for longer states takes 226 and 176.
+//
+// Weak at sequences of few queries: a chunk's place is free again once all its rows are stored, and there are as many places as stages, so where a
+// chunk is one tile the next one's copies start when a stage is through, in the open; all four quarters of a tile are computed and the whole
+// box of Q is fetched, however few rows there are.  512 sequences of 20 queries on 100 keys (16 heads of 64): 185 to 189 us, 9 times the bytes'
+// time; through the kernel for longer states 460.
 #include "hccs_cached.cuh"
 #include "hccs_tcgen05.cuh"
 
@@ -168,7 +173,7 @@ __device__ __forceinline__ void find_start(const CachedAttnArgs &a, const ShortP
     }
 }
 
-// Requantisation of a head (see Requant) without fp64: a quotient of num = c * 2^(sh-1) - less by M is estimated in fp32, off by less than one
+// Requantisation of a head (the rule and the fields of make_requant: a change to one is one to both) without fp64: a quotient of num = c * 2^(sh-1) - less by M is estimated in fp32, off by less than one
 // where it is below 2^22, and put right by its remainder; beyond that it is cut to the accumulators' range.
 struct HeadRequant {
     uint32_t mk, ck;
